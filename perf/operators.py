@@ -84,8 +84,8 @@ def draw(rng):
              allowed=0 if mask == "none" else _spread(rng, 1, 1000))
     if op == "head":
         group = rng.choice([32, 64, 128])
-        c |= dict(k=group * _spread(rng, -(-256 // group), 4096 // group), group=group, zeros=rng.random() < 0.5,
-                  out=rng.choice(["f32", c["dtype"]]))
+        k = rng.choice([1024, 2048, 4096, group * (_spread(rng, 256 // group, 4000 // group) | 1)])     # a usual one, or one that fills no tile
+        c |= dict(k=k, group=group, zeros=rng.random() < 0.5, out=rng.choice(["f32", c["dtype"]]))
         return c
     c |= dict(history=rng.choice([0, _spread(rng, 16, 8192)]), bias=rng.choice([0, _spread(rng, 1, 300)]))
     if op == "draw":
