@@ -194,7 +194,8 @@ def _rules_of(xgm, s, vocab):
                   d_n_prompt=_address(s["n_prompt"]), d_repetition=_address(s["repetition"]), d_frequency=_address(s["frequency"]),
                   d_presence=_address(s["presence"]))
     if s["bias_ids"] is not None:
-        r |= dict(d_bias_ids=_address(s["bias_ids"]), d_bias=_address(s["bias"]), d_bias_offsets=_address(s["bias_offsets"]))
+        r |= dict(d_bias_ids=_address(s["bias_ids"]), d_bias=_address(s["bias"]), d_bias_offsets=_address(s["bias_offsets"]),
+                  n_bias=s["bias_ids"].numel())
     return xgm.LogitRules(**r)
 
 
