@@ -48,6 +48,7 @@ typedef struct xgm_grammar xgm_grammar;
 typedef struct xgm_cache xgm_cache;
 typedef struct xgm_matcher xgm_matcher;
 typedef struct xgm_batch xgm_batch;
+typedef struct xgm_sampler xgm_sampler;
 
 typedef enum {
   XGM_OK = 0,
@@ -74,7 +75,10 @@ enum {
   XGM_BATCH_MAX_HISTORY = 63,/* older states a row of an xgm_batch can keep */
   XGM_BATCH_MAX_STACKS = 16, /* parallel stacks per row of an xgm_batch */
   XGM_BATCH_MAX_DEPTH = 128, /* frames per stack in an xgm_batch */
-  XGM_BATCH_MAX_ROWS = 1024  /* rows of an xgm_batch */
+  XGM_BATCH_MAX_ROWS = 1024, /* rows of an xgm_batch */
+  XGM_MAX_ROWS = 65535,      /* rows of a call below */
+  XGM_MAX_LOGITS = 1 << 20,  /* logits a row of an xgm_sampler (padding included) */
+  XGM_MAX_HIDDEN = 1 << 16   /* columns of xgm_q4_logits */
 };
 
 const char* xgm_last_error(void);
@@ -491,6 +495,100 @@ int xgm_apply_token_bitmask_inplace(void* d_logits, xgm_dtype dt, int32_t B, int
                                     int64_t row_stride_elems, const int32_t* d_bitmask,
                                     int32_t V_mask, const int32_t* d_row_index, int32_t n_rows,
                                     void* hip_stream);
+
+/* --------------------------------------------------- from hidden states to tokens
+ * What lies around the mask in a decode step, for engines that keep the whole
+ * step on the device: hidden states -> logits (6) -> penalties, biases, mask
+ * (7) or, in one go, a token id a row (8) -> xgm_batch_accept_tokens, which
+ * leaves a row with id -1 alone.  All calls are asynchronous, allocate nothing
+ * and may be captured into a graph.
+ *
+ * 6. Logits from hidden states, the output projection in 4 bits with a scale
+ * for each group of columns (section 2.1: a masked token's logit is -inf
+ * whatever its value, so rows of the matrix that no request may take are not
+ * read):
+ *   logits[b][v] = sum over k of hidden[b][k] * (code(v, k) - zero(v, k / group)) * scale(v, k / group),
+ * summed in 32 bits and rounded once; -inf where bit (b, v) of d_bitmask is 0
+ * (NULL: no mask), also where a hidden state is not finite.
+ * d_hidden: [B, K] of hidden_dt (XGM_BF16 or XGM_F16), row stride
+ * hidden_stride_elems.  d_codes: [V, K / 2] bytes, column 2 j in the low half of
+ * byte j.  d_scales: [V, K / group] of hidden_dt.  d_zeros: [V, K / group] bytes
+ * (0 .. 15), or NULL: 8 everywhere.  group: a multiple of 32 that divides K;
+ * K <= XGM_MAX_HIDDEN; B <= XGM_MAX_ROWS.  d_hidden, its row pitch and d_codes must be
+ * multiples of 16 bytes.  d_logits: [B, V] of logits_dt (any), row stride
+ * logits_stride_elems. */
+int xgm_q4_logits(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32_t K, int64_t hidden_stride_elems,
+                  const uint8_t* d_codes, const void* d_scales, const uint8_t* d_zeros, int32_t V, int32_t group,
+                  void* d_logits, xgm_dtype logits_dt, int64_t logits_stride_elems, const int32_t* d_bitmask,
+                  void* hip_stream);
+
+/* Rules on the logits of a batch.  The struct is host memory, read during the
+ * call; what it points to is device memory with a value or a row for each row
+ * b of the logits.  Any pointer may be NULL: the rule is off.
+ *  - history: d_tokens[b][0 .. n) with n = d_n_tokens[b], row stride
+ *    token_stride (n is cut off there); the first d_n_prompt[b] of them are
+ *    the prompt (NULL: none), the others were generated.  Ids outside the row of
+ *    logits count for nothing.
+ *  - a token that occurs in the history: x > 0 ? x / repetition : x * repetition;
+ *  - one generated c > 0 times: then x - frequency * c - presence;
+ *  - then x + bias, for the ids d_bias_ids[d_bias_offsets[b] .. d_bias_offsets[b + 1])
+ *    (d_bias_offsets: B + 1 values, n_bias entries in all; of several entries
+ *    of a row for one id the last counts);
+ *  - then -inf where the bit of d_bitmask ([B, xgm_bitmask_words(v_mask)]) is 0,
+ *    and from v_mask on.
+ * Computed in 64 bits, rounded once. */
+typedef struct {
+  const int32_t* d_bitmask;
+  const int32_t* d_tokens;
+  const int32_t* d_n_tokens;
+  const int32_t* d_n_prompt;
+  const float* d_repetition;
+  const float* d_frequency;
+  const float* d_presence;
+  const int32_t* d_bias_ids;
+  const float* d_bias;
+  const int32_t* d_bias_offsets;
+  int64_t token_stride;
+  int32_t v_mask;
+  int32_t n_bias;
+} xgm_logit_rules;
+/* 7. d_out[b][v] = d_logits[b][v] under the rules, both [B, V] of dt with their own row
+ * strides; d_out may be d_logits (with the same stride), and must not overlap
+ * it otherwise. */
+int xgm_process_logits(const void* d_logits, xgm_dtype dt, int32_t B, int32_t V, int64_t row_stride_elems,
+                       const xgm_logit_rules* rules, void* d_out, int64_t out_stride_elems, void* hip_stream);
+
+/* 8. One token a row.  A sampler holds the working memory of its calls, which
+ * must be ordered by the caller (one stream, or events): rows up to max_rows,
+ * V <= XGM_MAX_LOGITS logits each.  xgm_sampler_create synchronises hip_stream. */
+int xgm_sampler_create(int32_t max_rows, int32_t V, void* hip_stream, xgm_sampler** out);
+void xgm_sampler_destroy(xgm_sampler* s);
+/* How a row is drawn; as above, device memory, a value a row, NULL: off.
+ * d_temperature: NULL is 1; 0 or less takes the likeliest token (the lowest id
+ * of several).  d_top_k: 0 or less is off; d_top_p: 1 or more is off; d_min_p: 0 or
+ * less is off.  d_uniform: the random numbers, 0 <= u < 1 (NULL: the likeliest
+ * token in every row). */
+typedef struct {
+  const float* d_temperature;
+  const int32_t* d_top_k;
+  const float* d_top_p;
+  const float* d_min_p;
+  const double* d_uniform;
+} xgm_draw_rules;
+/* The logits ([B, V] of dt, B <= max_rows, V <= the sampler's) go through the rules (NULL: none) in
+ * 32 bits; nothing is written back to them.  NaN counts as -inf there, +inf as the
+ * largest finite number.  With w = exp((y - max) / temperature) and tokens in
+ * falling order of y, lower ids first among equals: the first top_k are kept;
+ * of those the shortest beginning with at least top_p of their sum of w; of those the ones with w >=
+ * min_p; always the first.  d_ids[b] becomes the lowest kept id at which the
+ * sum of w over the kept ids up to it exceeds u times the sum over all kept
+ * ids, and d_logprobs[b] (may be NULL) its logarithm of w / sum of w over all
+ * tokens of the row, kept or not (at temperature 1 where the likeliest is taken).  A row without a logit above -inf (nothing is
+ * allowed) gets -1 and -inf.  draw NULL: the likeliest token.  w and its sums are in 64
+ * bits, and the same inputs give the same results; a token whose w is below 2^-43 may never be drawn. */
+int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, int32_t V, int64_t row_stride_elems,
+               const xgm_logit_rules* rules, const xgm_draw_rules* draw, int32_t* d_ids, float* d_logprobs,
+               void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -107,6 +107,11 @@ SIGNATURES = {
     "xgm_batch_overflow_count_device": (_vp, [_vp]),
     "xgm_overflow_total": (_i64, []),
     "xgm_apply_token_bitmask_inplace": (_i32, [_vp, _i32, _i32, _i32, _i64, _vp, _i32, _vp, _i32, _vp]),
+    "xgm_q4_logits": (_i32, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _i64, _vp, _vp]),
+    "xgm_process_logits": (_i32, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _i64, _vp]),
+    "xgm_sampler_create": (_i32, [_i32, _i32, _vp, _pp]),
+    "xgm_sampler_destroy": (None, [_vp]),
+    "xgm_sample": (_i32, [_vp, _vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp]),
 }
 
 STATUS_NAMES = {
@@ -524,3 +529,61 @@ def overflow_total() -> int:
 def apply_token_bitmask_inplace(d_logits: int, dtype: int, B: int, V_logits: int, row_stride: int, d_bitmask: int,
                                 V_mask: int, d_row_index: int = 0, n_rows: int = None, stream: int = 0):
     _fast.apply(d_logits, dtype, B, V_logits, row_stride, d_bitmask, V_mask, d_row_index, B if n_rows is None else n_rows, stream)
+
+
+def q4_logits(d_hidden: int, dtype: int, rows: int, k: int, hidden_stride: int, d_codes: int, d_scales: int, d_zeros: int, v: int, group: int,
+              d_logits: int, logits_dtype: int, row_stride: int, d_bitmask: int = 0, stream: int = 0):
+    """Logits from hidden states and a 4-bit matrix, under the masks (xgm_q4_logits)."""
+    _fast.q4_logits(d_hidden, dtype, rows, k, hidden_stride, d_codes, d_scales, d_zeros, v, group, d_logits, logits_dtype, row_stride, d_bitmask, stream)
+
+
+class _Struct:
+    """A struct of the C interface in host memory: device addresses and numbers by name, absent ones are null."""
+
+    _pointers, _numbers = (), ()
+
+    def __init_subclass__(cls):
+        cls._type = type("_" + cls.__name__, (ctypes.Structure,), {"_fields_": [(n, _vp) for n in cls._pointers] + list(cls._numbers)})
+
+    def __init__(self, **values):
+        number = {n for n, _ in self._numbers}
+        unknown = set(values) - number - set(self._pointers)
+        if unknown:
+            raise TypeError(f"{type(self).__name__}: unknown {', '.join(sorted(unknown))}")
+        self._s = self._type(**{n: int(v) if n in number else (int(v) if v else None) for n, v in values.items()})
+        self._addr = ctypes.addressof(self._s)
+
+
+class LogitRules(_Struct):
+    """The rules on a batch's logits (xgm_logit_rules); the arrays are the caller's and must outlive the calls that read them."""
+
+    _pointers = ("d_bitmask", "d_tokens", "d_n_tokens", "d_n_prompt", "d_repetition", "d_frequency", "d_presence", "d_bias_ids", "d_bias",
+                 "d_bias_offsets")
+    _numbers = (("token_stride", _i64), ("v_mask", _i32), ("n_bias", _i32))
+
+
+class DrawRules(_Struct):
+    """How rows are drawn (xgm_draw_rules); the arrays are the caller's and must outlive the calls that read them."""
+
+    _pointers = ("d_temperature", "d_top_k", "d_top_p", "d_min_p", "d_uniform")
+
+
+def process_logits(d_logits: int, dtype: int, rows: int, v: int, row_stride: int, rules, d_out: int, out_stride: int, stream: int = 0):
+    """Logits under penalties, biases and masks (xgm_process_logits); rules: a LogitRules, or None."""
+    _fast.process_logits(d_logits, dtype, rows, v, row_stride, rules, d_out, out_stride, stream)
+
+
+class Sampler:
+    """One token a row from logits (xgm_sampler): working memory for up to max_rows rows of v logits."""
+
+    def __init__(self, max_rows: int, v: int, stream: int = 0):
+        h = ctypes.c_void_p()
+        _check(load_library().xgm_sampler_create(int(max_rows), int(v), ctypes.c_void_p(stream), ctypes.byref(h)))
+        self._h = h.value
+
+    def __del__(self, _destroy=_destroy):
+        _destroy("xgm_sampler_destroy", self)
+
+    def sample(self, d_logits: int, dtype: int, rows: int, v: int, row_stride: int, rules, draw, d_ids: int, d_logprobs: int = 0, stream: int = 0):
+        """rules: a LogitRules, or None; draw: a DrawRules, or None (the likeliest token)."""
+        _fast.sample(self, d_logits, dtype, rows, v, row_stride, rules, draw, d_ids, d_logprobs, stream)

@@ -19,6 +19,7 @@
 #include "engine.hpp"
 #include "schema.hpp"
 #include "kernels.hpp"
+#include "logits.hpp"
 #include "walk.hpp"
 
 using namespace xgm;
@@ -2241,6 +2242,156 @@ int xgm_apply_token_bitmask_inplace(void* d_logits, xgm_dtype dt, int32_t B, int
   require_device();
   launch_apply(d_logits, esize, ninf, V_logits, row_stride_elems, reinterpret_cast<const uint32_t*>(d_bitmask), V_mask,
                d_row_index, n_rows, static_cast<hipStream_t>(hip_stream));
+  HIP_OK(hipGetLastError());
+  return XGM_OK;
+  API_END
+}
+
+// ------------------------------------------------- from hidden states to tokens
+}  // extern "C"
+struct xgm_sampler {
+  int32_t max_rows = 0, V = 0;
+  void* memory = nullptr;
+};
+namespace {
+bool elem_of(xgm_dtype dt, Elem* e, int* size) {
+  switch (dt) {
+    case XGM_F32: *e = Elem::kF32; *size = 4; return true;
+    case XGM_BF16: *e = Elem::kBF16; *size = 2; return true;
+    case XGM_F16: *e = Elem::kF16; *size = 2; return true;
+  }
+  return false;
+}
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+// what is wrong with the logits of a call, or null
+const char* logits_fault(const void* d_logits, int size, int32_t B, int32_t V, int64_t stride) {
+  if (!d_logits) return "null logits";
+  if (B <= 0 || V <= 0) return "sizes must be positive";
+  if (B > XGM_MAX_ROWS) return "more than XGM_MAX_ROWS rows";
+  if (stride < V) return "row stride smaller than the row";
+  if (!aligned(d_logits, size)) return "logits pointer is not aligned to its element size";
+  return nullptr;
+}
+// the rules of a call, checked; null `r`: none
+const char* rules_fault(const xgm_logit_rules* r, LogitRules* out) {
+  *out = LogitRules{};
+  if (!r) return nullptr;
+  if (r->d_bitmask) {
+    if (r->v_mask <= 0) return "a bitmask without v_mask";
+    out->mask = reinterpret_cast<const uint32_t*>(r->d_bitmask);
+    out->W_mask = xgm_bitmask_words(r->v_mask);
+    out->V_mask = r->v_mask;
+  }
+  if (r->d_tokens) {
+    if (!r->d_n_tokens || r->token_stride <= 0) return "a history without its lengths or its stride";
+    if (r->token_stride > INT32_MAX) return "token stride beyond 2^31 - 1";
+    out->tokens = r->d_tokens;
+    out->token_stride = r->token_stride;
+    out->n_tokens = r->d_n_tokens;
+    out->n_prompt = r->d_n_prompt;
+    out->repetition = r->d_repetition;
+    out->frequency = r->d_frequency;
+    out->presence = r->d_presence;
+  } else if (r->d_repetition || r->d_frequency || r->d_presence) {
+    return "penalties without a history";
+  }
+  if (r->d_bias_ids) {
+    if (!r->d_bias || !r->d_bias_offsets || r->n_bias < 0) return "bias ids without biases, offsets or their number";
+    out->bias_ids = r->d_bias_ids;
+    out->bias = r->d_bias;
+    out->bias_offsets = r->d_bias_offsets;
+    out->n_bias = r->n_bias;
+  }
+  return nullptr;
+}
+}  // namespace
+extern "C" {
+int xgm_q4_logits(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32_t K, int64_t hidden_stride_elems, const uint8_t* d_codes,
+                  const void* d_scales, const uint8_t* d_zeros, int32_t V, int32_t group, void* d_logits, xgm_dtype logits_dt,
+                  int64_t logits_stride_elems, const int32_t* d_bitmask, void* hip_stream) {
+  API_BEGIN
+  if (!d_hidden || !d_codes || !d_scales) return fail(XGM_ERR_BAD_ARG, "q4_logits: null hidden states, codes or scales");
+  Elem hidden, logits;
+  int hidden_size, logits_size;
+  if (!elem_of(hidden_dt, &hidden, &hidden_size) || hidden == Elem::kF32) return fail(XGM_ERR_BAD_ARG, "q4_logits: hidden states are bf16 or f16");
+  if (!elem_of(logits_dt, &logits, &logits_size)) return fail(XGM_ERR_BAD_ARG, "q4_logits: unknown dtype");
+  if (const char* what = logits_fault(d_logits, logits_size, B, V, logits_stride_elems)) return fail(XGM_ERR_BAD_ARG, std::string("q4_logits: ") + what);
+  if (group <= 0 || group % 32 != 0 || K <= 0 || K % group != 0) return fail(XGM_ERR_BAD_ARG, "q4_logits: group must be a multiple of 32 that divides K");
+  if (K > XGM_MAX_HIDDEN) return fail(XGM_ERR_TOO_LARGE, "q4_logits: more than XGM_MAX_HIDDEN columns");
+  if (hidden_stride_elems < K) return fail(XGM_ERR_BAD_ARG, "q4_logits: hidden stride smaller than the row");
+  if (!aligned(d_hidden, 16) || hidden_stride_elems % 8 != 0 || !aligned(d_codes, 16))
+    return fail(XGM_ERR_BAD_ARG, "q4_logits: hidden rows and codes must be 16-byte aligned");
+  if (!aligned(d_scales, hidden_size)) return fail(XGM_ERR_BAD_ARG, "q4_logits: scales are not aligned to their element size");
+  require_device();
+  Head h{d_hidden, hidden_stride_elems, d_codes, d_scales, d_zeros, d_logits, logits_stride_elems, reinterpret_cast<const uint32_t*>(d_bitmask),
+         B, K, V, group, xgm_bitmask_words(V)};
+  launch_q4_logits(h, hidden, logits, static_cast<hipStream_t>(hip_stream));
+  HIP_OK(hipGetLastError());
+  return XGM_OK;
+  API_END
+}
+
+int xgm_process_logits(const void* d_logits, xgm_dtype dt, int32_t B, int32_t V, int64_t row_stride_elems, const xgm_logit_rules* rules, void* d_out,
+                       int64_t out_stride_elems, void* hip_stream) {
+  API_BEGIN
+  Elem type;
+  int size;
+  if (!elem_of(dt, &type, &size)) return fail(XGM_ERR_BAD_ARG, "process_logits: unknown dtype");
+  const char* what = logits_fault(d_logits, size, B, V, row_stride_elems);
+  if (!what) what = logits_fault(d_out, size, B, V, out_stride_elems);
+  if (!what && d_out == d_logits && out_stride_elems != row_stride_elems) what = "in place with two strides";
+  LogitRules r;
+  if (!what) what = rules_fault(rules, &r);
+  if (what) return fail(XGM_ERR_BAD_ARG, std::string("process_logits: ") + what);
+  require_device();
+  launch_process_logits(Logits{d_logits, row_stride_elems, V}, type, B, r, d_out, out_stride_elems, static_cast<hipStream_t>(hip_stream));
+  HIP_OK(hipGetLastError());
+  return XGM_OK;
+  API_END
+}
+
+int xgm_sampler_create(int32_t max_rows, int32_t V, void* hip_stream, xgm_sampler** out) {
+  API_BEGIN
+  if (!out) return fail(XGM_ERR_BAD_ARG, "sampler_create: out is null");
+  *out = nullptr;
+  if (max_rows <= 0 || V <= 0) return fail(XGM_ERR_BAD_ARG, "sampler_create: sizes must be positive");
+  if (max_rows > XGM_MAX_ROWS || V > XGM_MAX_LOGITS) return fail(XGM_ERR_TOO_LARGE, "sampler_create: more than XGM_MAX_ROWS rows or XGM_MAX_LOGITS logits");
+  require_device();
+  std::unique_ptr<xgm_sampler> s(new xgm_sampler());
+  s->max_rows = max_rows;
+  s->V = V;
+  const size_t bytes = sampler_bytes(max_rows, V);
+  s->memory = dev_alloc<char>(bytes);
+  hipError_t e = hipMemsetAsync(s->memory, 0, bytes, static_cast<hipStream_t>(hip_stream));
+  if (e == hipSuccess) e = hipStreamSynchronize(static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) {
+    (void)hipFree(s->memory);
+    hip_check(e, "sampler_create");
+  }
+  *out = s.release();
+  return XGM_OK;
+  API_END
+}
+void xgm_sampler_destroy(xgm_sampler* s) {
+  if (!s) return;
+  (void)hipFree(s->memory);
+  delete s;
+}
+int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, int32_t V, int64_t row_stride_elems, const xgm_logit_rules* rules,
+               const xgm_draw_rules* draw, int32_t* d_ids, float* d_logprobs, void* hip_stream) {
+  API_BEGIN
+  if (!s || !d_ids) return fail(XGM_ERR_BAD_ARG, "sample: null sampler or ids");
+  Elem type;
+  int size;
+  if (!elem_of(dt, &type, &size)) return fail(XGM_ERR_BAD_ARG, "sample: unknown dtype");
+  const char* what = logits_fault(d_logits, size, B, V, row_stride_elems);
+  LogitRules r;
+  if (!what) what = rules_fault(rules, &r);
+  if (what) return fail(XGM_ERR_BAD_ARG, std::string("sample: ") + what);
+  if (B > s->max_rows || V > s->V) return fail(XGM_ERR_BAD_ARG, "sample: more rows or logits than the sampler was created for");
+  require_device();
+  const DrawRules d = draw ? DrawRules{draw->d_temperature, draw->d_top_k, draw->d_top_p, draw->d_min_p, draw->d_uniform} : DrawRules{};
+  launch_sample(Logits{d_logits, row_stride_elems, V}, type, B, r, d, s->memory, d_ids, d_logprobs, static_cast<hipStream_t>(hip_stream));
   HIP_OK(hipGetLastError());
   return XGM_OK;
   API_END

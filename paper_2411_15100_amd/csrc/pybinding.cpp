@@ -28,6 +28,9 @@ struct {
   int (*batch_fork)(void*, const void*, void*);
   int (*batch_fill_next_token_bitmask)(void*, void*, void*);
   int (*batch_fill_and_apply)(void*, void*, void*, int, int32_t, int64_t, void*);
+  int (*q4_logits)(const void*, int, int32_t, int32_t, int64_t, const void*, const void*, const void*, int32_t, int32_t, void*, int, int64_t, const void*, void*);
+  int (*process_logits)(const void*, int, int32_t, int32_t, int64_t, const void*, void*, int64_t, void*);
+  int (*sample)(void*, const void*, int, int32_t, int32_t, int64_t, const void*, const void*, void*, void*, void*);
 } api;
 struct { const char* name; void** slot; } const kEntries[] = {
     {"xgm_last_error", (void**)&api.last_error},
@@ -43,6 +46,9 @@ struct { const char* name; void** slot; } const kEntries[] = {
     {"xgm_batch_fork", (void**)&api.batch_fork},
     {"xgm_batch_fill_next_token_bitmask", (void**)&api.batch_fill_next_token_bitmask},
     {"xgm_batch_fill_and_apply", (void**)&api.batch_fill_and_apply},
+    {"xgm_q4_logits", (void**)&api.q4_logits},
+    {"xgm_process_logits", (void**)&api.process_logits},
+    {"xgm_sample", (void**)&api.sample},
 };
 PyObject* g_error_class = nullptr;  // XgmError(status, message)
 PyObject *s_h, *s_addr, *s_matchers;
@@ -279,6 +285,60 @@ PyObject* apply(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return result(rc);
 }
 
+// q4_logits(d_hidden, dtype, rows, k, hidden_stride, d_codes, d_scales, d_zeros, v, group, d_logits, logits_dtype, row_stride, d_bitmask, stream)
+PyObject* q4_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 15) return PyErr_Format(PyExc_TypeError, "q4_logits takes 15 arguments");
+  int64_t v[15];
+  if (!values(args, v, "aiiiiaaaiiaiiaa")) return nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = api.q4_logits(pointer(v[0]), (int)v[1], (int32_t)v[2], (int32_t)v[3], v[4], pointer(v[5]), pointer(v[6]), pointer(v[7]), (int32_t)v[8], (int32_t)v[9],
+                     pointer(v[10]), (int)v[11], v[12], pointer(v[13]), pointer(v[14]));
+  Py_END_ALLOW_THREADS
+  return result(rc);
+}
+// rules: an object with the address of its struct, or None; a reference to it is held for the call
+class Rules {
+ public:
+  bool get(PyObject* o) {
+    if (!o || o == Py_None) return true;
+    Py_INCREF(o);
+    kept_ = o;
+    return attribute(o, s_addr, &at_);
+  }
+  ~Rules() { Py_XDECREF(kept_); }
+  void* at() const { return at_; }
+
+ private:
+  PyObject* kept_ = nullptr;
+  void* at_ = nullptr;
+};
+// process_logits(d_logits, dtype, rows, v, row_stride, rules, d_out, out_stride, stream)
+PyObject* process_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 9) return PyErr_Format(PyExc_TypeError, "process_logits takes 9 arguments");
+  int64_t v[5], o[3];
+  Rules r;
+  if (!values(args, v, "aiiii") || !r.get(args[5]) || !values(args + 6, o, "aia")) return nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = api.process_logits(pointer(v[0]), (int)v[1], (int32_t)v[2], (int32_t)v[3], v[4], r.at(), pointer(o[0]), o[1], pointer(o[2]));
+  Py_END_ALLOW_THREADS
+  return result(rc);
+}
+// sample(sampler, d_logits, dtype, rows, v, row_stride, rules, draw, d_ids, d_logprobs, stream)
+PyObject* sample(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 11) return PyErr_Format(PyExc_TypeError, "sample takes 11 arguments");
+  int64_t v[5], o[3];
+  Rules r, d;
+  void* h;
+  if (!attribute(args[0], s_h, &h) || !values(args + 1, v, "aiiii") || !r.get(args[6]) || !d.get(args[7]) || !values(args + 8, o, "aaa")) return nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = api.sample(h, pointer(v[0]), (int)v[1], (int32_t)v[2], (int32_t)v[3], v[4], r.at(), d.at(), pointer(o[0]), pointer(o[1]), pointer(o[2]));
+  Py_END_ALLOW_THREADS
+  return result(rc);
+}
+
 #define FAST(fn) (PyCFunction)(void (*)(void))(fn), METH_FASTCALL
 #define FAST_KW(fn) (PyCFunction)(void (*)(void))(fn), METH_FASTCALL | METH_KEYWORDS
 PyMethodDef kMatcherMethods[] = {
@@ -323,6 +383,9 @@ PyMethodDef kFunctions[] = {
     {"fill", FAST(fill), nullptr},
     {"fill_and_apply", FAST(fill_and_apply), nullptr},
     {"apply", FAST(apply), nullptr},
+    {"q4_logits", FAST(q4_logits), nullptr},
+    {"process_logits", FAST(process_logits), nullptr},
+    {"sample", FAST(sample), nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "the per-step calls of binding.py", -1, kFunctions, nullptr, nullptr, nullptr, nullptr};
