@@ -15,8 +15,8 @@ LIB = os.path.join(HERE, "libxgm.so")
 EXT = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
 EXT_UNTAGGED = os.path.join(HERE, "_native.so")  # (any Python would load it)
 EXT_SOURCE = os.path.join(CSRC, "pybinding.cpp")
-SOURCES = ["automaton.cpp", "engine.cpp", "schema.cpp", "api.cpp", "kernels.hip", "logits.hip"]
-HEADERS = ["automaton.hpp", "engine.hpp", "schema.hpp", "kernels.hpp", "logits.hpp", "walk.hpp", os.path.join("..", "..", "include", "xgm.h")]
+SOURCES = ["automaton.cpp", "engine.cpp", "schema.cpp", "api.cpp", "kernels.hip", "head.hip", "logits.hip"]
+HEADERS = ["automaton.hpp", "engine.hpp", "schema.hpp", "kernels.hpp", "logits.hpp", "elements.hpp", "walk.hpp", os.path.join("..", "..", "include", "xgm.h")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,64 +1,15 @@
-// What lies around the mask in a decode step (sections 2.1 and 3.5: the mask goes
-// to masked sampling): the output projection in 4 bits, rules on logits, and
-// drawing one token a row.
+// What lies behind the mask in a decode step (sections 2.1 and 3.5: the mask goes
+// to masked sampling): rules on logits, and drawing one token a row.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
 
+#include "elements.hpp"
 #include "logits.hpp"
 
 namespace xgm {
 
 namespace {
-
-typedef unsigned long long u64;
-
-template <Elem E> struct Type;
-template <> struct Type<Elem::kF32> { typedef uint32_t bits; };
-template <> struct Type<Elem::kBF16> { typedef uint16_t bits; };
-template <> struct Type<Elem::kF16> { typedef uint16_t bits; };
-
-template <Elem E> __device__ __forceinline__ float widened(typename Type<E>::bits v) {
-  if constexpr (E == Elem::kF32) return __uint_as_float(v);
-  if constexpr (E == Elem::kBF16) return __uint_as_float((uint32_t)v << 16);
-  if constexpr (E == Elem::kF16) return (float)__builtin_bit_cast(_Float16, v);
-}
-// rounded to nearest, ties to even; a NaN stays one
-template <Elem E> __device__ __forceinline__ typename Type<E>::bits narrowed(float f) {
-  if constexpr (E == Elem::kF32) return __float_as_uint(f);
-  if constexpr (E == Elem::kBF16) return __builtin_bit_cast(uint16_t, (__bf16)f);
-  if constexpr (E == Elem::kF16) return __builtin_bit_cast(uint16_t, (_Float16)f);
-}
-
-// ------------------------------------------------------- 4-bit output projection
-constexpr int kHeadThreads = 256;
-
-// A wave takes one row of the matrix and one of the batch; its lanes take the columns 8 at a time.
-template <Elem H, Elem O>
-__global__ __launch_bounds__(kHeadThreads) void q4_logits_kernel(Head h) {
-  const int32_t v = (int32_t)(blockIdx.x * (kHeadThreads / 64) + (threadIdx.x >> 6)), b = (int32_t)blockIdx.y, lane = (int32_t)(threadIdx.x & 63u);
-  if (v >= h.V) return;
-  typename Type<O>::bits* out = static_cast<typename Type<O>::bits*>(h.logits) + (int64_t)b * h.logits_stride + v;
-  if (h.mask && !(h.mask[(size_t)b * h.W_mask + (v >> 5)] >> (v & 31) & 1u)) {
-    if (lane == 0) *out = narrowed<O>(-__builtin_inff());
-    return;
-  }
-  const typename Type<H>::bits* x = static_cast<const typename Type<H>::bits*>(h.hidden) + (int64_t)b * h.hidden_stride;
-  const typename Type<H>::bits* scales = static_cast<const typename Type<H>::bits*>(h.scales) + (size_t)v * (h.K / h.group);
-  const uint8_t* zeros = h.zeros ? h.zeros + (size_t)v * (h.K / h.group) : nullptr;
-  const uint8_t* codes = h.codes + (size_t)v * (h.K / 2);
-  float sum = 0.0f;
-  for (int32_t k = lane * 8; k < h.K; k += 512) {
-    const uint32_t n = *reinterpret_cast<const uint32_t*>(codes + k / 2);
-    const int32_t g = k / h.group;
-    const float z = zeros ? (float)zeros[g] : 8.0f;
-    float part = 0.0f;
-    for (int j = 0; j < 8; ++j) part += widened<H>(x[k + j]) * ((float)(n >> (4 * j) & 15u) - z);
-    sum += part * widened<H>(scales[g]);
-  }
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  if (lane == 0) *out = narrowed<O>(sum);
-}
 
 // --------------------------------------------------------------- rules on logits
 constexpr int kRuleThreads = 256;
@@ -306,19 +257,7 @@ template <Elem E> struct Process {
     else launch_process<E, E>(in, B, r, out, out_stride, stream);
   }
 };
-template <Elem O> struct Project {
-  static void run(const Head& h, const bool& f16, const hipStream_t& stream) {
-    const dim3 grid((h.V + kHeadThreads / 64 - 1) / (kHeadThreads / 64), h.B);
-    if (f16) hipLaunchKernelGGL((q4_logits_kernel<Elem::kF16, O>), grid, dim3(kHeadThreads), 0, stream, h);
-    else hipLaunchKernelGGL((q4_logits_kernel<Elem::kBF16, O>), grid, dim3(kHeadThreads), 0, stream, h);
-  }
-};
-
 }  // namespace
-
-void launch_q4_logits(const Head& h, Elem hidden_type, Elem logits_type, hipStream_t stream) {
-  by_type<Project>(logits_type, h, hidden_type == Elem::kF16, stream);
-}
 
 void launch_process_logits(const Logits& in, Elem type, int32_t B, const LogitRules& rules, void* out, int64_t out_stride, hipStream_t stream) {
   by_type<Process>(type, in, B, rules, out, out_stride, false, stream);

@@ -1,5 +1,6 @@
 // Device-side views and launchers of what lies around the mask in a decode
-// step: 4-bit output projection, rules on logits, drawing tokens (logits.hip).
+// step: 4-bit output projection (head.hip), rules on
+// logits, drawing tokens (logits.hip).
 #pragma once
 #include <hip/hip_runtime_api.h>
 
