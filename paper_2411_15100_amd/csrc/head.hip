@@ -2,6 +2,8 @@
 // its value, so its row of the matrix need not be read).
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "elements.hpp"
 #include "logits.hpp"
 
@@ -24,14 +26,18 @@ template <Elem H> __device__ __forceinline__ float4v mfma(uint4v a, uint4v b, fl
 // A code n becomes the number 16 + n by one AND-OR: the code's bits are the top of the mantissa of 16.  Codes i and i + 4 of
 // a word end up next to each other, so columns are taken in the order 0 4 1 5 2 6 3 7 on both sides.  What the 16 and the
 // zero point add is (16 + zero) times the sum of the hidden states, exact in its products as the rest is.
-template <Elem H> __device__ __forceinline__ uint4v numbers(uint32_t w) {
-  if constexpr (H == Elem::kBF16)
-    return uint4v{(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u,
-                  (w >> 9 & 0x00780078u) | 0x41804180u};
-  else
-    return uint4v{(w << 6 & 0x03c003c0u) | 0x4c004c00u, (w << 2 & 0x03c003c0u) | 0x4c004c00u, (w >> 2 & 0x03c003c0u) | 0x4c004c00u,
-                  (w >> 6 & 0x03c003c0u) | 0x4c004c00u};
-}
+// (The two constants are kept from the compiler, which else spends an AND and an OR with a literal each: an instruction takes one
+// of them from a scalar register and the other from a vector register.)
+template <Elem H> struct Numbers {
+  uint32_t mask = H == Elem::kBF16 ? 0x00780078u : 0x03c003c0u, sixteen = H == Elem::kBF16 ? 0x41804180u : 0x4c004c00u;
+  __device__ __forceinline__ Numbers() { asm("" : "+s"(mask), "+v"(sixteen)); }
+  __device__ __forceinline__ uint4v operator()(uint32_t w) const {
+    if constexpr (H == Elem::kBF16)
+      return uint4v{(w << 3 & mask) | sixteen, (w >> 1 & mask) | sixteen, (w >> 5 & mask) | sixteen, (w >> 9 & mask) | sixteen};
+    else
+      return uint4v{(w << 6 & mask) | sixteen, (w << 2 & mask) | sixteen, (w >> 2 & mask) | sixteen, (w >> 6 & mask) | sixteen};
+  }
+};
 template <Elem H> constexpr uint32_t kOnes = H == Elem::kBF16 ? 0x3f803f80u : 0x3c003c00u;
 
 // 8 hidden states in that order
@@ -64,7 +70,8 @@ __device__ __forceinline__ void store_logit(const Head& h, Elem type, int64_t at
 // Under masks the workgroup lists the rows of its share that some request allows, and its waves take 16 of those at a time.
 // Where a workgroup has fewer tiles than waves, several waves take the steps of one in turn and their sums meet in LDS.
 // P: parts of a step that have a scale of their own: 4 (groups of 128 or a multiple), 8 (64) or 16 (32, or other multiples of it).
-constexpr int kFewMaxThreads = 1024;
+constexpr int kFewMaxThreads = 1024;  // of NB = 1; two rows of products need the registers of half as many waves
+template <int NB> constexpr int kFewThreads = kFewMaxThreads / NB;
 constexpr int kFewRows = 1024;  // of the matrix at a time (a list of them lies in LDS)
 constexpr int kChunks = 4;      // of a step
 constexpr size_t kFewHiddenBytes = 128 * 1024;  // at most, of hidden states in LDS
@@ -105,8 +112,42 @@ __device__ __forceinline__ void load_groups(StepGroups<P, Z>& g, const uint16_t*
   }
 }
 
+// Lists the rows of the matrix among the `here` <= kFewRows from `base` (a multiple of 16) on that some of the `rows` rows of the batch
+// from first_b on allows, as numbers behind base, and masks the logits of the others.  Returns how many.
+__device__ int32_t list_rows(const Head& h, Elem out_type, int32_t first_b, int32_t rows, int64_t base, int32_t here, int32_t* list, uint32_t* any, int32_t* n_listed) {
+  const int32_t tid = (int32_t)threadIdx.x, threads = (int32_t)blockDim.x;
+  __syncthreads();
+  if (tid < kFewRows / 32) any[tid] = 0;
+  if (tid == 0) *n_listed = 0;
+  __syncthreads();
+  const int32_t w0 = (int32_t)(base >> 5), shift = (int32_t)(base & 31), words = (here + shift + 31) / 32;
+  for (int32_t i = tid; i < words * rows; i += threads) {
+    const int32_t b = i / words, w = i % words;
+    const uint32_t m = h.mask[(size_t)(first_b + b) * h.W_mask + w0 + w];
+    if (m && shift) {
+      if (w > 0) atomicOr(&any[w - 1], m << 16);
+      if (w < kFewRows / 32) atomicOr(&any[w], m >> 16);
+    } else if (m) {
+      atomicOr(&any[w], m);
+    }
+  }
+  __syncthreads();
+  for (int32_t r = tid; r < here; r += threads) {
+    if (any[r >> 5] >> (r & 31) & 1u) {
+      int32_t place = __builtin_popcount(any[r >> 5] & ((1u << (r & 31)) - 1u));
+      for (int32_t w = 0; w < r >> 5; ++w) place += __builtin_popcount(any[w]);
+      list[place] = r;
+      atomicAdd(n_listed, 1);
+    } else {
+      for (int32_t b = 0; b < rows; ++b) store_logit(h, out_type, (int64_t)(first_b + b) * h.logits_stride + base + r, -__builtin_inff());
+    }
+  }
+  __syncthreads();
+  return *n_listed;
+}
+
 template <Elem H, int NB, int P, bool Z>
-__global__ __launch_bounds__(kFewMaxThreads) void q4_few_kernel(Head h, Elem out_type, int32_t tiles_each) {
+__global__ __launch_bounds__(kFewThreads<NB>) void q4_few_kernel(Head h, Elem out_type, int32_t tiles_each) {
   extern __shared__ __align__(16) char lds[];
   constexpr int kParts = P / kChunks, kProducts = 4 / kParts;  // of a chunk, of a part
   constexpr bool kAsTheyLie = kParts == 1;
@@ -136,6 +177,7 @@ __global__ __launch_bounds__(kFewMaxThreads) void q4_few_kernel(Head h, Elem out
   for (int nb = 0; nb < NB; ++nb) mine[nb] = hidden + q * rows + min(nb * 16 + n, rows - 1);
   auto state = [&](int32_t product, int nb) { return mine[nb][product * 4 * rows]; };  // (4 products to a chunk)
   bool summed = false;
+  const Numbers<H> numbers;
 
   const int32_t per_row = h.K / h.group, units = h.group / (512 / P);
   const uint32_t last_codes = (uint32_t)(h.K / 2 - 16);
@@ -144,34 +186,7 @@ __global__ __launch_bounds__(kFewMaxThreads) void q4_few_kernel(Head h, Elem out
     const int32_t here = (int32_t)min((int64_t)kFewRows, row1 - base);
     int32_t count = here;
     if (h.mask) {
-      __syncthreads();
-      if (tid < kFewRows / 32) any[tid] = 0;
-      if (tid == 0) *n_listed = 0;
-      __syncthreads();
-      const int32_t w0 = (int32_t)(base >> 5), shift = (int32_t)(base & 31), words = (here + shift + 31) / 32;  // (shares begin on 16)
-      for (int32_t i = tid; i < words * rows; i += threads) {
-        const int32_t b = i / words, w = i % words;
-        const uint32_t m = h.mask[(size_t)(first_b + b) * h.W_mask + w0 + w];
-        if (m && shift) {
-          if (w > 0) atomicOr(&any[w - 1], m << 16);
-          if (w < kFewRows / 32) atomicOr(&any[w], m >> 16);
-        } else if (m) {
-          atomicOr(&any[w], m);
-        }
-      }
-      __syncthreads();
-      for (int32_t r = tid; r < here; r += threads) {
-        if (any[r >> 5] >> (r & 31) & 1u) {
-          int32_t place = __builtin_popcount(any[r >> 5] & ((1u << (r & 31)) - 1u));
-          for (int32_t w = 0; w < r >> 5; ++w) place += __builtin_popcount(any[w]);
-          list[place] = r;
-          atomicAdd(n_listed, 1);
-        } else {
-          for (int32_t b = 0; b < rows; ++b) store_logit(h, out_type, (int64_t)(first_b + b) * h.logits_stride + base + r, -__builtin_inff());
-        }
-      }
-      __syncthreads();
-      count = *n_listed;
+      count = list_rows(h, out_type, first_b, rows, base, here, list, any, n_listed);
     }
     const int32_t tiles = (count + 15) / 16;
     int32_t sharing = 1;  // waves to a tile
@@ -239,7 +254,7 @@ __global__ __launch_bounds__(kFewMaxThreads) void q4_few_kernel(Head h, Elem out
               }
 #pragma unroll
               for (int i = r * kProducts; i < (r + 1) * kProducts; ++i) {
-                const uint4v w = numbers<H>(c[i]);
+                const uint4v w = numbers(c[i]);
                 for (int nb = 0; nb < NB; ++nb) part[nb] = mfma<H>(state((step * kChunks + j) * 4 + i, nb), w, part[nb]);
               }
               for (int nb = 0; nb < NB; ++nb) acc[nb] += part[nb] * scale;
@@ -274,34 +289,266 @@ __global__ __launch_bounds__(kFewMaxThreads) void q4_few_kernel(Head h, Elem out
   }
 }
 
-// ------------------------------------------------------------------ any number of columns
-constexpr int kAnyThreads = 256;
+// --------------------------------------------------------------- many rows in the batch
+// Up to 16 MW WM rows and any number of columns.  The eight waves of a workgroup form WM groups that share the rows of the batch, and
+// in each 8 / WM waves that share the matrix, up to four tiles each: 64 x 64 logits a wave for MW = 4, for which it reads 4 KB of
+// hidden states and 1 KB of codes out of LDS per 16 products.  Columns go by chunks of 128.  The codes of a chunk are read from
+// memory three chunks before they are needed, by all waves in equal parts, and go through two buffers in LDS, hidden states
+// through three; one barrier a chunk.
+// A workgroup's share is cut into passes of the tiles that its waves hold.
+constexpr int kManyThreads = 512, kManyTiles = 4;  // tiles of a wave
 
-// A wave takes one row of the matrix and one of the batch; its lanes take the columns 8 at a time.
-template <Elem H>
-__global__ __launch_bounds__(kAnyThreads) void q4_any_kernel(Head h, Elem out_type) {
-  const int32_t v = (int32_t)(blockIdx.x * (kAnyThreads / 64) + (threadIdx.x >> 6)), b = (int32_t)blockIdx.y, lane = (int32_t)(threadIdx.x & 63u);
-  if (v >= h.V) return;
-  const int64_t out = (int64_t)b * h.logits_stride + v;
-  if (h.mask && !(h.mask[(size_t)b * h.W_mask + (v >> 5)] >> (v & 31) & 1u)) {
-    if (lane == 0) store_logit(h, out_type, out, -__builtin_inff());
-    return;
+// How the parts of a chunk find their scales: one for the chunk, looked up by its number; halves; quarters; quarters that are looked up.
+enum Sharing : int { kWhole = 0, kHalves = 1, kQuarters = 2, kLookedUp = 3 };
+template <int S> constexpr int kPartsOf = S == kWhole ? 1 : S == kHalves ? 2 : 4;
+struct GroupIndex {
+  int32_t per_row;     // groups of a row
+  uint32_t reciprocal;  // of the parts in a group, in 2^-32 (0: one)
+};
+__device__ __forceinline__ int32_t group_of(GroupIndex g, int32_t part) {
+  return min(g.reciprocal ? (int32_t)__umulhi((uint32_t)part, g.reciprocal) : part, g.per_row - 1);
+}
+template <int S, bool Z> struct ChunkGroups {  // scales and zero points of a row over a chunk
+  uint32_t scales[S >= kQuarters ? 2 : 1];
+  uint32_t zeros;
+};
+// The row begins `row` groups behind the two addresses.  Parts behind the last column get some scale of the row (kLookedUp), or 0.
+template <int S, bool Z>
+__device__ __forceinline__ void load_chunk_groups(ChunkGroups<S, Z>& g, const uint16_t* scales, const uint8_t* zeros, uint32_t row, int32_t chunk, GroupIndex index) {
+  if constexpr (S == kWhole) {
+    const uint32_t at = row + (uint32_t)group_of(index, chunk);
+    g.scales[0] = scales[at];
+    if constexpr (Z) g.zeros = zeros[at];
+  } else if constexpr (S == kLookedUp) {
+    g.scales[0] = g.scales[1] = g.zeros = 0;
+    for (int p = 0; p < 4; ++p) {
+      const uint32_t at = row + (uint32_t)group_of(index, chunk * 4 + p);
+      g.scales[p / 2] |= (uint32_t)scales[at] << (16 * (p & 1));
+      if constexpr (Z) g.zeros |= (uint32_t)zeros[at] << (8 * p);
+    }
+  } else {
+    constexpr int P = kPartsOf<S>;
+    const int32_t first = min(chunk * P, index.per_row - P), behind = chunk * P - first;
+    if constexpr (S == kHalves) {
+      uint32_t x;
+      __builtin_memcpy(&x, scales + row + first, 4);
+      g.scales[0] = x >> (16 * behind);
+      if constexpr (Z) {
+        uint16_t z;
+        __builtin_memcpy(&z, zeros + row + first, 2);
+        g.zeros = (uint32_t)z >> (8 * behind);
+      }
+    } else {
+      uint64_t x;
+      __builtin_memcpy(&x, scales + row + first, 8);
+      x >>= 16 * behind;
+      g.scales[0] = (uint32_t)x;
+      g.scales[1] = (uint32_t)(x >> 32);
+      if constexpr (Z) {
+        uint32_t z;
+        __builtin_memcpy(&z, zeros + row + first, 4);
+        g.zeros = z >> (8 * behind);
+      }
+    }
   }
-  const uint16_t* x = static_cast<const uint16_t*>(h.hidden) + (int64_t)b * h.hidden_stride;
-  const uint16_t* scales = static_cast<const uint16_t*>(h.scales) + (size_t)v * (h.K / h.group);
-  const uint8_t* zeros = h.zeros ? h.zeros + (size_t)v * (h.K / h.group) : nullptr;
-  const uint8_t* codes = h.codes + (size_t)v * (h.K / 2);
-  float sum = 0.0f;
-  for (int32_t k = lane * 8; k < h.K; k += 512) {
-    const uint32_t n = *reinterpret_cast<const uint32_t*>(codes + k / 2);
-    const int32_t g = k / h.group;
-    const float z = zeros ? (float)zeros[g] : 8.0f;
-    float part = 0.0f;
-    for (int j = 0; j < 8; ++j) part += widened<H>(x[k + j]) * ((float)(n >> (4 * j) & 15u) - z);
-    sum += part * widened<H>(scales[g]);
+}
+
+template <Elem H, int MW, int WM, int S, bool Z>
+__global__ __launch_bounds__(kManyThreads, 2) void q4_many_kernel(Head h, Elem out_type, int32_t tiles_each, uint32_t reciprocal) {
+  constexpr int PC = kPartsOf<S>, kRows = 16 * MW * WM, kWaves = kManyThreads / 64, kWide = kWaves / WM;  // waves that share the matrix
+  constexpr int kPass = kWide * kManyTiles, kBring = kPass / kWaves;  // tiles of a pass; those of which a wave brings the codes
+  constexpr int kUnits = (kRows * 16 + kManyThreads - 1) / kManyThreads;  // 8 hidden states each, that a thread brings a chunk
+  constexpr int kProducts = 4 / PC;
+  __shared__ uint4v hidden[3][16 * (kRows + 1)];  // [product and quarter][row]; a row more keeps the writes of 16 quarters apart
+  __shared__ float4v sums[2][PC][kRows / 4];      // of the hidden states of a part
+  __shared__ uint4v codes[2][kPass][64];
+  __shared__ ChunkGroups<S, Z> groups[2][kPass][16];
+  __shared__ int32_t list[kFewRows];
+  __shared__ uint32_t any[kFewRows / 32];
+  __shared__ int32_t n_listed;
+  const int32_t tid = (int32_t)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t n = lane & 15, q = lane >> 4, wm = wave % WM, wn = wave / WM;
+  const int32_t first_b = (int32_t)blockIdx.y * kRows, rows = min(h.B - first_b, kRows);
+  const int32_t n_chunks = (h.K + 127) / 128;
+  const GroupIndex index{h.K / h.group, reciprocal};
+  const uint32_t last_codes = (uint32_t)(h.K / 2 - 16);
+  const Numbers<H> numbers;
+  const uint16_t* const all_states = static_cast<const uint16_t*>(h.hidden) + (int64_t)first_b * h.hidden_stride;
+
+  auto load_states = [&](int32_t chunk, uint4v (&x)[kUnits]) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int32_t at = u * kManyThreads + tid, b = min(at >> 4, rows - 1), k = chunk * 128 + (at & 15) * 8;
+      const uint4v v = *reinterpret_cast<const uint4v*>(all_states + (int64_t)b * h.hidden_stride + min(k, h.K - 8));
+      x[u] = k < h.K ? v : uint4v{0, 0, 0, 0};
+    }
+  };
+  auto put_states = [&](const uint4v (&x)[kUnits], int buffer) {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int32_t at = u * kManyThreads + tid, b = at >> 4, in = at & 15, place = PC == 1 ? (in & 3) * 4 + (in >> 2) : in;
+      if (kUnits * kManyThreads == kRows * 16 || b < kRows) hidden[buffer][place * (kRows + 1) + b] = in_order(x[u]);
+    }
+  };
+
+  const int64_t row0 = (int64_t)blockIdx.x * tiles_each * 16, row1 = min((int64_t)h.V, row0 + (int64_t)tiles_each * 16);
+  for (int64_t base = row0; base < row1; base += kFewRows) {
+    const int32_t here = (int32_t)min((int64_t)kFewRows, row1 - base);
+    int32_t count = here;
+    if (h.mask) count = list_rows(h, out_type, first_b, rows, base, here, list, any, &n_listed);
+    const int32_t tiles = (count + 15) / 16;
+    const uint8_t* const base_codes = h.codes + base * (h.K / 2);
+    const uint16_t* const base_scales = static_cast<const uint16_t*>(h.scales) + base * index.per_row;
+    const uint8_t* const base_zeros = Z ? h.zeros + base * index.per_row : nullptr;
+    auto row_of = [&](int32_t tile) -> uint32_t {
+      const int32_t i = min(tile * 16 + n, count - 1);
+      return (uint32_t)(h.mask ? list[i] : i);
+    };
+    for (int32_t pass = 0; pass < tiles; pass += kPass) {
+      const int32_t pass_tiles = min(kPass, tiles - pass), each = (pass_tiles + kWide - 1) / kWide;
+      const int32_t first = wn * each, mine = max(0, min(each, pass_tiles - first));
+      const int32_t bring = max(0, min(kBring, pass_tiles - wave * kBring));
+      uint32_t code_at[kBring], group_at[kBring];
+#pragma unroll
+      for (int c = 0; c < kBring; ++c) {
+        const uint32_t v = row_of(pass + wave * kBring + c);
+        code_at[c] = v * (uint32_t)(h.K / 2);
+        group_at[c] = v * (uint32_t)index.per_row;
+      }
+      struct Brought {
+        uint4v codes[kBring];
+        ChunkGroups<S, Z> groups[kBring];
+      };
+      auto load = [&](int32_t chunk, Brought& to) {
+        const uint32_t in_row = min((uint32_t)(chunk * 64 + q * 16), last_codes);
+#pragma unroll
+        for (int c = 0; c < kBring; ++c) {
+          if (c >= bring) break;
+          to.codes[c] = *reinterpret_cast<const uint4v*>(base_codes + (code_at[c] + in_row));
+          load_chunk_groups<S, Z>(to.groups[c], base_scales, base_zeros, group_at[c], chunk, index);
+        }
+      };
+      auto put = [&](const Brought& from, int buffer) {
+#pragma unroll
+        for (int c = 0; c < kBring; ++c) {
+          if (c >= bring) break;
+          codes[buffer][wave * kBring + c][lane] = PC == 1 ? from.codes[c] : exchanged(from.codes[c]);
+          if (q == 0) groups[buffer][wave * kBring + c][n] = from.groups[c];
+        }
+      };
+      float4v acc[kManyTiles][MW];
+#pragma unroll
+      for (int c = 0; c < kManyTiles; ++c)
+        for (int m = 0; m < MW; ++m) acc[c][m] = float4v{0, 0, 0, 0};
+      // the sums over the parts of a chunk, 16 rows to a wave
+      auto add_up = [&](int at, int buffer) {
+        if (wave >= kRows / 16) return;
+        const uint4v* const states = &hidden[at][q * (kRows + 1) + wave * 16 + n];
+        const uint4v ones = {kOnes<H>, kOnes<H>, kOnes<H>, kOnes<H>};
+#pragma unroll
+        for (int r = 0; r < PC; ++r) {
+          float4v s = {0, 0, 0, 0};
+          for (int i = r * kProducts; i < (r + 1) * kProducts; ++i) s = mfma<H>(states[i * 4 * (kRows + 1)], ones, s);
+          if (n == 0) sums[buffer][r][wave * 4 + q] = Z ? s : s * -24.0f;
+        }
+      };
+      auto multiply = [&](int at, int buffer) {
+        const uint4v* const states = &hidden[at][q * (kRows + 1) + wm * MW * 16 + n];
+#pragma unroll
+        for (int r = 0; r < PC; ++r) {
+          uint4v a[kProducts][MW];
+#pragma unroll
+          for (int i = 0; i < kProducts; ++i)
+            for (int m = 0; m < MW; ++m) a[i][m] = states[(r * kProducts + i) * 4 * (kRows + 1) + m * 16];
+          // the sums of a tile are scaled while the next one's products are made
+          float4v part[2][MW];
+          float scale[2] = {0.0f, 0.0f};
+#pragma unroll
+          for (int c = 0; c <= kManyTiles; ++c) {
+            if (c < mine && c < kManyTiles) {
+              const ChunkGroups<S, Z> g = groups[buffer][first + c][n];
+              const uint4v four = codes[buffer][first + c][lane];
+              scale[c & 1] = widened<H>((uint16_t)(g.scales[r / 2] >> (16 * (r & 1))));
+              const float shift = Z ? -16.0f - (float)(g.zeros >> (8 * r) & 255u) : 1.0f;
+              for (int m = 0; m < MW; ++m) {
+                part[c & 1][m] = sums[buffer][r][(wm * MW + m) * 4 + q];
+                if constexpr (Z) part[c & 1][m] *= shift;
+              }
+#pragma unroll
+              for (int i = 0; i < kProducts; ++i) {
+                const uint4v w = numbers(four[r * kProducts + i]);
+                for (int m = 0; m < MW; ++m) part[c & 1][m] = mfma<H>(a[i][m], w, part[c & 1][m]);
+              }
+            }
+            if (c > 0 && c <= mine)
+              for (int m = 0; m < MW; ++m) acc[c - 1][m] += part[(c - 1) & 1][m] * scale[(c - 1) & 1];
+            __builtin_amdgcn_sched_barrier(0);  // (what belongs to all tiles at once would not fit the registers)
+          }
+        }
+      };
+      uint4v x[kUnits];
+      Brought next_codes;
+      load_states(0, x);
+      load(0, next_codes);
+      __syncthreads();  // (the last pass has read its last chunk)
+      put_states(x, 0);
+      if (n_chunks > 1) {
+        load_states(1, x);
+        put_states(x, 1);
+      }
+      put(next_codes, 0);
+      if (n_chunks > 2) load_states(2, x);
+      if (n_chunks > 1) load(1, next_codes);
+      __syncthreads();
+      add_up(0, 0);
+      __syncthreads();
+      // multiplies a chunk, adds up the next one and puts into LDS what comes then: hidden states of the one after, in a ring
+      // of three buffers, and codes of the next
+      int ring = 0;
+#pragma unroll 1
+      for (int32_t chunk = 0; chunk < n_chunks; ++chunk) {
+        const int buffer = chunk & 1, next = ring == 2 ? 0 : ring + 1, last = next == 2 ? 0 : next + 1;
+        if (chunk + 1 < n_chunks) add_up(next, buffer ^ 1);
+        multiply(ring, buffer);
+        if (chunk + 2 < n_chunks) {
+          put_states(x, last);
+          if (chunk + 3 < n_chunks) load_states(chunk + 3, x);
+        }
+        if (chunk + 1 < n_chunks) {
+          put(next_codes, buffer ^ 1);
+          if (chunk + 2 < n_chunks) load(chunk + 2, next_codes);
+        }
+        ring = next;
+        __syncthreads();
+      }
+      auto store = [&](auto type) {
+        constexpr Elem O = decltype(type)::value;
+        int32_t row = wm * MW * 16 + q * 4;
+        asm volatile("" : "+v"(row));  // (else the addresses of all rows are computed ahead of the loops and fill the registers)
+        typename Type<O>::bits* const out = static_cast<typename Type<O>::bits*>(h.logits) + (int64_t)(first_b + row) * h.logits_stride + base;
+        for (int c = 0; c < kManyTiles; ++c) {
+          if (c >= mine || (pass + first + c) * 16 + n >= count) continue;
+          const uint32_t v = row_of(pass + first + c);
+          const int64_t token = base + v;
+#pragma unroll
+          for (int m = 0; m < MW; ++m)
+            for (int i = 0; i < 4; ++i) {
+              const int32_t b = row + m * 16 + i;
+              if (b >= rows) continue;
+              const bool ok = !h.mask || (h.mask[(size_t)(first_b + b) * h.W_mask + (token >> 5)] >> (token & 31) & 1u);
+              float y = 0.0f;
+#pragma unroll
+              for (int e = 0; e < kManyTiles; ++e)
+                if (e == c) y = acc[e][m][i];
+              out[(int64_t)(m * 16 + i) * h.logits_stride + v] = narrowed<O>(ok ? y : -__builtin_inff());
+            }
+        }
+      };
+      if (out_type == Elem::kF32) store(std::integral_constant<Elem, Elem::kF32>());
+      else if (out_type == Elem::kBF16) store(std::integral_constant<Elem, Elem::kBF16>());
+      else store(std::integral_constant<Elem, Elem::kF16>());
+    }
   }
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  if (lane == 0) store_logit(h, out_type, out, sum);
 }
 
 constexpr int kComputeUnits = 256;
@@ -311,7 +558,7 @@ template <Elem H, int NB, int P, bool Z> void launch_few(const Head& h, Elem out
   (void)prepared;
   const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), each = (tiles + kComputeUnits - 1) / kComputeUnits, steps = few_steps(h.K);
   int32_t threads = 64;  // waves for its tiles, or for the steps of the few that masks leave
-  while (threads < kFewMaxThreads && threads < 64 * (h.mask && steps > each ? steps : each * (each < 16 ? steps : 1))) threads *= 2;
+  while (threads < kFewThreads<NB> && threads < 64 * (h.mask && steps > each ? steps : each * (each < 16 ? steps : 1))) threads *= 2;
   const dim3 grid((tiles + each - 1) / each, (h.B + 16 * NB - 1) / (16 * NB));
   hipLaunchKernelGGL((q4_few_kernel<H, NB, P, Z>), grid, dim3(threads), few_layout(h.K, h.B < 16 * NB ? h.B : 16 * NB, P, NB).end, stream, h, out_type, each);
 }
@@ -324,12 +571,29 @@ template <Elem H, int NB> void launch_few_groups(const Head& h, Elem out_type, h
   else if (h.group == 64) launch_few_zeros<H, NB, 8>(h, out_type, stream);
   else launch_few_zeros<H, NB, 16>(h, out_type, stream);
 }
+template <Elem H, int MW, int WM, int S, bool Z> void launch_many(const Head& h, Elem out_type, hipStream_t stream) {
+  const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), each = (tiles + kComputeUnits - 1) / kComputeUnits;
+  const dim3 grid((tiles + each - 1) / each, (h.B + 16 * MW * WM - 1) / (16 * MW * WM));
+  const uint32_t parts = (uint32_t)(h.group / (128 / kPartsOf<S>));
+  hipLaunchKernelGGL((q4_many_kernel<H, MW, WM, S, Z>), grid, dim3(kManyThreads), 0, stream, h, out_type, each, parts > 1 ? (uint32_t)(((1ull << 32) + parts - 1) / parts) : 0u);
+}
+template <Elem H, int MW, int WM, int S> void launch_many_zeros(const Head& h, Elem out_type, hipStream_t stream) {
+  if (h.zeros) launch_many<H, MW, WM, S, true>(h, out_type, stream);
+  else launch_many<H, MW, WM, S, false>(h, out_type, stream);
+}
+template <Elem H, int MW, int WM> void launch_many_groups(const Head& h, Elem out_type, hipStream_t stream) {
+  if (h.group % 128 == 0) launch_many_zeros<H, MW, WM, kWhole>(h, out_type, stream);
+  else if (h.group == 64 && h.K >= 128) launch_many_zeros<H, MW, WM, kHalves>(h, out_type, stream);
+  else if (h.group == 32 && h.K >= 128) launch_many_zeros<H, MW, WM, kQuarters>(h, out_type, stream);
+  else launch_many_zeros<H, MW, WM, kLookedUp>(h, out_type, stream);
+}
 template <Elem H> void launch_head(const Head& h, Elem out_type, hipStream_t stream) {
   const size_t row = (size_t)few_steps(h.K) * kChunks * 256;  // bytes of LDS for a row of hidden states
-  if (h.B > 16 && row * (h.B < 32 ? h.B : 32) <= kFewHiddenBytes) return launch_few_groups<H, 2>(h, out_type, stream);
-  if (row * (h.B < 16 ? h.B : 16) <= kFewHiddenBytes) return launch_few_groups<H, 1>(h, out_type, stream);
-  const dim3 grid((h.V + kAnyThreads / 64 - 1) / (kAnyThreads / 64), h.B);
-  hipLaunchKernelGGL(q4_any_kernel<H>, grid, dim3(kAnyThreads), 0, stream, h, out_type);
+  if (h.B <= 16 && row * h.B <= kFewHiddenBytes) return launch_few_groups<H, 1>(h, out_type, stream);
+  if (h.B <= 32 && row * h.B <= kFewHiddenBytes) return launch_few_groups<H, 2>(h, out_type, stream);
+  if (h.B <= 32) return launch_many_groups<H, 2, 1>(h, out_type, stream);
+  if (h.B <= 64) return launch_many_groups<H, 4, 1>(h, out_type, stream);
+  launch_many_groups<H, 4, 2>(h, out_type, stream);
 }
 
 }  // namespace
