@@ -359,7 +359,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void q4_many_kernel(Head h, Elem o
   constexpr int kPass = kWide * kManyTiles, kBring = kPass / kWaves;  // tiles of a pass; those of which a wave brings the codes
   constexpr int kUnits = (kRows * 16 + kManyThreads - 1) / kManyThreads;  // 8 hidden states each, that a thread brings a chunk
   constexpr int kProducts = 4 / PC;
-  __shared__ uint4v hidden[3][16 * (kRows + 1)];  // [product and quarter][row]; a row more keeps the writes of 16 quarters apart
+  // [product and quarter][row], rows exchanged by the number of the first index: 16 rows of one, and one row of 16, lie in different banks
+  __shared__ uint4v hidden[3][16 * kRows];
   __shared__ float4v sums[2][PC][kRows / 4];      // of the hidden states of a part
   __shared__ uint4v codes[2][kPass][64];
   __shared__ ChunkGroups<S, Z> groups[2][kPass][16];
@@ -375,20 +376,32 @@ __global__ __launch_bounds__(kManyThreads, 2) void q4_many_kernel(Head h, Elem o
   const Numbers<H> numbers;
   const uint16_t* const all_states = static_cast<const uint16_t*>(h.hidden) + (int64_t)first_b * h.hidden_stride;
 
-  auto load_states = [&](int32_t chunk, uint4v (&x)[kUnits]) {
+  // Rows of the matrix and of the hidden states lie a power of two apart as a rule, so that the same columns of all of them are on few
+  // channels of the L2: the workgroups of an XCD begin with different chunks.
+  const int32_t begin = (int32_t)(blockIdx.x >> 3) % n_chunks;
+  auto turned = [&](int32_t chunk) { return chunk + begin < n_chunks ? chunk + begin : chunk + begin - n_chunks; };
+  int64_t state_at[kUnits];  // where the thread's hidden states of a chunk begin, and where in a buffer they go
+  int32_t state_to[kUnits];
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
+    const int32_t at = u * kManyThreads + tid, b = at >> 4, in = at & 15, place = PC == 1 ? (in & 3) * 4 + (in >> 2) : in;
+    state_at[u] = (int64_t)min(b, rows - 1) * h.hidden_stride + in * 8;
+    state_to[u] = place * kRows + (b ^ place);
+  }
+  const int32_t states_left = h.K - (tid & 15) * 8;  // columns from the thread's place on
+  auto load_states = [&](int32_t turn, uint4v (&x)[kUnits]) {
+    const int32_t chunk = turned(turn);
+    const bool there = chunk * 128 < states_left;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      const int32_t at = u * kManyThreads + tid, b = min(at >> 4, rows - 1), k = chunk * 128 + (at & 15) * 8;
-      const uint4v v = *reinterpret_cast<const uint4v*>(all_states + (int64_t)b * h.hidden_stride + min(k, h.K - 8));
-      x[u] = k < h.K ? v : uint4v{0, 0, 0, 0};
+      x[u] = uint4v{0, 0, 0, 0};
+      if (there) x[u] = *reinterpret_cast<const uint4v*>(all_states + chunk * 128 + state_at[u]);
     }
   };
   auto put_states = [&](const uint4v (&x)[kUnits], int buffer) {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int32_t at = u * kManyThreads + tid, b = at >> 4, in = at & 15, place = PC == 1 ? (in & 3) * 4 + (in >> 2) : in;
-      if (kUnits * kManyThreads == kRows * 16 || b < kRows) hidden[buffer][place * (kRows + 1) + b] = in_order(x[u]);
-    }
+    for (int u = 0; u < kUnits; ++u)
+      if (kUnits * kManyThreads == kRows * 16 || u * kManyThreads + tid < kRows * 16) hidden[buffer][state_to[u]] = in_order(x[u]);
   };
 
   const int64_t row0 = (int64_t)blockIdx.x * tiles_each * 16, row1 = min((int64_t)h.V, row0 + (int64_t)tiles_each * 16);
@@ -419,7 +432,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void q4_many_kernel(Head h, Elem o
         uint4v codes[kBring];
         ChunkGroups<S, Z> groups[kBring];
       };
-      auto load = [&](int32_t chunk, Brought& to) {
+      auto load = [&](int32_t turn, Brought& to) {
+        const int32_t chunk = turned(turn);
         const uint32_t in_row = min((uint32_t)(chunk * 64 + q * 16), last_codes);
 #pragma unroll
         for (int c = 0; c < kBring; ++c) {
@@ -443,28 +457,31 @@ __global__ __launch_bounds__(kManyThreads, 2) void q4_many_kernel(Head h, Elem o
       // the sums over the parts of a chunk, 16 rows to a wave
       auto add_up = [&](int at, int buffer) {
         if (wave >= kRows / 16) return;
-        const uint4v* const states = &hidden[at][q * (kRows + 1) + wave * 16 + n];
         const uint4v ones = {kOnes<H>, kOnes<H>, kOnes<H>, kOnes<H>};
 #pragma unroll
         for (int r = 0; r < PC; ++r) {
           float4v s = {0, 0, 0, 0};
-          for (int i = r * kProducts; i < (r + 1) * kProducts; ++i) s = mfma<H>(states[i * 4 * (kRows + 1)], ones, s);
+          for (int i = r * kProducts; i < (r + 1) * kProducts; ++i) s = mfma<H>(hidden[at][(i * 4 + q) * kRows + wave * 16 + (n ^ (i * 4 + q))], ones, s);
           if (n == 0) sums[buffer][r][wave * 4 + q] = Z ? s : s * -24.0f;
         }
       };
-      auto multiply = [&](int at, int buffer) {
-        const uint4v* const states = &hidden[at][q * (kRows + 1) + wm * MW * 16 + n];
+      const int refill_at = wave < kWaves / 2 ? 0 : 2;  // (the two waves of a SIMD at different times: one multiplies while the other waits)
+      auto multiply = [&](int at, int buffer, auto&& refill) {
 #pragma unroll
         for (int r = 0; r < PC; ++r) {
           uint4v a[kProducts][MW];
 #pragma unroll
           for (int i = 0; i < kProducts; ++i)
-            for (int m = 0; m < MW; ++m) a[i][m] = states[(r * kProducts + i) * 4 * (kRows + 1) + m * 16];
+            for (int m = 0; m < MW; ++m) {
+              const int32_t place = (r * kProducts + i) * 4 + q;
+              a[i][m] = hidden[at][place * kRows + (wm * MW + m) * 16 + (n ^ place)];
+            }
           // the sums of a tile are scaled while the next one's products are made
           float4v part[2][MW];
           float scale[2] = {0.0f, 0.0f};
 #pragma unroll
           for (int c = 0; c <= kManyTiles; ++c) {
+            if (r == 0 && (c == 0 || c == 2) && c == refill_at) refill();
             if (c < mine && c < kManyTiles) {
               const ChunkGroups<S, Z> g = groups[buffer][first + c][n];
               const uint4v four = codes[buffer][first + c][lane];
@@ -508,16 +525,17 @@ __global__ __launch_bounds__(kManyThreads, 2) void q4_many_kernel(Head h, Elem o
 #pragma unroll 1
       for (int32_t chunk = 0; chunk < n_chunks; ++chunk) {
         const int buffer = chunk & 1, next = ring == 2 ? 0 : ring + 1, last = next == 2 ? 0 : next + 1;
-        if (chunk + 1 < n_chunks) add_up(next, buffer ^ 1);
-        multiply(ring, buffer);
-        if (chunk + 2 < n_chunks) {
-          put_states(x, last);
-          if (chunk + 3 < n_chunks) load_states(chunk + 3, x);
-        }
-        if (chunk + 1 < n_chunks) {
-          put(next_codes, buffer ^ 1);
-          if (chunk + 2 < n_chunks) load(chunk + 2, next_codes);
-        }
+        multiply(ring, buffer, [&] {
+          if (chunk + 2 < n_chunks) {
+            put_states(x, last);
+            if (chunk + 3 < n_chunks) load_states(chunk + 3, x);
+          }
+          if (chunk + 1 < n_chunks) {
+            put(next_codes, buffer ^ 1);
+            if (chunk + 2 < n_chunks) load(chunk + 2, next_codes);
+            add_up(next, buffer ^ 1);
+          }
+        });
         ring = next;
         __syncthreads();
       }
