@@ -2391,7 +2391,7 @@ int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, in
   if (B > s->max_rows || V > s->V) return fail(XGM_ERR_BAD_ARG, "sample: more rows or logits than the sampler was created for");
   require_device();
   const DrawRules d = draw ? DrawRules{draw->d_temperature, draw->d_top_k, draw->d_top_p, draw->d_min_p, draw->d_uniform} : DrawRules{};
-  launch_sample(Logits{d_logits, row_stride_elems, V}, type, B, r, d, s->memory, d_ids, d_logprobs, static_cast<hipStream_t>(hip_stream));
+  launch_sample(Logits{d_logits, row_stride_elems, V}, type, B, r, d, s->memory, s->max_rows, s->V, d_ids, d_logprobs, static_cast<hipStream_t>(hip_stream));
   HIP_OK(hipGetLastError());
   return XGM_OK;
   API_END

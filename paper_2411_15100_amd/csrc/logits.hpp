@@ -53,7 +53,7 @@ struct Logits {
 void launch_process_logits(const Logits& in, Elem type, int32_t B, const LogitRules& rules, void* out, int64_t out_stride, hipStream_t stream);
 
 size_t sampler_bytes(int32_t max_rows, int32_t V);
-void launch_sample(const Logits& in, Elem type, int32_t B, const LogitRules& rules, const DrawRules& draw, void* memory, int32_t* ids, float* logprobs,
-                   hipStream_t stream);
+void launch_sample(const Logits& in, Elem type, int32_t B, const LogitRules& rules, const DrawRules& draw, void* memory, int32_t max_rows, int32_t max_V,
+                   int32_t* ids, float* logprobs, hipStream_t stream);  // memory: sampler_bytes(max_rows, max_V), zeros at first
 
 }  // namespace xgm
