@@ -278,7 +278,8 @@ struct RowPlan {  // what the first kernel leaves of a row for the second
   u64 wanted[kBins / 64];  // bins of which it needs the tokens
   double E;
   float top;
-  int32_t cut;  // 0: the row is done
+  int32_t cut;       // 0: the row is done
+  uint32_t min_key;  // tokens with a smaller key weigh less than min_p
 };
 struct DrawMemory {
   uint32_t *arrived, *n_candidates;  // [2][rows], [rows]: zero between calls
@@ -316,17 +317,21 @@ __device__ __forceinline__ void put_out(Slot* to, const Slot& s) {
 }
 __device__ __forceinline__ Slot take_in(const Slot* from) { return Slot{take_in(&from->E), take_in(&from->sum), take_in(&from->top), take_in(&from->top_id)}; }
 
+constexpr int kMostSlices = (1 << 20) / kSliceTokens + 1;
+constexpr int kFew = 2048;  // candidates that are kept in LDS
 struct Shared {
-  double sum[2][kWaves];
-  u64 part[kWaves];
+  double sum[kGroups][kWaves];
+  u64 part[kWaves], mass_part[kWaves];
   float top[kWaves];
   int32_t id[kWaves];
-  u64 bins[1024];       // of the slice, the row, or a selection
+  u64 bins[1024];  // of the slice, the row, or a selection
   uint32_t counts[1024];
   double before_mass[kBins + 1];
   uint32_t before_count[kBins + 1];
-  double slice_sum[(1 << 20) / kSliceTokens + 2];
-  u64 slice_more[(1 << 20) / kSliceTokens + 2];
+  Slot slots[kMostSlices];
+  double slice_sum[kMostSlices];
+  u64 slice_more[kMostSlices];
+  u64 few[kFew];
   uint32_t flag[2];
   int32_t found[2];
   double rest;
@@ -383,23 +388,38 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
 }
 template <Elem E> __device__ __forceinline__ int32_t token_of(int32_t first, int j, int i) { return first + (j * kSliceThreads + (int32_t)threadIdx.x) * 8 + i; }
 
-// The token of a slice at which the running sum of weights (w of a token's logit and id) first exceeds `rest`; the last one
-// with a weight if rounding leaves none; -1 if none has any.
-template <Elem E, class W> __device__ int32_t find_token(const float (&y)[kGroups][8], int32_t first, double rest, Shared& s, W&& w) {
-  const int32_t lane = (int32_t)threadIdx.x & 63, wave = (int32_t)threadIdx.x >> 6;
-  double run[kGroups];
-  int32_t last = -1;
+// Calls f(logit, token) for the thread's tokens of a slice in order of their ids.  The logits go round in their registers instead of the
+// loop being unrolled: what a single workgroup does once costs as much for fetching its instructions as for carrying them out.
+template <class F> __device__ __forceinline__ void for_tokens(float (&y)[kGroups][8], int32_t first, F&& f) {
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
-    run[j] = 0.0;
-#pragma unroll
+    const int32_t t = first + (j * kSliceThreads + (int32_t)threadIdx.x) * 8;
+#pragma unroll 1
     for (int i = 0; i < 8; ++i) {
-      const double x = w(y[j][i], token_of<E>(first, j, i));
-      run[j] += x;
-      if (x > 0.0) last = token_of<E>(first, j, i);
-    }
+      const float v = y[j][0];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
+      for (int k = 0; k < 7; ++k) y[j][k] = y[j][k + 1];
+      y[j][7] = v;
+      f(v, t + i, j);
+    }
+  }
+}
+
+// The token of a slice at which the running sum of weights (w of a token's logit and id) first exceeds `rest`, and its logit; the
+// last one with a weight if rounding leaves none; -1 if none has any.
+template <class W> __device__ int32_t find_token(float (&y)[kGroups][8], int32_t first, double rest, float* logit, Shared& s, W&& w) {
+  const int32_t lane = (int32_t)threadIdx.x & 63, wave = (int32_t)threadIdx.x >> 6;
+  double run[kGroups] = {};
+  int32_t last = -1;
+  for_tokens(y, first, [&](float v, int32_t t, int j) {
+    const double x = w(v, t);
+    run[j] += x;
+    if (x > 0.0) last = t;
+  });
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j) {
       const double other = __shfl_up(run[j], d);
       if (lane >= d) run[j] += other;
     }
@@ -412,30 +432,37 @@ template <Elem E, class W> __device__ int32_t find_token(const float (&y)[kGroup
   }
   __syncthreads();
   if (last >= 0) atomicMax(&s.found[1], last);
-  double base = 0.0;
+  double base = 0.0, at[kGroups];
+  bool mine[kGroups], any = false;
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
     double before = base;
+#pragma unroll
     for (int k = 0; k < kWaves; ++k) {
       if (k == wave) before = base;
       base += s.sum[j][k];
     }
-    const double end = before + run[j];
-    double at = __shfl_up(run[j], 1);
-    at = lane ? before + at : before;
-    if (at <= rest && rest < end) {
-      int32_t token = -1;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const double x = w(y[j][i], token_of<E>(first, j, i));
-        at += x;
-        if (x > 0.0 && (token < 0 || at - x <= rest)) token = token_of<E>(first, j, i);  // (the last whose stretch begins at or before)
-      }
-      if (token >= 0) atomicMin(&s.found[0], token);
-    }
+    const double up = __shfl_up(run[j], 1);
+    at[j] = lane ? before + up : before;
+    mine[j] = at[j] <= rest && rest < before + run[j];
+    any |= mine[j];
+  }
+  if (any) {
+    int32_t token = -1;
+    for_tokens(y, first, [&](float v, int32_t t, int j) {
+      if (!mine[j]) return;
+      const double x = w(v, t);
+      if (x > 0.0 && (token < 0 || at[j] <= rest)) token = t;  // (the last whose stretch begins at or before)
+      at[j] += x;
+    });
+    if (token >= 0) atomicMin(&s.found[0], token);
   }
   __syncthreads();
-  return s.found[0] != INT32_MAX ? s.found[0] : s.found[1];
+  const int32_t id = s.found[0] != INT32_MAX ? s.found[0] : s.found[1];
+  for_tokens(y, first, [&](float v, int32_t t, int) { if (t == id) s.top[0] = v; });
+  __syncthreads();
+  *logit = s.top[0];
+  return id;
 }
 
 struct RowDraw {  // how a row is drawn
@@ -458,65 +485,77 @@ struct RowDraw {  // how a row is drawn
   }
 };
 
-// The row's largest logit, its lowest id, octave and sum (thread by thread the same), from its slots; slices lie in s.slice_sum.
+// The row's largest logit, its lowest id, octave and sum (thread by thread the same), from its slots, which are brought to s.slots;
+// the slices' sums relative to the row's octave lie in s.slice_sum.  FRESH: the slots come from other workgroups of this kernel.
 struct RowTotal {
   double E, sum;
   float top;
   int32_t top_id;
 };
-__device__ RowTotal row_total(const Slot* slots, int32_t n, Shared& s) {
-  RowTotal r{0.0, 0.0, -__builtin_inff(), -1};
+template <bool FRESH> __device__ RowTotal row_total(const Slot* slots, int32_t n, Shared& s) {
   const int32_t lane = (int32_t)threadIdx.x & 63;
-  // (every wave by itself: at most three slots a lane)
-  Slot mine[3];
-  int32_t k = 0;
-  float top = -__builtin_inff();
-  double E = -__builtin_inf();
+  if ((int32_t)threadIdx.x < n) s.slots[threadIdx.x] = FRESH ? take_in(slots + threadIdx.x) : slots[threadIdx.x];
+  __syncthreads();
+  RowTotal r{-__builtin_inf(), 0.0, -__builtin_inff(), INT32_MAX};
+  for (int32_t i = lane; i < n; i += 64)
+    if (s.slots[i].top > -__builtin_inff()) {
+      r.top = fmaxf(r.top, s.slots[i].top);
+      r.E = fmax(r.E, s.slots[i].E);
+    }
 #pragma unroll
-  for (k = 0; k < 3; ++k) {
-    const int32_t i = lane + 64 * k;
-    mine[k] = i < n ? take_in(slots + i) : Slot{0.0, 0.0, -__builtin_inff(), -1};
-    if (mine[k].top > -__builtin_inff()) { top = fmaxf(top, mine[k].top); E = fmax(E, mine[k].E); }
+  for (int d = 32; d; d >>= 1) {
+    r.top = fmaxf(r.top, __shfl_xor(r.top, d));
+    r.E = fmax(r.E, __shfl_xor(r.E, d));
+  }
+  for (int32_t i = lane; i < n; i += 64) {
+    const Slot& one = s.slots[i];
+    const bool some = one.top > -__builtin_inff();
+    const double d = one.E - r.E, x = some && d > -1000.0 ? ldexp(one.sum, (int)d) : 0.0;
+    if (some && one.top == r.top) r.top_id = min(r.top_id, one.top_id);
+    r.sum += x;
+    if (threadIdx.x < 64) s.slice_sum[i] = x;
   }
 #pragma unroll
-  for (int d = 32; d; d >>= 1) { top = fmaxf(top, __shfl_xor(top, d)); E = fmax(E, __shfl_xor(E, d)); }
-  r.top = top;
-  r.E = E;
-  int32_t id = INT32_MAX;
-  double sum = 0.0;
-#pragma unroll
-  for (k = 0; k < 3; ++k) {
-    if (mine[k].top == top && mine[k].top_id >= 0) id = min(id, mine[k].top_id);
-    const double d = mine[k].E - E;
-    const double x = mine[k].top > -__builtin_inff() && d > -1000.0 ? ldexp(mine[k].sum, (int)d) : 0.0;
-    sum += x;
-    if (threadIdx.x < 64 && lane + 64 * k < n) s.slice_sum[lane + 64 * k] = x;
-  }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) id = min(id, __shfl_xor(id, d));
-  r.top_id = id;
-  r.sum = wave_sum(sum);
+  for (int d = 32; d; d >>= 1) r.top_id = min(r.top_id, __shfl_xor(r.top_id, d));
+  r.sum = wave_sum(r.sum);
   __syncthreads();
   return r;
 }
 // Which slice the random number falls into and what is left of it there: s.slice, s.rest.
 __device__ void find_slice(double u, int32_t n, Shared& s) {
-  if (threadIdx.x == 0) {
-    double total = 0.0;
-    for (int32_t i = 0; i < n; ++i) total += s.slice_sum[i];
-    double rest = u * total;
-    int32_t at = -1;
-    for (int32_t i = 0; i < n; ++i) {
-      const double x = s.slice_sum[i];
-      if (!(x > 0.0)) continue;
-      if (at >= 0) {
-        if (rest < s.slice_sum[at]) break;
-        rest -= s.slice_sum[at];
-      }
-      at = i;
+  constexpr int kEach = (kMostSlices + 63) / 64;  // neighbours a lane
+  const int32_t lane = (int32_t)threadIdx.x;
+  if (lane < 64) {
+    double x[kEach], run = 0.0;
+    int32_t last = -1;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int32_t i = lane * kEach + k;
+      x[k] = i < n ? s.slice_sum[i] : 0.0;
+      run += x[k];
+      if (x[k] > 0.0) last = i;
     }
-    s.slice = at;
-    s.rest = rest;
+    double all = run;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const double other = __shfl_up(all, d);
+      if (lane >= d) all += other;
+    }
+    const double rest = u * __shfl(all, 63), up = __shfl_up(all, 1), front = lane ? up : 0.0;
+    // the last slice with a weight that begins at or before the number
+    int32_t at = -1;
+    double begin = front, left = 0.0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (x[k] > 0.0 && begin <= rest) { at = lane * kEach + k; left = rest - begin; }
+      begin += x[k];
+    }
+    const u64 who = __ballot(at >= 0), some = __ballot(last >= 0);
+    const int owner = who ? 63 - __builtin_clzll(who) : some ? __builtin_ctzll(some) : 0;
+    if (lane == owner) {
+      s.slice = at >= 0 ? at : max(last, 0);
+      s.rest = at >= 0 ? left : 0.0;
+    }
   }
   __syncthreads();
 }
@@ -528,24 +567,26 @@ __device__ __forceinline__ void write_out(const RowDraw& d, const RowTotal& r, i
 }
 
 // The row's bins from its slices' into s.bins and s.counts, relative to the octave E, and what lies in front of each (s.before_*;
-// masses in 2^E).  All threads.
-__device__ void row_bins(const Slot* slots, const u64* bins, int32_t n, double E, Shared& s) {
-  const int32_t tid = (int32_t)threadIdx.x;
+// masses in 2^E).  All threads, after row_total: half of them take the even slices and half the odd ones.
+template <bool FRESH> __device__ void row_bins(const u64* bins, int32_t n, double E, Shared& s) {
+  static_assert(kSliceThreads == 2 * kBins, "two threads a bin");
+  const int32_t tid = (int32_t)threadIdx.x, bin = tid & (kBins - 1);
   __syncthreads();
-  if (tid < kBins) {
-    u64 mass = 0;
-    uint32_t count = 0;
-    for (int32_t i = 0; i < n; ++i) {
-      if (!(take_in(&slots[i].top) > -__builtin_inff())) continue;
-      const double d = (E - take_in(&slots[i].E)) * kBinsAnOctave;
-      if (!(d <= (double)tid)) continue;
-      const u64 x = take_in(bins + (size_t)i * kBins + (tid - (int32_t)d));
-      mass += x & kMassMask;
-      count += (uint32_t)(x >> kCountShift);
-    }
-    s.bins[tid] = mass;
-    s.counts[tid] = count;
+  u64 mass = 0;
+  uint32_t count = 0;
+#pragma unroll 4
+  for (int32_t i = tid / kBins; i < n; i += 2) {
+    const double d = s.slots[i].top > -__builtin_inff() ? (E - s.slots[i].E) * kBinsAnOctave : (double)kBins;
+    const bool some = d <= (double)bin;
+    const u64* at = bins + (size_t)i * kBins + (some ? bin - (int32_t)d : 0);
+    u64 x = FRESH ? take_in(at) : *at;
+    if (!some) x = 0;
+    mass += x & kMassMask;
+    count += (uint32_t)(x >> kCountShift);
   }
+  if (tid < kBins) { s.bins[tid] = mass; s.counts[tid] = count; }
+  __syncthreads();
+  if (tid >= kBins) { s.bins[bin] += mass; s.counts[bin] += count; }
   __syncthreads();
   if (tid < 64) {  // one wave: four bins a lane, an octave
     const double scale = ldexp(1.0, -kMassBits - tid);
@@ -578,7 +619,6 @@ __device__ void row_bins(const Slot* slots, const u64* bins, int32_t n, double E
   }
   __syncthreads();
 }
-__device__ __forceinline__ double bin_mass(const Shared& s, int32_t bin) { return ldexp((double)s.bins[bin], -kMassBits - bin / kBinsAnOctave); }
 // the first bin up to and with which at least `count` tokens, or `mass`, lie; kBins - 1 if there are fewer
 __device__ int32_t bin_of_count(const Shared& s, uint32_t count) {
   int32_t lo = 0, hi = kBins - 1;
@@ -599,12 +639,23 @@ __device__ int32_t bin_of_mass(const Shared& s, double mass) {
   }
   return lo;
 }
-// the bin in which min_p of the largest weight lies, kBins if below all
-__device__ int32_t bin_of_min(const RowDraw& d, float top, double E) {
-  if (!(d.min_p > 0.0f)) return kBins;
-  const double t = octaves(top, d.per) + log2((double)d.min_p);
-  const int32_t b = Power(t).bin(t, E);
-  return b < 0 ? 0 : b;
+// The smallest key whose weight is min_p of the largest or more: the logarithm says about where, the exponential function where.
+__device__ uint32_t key_of_min(const RowDraw& d, float top) {
+  if (!(d.min_p > 0.0f)) return 0;
+  const double t = (double)d.temperature;
+  uint32_t key = key_of((float)fmax((double)top + t * log((double)d.min_p), -(double)FLT_MAX));
+  const uint32_t most = key_of(top);
+  key = min(key, most);
+  int steps = 0;
+#pragma unroll 1
+  for (bool up = false; steps < 64; ++steps) {
+    const bool enough = exp(((double)value_of(key) - (double)top) / t) >= (double)d.min_p;
+    if (up && enough) break;
+    if (!up && !enough) up = true;
+    key = up ? min(key + 1, most) : key - 1;
+    if (key == most && up) break;
+  }
+  return key;
 }
 
 template <Elem E>
@@ -644,21 +695,29 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
   if (top > -__builtin_inff()) {
     slot.E = floor(octaves(top, d.per));
     double sum = 0.0;
+    auto add = [&](float v) {
+      if (!(v > -__builtin_inff())) return;
+      const double t = octaves(v, d.per);
+      const Power w(t);
+      sum += w.weight(slot.E);
+      if (d.cut) {
+        const int32_t bin = w.bin(t, slot.E);
+        if (bin < kBins) atomicAdd(&s.bins[bin], w.mass() + (1ull << kCountShift));
+      }
+    };
 #pragma unroll
     for (int j = 0; j < kGroups; ++j)
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (y[j][i] > -__builtin_inff()) {
-          const double t = octaves(y[j][i], d.per);
-          const Power w(t);
-          sum += w.weight(slot.E);
-          if (d.cut) {
-            const int32_t bin = w.bin(t, slot.E);
-            if (bin < kBins) atomicAdd(&s.bins[bin], w.mass() + (1ull << kCountShift));
-          }
+        for (int i = 0; i < 4; ++i) {
+          const float v = y[j][i];
+          y[j][i] = y[j][i + 4];
+          y[j][i + 4] = v;
+          add(v);
         }
+      }
     sum = wave_sum(sum);
-    __syncthreads();
     if (lane == 0) s.sum[0][wave] = sum;
     __syncthreads();
 #pragma unroll
@@ -668,38 +727,33 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
   if (d.cut && tid < kBins) put_out(bins + (size_t)slice * kBins + tid, s.bins[tid]);
   if (!last_of(m.arrived + b, (uint32_t)n_slices, s)) return;
 
-  const RowTotal total = row_total(slots, n_slices, s);
-  if (total.top == -__builtin_inff() || d.greedy) {
+  const RowTotal total = row_total<true>(slots, n_slices, s);
+  const bool empty = total.top == -__builtin_inff();
+  if (empty || !d.cut) {
+    int32_t id = empty ? -1 : total.top_id;
+    float logit = total.top;
+    if (!empty && !d.greedy) {
+      find_slice(d.u, n_slices, s);
+      const double rest = s.rest;
+      first = row.first_token(s.slice);
+      load_slice<E>(row, r, b, first, tables, y);
+      id = find_token(y, first, rest, &logit, s, [&](float v, int32_t) { return v > -__builtin_inff() ? Power(octaves(v, d.per)).weight(total.E) : 0.0; });
+    }
     if (tid == 0) {
-      write_out(d, total, total.top == -__builtin_inff() ? -1 : total.top_id, total.top, ids + b, logprobs ? logprobs + b : nullptr);
+      write_out(d, total, id, logit, ids + b, logprobs ? logprobs + b : nullptr);
       m.plans[b].cut = 0;
     }
     return;
   }
-  if (!d.cut) {
-    find_slice(d.u, n_slices, s);
-    const double rest = s.rest, Es = total.E;
-    first = row.first_token(s.slice);
-    load_slice<E>(row, r, b, first, tables, y);
-    auto weight = [&](float v, int32_t) { return v > -__builtin_inff() ? Power(octaves(v, d.per)).weight(Es) : 0.0; };
-    const int32_t id = find_token<E>(y, first, rest, s, weight);
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (token_of<E>(first, j, i) == id) write_out(d, total, id, y[j][i], ids + b, logprobs ? logprobs + b : nullptr);
-    if (tid == 0 && id < 0) write_out(d, total, -1, 0.0f, ids + b, logprobs ? logprobs + b : nullptr);
-    if (tid == 0) m.plans[b].cut = 0;
-    return;
-  }
   // the bins in which a cut can lie: that of the k-th token unless it ends there, those of p of what lies up to it, that of min_p
-  row_bins(slots, bins, n_slices, total.E, s);
+  row_bins<true>(bins, n_slices, total.E, s);
   if (tid == 0) {
     RowPlan plan{};
     plan.E = total.E;
     plan.top = total.top;
     plan.cut = 1;
-    auto want = [&](int32_t bin) { plan.wanted[bin / 64] |= 1ull << (bin & 63); };
+    plan.min_key = key_of_min(d, total.top);
+    int32_t from = kBins, to = -1, k_bin = -1, low = -1;
     double least = s.before_mass[kBins], most = least;
     int32_t last = kBins - 1;
     if (d.top_k && (uint32_t)d.top_k < s.before_count[kBins]) {
@@ -707,27 +761,39 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
       most = s.before_mass[last + 1];
       least = most;
       if ((uint32_t)d.top_k != s.before_count[last + 1]) {
-        want(last);
+        k_bin = last;
         least = s.before_mass[last];
       }
     }
     if (d.top_p < 1.0f) {
-      const int32_t from = bin_of_mass(s, (double)d.top_p * least * (1.0 - 1e-9)), to = min(last, bin_of_mass(s, fmin((double)d.top_p * most * (1.0 + 1e-9), s.before_mass[kBins])));
-      for (int32_t k = min(from, to); k <= to; ++k) want(k);
+      from = bin_of_mass(s, (double)d.top_p * least * (1.0 - 1e-9));
+      to = min(last, bin_of_mass(s, fmin((double)d.top_p * most * (1.0 + 1e-9), s.before_mass[kBins])));
+      from = min(from, to);
     }
-    const int32_t low = bin_of_min(d, total.top, total.E);
-    if (low < kBins) want(low);
+    if (plan.min_key) {
+      const double t = octaves(value_of(plan.min_key), d.per);
+      low = Power(t).bin(t, total.E);
+    }
+#pragma unroll
+    for (int k = 0; k < kBins / 64; ++k) {
+      const int32_t lo = max(from - 64 * k, 0), hi = min(to - 64 * k, 63);
+      u64 bits = lo <= hi ? (~0ull << lo) & (~0ull >> (63 - hi)) : 0;
+      if (k_bin >= 0 && k_bin / 64 == k) bits |= 1ull << (k_bin & 63);
+      if (low >= 0 && low / 64 == k) bits |= 1ull << (low & 63);
+      plan.wanted[k] = bits;
+    }
     m.plans[b] = plan;
   }
 }
 
-// Goes through the tokens of the wanted bins: f(key, bin, id).  All threads; `listed` of them, or more than the list holds.
+// Goes through the tokens of the wanted bins: f(key, bin, id).  All threads; `listed` of them, a few in s.few, or more than the list holds.
 template <Elem E, class F>
 __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRules& r, const RowDraw& d, const RowPlan& plan, int32_t b, int32_t n_slices, const u64* list,
-                                               uint32_t listed, uint32_t* tables, F&& f) {
+                                               uint32_t listed, uint32_t* tables, const Shared& s, F&& f) {
   if (listed <= kMostCandidates) {
+#pragma unroll 1
     for (uint32_t i = threadIdx.x; i < listed; i += kSliceThreads) {
-      const u64 x = take_in(list + i);
+      const u64 x = listed <= kFew ? s.few[i] : take_in(list + i);
       f((uint32_t)(x >> 32), (int32_t)(x >> 24 & 255u), (int32_t)(x & 0xffffffu));
     }
     return;
@@ -737,14 +803,12 @@ __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRul
     float y[kGroups][8];
     __syncthreads();  // (the tables of the last slice have been read)
     load_slice<E>(row, r, b, first, tables, y);
-    for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (!(y[j][i] > -__builtin_inff())) continue;
-        const double t = octaves(y[j][i], d.per);
-        const int32_t bin = Power(t).bin(t, plan.E);
-        if (bin < kBins && (plan.wanted[bin / 64] >> (bin & 63) & 1u)) f(key_of(y[j][i]), bin, token_of<E>(first, j, i));
-      }
+    for_tokens(y, first, [&](float v, int32_t id, int) {
+      if (!(v > -__builtin_inff())) return;
+      const double t = octaves(v, d.per);
+      const int32_t bin = Power(t).bin(t, plan.E);
+      if (bin < kBins && (plan.wanted[bin / 64] >> (bin & 63) & 1u)) f(key_of(v), bin, id);
+    });
   }
 }
 
@@ -756,124 +820,6 @@ struct Cut {
   int32_t id;
   __device__ __forceinline__ bool keeps(int32_t in, uint32_t k, int32_t i) const { return in < bin || (in == bin && (k > key || (k == key && i <= id))); }
 };
-
-// Narrows the tokens of a bin that `within` keeps down to the one at which `need` (tokens, or mass in the bin's whole numbers) is reached.
-// each(f) goes through the candidates.  Returns the mass up to there.
-template <class Each> __device__ u64 select(Each&& each, Cut within, int32_t bin, bool by_count, u64 need, double per, int32_t V, Cut* out, Shared& s) {
-  const int32_t tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint32_t lo = ~0u, hi = 0;
-  each([&](uint32_t key, int32_t in, int32_t id) {
-    if (in == bin && within.keeps(in, key, id)) { lo = min(lo, key); hi = max(hi, key); }
-  });
-  __syncthreads();
-  if (tid == 0) { s.flag[0] = ~0u; s.flag[1] = 0; }
-  __syncthreads();
-  atomicMin(&s.flag[0], lo);
-  atomicMax(&s.flag[1], hi);
-  __syncthreads();
-  lo = s.flag[0];
-  hi = s.flag[1];
-  if (lo > hi) {
-    *out = within;
-    return 0;
-  }
-  u64 up_to = 0, tied_mass = 0;
-  uint32_t tied = 0;
-  // a pass: which of 1024 stretches of [from, to], in falling order of what, has the token
-  auto narrow = [&](auto&& what, bool weighed) {
-    for (int i = tid; i < 1024; i += kSliceThreads) { s.bins[i] = 0; s.counts[i] = 0; }
-    __syncthreads();
-    each([&](uint32_t key, int32_t in, int32_t id) {
-      if (in != bin || !within.keeps(in, key, id)) return;
-      const int32_t at = what(key, id);
-      if (at < 0) return;
-      atomicAdd(&s.counts[at], 1u);
-      if (weighed) atomicAdd(&s.bins[at], Power(octaves(value_of(key), per)).mass());
-    });
-    __syncthreads();
-    // two neighbours a thread
-    const bool counted = by_count || !weighed;
-    const u64 m0 = s.bins[2 * tid], m1 = s.bins[2 * tid + 1];
-    const uint32_t c0 = s.counts[2 * tid], c1 = s.counts[2 * tid + 1];
-    u64 all_mass = m0 + m1, all = counted ? (u64)c0 + c1 : m0 + m1;
-#pragma unroll
-    for (int e = 1; e < 64; e <<= 1) {
-      const u64 other = __shfl_up(all, e), other_mass = __shfl_up(all_mass, e);
-      if (lane >= e) { all += other; all_mass += other_mass; }
-    }
-    if (lane == 63) { s.part[wave] = all; s.sum[0][wave] = __longlong_as_double((long long)all_mass); }
-    if (tid == 0) s.found[0] = 1023;
-    __syncthreads();
-    u64 in_front = 0, mass_in_front = 0;
-    for (int k = 0; k < wave; ++k) { in_front += s.part[k]; mass_in_front += (u64)__double_as_longlong(s.sum[0][k]); }
-    all += in_front;
-    all_mass += mass_in_front;
-    const u64 v0 = counted ? (u64)c0 : m0, v1 = counted ? (u64)c1 : m1, begin = all - v0 - v1;
-    const bool here = begin < need && need <= all;
-    const int which = need <= begin + v0 ? 0 : 1;
-    __syncthreads();
-    if (here) {
-      s.found[0] = 2 * tid + which;
-      s.part[0] = begin + (which ? v0 : 0);                     // in front of the stretch
-      s.part[1] = all_mass - m0 - m1 + (which ? m0 : 0);
-      s.part[2] = which ? m1 : m0;
-      s.counts[0] = which ? c1 : c0;
-    }
-    __syncthreads();
-    need -= s.part[0];
-    if (weighed) { up_to += s.part[1]; tied_mass = s.part[2]; }
-    tied = s.counts[0];
-    const int32_t at = s.found[0];
-    __syncthreads();
-    return at;
-  };
-  // rounding can leave a need above what there is: the last token then
-  {
-    u64 all = 0;
-    each([&](uint32_t key, int32_t in, int32_t id) {
-      if (in == bin && within.keeps(in, key, id)) all += by_count ? 1 : Power(octaves(value_of(key), per)).mass();
-    });
-#pragma unroll
-    for (int e = 32; e; e >>= 1) all += __shfl_xor(all, e);
-    if (lane == 0) s.part[wave] = all;
-    __syncthreads();
-    all = 0;
-    for (int k = 0; k < kWaves; ++k) all += s.part[k];
-    __syncthreads();
-    if (need > all) need = all;
-    if (need == 0) need = 1;
-  }
-  for (int pass = 0; pass < 5; ++pass) {  // (10 bits each)
-    const uint32_t width = hi - lo;
-    const int shift = width < 1024 ? 0 : 22 - __clz((int)width);
-    const uint32_t from = hi, floor_key = lo;
-    const int32_t at = narrow([&](uint32_t key, int32_t) { return key <= from && key >= floor_key ? (int32_t)((from - key) >> shift) : -1; }, true);
-    hi = from - ((uint32_t)at << shift);
-    lo = shift == 0 ? hi : max(floor_key, hi - ((1u << shift) - 1u));
-    if (hi == lo) break;
-  }
-  // of the tokens with this key the first so many
-  const u64 each_mass = tied_mass / max(tied, 1u);
-  const u64 mass_in_front = up_to;
-  u64 wanted = by_count ? need : (need + each_mass - 1) / max(each_mass, (u64)1);
-  if (wanted >= tied) {
-    *out = Cut{bin, hi, within.bin == bin && within.key == hi ? within.id : INT32_MAX};
-    return mass_in_front + tied_mass;
-  }
-  need = wanted;
-  int32_t first = 0, last = V - 1;
-  const uint32_t only = hi;
-  for (int pass = 0; pass < 4 && first != last; ++pass) {
-    const uint32_t width = (uint32_t)(last - first);
-    const int shift = width < 1024 ? 0 : 22 - __clz((int)width);
-    const int32_t from = first, to = last;
-    const int32_t at = narrow([&](uint32_t key, int32_t id) { return key == only && id >= from && id <= to ? (int32_t)((uint32_t)(id - from) >> shift) : -1; }, false);
-    first = from + (at << shift);
-    last = min(to, first + (1 << shift) - 1);
-  }
-  *out = Cut{bin, only, first};
-  return mass_in_front + wanted * each_mass;
-}
 
 template <Elem E>
 __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m, int32_t n_slices, int32_t* __restrict__ ids,
@@ -902,87 +848,205 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   if (s.flag[1]) {
     const int32_t first = row.first_token(slice);
     load_slice<E>(row, r, b, first, tables, y);
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const double t = octaves(y[j][i], d.per);
-        const int32_t bin = y[j][i] > -__builtin_inff() ? Power(t).bin(t, plan.E) : kBins;
-        const bool mine = bin < kBins && (plan.wanted[bin / 64] >> (bin & 63) & 1u);
-        const u64 who = __ballot(mine);
-        if (!who) continue;
-        uint32_t at = 0;
-        if (lane == 0) at = __hip_atomic_fetch_add(m.n_candidates + b, (uint32_t)__popcll(who), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        at = __builtin_amdgcn_readfirstlane(at) + (uint32_t)__popcll(who & ((1ull << lane) - 1ull));
-        if (mine && at < kMostCandidates) put_out(list + at, (u64)key_of(y[j][i]) << 32 | (u64)bin << 24 | (u64)(uint32_t)token_of<E>(first, j, i));
-      }
+    for_tokens(y, first, [&](float v, int32_t id, int) {
+      const double t = octaves(v, d.per);
+      const int32_t bin = v > -__builtin_inff() ? Power(t).bin(t, plan.E) : kBins;
+      const bool mine = bin < kBins && (plan.wanted[bin / 64] >> (bin & 63) & 1u);
+      const u64 who = __ballot(mine);
+      if (!who) return;
+      uint32_t at = 0;
+      if (lane == 0) at = __hip_atomic_fetch_add(m.n_candidates + b, (uint32_t)__popcll(who), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      at = __builtin_amdgcn_readfirstlane(at) + (uint32_t)__popcll(who & ((1ull << lane) - 1ull));
+      if (mine && at < kMostCandidates) put_out(list + at, (u64)key_of(v) << 32 | (u64)bin << 24 | (u64)(uint32_t)id);
+    });
   }
   if (!last_of(m.arrived + m.rows + b, (uint32_t)n_slices, s)) return;
 
   const uint32_t listed = take_in(m.n_candidates + b);
+  if (listed <= kFew)
+    for (uint32_t i = (uint32_t)tid; i < listed; i += kSliceThreads) s.few[i] = take_in(list + i);
   __syncthreads();
   if (tid == 0) put_out(m.n_candidates + b, 0u);
-  auto each = [&](auto&& f) { for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, tables, f); };
-  const RowTotal total = row_total(slots, n_slices, s);
-  row_bins(slots, bins, n_slices, total.E, s);
-  // what the selections below need of the bins, before they use the same memory
-  const bool by_k = d.top_k && (uint32_t)d.top_k < s.before_count[kBins];
+  const RowTotal total = row_total<false>(slots, n_slices, s);
+  row_bins<false>(bins, n_slices, total.E, s);
   Cut cut{kBins, 0, INT32_MAX};
-  int32_t k_bin = kBins - 1;
-  u64 k_need = 0;
-  bool k_inside = false;
-  double up_to = s.before_mass[kBins], k_before = 0.0;
-  if (by_k) {
+  int32_t k_bin = kBins - 1, in_bin = -1;  // in_bin: where the cut of a selection lies
+  double up_to = s.before_mass[kBins];
+  u64 need = 0;  // what the rest of the kept beginning has to reach there: tokens, or mass in the bin's whole numbers
+  if (d.top_k && (uint32_t)d.top_k < s.before_count[kBins]) {
     k_bin = bin_of_count(s, (uint32_t)d.top_k);
-    k_before = s.before_mass[k_bin];
-    k_need = (uint32_t)d.top_k - s.before_count[k_bin];
-    k_inside = (uint32_t)d.top_k != s.before_count[k_bin + 1];
     up_to = s.before_mass[k_bin + 1];
     cut = Cut{k_bin, 0, INT32_MAX};
+    need = (uint32_t)d.top_k - s.before_count[k_bin];
+    if ((uint32_t)d.top_k != s.before_count[k_bin + 1]) in_bin = k_bin;
   }
-  if (k_inside) {
-    const u64 mass = select(each, cut, k_bin, true, k_need, d.per, in.V, &cut, s);
-    up_to = k_before + ldexp((double)mass, -kMassBits - k_bin / kBinsAnOctave);
-    row_bins(slots, bins, n_slices, total.E, s);
-  }
-  if (d.top_p < 1.0f) {
-    const double target = (double)d.top_p * up_to;
-    const int32_t p_bin = min(k_bin, bin_of_mass(s, target));
-    const double need = ldexp(target - s.before_mass[p_bin], kMassBits + p_bin / kBinsAnOctave);
-    if (plan.wanted[p_bin / 64] >> (p_bin & 63) & 1u) {
-      const Cut within = cut;
-      select(each, within, p_bin, false, need >= 1.0 ? (u64)ceil(need) : 1u, d.per, in.V, &cut, s);
+  const double t_low = octaves(value_of(plan.min_key), d.per);
+  const int32_t low = plan.min_key ? Power(t_low).bin(t_low, total.E) : kBins;
+  auto kept = [&](uint32_t key, int32_t bin, int32_t id) { return key >= plan.min_key && cut.keeps(bin, key, id); };
+
+  // Two selections, top-k and top-p of what it keeps, then the sums of the slices.  A selection goes through the tokens of its bin
+  // that are kept so far: their range of keys; then passes that sort them into 1024 stretches of the range and narrow it to the
+  // one in which the need is reached, down to one key; then the same by id among the tokens with that key.
+  enum { kRange, kKeys, kIds, kSums };
+  int mode = kRange, what = 0;
+  bool begins = true, divided = false;
+  Cut within = cut;
+  uint32_t lo = 0, hi = 0;
+  int32_t first_id = 0, last_id = 0, shift = 0, edge = kBins;
+  u64 up_to_key = 0, key_mass = 0, wanted = 0;
+  const int32_t row_first = row.first_token(0);
+#pragma unroll 1
+  for (int step = 0; step < 32; ++step) {  // (a selection takes 1 + 4 + 3 at most)
+    if (begins) {
+      begins = false;
+      if (what == 0 && in_bin < 0) what = 1;
+      if (what == 1) {
+        in_bin = -1;
+        if (d.top_p < 1.0f) {
+          const double target = (double)d.top_p * up_to;
+          const int32_t p_bin = min(k_bin, bin_of_mass(s, target));
+          const double inside = ldexp(target - s.before_mass[p_bin], kMassBits + p_bin / kBinsAnOctave);
+          need = inside >= 1.0 ? (u64)ceil(inside) : 1u;
+          if (plan.wanted[p_bin / 64] >> (p_bin & 63) & 1u) in_bin = p_bin;
+        }
+        if (in_bin < 0) what = 2;
+      }
+      __syncthreads();
+      if (what < 2) {
+        mode = kRange;
+        within = cut;
+        up_to_key = 0;
+        if (tid == 0) { s.flag[0] = ~0u; s.flag[1] = 0; }
+      } else {
+        // bins in front of the edge count as they are, the edge's tokens one by one if it is divided
+        mode = kSums;
+        edge = min(cut.bin, low);
+        divided = edge < kBins && (edge == low || cut.key != 0 || cut.id != INT32_MAX);
+        for (int32_t i = tid; i < n_slices; i += kSliceThreads) s.slice_more[i] = 0;
+        if (!divided) break;
+      }
+    }
+    if (mode == kKeys || mode == kIds) {
+      s.bins[tid] = s.bins[tid + kSliceThreads] = 0;
+      s.counts[tid] = s.counts[tid + kSliceThreads] = 0;
+    }
+    __syncthreads();
+    uint32_t my_lo = ~0u, my_hi = 0;
+    for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, tables, s, [&](uint32_t key, int32_t bin, int32_t id) {
+      if (mode == kSums) {
+        if (bin == edge && kept(key, bin, id)) atomicAdd(&s.slice_more[(uint32_t)(id - row_first) / kSliceTokens], Power(octaves(value_of(key), d.per)).mass());
+        return;
+      }
+      if (bin != in_bin || !within.keeps(bin, key, id)) return;
+      if (mode == kRange) {
+        my_lo = min(my_lo, key);
+        my_hi = max(my_hi, key);
+        return;
+      }
+      if (key > hi || key < lo || (mode == kIds && (id < first_id || id > last_id))) return;
+      const uint32_t at = mode == kKeys ? (hi - key) >> shift : (uint32_t)(id - first_id) >> shift;
+      atomicAdd(&s.counts[at], 1u);
+      if (mode == kKeys) atomicAdd(&s.bins[at], Power(octaves(value_of(key), d.per)).mass());
+    });
+    if (mode == kSums) break;
+    if (mode == kRange) {
+      atomicMin(&s.flag[0], my_lo);
+      atomicMax(&s.flag[1], my_hi);
+      __syncthreads();
+      lo = s.flag[0];
+      hi = s.flag[1];
+      if (lo > hi) {  // (no such token)
+        ++what;
+        begins = true;
+        continue;
+      }
+      mode = kKeys;
+      shift = hi - lo < 1024 ? 0 : 22 - __clz((int)(hi - lo));
+      continue;
+    }
+    __syncthreads();
+    // the stretch with the need: two neighbours a thread
+    const bool counted = what == 0 || mode == kIds;
+    const u64 m0 = s.bins[2 * tid], m1 = s.bins[2 * tid + 1];
+    const uint32_t c0 = s.counts[2 * tid], c1 = s.counts[2 * tid + 1];
+    const u64 v0 = counted ? (u64)c0 : m0, v1 = counted ? (u64)c1 : m1;
+    u64 all = v0 + v1, all_mass = m0 + m1;
+#pragma unroll
+    for (int e = 1; e < 64; e <<= 1) {
+      const u64 other = __shfl_up(all, e), other_mass = __shfl_up(all_mass, e);
+      if (lane >= e) { all += other; all_mass += other_mass; }
+    }
+    if (lane == 63) { s.part[wave] = all; s.mass_part[wave] = all_mass; }
+    __syncthreads();
+    u64 whole = 0;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      if (k < wave) { all += s.part[k]; all_mass += s.mass_part[k]; }
+      whole += s.part[k];
+    }
+    need = min(max(need, (u64)1), whole);  // (rounding can leave a need above what there is: the last token then)
+    const u64 begin = all - v0 - v1;
+    __syncthreads();
+    if (begin < need && need <= all) {
+      const bool second = need > begin + v0;
+      s.found[0] = 2 * tid + (second ? 1 : 0);
+      s.part[0] = begin + (second ? v0 : 0);  // in front of the stretch
+      s.part[1] = all_mass - m0 - m1 + (second ? m0 : 0);
+      s.part[2] = second ? m1 : m0;
+      s.counts[0] = second ? c1 : c0;
+    }
+    __syncthreads();
+    need -= s.part[0];
+    const int32_t at = s.found[0];
+    bool done = false;
+    if (mode == kKeys) {
+      up_to_key += s.part[1];
+      const uint32_t floor_key = lo;
+      hi -= (uint32_t)at << shift;
+      lo = shift == 0 ? hi : max(floor_key, hi - ((1u << shift) - 1u));
+      if (hi == lo) {
+        // one key: of its tokens the first so many
+        const uint32_t tied = max(s.counts[0], 1u);
+        key_mass = s.part[2] / tied;
+        wanted = what == 0 ? need : (need + key_mass - 1) / max(key_mass, (u64)1);
+        if (wanted >= tied) {
+          wanted = tied;
+          last_id = within.bin == in_bin && within.key == hi ? within.id : INT32_MAX;
+          done = true;
+        } else {
+          need = wanted;
+          mode = kIds;
+          first_id = 0;
+          last_id = in.V - 1;
+        }
+      }
+      shift = mode == kKeys ? hi - lo < 1024 ? 0 : 22 - __clz((int)(hi - lo)) : in.V <= 1024 ? 0 : 22 - __clz(in.V - 1);
+    } else {
+      first_id += at << shift;
+      last_id = min(last_id, first_id + (1 << shift) - 1);
+      done = first_id == last_id;
+      shift = last_id - first_id < 1024 ? 0 : 22 - __clz(last_id - first_id);
+    }
+    __syncthreads();
+    if (done) {
+      cut = Cut{in_bin, hi, last_id};
+      up_to = s.before_mass[in_bin] + ldexp((double)(up_to_key + wanted * key_mass), -kMassBits - in_bin / kBinsAnOctave);
+      ++what;
+      begins = true;
     }
   }
-  const int32_t low = bin_of_min(d, total.top, total.E), edge = min(cut.bin, low);
-  // kept: what the cut keeps and min_p does not drop; always the largest
-  auto kept = [&](uint32_t key, int32_t bin, int32_t id) {
-    if (!cut.keeps(bin, key, id) || bin > low) return false;
-    return bin < low || exp(((double)value_of(key) - (double)total.top) / (double)d.temperature) >= (double)d.min_p;
-  };
-  // the slices' sums: bins in front of the edge as they are, those of its tokens one by one if it is divided
-  const bool divided = edge < kBins && (edge == low || cut.key != 0 || cut.id != INT32_MAX);
-  for (int32_t i = tid; i < n_slices; i += kSliceThreads) s.slice_more[i] = 0;
   __syncthreads();
-  if (divided) {
-    const int32_t first = row.first_token(0);
-    each([&](uint32_t key, int32_t in_bin, int32_t id) {
-      if (in_bin != edge) return;
-      const Power w(octaves(value_of(key), d.per));
-      if (kept(key, in_bin, id)) atomicAdd(&s.slice_more[(uint32_t)(id - first) / kSliceTokens], w.mass());
-    });
-  }
-  __syncthreads();
+  const double up_to_bin = (double)(divided ? edge : min(edge + 1, kBins));
+#pragma unroll 1
   for (int32_t i = wave; i < n_slices; i += kWaves) {
-    const Slot one = slots[i];
     double sum = 0.0;
-    if (one.top > -__builtin_inff()) {
-      const double off = (total.E - one.E) * kBinsAnOctave;  // of the slice's bins in the row's
+    if (s.slots[i].top > -__builtin_inff()) {
+      const double off = (total.E - s.slots[i].E) * kBinsAnOctave;  // of the slice's bins in the row's
 #pragma unroll
       for (int k = 0; k < kBins / 64; ++k) {
-        const int32_t bin = lane * (kBins / 64) + k;  // of the slice
+        const int32_t bin = k * 64 + lane;  // of the slice
         const double at = off + (double)bin;
-        if (at < (double)(divided ? edge : min(edge + 1, kBins))) sum += ldexp((double)(bins[(size_t)i * kBins + bin] & kMassMask), -kMassBits - (int32_t)at / kBinsAnOctave);
+        if (at < up_to_bin) sum += ldexp((double)(bins[(size_t)i * kBins + bin] & kMassMask), -kMassBits - (int32_t)at / kBinsAnOctave);
       }
     }
     sum = wave_sum(sum);
@@ -992,20 +1056,17 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   find_slice(d.u, n_slices, s);
   const double rest = s.rest;
   const int32_t first = row.first_token(s.slice);
+  __syncthreads();
   load_slice<E>(row, r, b, first, tables, y);
-  const int32_t id = find_token<E>(y, first, rest, s, [&](float v, int32_t token) {
+  float logit = 0.0f;
+  const int32_t id = find_token(y, first, rest, &logit, s, [&](float v, int32_t token) {
     if (!(v > -__builtin_inff())) return 0.0;
     const double t = octaves(v, d.per);
     const Power w(t);
     const int32_t bin = w.bin(t, total.E);
     return bin < kBins && kept(key_of(v), bin, token) ? w.weight(total.E) : 0.0;
   });
-#pragma unroll
-  for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (token_of<E>(first, j, i) == id) write_out(d, total, id, y[j][i], ids + b, logprobs ? logprobs + b : nullptr);
-  if (tid == 0 && id < 0) write_out(d, total, -1, 0.0f, ids + b, logprobs ? logprobs + b : nullptr);
+  if (tid == 0) write_out(d, total, id, logit, ids + b, logprobs ? logprobs + b : nullptr);
 }
 
 template <template <Elem> class Launch, class... Args>
