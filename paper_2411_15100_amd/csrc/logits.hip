@@ -16,7 +16,7 @@ namespace {
 // A workgroup takes kSliceTokens tokens of a row, a thread two groups of 8 neighbours.  A slice begins on 16 bytes, up to a group less
 // one token in front of a row that does not, so that a group is one load of 16 bytes (two of them in 32 bits); groups that reach over
 // an end of the row are taken token by token.
-constexpr int kSliceThreads = 512, kSliceTokens = 8192, kGroups = kSliceTokens / 8 / kSliceThreads;
+constexpr int kSliceThreads = 512, kSliceTokens = 8192, kGroups = kSliceTokens / 8 / kSliceThreads, kTokens = 8 * kGroups;
 
 template <Elem E> struct Row {
   const typename Type<E>::bits* at;
@@ -318,7 +318,8 @@ __device__ __forceinline__ void put_out(Slot* to, const Slot& s) {
 __device__ __forceinline__ Slot take_in(const Slot* from) { return Slot{take_in(&from->E), take_in(&from->sum), take_in(&from->top), take_in(&from->top_id)}; }
 
 constexpr int kMostSlices = (1 << 20) / kSliceTokens + 1;
-constexpr int kFew = 2048;  // candidates that are kept in LDS
+constexpr int kFew = 2048;    // candidates that are kept in LDS
+constexpr int kRanked = 256;  // and so many are compared each with each
 struct Shared {
   double sum[kGroups][kWaves];
   u64 part[kWaves], mass_part[kWaves];
@@ -331,7 +332,7 @@ struct Shared {
   Slot slots[kMostSlices];
   double slice_sum[kMostSlices];
   u64 slice_more[kMostSlices];
-  u64 few[kFew];
+  u64 few[kFew], ranked[kRanked];
   uint32_t flag[2];
   int32_t found[2];
   double rest;
@@ -360,7 +361,7 @@ __device__ __forceinline__ double wave_sum(double x) {
 
 // The logits of a slice under the rules.
 template <Elem E>
-__device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& r, int32_t b, int32_t first, uint32_t* tables, float (&y)[kGroups][8]) {
+__device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& r, int32_t b, int32_t first, uint32_t* tables, float (&y)[kTokens]) {
   uint32_t *counts = tables, *entries = tables + (r.tokens ? kSliceTokens : 0);
   const bool ruled = r.tokens || r.bias_ids;
   const History h = history_ahead(r, b);
@@ -378,88 +379,82 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[j][i] = ok[j] >> i & 1u ? widened<E>(x[j][i]) : -__builtin_inff();
+    for (int i = 0; i < 8; ++i) y[8 * j + i] = ok[j] >> i & 1u ? widened<E>(x[j][i]) : -__builtin_inff();
     if (ruled && ok[j])
       touched(r, counts, entries, (j * kSliceThreads + (int32_t)threadIdx.x) * 8,
-              [&](int i, uint32_t count, uint32_t entry) { if (ok[j] >> i & 1u) y[j][i] = rule(y[j][i], count, entry); });
+              [&](int i, uint32_t count, uint32_t entry) { if (ok[j] >> i & 1u) y[8 * j + i] = rule(y[8 * j + i], count, entry); });
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[j][i] = drawable(y[j][i]);
+    for (int i = 0; i < 8; ++i) y[8 * j + i] = drawable(y[8 * j + i]);
   }
 }
-template <Elem E> __device__ __forceinline__ int32_t token_of(int32_t first, int j, int i) { return first + (j * kSliceThreads + (int32_t)threadIdx.x) * 8 + i; }
+__device__ __forceinline__ int32_t token_of(int32_t first, int k) { return first + (k / 8 * kSliceThreads + (int32_t)threadIdx.x) * 8 + k % 8; }
 
 // Calls f(logit, token) for the thread's tokens of a slice in order of their ids.  The logits go round in their registers instead of the
 // loop being unrolled: what a single workgroup does once costs as much for fetching its instructions as for carrying them out.
-template <class F> __device__ __forceinline__ void for_tokens(float (&y)[kGroups][8], int32_t first, F&& f) {
-#pragma unroll
-  for (int j = 0; j < kGroups; ++j) {
-    const int32_t t = first + (j * kSliceThreads + (int32_t)threadIdx.x) * 8;
+template <class F> __device__ __forceinline__ void for_tokens(float (&y)[kTokens], int32_t first, F&& f) {
 #pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-      const float v = y[j][0];
+  for (int k = 0; k < kTokens; ++k) {
+    const float v = y[0];
 #pragma unroll
-      for (int k = 0; k < 7; ++k) y[j][k] = y[j][k + 1];
-      y[j][7] = v;
-      f(v, t + i, j);
-    }
+    for (int i = 0; i < kTokens - 1; ++i) y[i] = y[i + 1];
+    y[kTokens - 1] = v;
+    f(v, token_of(first, k), k / 8);
   }
 }
 
 // The token of a slice at which the running sum of weights (w of a token's logit and id) first exceeds `rest`, and its logit; the
 // last one with a weight if rounding leaves none; -1 if none has any.
-template <class W> __device__ int32_t find_token(float (&y)[kGroups][8], int32_t first, double rest, float* logit, Shared& s, W&& w) {
+template <class W> __device__ int32_t find_token(float (&y)[kTokens], int32_t first, double rest, float* logit, Shared& s, W&& w) {
+  static_assert(kGroups == 2, "two groups a thread");
   const int32_t lane = (int32_t)threadIdx.x & 63, wave = (int32_t)threadIdx.x >> 6;
-  double run[kGroups] = {};
+  double run0 = 0.0, run1 = 0.0;
   int32_t last = -1;
   for_tokens(y, first, [&](float v, int32_t t, int j) {
     const double x = w(v, t);
-    run[j] += x;
+    run0 += j ? 0.0 : x;
+    run1 += j ? x : 0.0;
     if (x > 0.0) last = t;
   });
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j) {
-      const double other = __shfl_up(run[j], d);
-      if (lane >= d) run[j] += other;
-    }
+    const double other0 = __shfl_up(run0, d), other1 = __shfl_up(run1, d);
+    if (lane >= d) { run0 += other0; run1 += other1; }
   }
   __syncthreads();
   if (threadIdx.x == 0) { s.found[0] = INT32_MAX; s.found[1] = -1; }
-  if (lane == 63) {
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j) s.sum[j][wave] = run[j];
-  }
+  if (lane == 63) { s.sum[0][wave] = run0; s.sum[1][wave] = run1; }
   __syncthreads();
   if (last >= 0) atomicMax(&s.found[1], last);
-  double base = 0.0, at[kGroups];
-  bool mine[kGroups], any = false;
+  double base = 0.0, before0 = 0.0, before1 = 0.0;
 #pragma unroll
-  for (int j = 0; j < kGroups; ++j) {
-    double before = base;
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
-      if (k == wave) before = base;
-      base += s.sum[j][k];
-    }
-    const double up = __shfl_up(run[j], 1);
-    at[j] = lane ? before + up : before;
-    mine[j] = at[j] <= rest && rest < before + run[j];
-    any |= mine[j];
+  for (int k = 0; k < kWaves; ++k) {
+    if (k == wave) before0 = base;
+    base += s.sum[0][k];
   }
-  if (any) {
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) {
+    if (k == wave) before1 = base;
+    base += s.sum[1][k];
+  }
+  const double up0 = __shfl_up(run0, 1), up1 = __shfl_up(run1, 1);
+  const double at0 = lane ? before0 + up0 : before0, at1 = lane ? before1 + up1 : before1;
+  const bool in0 = at0 <= rest && rest < before0 + run0, in1 = at1 <= rest && rest < before1 + run1;
+  if (in0 || in1) {
     int32_t token = -1;
+    double at = in0 ? at0 : at1;
     for_tokens(y, first, [&](float v, int32_t t, int j) {
-      if (!mine[j]) return;
+      if ((j == 0) != in0) return;
       const double x = w(v, t);
-      if (x > 0.0 && (token < 0 || at[j] <= rest)) token = t;  // (the last whose stretch begins at or before)
-      at[j] += x;
+      if (x > 0.0 && (token < 0 || at <= rest)) token = t;  // (the last whose stretch begins at or before)
+      at += x;
     });
     if (token >= 0) atomicMin(&s.found[0], token);
   }
   __syncthreads();
   const int32_t id = s.found[0] != INT32_MAX ? s.found[0] : s.found[1];
-  for_tokens(y, first, [&](float v, int32_t t, int) { if (t == id) s.top[0] = v; });
+#pragma unroll
+  for (int k = 0; k < kTokens; ++k)
+    if (token_of(first, k) == id) s.top[0] = y[k];
   __syncthreads();
   *logit = s.top[0];
   return id;
@@ -669,16 +664,14 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
   Slot* const slots = m.slots + (size_t)b * m.slices;
   u64* const bins = m.bins + (size_t)b * m.slices * kBins;
   int32_t first = row.first_token(slice);
-  float y[kGroups][8];
+  float y[kTokens];
   load_slice<E>(row, r, b, first, tables, y);
 
   float top = -__builtin_inff();
   int32_t top_id = -1;
 #pragma unroll
-  for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (y[j][i] > top) { top = y[j][i]; top_id = token_of<E>(first, j, i); }
+  for (int k = 0; k < kTokens; ++k)
+    if (y[k] > top) { top = y[k]; top_id = token_of(first, k); }
 #pragma unroll
   for (int k = 32; k; k >>= 1) {
     const float other = __shfl_xor(top, k);
@@ -705,18 +698,14 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
         if (bin < kBins) atomicAdd(&s.bins[bin], w.mass() + (1ull << kCountShift));
       }
     };
-#pragma unroll
-    for (int j = 0; j < kGroups; ++j)
 #pragma unroll 1
-      for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < kTokens / 4; ++h) {
+      const float a = y[0], b0 = y[1], c = y[2], e = y[3];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float v = y[j][i];
-          y[j][i] = y[j][i + 4];
-          y[j][i + 4] = v;
-          add(v);
-        }
-      }
+      for (int i = 0; i < kTokens - 4; ++i) y[i] = y[i + 4];
+      y[kTokens - 4] = a; y[kTokens - 3] = b0; y[kTokens - 2] = c; y[kTokens - 1] = e;
+      add(a); add(b0); add(c); add(e);
+    }
     sum = wave_sum(sum);
     if (lane == 0) s.sum[0][wave] = sum;
     __syncthreads();
@@ -786,6 +775,17 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
   }
 }
 
+// A range of keys that holds the tokens of the bins first .. last: where the bins' borders lie, and two keys more at both ends for
+// what the divisions round.
+struct KeyRange { uint32_t lo, hi; };
+__device__ KeyRange keys_of_bins(int32_t first, int32_t last, double E, double per) {
+  if (!(per > 0.0)) return KeyRange{0, ~0u};
+  const double t_hi = E + 1.0 - (double)first / kBinsAnOctave, t_lo = E + 1.0 - (double)(last + 1) / kBinsAnOctave;
+  const float hi = (float)fmin(fmax(t_hi / per, -(double)FLT_MAX), (double)FLT_MAX), lo = (float)fmin(fmax(t_lo / per, -(double)FLT_MAX), (double)FLT_MAX);
+  const uint32_t a = key_of(lo), b = key_of(hi);
+  return KeyRange{a > 2 ? a - 2 : 0, b < ~0u - 2 ? b + 2 : ~0u};
+}
+
 // Goes through the tokens of the wanted bins: f(key, bin, id).  All threads; `listed` of them, a few in s.few, or more than the list holds.
 template <Elem E, class F>
 __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRules& r, const RowDraw& d, const RowPlan& plan, int32_t b, int32_t n_slices, const u64* list,
@@ -800,7 +800,7 @@ __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRul
   }
   for (int32_t slice = 0; slice < n_slices; ++slice) {
     const int32_t first = row.first_token(slice);
-    float y[kGroups][8];
+    float y[kTokens];
     __syncthreads();  // (the tables of the last slice have been read)
     load_slice<E>(row, r, b, first, tables, y);
     for_tokens(y, first, [&](float v, int32_t id, int) {
@@ -834,7 +834,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   const Slot* const slots = m.slots + (size_t)b * m.slices;
   const u64* const bins = m.bins + (size_t)b * m.slices * kBins;
   u64* const list = m.candidates + (size_t)b * kMostCandidates;
-  float y[kGroups][8];
+  float y[kTokens];
 
   // the tokens of the wanted bins, if the slice has any
   if (tid == 0) s.flag[1] = 0;
@@ -846,19 +846,38 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   }
   __syncthreads();
   if (s.flag[1]) {
+    int32_t lightest = -1, heaviest = kBins;
+#pragma unroll
+    for (int k = 0; k < kBins / 64; ++k) {
+      if (plan.wanted[k]) lightest = k * 64 + 63 - __builtin_clzll(plan.wanted[k]);
+      if (plan.wanted[k] && heaviest == kBins) heaviest = k * 64 + __builtin_ctzll(plan.wanted[k]);
+    }
+    const KeyRange range = keys_of_bins(heaviest, lightest, plan.E, d.per);
+    if (tid == 0) s.flag[0] = 0;
     const int32_t first = row.first_token(slice);
     load_slice<E>(row, r, b, first, tables, y);
+    __syncthreads();
     for_tokens(y, first, [&](float v, int32_t id, int) {
+      const uint32_t key = key_of(v);
+      if (!(v > -__builtin_inff()) || key < range.lo || key > range.hi) return;
       const double t = octaves(v, d.per);
-      const int32_t bin = v > -__builtin_inff() ? Power(t).bin(t, plan.E) : kBins;
-      const bool mine = bin < kBins && (plan.wanted[bin / 64] >> (bin & 63) & 1u);
-      const u64 who = __ballot(mine);
-      if (!who) return;
-      uint32_t at = 0;
-      if (lane == 0) at = __hip_atomic_fetch_add(m.n_candidates + b, (uint32_t)__popcll(who), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      at = __builtin_amdgcn_readfirstlane(at) + (uint32_t)__popcll(who & ((1ull << lane) - 1ull));
-      if (mine && at < kMostCandidates) put_out(list + at, (u64)key_of(v) << 32 | (u64)bin << 24 | (u64)(uint32_t)id);
+      const int32_t bin = Power(t).bin(t, plan.E);
+      if (bin >= kBins || !(plan.wanted[bin / 64] >> (bin & 63) & 1u)) return;
+      const u64 x = (u64)key << 32 | (u64)bin << 24 | (u64)(uint32_t)id;
+      const uint32_t at = atomicAdd(&s.flag[0], 1u);
+      if (at < kFew) {
+        s.few[at] = x;
+      } else {  // (more than the workgroup collects: one by one)
+        const uint32_t place = __hip_atomic_fetch_add(m.n_candidates + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (place < kMostCandidates) put_out(list + place, x);
+      }
     });
+    __syncthreads();
+    const uint32_t n = min(s.flag[0], (uint32_t)kFew);
+    if (tid == 0 && n) s.counts[0] = __hip_atomic_fetch_add(m.n_candidates + b, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    for (uint32_t i = (uint32_t)tid; i < n; i += kSliceThreads)
+      if (s.counts[0] + i < kMostCandidates) put_out(list + s.counts[0] + i, s.few[i]);
   }
   if (!last_of(m.arrived + m.rows + b, (uint32_t)n_slices, s)) return;
 
@@ -884,19 +903,19 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   const int32_t low = plan.min_key ? Power(t_low).bin(t_low, total.E) : kBins;
   auto kept = [&](uint32_t key, int32_t bin, int32_t id) { return key >= plan.min_key && cut.keeps(bin, key, id); };
 
-  // Two selections, top-k and top-p of what it keeps, then the sums of the slices.  A selection goes through the tokens of its bin
-  // that are kept so far: their range of keys; then passes that sort them into 1024 stretches of the range and narrow it to the
-  // one in which the need is reached, down to one key; then the same by id among the tokens with that key.
-  enum { kRange, kKeys, kIds, kSums };
-  int mode = kRange, what = 0;
+  // Two selections, top-k and top-p of what it keeps, then the sums of the slices.  A selection goes through the tokens of its bin that
+  // are kept so far: passes that sort them into 1024 stretches of their range of keys, and then of ids among the tokens with one
+  // key, and narrow the range to the stretch in which the need is reached, until few are left; each of those is then compared with all others.
+  enum { kKeys, kIds, kRank, kSums };
+  int mode = kKeys, what = 0;
   bool begins = true, divided = false;
   Cut within = cut;
-  uint32_t lo = 0, hi = 0;
+  uint32_t lo = 0, hi = 0, left = 0;
   int32_t first_id = 0, last_id = 0, shift = 0, edge = kBins;
-  u64 up_to_key = 0, key_mass = 0, wanted = 0;
+  u64 up_to_key = 0, key_mass = 0;
   const int32_t row_first = row.first_token(0);
 #pragma unroll 1
-  for (int step = 0; step < 32; ++step) {  // (a selection takes 1 + 4 + 3 at most)
+  for (int step = 0; step < 32; ++step) {  // (a selection takes 4 + 3 + 1 at most)
     if (begins) {
       begins = false;
       if (what == 0 && in_bin < 0) what = 1;
@@ -913,10 +932,15 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
       }
       __syncthreads();
       if (what < 2) {
-        mode = kRange;
+        const KeyRange range = keys_of_bins(in_bin, in_bin, total.E, d.per);
+        lo = range.lo;
+        hi = range.hi;
+        first_id = 0;
+        last_id = in.V - 1;
         within = cut;
         up_to_key = 0;
-        if (tid == 0) { s.flag[0] = ~0u; s.flag[1] = 0; }
+        mode = kKeys;
+        left = listed;
       } else {
         // bins in front of the edge count as they are, the edge's tokens one by one if it is divided
         mode = kSums;
@@ -926,45 +950,65 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
         if (!divided) break;
       }
     }
-    if (mode == kKeys || mode == kIds) {
+    if (mode != kSums && left <= kRanked) {
+      mode = kRank;
+      if (tid == 0) { s.flag[0] = 0; s.found[0] = -1; }
+    } else if (mode != kSums) {
       s.bins[tid] = s.bins[tid + kSliceThreads] = 0;
       s.counts[tid] = s.counts[tid + kSliceThreads] = 0;
+      const uint32_t width = mode == kKeys ? hi - lo : (uint32_t)(last_id - first_id);
+      shift = width < 1024 ? 0 : 22 - __clz((int)width);
     }
     __syncthreads();
-    uint32_t my_lo = ~0u, my_hi = 0;
     for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, tables, s, [&](uint32_t key, int32_t bin, int32_t id) {
       if (mode == kSums) {
         if (bin == edge && kept(key, bin, id)) atomicAdd(&s.slice_more[(uint32_t)(id - row_first) / kSliceTokens], Power(octaves(value_of(key), d.per)).mass());
         return;
       }
-      if (bin != in_bin || !within.keeps(bin, key, id)) return;
-      if (mode == kRange) {
-        my_lo = min(my_lo, key);
-        my_hi = max(my_hi, key);
+      if (bin != in_bin || !within.keeps(bin, key, id) || key > hi || key < lo || id < first_id || id > last_id) return;
+      const u64 mass = mode != kIds ? Power(octaves(value_of(key), d.per)).mass() : 0;
+      if (mode == kRank) {
+        const uint32_t at = atomicAdd(&s.flag[0], 1u);
+        s.ranked[at] = (u64)~key << 32 | (uint32_t)id;
+        s.bins[at] = mass;
         return;
       }
-      if (key > hi || key < lo || (mode == kIds && (id < first_id || id > last_id))) return;
       const uint32_t at = mode == kKeys ? (hi - key) >> shift : (uint32_t)(id - first_id) >> shift;
       atomicAdd(&s.counts[at], 1u);
-      if (mode == kKeys) atomicAdd(&s.bins[at], Power(octaves(value_of(key), d.per)).mass());
+      if (mode == kKeys) atomicAdd(&s.bins[at], mass);
     });
     if (mode == kSums) break;
-    if (mode == kRange) {
-      atomicMin(&s.flag[0], my_lo);
-      atomicMax(&s.flag[1], my_hi);
-      __syncthreads();
-      lo = s.flag[0];
-      hi = s.flag[1];
-      if (lo > hi) {  // (no such token)
-        ++what;
-        begins = true;
-        continue;
+    __syncthreads();
+    if (mode == kRank) {
+      const uint32_t n = s.flag[0];
+      if (n > 0 && (uint32_t)tid < n) {
+        const u64 mine = s.ranked[tid], own = s.bins[tid];
+        u64 before = 0, whole = 0;
+        uint32_t rank = 0;
+        for (uint32_t i = 0; i < n; ++i) {
+          const u64 x = s.bins[i];
+          const bool front = s.ranked[i] < mine;
+          before += front ? x : 0;
+          rank += front ? 1 : 0;
+          whole += x;
+        }
+        // (rounding can leave a need above what there is: the last token then)
+        const u64 wanted = min(max(need, (u64)1), what == 0 ? (u64)n : whole), at = what == 0 ? (u64)rank : before;
+        if (at < wanted && wanted <= at + (what == 0 ? 1 : own)) {
+          s.found[0] = tid;
+          s.part[0] = before + own;
+        }
       }
-      mode = kKeys;
-      shift = hi - lo < 1024 ? 0 : 22 - __clz((int)(hi - lo));
+      __syncthreads();
+      const int32_t at = s.found[0];
+      if (at >= 0) {
+        cut = Cut{in_bin, ~(uint32_t)(s.ranked[at] >> 32), (int32_t)(uint32_t)s.ranked[at]};
+        up_to = s.before_mass[in_bin] + ldexp((double)(up_to_key + s.part[0]), -kMassBits - in_bin / kBinsAnOctave);
+      }
+      ++what;
+      begins = true;
       continue;
     }
-    __syncthreads();
     // the stretch with the need: two neighbours a thread
     const bool counted = what == 0 || mode == kIds;
     const u64 m0 = s.bins[2 * tid], m1 = s.bins[2 * tid + 1];
@@ -977,6 +1021,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
       if (lane >= e) { all += other; all_mass += other_mass; }
     }
     if (lane == 63) { s.part[wave] = all; s.mass_part[wave] = all_mass; }
+    if (tid == 0) s.found[0] = -1;
     __syncthreads();
     u64 whole = 0;
 #pragma unroll
@@ -984,7 +1029,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
       if (k < wave) { all += s.part[k]; all_mass += s.mass_part[k]; }
       whole += s.part[k];
     }
-    need = min(max(need, (u64)1), whole);  // (rounding can leave a need above what there is: the last token then)
+    need = min(max(need, (u64)1), whole);
     const u64 begin = all - v0 - v1;
     __syncthreads();
     if (begin < need && need <= all) {
@@ -993,47 +1038,37 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
       s.part[0] = begin + (second ? v0 : 0);  // in front of the stretch
       s.part[1] = all_mass - m0 - m1 + (second ? m0 : 0);
       s.part[2] = second ? m1 : m0;
-      s.counts[0] = second ? c1 : c0;
+      s.flag[0] = second ? c1 : c0;
     }
     __syncthreads();
-    need -= s.part[0];
     const int32_t at = s.found[0];
-    bool done = false;
+    if (at < 0) {  // (no token at all)
+      ++what;
+      begins = true;
+      continue;
+    }
+    left = s.flag[0];
     if (mode == kKeys) {
+      need -= s.part[0];
       up_to_key += s.part[1];
       const uint32_t floor_key = lo;
       hi -= (uint32_t)at << shift;
       lo = shift == 0 ? hi : max(floor_key, hi - ((1u << shift) - 1u));
-      if (hi == lo) {
+      if (hi == lo && left > kRanked) {
         // one key: of its tokens the first so many
-        const uint32_t tied = max(s.counts[0], 1u);
-        key_mass = s.part[2] / tied;
-        wanted = what == 0 ? need : (need + key_mass - 1) / max(key_mass, (u64)1);
-        if (wanted >= tied) {
-          wanted = tied;
-          last_id = within.bin == in_bin && within.key == hi ? within.id : INT32_MAX;
-          done = true;
-        } else {
-          need = wanted;
-          mode = kIds;
-          first_id = 0;
-          last_id = in.V - 1;
-        }
+        key_mass = s.part[2] / left;
+        if (what == 1) need = (need + key_mass - 1) / max(key_mass, (u64)1);
+        need = min(max(need, (u64)1), (u64)left);
+        mode = kIds;
       }
-      shift = mode == kKeys ? hi - lo < 1024 ? 0 : 22 - __clz((int)(hi - lo)) : in.V <= 1024 ? 0 : 22 - __clz(in.V - 1);
     } else {
+      need -= s.part[0];
+      up_to_key += s.part[0] * key_mass;
       first_id += at << shift;
       last_id = min(last_id, first_id + (1 << shift) - 1);
-      done = first_id == last_id;
-      shift = last_id - first_id < 1024 ? 0 : 22 - __clz(last_id - first_id);
+      if (left <= kRanked && what == 1) need *= key_mass;  // (in mass again for the comparison)
     }
     __syncthreads();
-    if (done) {
-      cut = Cut{in_bin, hi, last_id};
-      up_to = s.before_mass[in_bin] + ldexp((double)(up_to_key + wanted * key_mass), -kMassBits - in_bin / kBinsAnOctave);
-      ++what;
-      begins = true;
-    }
   }
   __syncthreads();
   const double up_to_bin = (double)(divided ? edge : min(edge + 1, kBins));
@@ -1059,8 +1094,9 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   __syncthreads();
   load_slice<E>(row, r, b, first, tables, y);
   float logit = 0.0f;
+  const uint32_t least_key = max(max(plan.min_key, cut.key), keys_of_bins(edge, min(edge, kBins - 1), total.E, d.per).lo);  // of what is kept
   const int32_t id = find_token(y, first, rest, &logit, s, [&](float v, int32_t token) {
-    if (!(v > -__builtin_inff())) return 0.0;
+    if (!(v > -__builtin_inff()) || key_of(v) < least_key) return 0.0;
     const double t = octaves(v, d.per);
     const Power w(t);
     const int32_t bin = w.bin(t, total.E);
