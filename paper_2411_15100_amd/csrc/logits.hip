@@ -18,6 +18,8 @@ namespace {
 // an end of the row are taken token by token.
 constexpr int kSliceThreads = 512, kSliceTokens = 8192, kGroups = kSliceTokens / 8 / kSliceThreads, kTokens = 8 * kGroups;
 
+typedef float Tokens __attribute__((ext_vector_type(kTokens)));  // of a thread; a vector, so that it never leaves the registers
+
 template <Elem E> struct Row {
   const typename Type<E>::bits* at;
   int32_t V;
@@ -210,8 +212,8 @@ template <Elem E> int32_t slices_of(const Logits& in) {
 // down, with the number of tokens and the sum of their weights in whole numbers (2^-35 of the bin's octave), which do not depend on
 // the order of the atomics.  The workgroup that finishes last for its row puts the slices together.  Without a cut it then
 // knows the slice of the drawn token and goes through that one again; with a cut it knows the few bins in which the cuts lie.
-// Second kernel, for rows with a cut: the tokens of those bins are listed (where there are too many, gone through again each time);
-// the workgroup that finishes last finds the cuts in them, the slice and the token.
+// Second kernel, for rows with a cut, one workgroup per slice: the tokens of those bins are listed.  Third, one workgroup per row: it finds the
+// cuts among them (where there are too many for the list it goes through the row again each time), the slice and the token.
 // What workgroups of one kernel hand to each other goes through atomics of the device, which no cache of an XCD holds back.
 constexpr int kWaves = kSliceThreads / 64;
 constexpr int kBins = 256, kBinsAnOctave = 4;
@@ -274,15 +276,21 @@ struct Slot {  // what a slice leaves
   float top;     // -inf: nothing can be drawn
   int32_t top_id;
 };
-struct RowPlan {  // what the first kernel leaves of a row for the second
-  u64 wanted[kBins / 64];  // bins of which it needs the tokens
-  double E;
+struct RowTotal {  // of a row: its octave, sum, largest logit and its lowest id
+  double E, sum;
   float top;
+  int32_t top_id;
+};
+struct RowPlan {  // what the first kernel leaves of a row for the others
+  u64 wanted[kBins / 64];  // bins of which they need the tokens
+  RowTotal total;
   int32_t cut;       // 0: the row is done
   uint32_t min_key;  // tokens with a smaller key weigh less than min_p
+  int32_t k_bin, k_need;  // where top-k ends and how many of its tokens there (0: all); k_bin = kBins: nowhere
+  double before[kBins + 1];  // mass in front of each bin, in 2^E
 };
 struct DrawMemory {
-  uint32_t *arrived, *n_candidates;  // [2][rows], [rows]: zero between calls
+  uint32_t *arrived, *n_candidates;  // [rows]: zero between calls
   RowPlan* plans;
   Slot* slots;       // [rows][slices]
   u64* bins;         // [rows][slices][kBins]
@@ -297,7 +305,7 @@ DrawMemory memory_at(void* at, int32_t rows, int32_t V, size_t* bytes) {
   m.slices = most_slices(V);
   char* p = static_cast<char*>(at);
   auto take = [&](size_t n) { char* q = p; p += rounded(n); return q; };
-  m.arrived = reinterpret_cast<uint32_t*>(take((size_t)rows * 8));
+  m.arrived = reinterpret_cast<uint32_t*>(take((size_t)rows * 4));
   m.n_candidates = reinterpret_cast<uint32_t*>(take((size_t)rows * 4));
   m.plans = reinterpret_cast<RowPlan*>(take((size_t)rows * sizeof(RowPlan)));
   m.slots = reinterpret_cast<Slot*>(take((size_t)rows * m.slices * sizeof(Slot)));
@@ -332,11 +340,12 @@ struct Shared {
   Slot slots[kMostSlices];
   double slice_sum[kMostSlices];
   u64 slice_more[kMostSlices];
-  u64 few[kFew], ranked[kRanked];
   uint32_t flag[2];
   int32_t found[2];
   double rest;
   int32_t slice;
+  u64 few[kFew];        // (not in the first kernel)
+  u64 ranked[kRanked];  // (only in the third)
 };
 
 // Whether this workgroup is the last of the row's n to come here; what the others have put out before can be taken in then.
@@ -361,7 +370,7 @@ __device__ __forceinline__ double wave_sum(double x) {
 
 // The logits of a slice under the rules.
 template <Elem E>
-__device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& r, int32_t b, int32_t first, uint32_t* tables, float (&y)[kTokens]) {
+__device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& r, int32_t b, int32_t first, uint32_t* tables, Tokens& y) {
   uint32_t *counts = tables, *entries = tables + (r.tokens ? kSliceTokens : 0);
   const bool ruled = r.tokens || r.bias_ids;
   const History h = history_ahead(r, b);
@@ -386,25 +395,24 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[8 * j + i] = drawable(y[8 * j + i]);
   }
+  if (ruled) __syncthreads();  // (other things lie where the tables were)
 }
 __device__ __forceinline__ int32_t token_of(int32_t first, int k) { return first + (k / 8 * kSliceThreads + (int32_t)threadIdx.x) * 8 + k % 8; }
 
 // Calls f(logit, token) for the thread's tokens of a slice in order of their ids.  The logits go round in their registers instead of the
 // loop being unrolled: what a single workgroup does once costs as much for fetching its instructions as for carrying them out.
-template <class F> __device__ __forceinline__ void for_tokens(float (&y)[kTokens], int32_t first, F&& f) {
+template <class F> __device__ __forceinline__ void for_tokens(Tokens& y, int32_t first, F&& f) {
 #pragma unroll 1
   for (int k = 0; k < kTokens; ++k) {
     const float v = y[0];
-#pragma unroll
-    for (int i = 0; i < kTokens - 1; ++i) y[i] = y[i + 1];
-    y[kTokens - 1] = v;
+    y = __builtin_shufflevector(y, y, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0);
     f(v, token_of(first, k), k / 8);
   }
 }
 
 // The token of a slice at which the running sum of weights (w of a token's logit and id) first exceeds `rest`, and its logit; the
 // last one with a weight if rounding leaves none; -1 if none has any.
-template <class W> __device__ int32_t find_token(float (&y)[kTokens], int32_t first, double rest, float* logit, Shared& s, W&& w) {
+template <class W> __device__ int32_t find_token(Tokens& y, int32_t first, double rest, float* logit, Shared& s, W&& w) {
   static_assert(kGroups == 2, "two groups a thread");
   const int32_t lane = (int32_t)threadIdx.x & 63, wave = (int32_t)threadIdx.x >> 6;
   double run0 = 0.0, run1 = 0.0;
@@ -481,15 +489,10 @@ struct RowDraw {  // how a row is drawn
 };
 
 // The row's largest logit, its lowest id, octave and sum (thread by thread the same), from its slots, which are brought to s.slots;
-// the slices' sums relative to the row's octave lie in s.slice_sum.  FRESH: the slots come from other workgroups of this kernel.
-struct RowTotal {
-  double E, sum;
-  float top;
-  int32_t top_id;
-};
-template <bool FRESH> __device__ RowTotal row_total(const Slot* slots, int32_t n, Shared& s) {
+// the slices' sums relative to the row's octave lie in s.slice_sum.
+__device__ RowTotal row_total(const Slot* slots, int32_t n, Shared& s) {
   const int32_t lane = (int32_t)threadIdx.x & 63;
-  if ((int32_t)threadIdx.x < n) s.slots[threadIdx.x] = FRESH ? take_in(slots + threadIdx.x) : slots[threadIdx.x];
+  if ((int32_t)threadIdx.x < n) s.slots[threadIdx.x] = take_in(slots + threadIdx.x);
   __syncthreads();
   RowTotal r{-__builtin_inf(), 0.0, -__builtin_inff(), INT32_MAX};
   for (int32_t i = lane; i < n; i += 64)
@@ -563,7 +566,7 @@ __device__ __forceinline__ void write_out(const RowDraw& d, const RowTotal& r, i
 
 // The row's bins from its slices' into s.bins and s.counts, relative to the octave E, and what lies in front of each (s.before_*;
 // masses in 2^E).  All threads, after row_total: half of them take the even slices and half the odd ones.
-template <bool FRESH> __device__ void row_bins(const u64* bins, int32_t n, double E, Shared& s) {
+__device__ void row_bins(const u64* bins, int32_t n, double E, Shared& s) {
   static_assert(kSliceThreads == 2 * kBins, "two threads a bin");
   const int32_t tid = (int32_t)threadIdx.x, bin = tid & (kBins - 1);
   __syncthreads();
@@ -574,7 +577,7 @@ template <bool FRESH> __device__ void row_bins(const u64* bins, int32_t n, doubl
     const double d = s.slots[i].top > -__builtin_inff() ? (E - s.slots[i].E) * kBinsAnOctave : (double)kBins;
     const bool some = d <= (double)bin;
     const u64* at = bins + (size_t)i * kBins + (some ? bin - (int32_t)d : 0);
-    u64 x = FRESH ? take_in(at) : *at;
+    u64 x = take_in(at);
     if (!some) x = 0;
     mass += x & kMassMask;
     count += (uint32_t)(x >> kCountShift);
@@ -657,14 +660,14 @@ template <Elem E>
 __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m, int32_t n_slices, int32_t* __restrict__ ids,
                                                                     float* __restrict__ logprobs) {
   extern __shared__ __align__(16) uint32_t tables[];
-  __shared__ Shared s;
+  Shared& s = *reinterpret_cast<Shared*>(tables);
   const int32_t b = (int32_t)blockIdx.y, slice = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Row<E> row(in, b);
   const RowDraw d(dr, b, in.V);
   Slot* const slots = m.slots + (size_t)b * m.slices;
   u64* const bins = m.bins + (size_t)b * m.slices * kBins;
   int32_t first = row.first_token(slice);
-  float y[kTokens];
+  Tokens y;
   load_slice<E>(row, r, b, first, tables, y);
 
   float top = -__builtin_inff();
@@ -700,11 +703,8 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
     };
 #pragma unroll 1
     for (int h = 0; h < kTokens / 4; ++h) {
-      const float a = y[0], b0 = y[1], c = y[2], e = y[3];
-#pragma unroll
-      for (int i = 0; i < kTokens - 4; ++i) y[i] = y[i + 4];
-      y[kTokens - 4] = a; y[kTokens - 3] = b0; y[kTokens - 2] = c; y[kTokens - 1] = e;
-      add(a); add(b0); add(c); add(e);
+      add(y[0]); add(y[1]); add(y[2]); add(y[3]);
+      y = __builtin_shufflevector(y, y, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0, 1, 2, 3);
     }
     sum = wave_sum(sum);
     if (lane == 0) s.sum[0][wave] = sum;
@@ -716,7 +716,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
   if (d.cut && tid < kBins) put_out(bins + (size_t)slice * kBins + tid, s.bins[tid]);
   if (!last_of(m.arrived + b, (uint32_t)n_slices, s)) return;
 
-  const RowTotal total = row_total<true>(slots, n_slices, s);
+  const RowTotal total = row_total(slots, n_slices, s);
   const bool empty = total.top == -__builtin_inff();
   if (empty || !d.cut) {
     int32_t id = empty ? -1 : total.top_id;
@@ -735,22 +735,24 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
     return;
   }
   // the bins in which a cut can lie: that of the k-th token unless it ends there, those of p of what lies up to it, that of min_p
-  row_bins<true>(bins, n_slices, total.E, s);
+  row_bins(bins, n_slices, total.E, s);
   if (tid == 0) {
-    RowPlan plan{};
-    plan.E = total.E;
-    plan.top = total.top;
+    RowPlan plan;
+    plan.k_need = 0;
+    plan.total = total;
     plan.cut = 1;
+    plan.k_bin = kBins;
     plan.min_key = key_of_min(d, total.top);
     int32_t from = kBins, to = -1, k_bin = -1, low = -1;
     double least = s.before_mass[kBins], most = least;
     int32_t last = kBins - 1;
     if (d.top_k && (uint32_t)d.top_k < s.before_count[kBins]) {
-      last = bin_of_count(s, (uint32_t)d.top_k);
+      last = plan.k_bin = bin_of_count(s, (uint32_t)d.top_k);
       most = s.before_mass[last + 1];
       least = most;
       if ((uint32_t)d.top_k != s.before_count[last + 1]) {
         k_bin = last;
+        plan.k_need = d.top_k - (int32_t)s.before_count[last];
         least = s.before_mass[last];
       }
     }
@@ -771,8 +773,16 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
       if (low >= 0 && low / 64 == k) bits |= 1ull << (low & 63);
       plan.wanted[k] = bits;
     }
-    m.plans[b] = plan;
+    RowPlan& out = m.plans[b];
+#pragma unroll
+    for (int k = 0; k < kBins / 64; ++k) out.wanted[k] = plan.wanted[k];
+    out.total = plan.total;
+    out.cut = 1;
+    out.min_key = plan.min_key;
+    out.k_bin = plan.k_bin;
+    out.k_need = plan.k_need;
   }
+  if (tid <= kBins) m.plans[b].before[tid] = s.before_mass[tid];
 }
 
 // A range of keys that holds the tokens of the bins first .. last: where the bins' borders lie, and two keys more at both ends for
@@ -789,7 +799,7 @@ __device__ KeyRange keys_of_bins(int32_t first, int32_t last, double E, double p
 // Goes through the tokens of the wanted bins: f(key, bin, id).  All threads; `listed` of them, a few in s.few, or more than the list holds.
 template <Elem E, class F>
 __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRules& r, const RowDraw& d, const RowPlan& plan, int32_t b, int32_t n_slices, const u64* list,
-                                               uint32_t listed, uint32_t* tables, const Shared& s, F&& f) {
+                                               uint32_t listed, uint32_t* tables, const Shared& s, const uint32_t* wanted, F&& f) {
   if (listed <= kMostCandidates) {
 #pragma unroll 1
     for (uint32_t i = threadIdx.x; i < listed; i += kSliceThreads) {
@@ -800,14 +810,14 @@ __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRul
   }
   for (int32_t slice = 0; slice < n_slices; ++slice) {
     const int32_t first = row.first_token(slice);
-    float y[kTokens];
+    Tokens y;
     __syncthreads();  // (the tables of the last slice have been read)
     load_slice<E>(row, r, b, first, tables, y);
     for_tokens(y, first, [&](float v, int32_t id, int) {
       if (!(v > -__builtin_inff())) return;
       const double t = octaves(v, d.per);
-      const int32_t bin = Power(t).bin(t, plan.E);
-      if (bin < kBins && (plan.wanted[bin / 64] >> (bin & 63) & 1u)) f(key_of(v), bin, id);
+      const int32_t bin = Power(t).bin(t, plan.total.E);
+      if (bin < kBins && (wanted[bin / 32] >> (bin & 31) & 1u)) f(key_of(v), bin, id);
     });
   }
 }
@@ -822,86 +832,99 @@ struct Cut {
 };
 
 template <Elem E>
+__global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m) {
+  extern __shared__ __align__(16) uint32_t tables[];
+  __shared__ uint32_t wanted[kBins / 32];
+  Shared& s = *reinterpret_cast<Shared*>(tables);
+  const int32_t b = (int32_t)blockIdx.y, slice = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x;
+  const RowPlan& plan = m.plans[b];
+  if (!plan.cut) return;
+  const Row<E> row(in, b);
+  const RowDraw d(dr, b, in.V);
+  u64* const list = m.candidates + (size_t)b * kMostCandidates;
+  Tokens y;
+
+  // the tokens of the wanted bins, if the slice has any
+  if (tid == 0) s.flag[1] = 0;
+  if (tid < kBins / 32) wanted[tid] = reinterpret_cast<const uint32_t*>(plan.wanted)[tid];
+  const double E_row = plan.total.E;
+  const Slot slot = m.slots[(size_t)b * m.slices + slice];
+  __syncthreads();
+  if (slot.top > -__builtin_inff() && tid < kBins && (wanted[tid / 32] >> (tid & 31) & 1u)) {
+    const double at = (double)tid - (E_row - slot.E) * kBinsAnOctave;
+    if (at >= 0.0 && m.bins[((size_t)b * m.slices + slice) * kBins + (int32_t)at] >> kCountShift) s.flag[1] = 1;
+  }
+  __syncthreads();
+  if (!s.flag[1]) return;
+  int32_t lightest = -1, heaviest = kBins;
+#pragma unroll
+  for (int k = 0; k < kBins / 64; ++k) {
+    const u64 bits = plan.wanted[k];
+    if (bits) lightest = k * 64 + 63 - __builtin_clzll(bits);
+    if (bits && heaviest == kBins) heaviest = k * 64 + __builtin_ctzll(bits);
+  }
+  const KeyRange range = keys_of_bins(heaviest, lightest, E_row, d.per);
+  const int32_t first = row.first_token(slice);
+  __syncthreads();
+  load_slice<E>(row, r, b, first, tables, y);
+  if (tid == 0) s.flag[0] = 0;
+  __syncthreads();
+  for_tokens(y, first, [&](float v, int32_t id, int) {
+    const uint32_t key = key_of(v);
+    if (!(v > -__builtin_inff()) || key < range.lo || key > range.hi) return;
+    const double t = octaves(v, d.per);
+    const int32_t bin = Power(t).bin(t, E_row);
+    if (bin >= kBins || !(wanted[bin / 32] >> (bin & 31) & 1u)) return;
+    const u64 x = (u64)key << 32 | (u64)bin << 24 | (u64)(uint32_t)id;
+    const uint32_t at = atomicAdd(&s.flag[0], 1u);
+    if (at < kFew) {
+      s.few[at] = x;
+    } else {  // (more than the workgroup collects: one by one)
+      const uint32_t place = atomicAdd(m.n_candidates + b, 1u);
+      if (place < kMostCandidates) list[place] = x;
+    }
+  });
+  __syncthreads();
+  const uint32_t n = min(s.flag[0], (uint32_t)kFew);
+  if (tid == 0 && n) s.counts[0] = atomicAdd(m.n_candidates + b, n);
+  __syncthreads();
+  for (uint32_t i = (uint32_t)tid; i < n; i += kSliceThreads)
+    if (s.counts[0] + i < kMostCandidates) list[s.counts[0] + i] = s.few[i];
+}
+
+// One workgroup per row with a cut: the cuts among the listed tokens, the slice and the token.
+template <Elem E>
 __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m, int32_t n_slices, int32_t* __restrict__ ids,
                                                                  float* __restrict__ logprobs) {
   extern __shared__ __align__(16) uint32_t tables[];
   __shared__ Shared s;
-  const int32_t b = (int32_t)blockIdx.y, slice = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const RowPlan plan = m.plans[b];
+  __shared__ uint32_t wanted[kBins / 32];
+  const int32_t b = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const RowPlan& plan = m.plans[b];
   if (!plan.cut) return;
   const Row<E> row(in, b);
   const RowDraw d(dr, b, in.V);
   const Slot* const slots = m.slots + (size_t)b * m.slices;
   const u64* const bins = m.bins + (size_t)b * m.slices * kBins;
-  u64* const list = m.candidates + (size_t)b * kMostCandidates;
-  float y[kTokens];
-
-  // the tokens of the wanted bins, if the slice has any
-  if (tid == 0) s.flag[1] = 0;
-  __syncthreads();
-  const Slot slot = slots[slice];
-  if (slot.top > -__builtin_inff() && tid < kBins && (plan.wanted[tid / 64] >> (tid & 63) & 1u)) {
-    const double at = (double)tid - (plan.E - slot.E) * kBinsAnOctave;
-    if (at >= 0.0 && bins[(size_t)slice * kBins + (int32_t)at] >> kCountShift) s.flag[1] = 1;
-  }
-  __syncthreads();
-  if (s.flag[1]) {
-    int32_t lightest = -1, heaviest = kBins;
-#pragma unroll
-    for (int k = 0; k < kBins / 64; ++k) {
-      if (plan.wanted[k]) lightest = k * 64 + 63 - __builtin_clzll(plan.wanted[k]);
-      if (plan.wanted[k] && heaviest == kBins) heaviest = k * 64 + __builtin_ctzll(plan.wanted[k]);
-    }
-    const KeyRange range = keys_of_bins(heaviest, lightest, plan.E, d.per);
-    if (tid == 0) s.flag[0] = 0;
-    const int32_t first = row.first_token(slice);
-    load_slice<E>(row, r, b, first, tables, y);
-    __syncthreads();
-    for_tokens(y, first, [&](float v, int32_t id, int) {
-      const uint32_t key = key_of(v);
-      if (!(v > -__builtin_inff()) || key < range.lo || key > range.hi) return;
-      const double t = octaves(v, d.per);
-      const int32_t bin = Power(t).bin(t, plan.E);
-      if (bin >= kBins || !(plan.wanted[bin / 64] >> (bin & 63) & 1u)) return;
-      const u64 x = (u64)key << 32 | (u64)bin << 24 | (u64)(uint32_t)id;
-      const uint32_t at = atomicAdd(&s.flag[0], 1u);
-      if (at < kFew) {
-        s.few[at] = x;
-      } else {  // (more than the workgroup collects: one by one)
-        const uint32_t place = __hip_atomic_fetch_add(m.n_candidates + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (place < kMostCandidates) put_out(list + place, x);
-      }
-    });
-    __syncthreads();
-    const uint32_t n = min(s.flag[0], (uint32_t)kFew);
-    if (tid == 0 && n) s.counts[0] = __hip_atomic_fetch_add(m.n_candidates + b, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    for (uint32_t i = (uint32_t)tid; i < n; i += kSliceThreads)
-      if (s.counts[0] + i < kMostCandidates) put_out(list + s.counts[0] + i, s.few[i]);
-  }
-  if (!last_of(m.arrived + m.rows + b, (uint32_t)n_slices, s)) return;
-
-  const uint32_t listed = take_in(m.n_candidates + b);
+  const u64* const list = m.candidates + (size_t)b * kMostCandidates;
+  const RowTotal total = plan.total;
+  const uint32_t min_key = plan.min_key, listed = m.n_candidates[b];
+  Tokens y;
+  if (tid <= kBins) s.before_mass[tid] = plan.before[tid];
+  if (tid < n_slices) s.slots[tid] = slots[tid];
+  if (tid < kBins / 32) wanted[tid] = reinterpret_cast<const uint32_t*>(plan.wanted)[tid];
   if (listed <= kFew)
-    for (uint32_t i = (uint32_t)tid; i < listed; i += kSliceThreads) s.few[i] = take_in(list + i);
+    for (uint32_t i = (uint32_t)tid; i < listed; i += kSliceThreads) s.few[i] = list[i];
+  int32_t k_bin = plan.k_bin, in_bin = plan.k_need ? k_bin : -1;  // in_bin: where the cut of a selection lies
+  u64 need = (u64)plan.k_need;  // what the rest of the kept beginning has to reach there: tokens, or mass in the bin's whole numbers
+  Cut cut{k_bin, 0, INT32_MAX};
   __syncthreads();
-  if (tid == 0) put_out(m.n_candidates + b, 0u);
-  const RowTotal total = row_total<false>(slots, n_slices, s);
-  row_bins<false>(bins, n_slices, total.E, s);
-  Cut cut{kBins, 0, INT32_MAX};
-  int32_t k_bin = kBins - 1, in_bin = -1;  // in_bin: where the cut of a selection lies
-  double up_to = s.before_mass[kBins];
-  u64 need = 0;  // what the rest of the kept beginning has to reach there: tokens, or mass in the bin's whole numbers
-  if (d.top_k && (uint32_t)d.top_k < s.before_count[kBins]) {
-    k_bin = bin_of_count(s, (uint32_t)d.top_k);
-    up_to = s.before_mass[k_bin + 1];
-    cut = Cut{k_bin, 0, INT32_MAX};
-    need = (uint32_t)d.top_k - s.before_count[k_bin];
-    if ((uint32_t)d.top_k != s.before_count[k_bin + 1]) in_bin = k_bin;
-  }
-  const double t_low = octaves(value_of(plan.min_key), d.per);
-  const int32_t low = plan.min_key ? Power(t_low).bin(t_low, total.E) : kBins;
-  auto kept = [&](uint32_t key, int32_t bin, int32_t id) { return key >= plan.min_key && cut.keeps(bin, key, id); };
+  if (tid == 0) m.n_candidates[b] = 0;
+  double up_to = s.before_mass[min(k_bin, kBins - 1) + 1];
+  k_bin = min(k_bin, kBins - 1);
+  const double t_low = octaves(value_of(min_key), d.per);
+  const int32_t low = min_key ? Power(t_low).bin(t_low, total.E) : kBins;
+  auto kept = [&](uint32_t key, int32_t bin, int32_t id) { return key >= min_key && cut.keeps(bin, key, id); };
 
   // Two selections, top-k and top-p of what it keeps, then the sums of the slices.  A selection goes through the tokens of its bin that
   // are kept so far: passes that sort them into 1024 stretches of their range of keys, and then of ids among the tokens with one
@@ -926,7 +949,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
           const int32_t p_bin = min(k_bin, bin_of_mass(s, target));
           const double inside = ldexp(target - s.before_mass[p_bin], kMassBits + p_bin / kBinsAnOctave);
           need = inside >= 1.0 ? (u64)ceil(inside) : 1u;
-          if (plan.wanted[p_bin / 64] >> (p_bin & 63) & 1u) in_bin = p_bin;
+          if (wanted[p_bin / 32] >> (p_bin & 31) & 1u) in_bin = p_bin;
         }
         if (in_bin < 0) what = 2;
       }
@@ -960,7 +983,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
       shift = width < 1024 ? 0 : 22 - __clz((int)width);
     }
     __syncthreads();
-    for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, tables, s, [&](uint32_t key, int32_t bin, int32_t id) {
+    for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, tables, s, wanted, [&](uint32_t key, int32_t bin, int32_t id) {
       if (mode == kSums) {
         if (bin == edge && kept(key, bin, id)) atomicAdd(&s.slice_more[(uint32_t)(id - row_first) / kSliceTokens], Power(octaves(value_of(key), d.per)).mass());
         return;
@@ -1094,7 +1117,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   __syncthreads();
   load_slice<E>(row, r, b, first, tables, y);
   float logit = 0.0f;
-  const uint32_t least_key = max(max(plan.min_key, cut.key), keys_of_bins(edge, min(edge, kBins - 1), total.E, d.per).lo);  // of what is kept
+  const uint32_t least_key = max(max(min_key, cut.key), keys_of_bins(edge, min(edge, kBins - 1), total.E, d.per).lo);  // of what is kept
   const int32_t id = find_token(y, first, rest, &logit, s, [&](float v, int32_t token) {
     if (!(v > -__builtin_inff()) || key_of(v) < least_key) return 0.0;
     const double t = octaves(v, d.per);
@@ -1120,15 +1143,18 @@ template <Elem E> struct Process {
 template <class K> void more_lds(K kernel) {
   (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kSliceTokens * 4);
 }
+// LDS of a kernel that has no use for its tables any more when it needs the first `bytes` of Shared
+size_t lds_with(const LogitRules& r, size_t bytes) { return bytes < rule_table_bytes(r) ? rule_table_bytes(r) : bytes; }
 template <Elem E> struct Draw {
   static void run(const Logits& in, const int32_t& B, const LogitRules& r, const DrawRules& d, const DrawMemory& m, int32_t* const& ids, float* const& logprobs,
                   const hipStream_t& stream) {
-    static const bool prepared = (more_lds(&draw_slices_kernel<E>), more_lds(&draw_cut_kernel<E>), true);
+    static const bool prepared = (more_lds(&draw_slices_kernel<E>), more_lds(&draw_list_kernel<E>), more_lds(&draw_cut_kernel<E>), true);
     (void)prepared;
     const int32_t n = slices_of<E>(in);
-    hipLaunchKernelGGL(draw_slices_kernel<E>, dim3(n, B), dim3(kSliceThreads), rule_table_bytes(r), stream, in, r, d, m, n, ids, logprobs);
-    if (d.uniform && (d.top_k || d.top_p || d.min_p))
-      hipLaunchKernelGGL(draw_cut_kernel<E>, dim3(n, B), dim3(kSliceThreads), rule_table_bytes(r), stream, in, r, d, m, n, ids, logprobs);
+    hipLaunchKernelGGL(draw_slices_kernel<E>, dim3(n, B), dim3(kSliceThreads), lds_with(r, offsetof(Shared, few)), stream, in, r, d, m, n, ids, logprobs);
+    if (!d.uniform || !(d.top_k || d.top_p || d.min_p)) return;
+    hipLaunchKernelGGL(draw_list_kernel<E>, dim3(n, B), dim3(kSliceThreads), lds_with(r, offsetof(Shared, ranked)), stream, in, r, d, m);
+    hipLaunchKernelGGL(draw_cut_kernel<E>, dim3(B), dim3(kSliceThreads), rule_table_bytes(r), stream, in, r, d, m, n, ids, logprobs);
   }
 };
 
