@@ -78,7 +78,8 @@ enum {
   XGM_BATCH_MAX_ROWS = 1024, /* rows of an xgm_batch */
   XGM_MAX_ROWS = 65535,      /* rows of a call below */
   XGM_MAX_LOGITS = 1 << 20,  /* logits a row of an xgm_sampler (padding included) */
-  XGM_MAX_HIDDEN = 1 << 16   /* columns of xgm_q4_logits */
+  XGM_MAX_HIDDEN = 1 << 16,  /* columns of xgm_q4_logits */
+  XGM_MAX_HISTORY = 1 << 20  /* tokens of a history, and one more (xgm_logit_rules.token_stride is less) */
 };
 
 const char* xgm_last_error(void);

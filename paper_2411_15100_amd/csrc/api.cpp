@@ -2284,7 +2284,7 @@ const char* rules_fault(const xgm_logit_rules* r, LogitRules* out) {
   }
   if (r->d_tokens) {
     if (!r->d_n_tokens || r->token_stride <= 0) return "a history without its lengths or its stride";
-    if (r->token_stride > INT32_MAX) return "token stride beyond 2^31 - 1";
+    if (r->token_stride >= XGM_MAX_HISTORY) return "a history of XGM_MAX_HISTORY tokens or more";
     out->tokens = r->d_tokens;
     out->token_stride = r->token_stride;
     out->n_tokens = r->d_n_tokens;

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
+#include <cstddef>
 #include <cstdint>
 
 #include "elements.hpp"
@@ -72,16 +73,26 @@ template <Elem E> __device__ __forceinline__ Group<E> load_group(const Row<E>& r
 }
 
 // --------------------------------------------------------------- rules on logits
-// The history and the biases of row b in the tokens [first, first + kSliceTokens), as two tables: how often a token was
-// generated, with the top bit if it occurs in the prompt, and which entry of the row's biases is the token's (0: none).
-// Counts are whole numbers and of the entries the last wins, so the order of the atomics does not matter.
+// What the history and the biases of a row say about the tokens of a slice, a word each: how often the token was generated, a bit if it
+// occurs in the prompt, and which of the row's biases it has (one more; the highest number: one from there on, to be looked for).  Biases
+// are entered first, of those of a token the last wins; counts are whole numbers: the order of the atomics does not matter.
 // The first tokens of the history are read before its length is known (they lie in the row's memory whatever it is).
+constexpr uint32_t kInPrompt = 0x80000000u, kCount = 0xfffffu;  // (a history is shorter than 2^20)
+constexpr int kBiasShift = 20;
+constexpr uint32_t kBiasMask = 0x7ffu;
+struct RuleTable {
+  uint32_t word[kSliceTokens];
+};
 constexpr int kHistoryAhead = 4;
 struct History {
-  int32_t token[kHistoryAhead], n, prompt;
+  int32_t token[kHistoryAhead], n, prompt, bias_begin, bias_end;
 };
 __device__ __forceinline__ History history_ahead(const LogitRules& r, int32_t b) {
   History h{};
+  if (r.bias_ids) {
+    h.bias_begin = max(r.bias_offsets[b], 0);
+    h.bias_end = min(r.bias_offsets[b + 1], r.n_bias);
+  }
   if (!r.tokens) return h;
   const int32_t* tokens = r.tokens + (int64_t)b * r.token_stride;
   h.n = (int32_t)min((int64_t)r.n_tokens[b], r.token_stride);
@@ -93,29 +104,32 @@ __device__ __forceinline__ History history_ahead(const LogitRules& r, int32_t b)
   }
   return h;
 }
-__device__ __forceinline__ void gather_rules(const LogitRules& r, int32_t b, int32_t first, const History& h, uint32_t* counts, uint32_t* entries) {
-  uint4* const tables = reinterpret_cast<uint4*>(counts);
-  const int32_t words = ((r.tokens ? 1 : 0) + (r.bias_ids ? 1 : 0)) * kSliceTokens / 4;
-  for (int32_t i = (int32_t)threadIdx.x; i < words; i += kSliceThreads) tables[i] = uint4{0, 0, 0, 0};
+__host__ __device__ inline bool has_rules(const LogitRules& r) { return r.tokens || r.bias_ids; }
+__device__ __forceinline__ void gather_rules(const LogitRules& r, int32_t b, int32_t first, const History& h, RuleTable& table) {
+  uint4* const words = reinterpret_cast<uint4*>(table.word);
+#pragma unroll
+  for (int i = 0; i < kSliceTokens / 4 / kSliceThreads; ++i) words[i * kSliceThreads + (int32_t)threadIdx.x] = uint4{0, 0, 0, 0};
   __syncthreads();
+  if (r.bias_ids) {
+    for (int32_t e = h.bias_begin + (int32_t)threadIdx.x; e < h.bias_end; e += kSliceThreads) {
+      const int32_t token = r.bias_ids[e];
+      const int64_t at = (int64_t)token - first;
+      if (token >= 0 && at >= 0 && at < kSliceTokens) atomicMax(&table.word[at], min((uint32_t)(e - h.bias_begin + 1), kBiasMask) << kBiasShift);
+    }
+    __syncthreads();
+  }
   if (r.tokens) {
     auto enter = [&](int32_t i, int32_t token) {
       const int64_t at = (int64_t)token - first;
       if (i >= h.n || token < 0 || at < 0 || at >= kSliceTokens) return;
-      if (i < h.prompt) atomicOr(&counts[at], 0x80000000u);
-      else atomicAdd(&counts[at], 1u);
+      if (i < h.prompt) atomicOr(&table.word[at], kInPrompt);
+      else atomicAdd(&table.word[at], 1u);
     };
 #pragma unroll
     for (int k = 0; k < kHistoryAhead; ++k) enter((int32_t)threadIdx.x + k * kSliceThreads, h.token[k]);
     const int32_t* tokens = r.tokens + (int64_t)b * r.token_stride;
+#pragma unroll 4
     for (int32_t i = (int32_t)threadIdx.x + kHistoryAhead * kSliceThreads; i < h.n; i += kSliceThreads) enter(i, tokens[i]);
-  }
-  if (r.bias_ids) {
-    const int32_t e0 = max(r.bias_offsets[b], 0), e1 = min(r.bias_offsets[b + 1], r.n_bias);
-    for (int32_t e = e0 + (int32_t)threadIdx.x; e < e1; e += kSliceThreads) {
-      const int64_t at = (int64_t)r.bias_ids[e] - first;
-      if (r.bias_ids[e] >= 0 && at >= 0 && at < kSliceTokens) atomicMax(&entries[at], (uint32_t)(e + 1));
-    }
   }
   __syncthreads();
 }
@@ -123,46 +137,47 @@ __device__ __forceinline__ void gather_rules(const LogitRules& r, int32_t b, int
 // compiler's contractions can change a bit of the 32 that are kept.
 struct RowRules {
   double repetition, frequency, presence;
-  const float* bias;
-  __device__ RowRules(const LogitRules& r, int32_t b)
-      : repetition(r.repetition ? (double)r.repetition[b] : 1.0), frequency(r.frequency ? (double)r.frequency[b] : 0.0),
-        presence(r.presence ? (double)r.presence[b] : 0.0), bias(r.bias) {}
-  __device__ float operator()(float x, uint32_t count, uint32_t entry) const {
+  const LogitRules& r;
+  int32_t begin, end;  // of the row's biases
+  __device__ RowRules(const LogitRules& rules, const History& h, int32_t b)
+      : repetition(rules.repetition ? (double)rules.repetition[b] : 1.0), frequency(rules.frequency ? (double)rules.frequency[b] : 0.0),
+        presence(rules.presence ? (double)rules.presence[b] : 0.0), r(rules), begin(h.bias_begin), end(h.bias_end) {}
+  __device__ float operator()(float x, uint32_t word, int32_t token) const {
     double y = (double)x;
-    if (count) y = y > 0.0 ? y / repetition : y * repetition;
-    if (count & 0x7fffffffu) y = y - frequency * (double)(count & 0x7fffffffu) - presence;
-    if (entry) y += (double)bias[entry - 1];
+    if (word & (kInPrompt | kCount)) y = y > 0.0 ? y / repetition : y * repetition;
+    if (word & kCount) y = y - frequency * (double)(word & kCount) - presence;
+    if (uint32_t entry = word >> kBiasShift & kBiasMask) {
+      int32_t e = begin + (int32_t)entry - 1;
+      if (entry == kBiasMask)
+        for (int32_t k = end - 1; k > e; --k)
+          if (r.bias_ids[k] == token) { e = k; break; }
+      y += (double)r.bias[e];
+    }
     return (float)y;
   }
 };
-// calls f(i, count, entry) for those of the 8 tokens from `at` on in the tables that a rule touches
-template <class F> __device__ __forceinline__ void touched(const LogitRules& r, const uint32_t* counts, const uint32_t* entries, int32_t at, F&& f) {
-  uint32_t c[8] = {}, e[8] = {};
-  if (r.tokens) {
-    const uint4 a = *reinterpret_cast<const uint4*>(counts + at), b = *reinterpret_cast<const uint4*>(counts + at + 4);
-    c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w; c[4] = b.x; c[5] = b.y; c[6] = b.z; c[7] = b.w;
-  }
-  if (r.bias_ids) {
-    const uint4 a = *reinterpret_cast<const uint4*>(entries + at), b = *reinterpret_cast<const uint4*>(entries + at + 4);
-    e[0] = a.x; e[1] = a.y; e[2] = a.z; e[3] = a.w; e[4] = b.x; e[5] = b.y; e[6] = b.z; e[7] = b.w;
-  }
+// calls f(i, word) for those of the 8 tokens from `at` on that a rule touches
+template <class F> __device__ __forceinline__ void touched(const RuleTable& table, int32_t at, F&& f) {
+  const uint4 a = *reinterpret_cast<const uint4*>(table.word + at), b = *reinterpret_cast<const uint4*>(table.word + at + 4);
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (!(a.x | a.y | a.z | a.w | b.x | b.y | b.z | b.w)) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (c[i] | e[i]) f(i, c[i], e[i]);
+    if (w[i]) f(i, w[i]);
 }
 
 // One workgroup per slice.  Bound by the bytes where the batch is large (a logit that nothing touches is copied as it is, one that
-// is masked is not read); the tables cost 64 KB of LDS at most, two workgroups a compute unit.
+// is masked is not read); the table takes 32 KB of LDS, so that four workgroups run on a compute unit.
 template <Elem E>
 __global__ __launch_bounds__(kSliceThreads) void process_logits_kernel(Logits in, LogitRules r, typename Type<E>::bits* out, int64_t out_stride) {
   typedef typename Type<E>::bits bits;
-  extern __shared__ __align__(16) uint32_t tables[];
-  uint32_t *counts = tables, *entries = tables + (r.tokens ? kSliceTokens : 0);
+  extern __shared__ __align__(16) char lds[];
+  RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   const int32_t b = (int32_t)blockIdx.y;
   const Row<E> row(in, b);
   const int32_t first = row.first_token((int32_t)blockIdx.x);
   if (first >= in.V) return;
-  const bool ruled = r.tokens || r.bias_ids;
+  const bool ruled = has_rules(r);
   const History h = history_ahead(r, b);
   Group<E> x[kGroups];
   uint32_t ok[kGroups];
@@ -173,14 +188,14 @@ __global__ __launch_bounds__(kSliceThreads) void process_logits_kernel(Logits in
     x[j] = Group<E>{};
     if (ok[j]) x[j] = load_group(row, t);
   }
-  if (ruled) gather_rules(r, b, first, h, counts, entries);
-  const RowRules rule(r, b);
+  if (ruled) gather_rules(r, b, first, h, table);
+  const RowRules rule(r, h, b);
   bits* const to = out + (int64_t)b * out_stride;
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
     const int32_t at = (j * kSliceThreads + (int32_t)threadIdx.x) * 8, t = first + at;
     if (ruled && ok[j])
-      touched(r, counts, entries, at, [&](int i, uint32_t count, uint32_t entry) { x[j].set(i, narrowed<E>(rule(widened<E>(x[j][i]), count, entry))); });
+      touched(table, at, [&](int i, uint32_t word) { x[j].set(i, narrowed<E>(rule(widened<E>(x[j][i]), word, t + i))); });
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (!(ok[j] >> i & 1u)) x[j].set(i, narrowed<E>(-__builtin_inff()));
@@ -195,7 +210,7 @@ __global__ __launch_bounds__(kSliceThreads) void process_logits_kernel(Logits in
     }
   }
 }
-size_t rule_table_bytes(const LogitRules& r) { return (size_t)kSliceTokens * 4 * ((r.tokens ? 1 : 0) + (r.bias_ids ? 1 : 0)); }
+size_t rule_table_bytes(const LogitRules& r) { return has_rules(r) ? sizeof(RuleTable) : 0; }
 // slices of a row, wherever it begins
 template <Elem E> int32_t slices_of(const Logits& in) {
   constexpr int32_t size = sizeof(typename Type<E>::bits);
@@ -370,9 +385,8 @@ __device__ __forceinline__ double wave_sum(double x) {
 
 // The logits of a slice under the rules.
 template <Elem E>
-__device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& r, int32_t b, int32_t first, uint32_t* tables, Tokens& y) {
-  uint32_t *counts = tables, *entries = tables + (r.tokens ? kSliceTokens : 0);
-  const bool ruled = r.tokens || r.bias_ids;
+__device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& r, int32_t b, int32_t first, RuleTable& table, Tokens& y) {
+  const bool ruled = has_rules(r);
   const History h = history_ahead(r, b);
   Group<E> x[kGroups];
   uint32_t ok[kGroups];
@@ -383,15 +397,16 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
     x[j] = Group<E>{};
     if (ok[j]) x[j] = load_group(row, t);
   }
-  if (ruled) gather_rules(r, b, first, h, counts, entries);
-  const RowRules rule(r, b);
+  if (ruled) gather_rules(r, b, first, h, table);
+  const RowRules rule(r, h, b);
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[8 * j + i] = ok[j] >> i & 1u ? widened<E>(x[j][i]) : -__builtin_inff();
     if (ruled && ok[j])
-      touched(r, counts, entries, (j * kSliceThreads + (int32_t)threadIdx.x) * 8,
-              [&](int i, uint32_t count, uint32_t entry) { if (ok[j] >> i & 1u) y[8 * j + i] = rule(y[8 * j + i], count, entry); });
+      touched(table, (j * kSliceThreads + (int32_t)threadIdx.x) * 8, [&](int i, uint32_t word) {
+        if (ok[j] >> i & 1u) y[8 * j + i] = rule(y[8 * j + i], word, first + (j * kSliceThreads + (int32_t)threadIdx.x) * 8 + i);
+      });
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[8 * j + i] = drawable(y[8 * j + i]);
   }
@@ -659,8 +674,9 @@ __device__ uint32_t key_of_min(const RowDraw& d, float top) {
 template <Elem E>
 __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m, int32_t n_slices, int32_t* __restrict__ ids,
                                                                     float* __restrict__ logprobs) {
-  extern __shared__ __align__(16) uint32_t tables[];
-  Shared& s = *reinterpret_cast<Shared*>(tables);
+  extern __shared__ __align__(16) char lds[];
+  RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
+  Shared& s = *reinterpret_cast<Shared*>(lds);
   const int32_t b = (int32_t)blockIdx.y, slice = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Row<E> row(in, b);
   const RowDraw d(dr, b, in.V);
@@ -668,7 +684,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
   u64* const bins = m.bins + (size_t)b * m.slices * kBins;
   int32_t first = row.first_token(slice);
   Tokens y;
-  load_slice<E>(row, r, b, first, tables, y);
+  load_slice<E>(row, r, b, first, table, y);
 
   float top = -__builtin_inff();
   int32_t top_id = -1;
@@ -725,7 +741,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, L
       find_slice(d.u, n_slices, s);
       const double rest = s.rest;
       first = row.first_token(s.slice);
-      load_slice<E>(row, r, b, first, tables, y);
+      load_slice<E>(row, r, b, first, table, y);
       id = find_token(y, first, rest, &logit, s, [&](float v, int32_t) { return v > -__builtin_inff() ? Power(octaves(v, d.per)).weight(total.E) : 0.0; });
     }
     if (tid == 0) {
@@ -799,7 +815,7 @@ __device__ KeyRange keys_of_bins(int32_t first, int32_t last, double E, double p
 // Goes through the tokens of the wanted bins: f(key, bin, id).  All threads; `listed` of them, a few in s.few, or more than the list holds.
 template <Elem E, class F>
 __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRules& r, const RowDraw& d, const RowPlan& plan, int32_t b, int32_t n_slices, const u64* list,
-                                               uint32_t listed, uint32_t* tables, const Shared& s, const uint32_t* wanted, F&& f) {
+                                               uint32_t listed, RuleTable& table, const Shared& s, const uint32_t* wanted, F&& f) {
   if (listed <= kMostCandidates) {
 #pragma unroll 1
     for (uint32_t i = threadIdx.x; i < listed; i += kSliceThreads) {
@@ -812,7 +828,7 @@ __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRul
     const int32_t first = row.first_token(slice);
     Tokens y;
     __syncthreads();  // (the tables of the last slice have been read)
-    load_slice<E>(row, r, b, first, tables, y);
+    load_slice<E>(row, r, b, first, table, y);
     for_tokens(y, first, [&](float v, int32_t id, int) {
       if (!(v > -__builtin_inff())) return;
       const double t = octaves(v, d.per);
@@ -833,9 +849,10 @@ struct Cut {
 
 template <Elem E>
 __global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m) {
-  extern __shared__ __align__(16) uint32_t tables[];
+  extern __shared__ __align__(16) char lds[];
+  RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   __shared__ uint32_t wanted[kBins / 32];
-  Shared& s = *reinterpret_cast<Shared*>(tables);
+  Shared& s = *reinterpret_cast<Shared*>(lds);
   const int32_t b = (int32_t)blockIdx.y, slice = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x;
   const RowPlan& plan = m.plans[b];
   if (!plan.cut) return;
@@ -866,7 +883,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, Log
   const KeyRange range = keys_of_bins(heaviest, lightest, E_row, d.per);
   const int32_t first = row.first_token(slice);
   __syncthreads();
-  load_slice<E>(row, r, b, first, tables, y);
+  load_slice<E>(row, r, b, first, table, y);
   if (tid == 0) s.flag[0] = 0;
   __syncthreads();
   for_tokens(y, first, [&](float v, int32_t id, int) {
@@ -896,7 +913,8 @@ __global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, Log
 template <Elem E>
 __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m, int32_t n_slices, int32_t* __restrict__ ids,
                                                                  float* __restrict__ logprobs) {
-  extern __shared__ __align__(16) uint32_t tables[];
+  extern __shared__ __align__(16) char lds[];
+  RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   __shared__ Shared s;
   __shared__ uint32_t wanted[kBins / 32];
   const int32_t b = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -983,7 +1001,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
       shift = width < 1024 ? 0 : 22 - __clz((int)width);
     }
     __syncthreads();
-    for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, tables, s, wanted, [&](uint32_t key, int32_t bin, int32_t id) {
+    for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, table, s, wanted, [&](uint32_t key, int32_t bin, int32_t id) {
       if (mode == kSums) {
         if (bin == edge && kept(key, bin, id)) atomicAdd(&s.slice_more[(uint32_t)(id - row_first) / kSliceTokens], Power(octaves(value_of(key), d.per)).mass());
         return;
@@ -1115,7 +1133,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   const double rest = s.rest;
   const int32_t first = row.first_token(s.slice);
   __syncthreads();
-  load_slice<E>(row, r, b, first, tables, y);
+  load_slice<E>(row, r, b, first, table, y);
   float logit = 0.0f;
   const uint32_t least_key = max(max(min_key, cut.key), keys_of_bins(edge, min(edge, kBins - 1), total.E, d.per).lo);  // of what is kept
   const int32_t id = find_token(y, first, rest, &logit, s, [&](float v, int32_t token) {
@@ -1141,7 +1159,7 @@ template <Elem E> struct Process {
   }
 };
 template <class K> void more_lds(K kernel) {
-  (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kSliceTokens * 4);
+  (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RuleTable));
 }
 // LDS of a kernel that has no use for its tables any more when it needs the first `bytes` of Shared
 size_t lds_with(const LogitRules& r, size_t bytes) { return bytes < rule_table_bytes(r) ? rule_table_bytes(r) : bytes; }

@@ -207,7 +207,7 @@ RULES = [dict(rows=1, V=1, dtype="f32", history=3, bias=2), dict(rows=2, V=31, d
          dict(rows=5, V=8193, dtype="f32", history=300, mask="full", offset=3), dict(rows=3, V=50001, dtype="bf16", history=5000, bias=300, offset=5),
          dict(rows=2, V=100003, dtype="f16", history=33000, bias=1, mask="short"), dict(rows=7, V=32000, dtype="f32", mask="full"),
          dict(rows=9, V=4099, dtype="bf16"), dict(rows=6, V=20011, dtype="f16", history=64, prompt=False, pad=13, mask="full"),
-         dict(rows=1, V=151936, dtype="bf16", history=2048, bias=16, mask="full"), dict(rows=65, V=1031, dtype="f32", history=50, bias=5, mask="full")]
+         dict(rows=1, V=151936, dtype="bf16", history=2048, bias=16, mask="full"), dict(rows=65, V=1031, dtype="f32", history=50, bias=5, mask="full"), dict(rows=3, V=5000, dtype="bf16", history=9, bias=6000)]
 
 
 @pytest.mark.parametrize("how", ["apart", "in place", "shifted"])

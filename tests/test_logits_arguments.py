@@ -29,7 +29,7 @@ def test_projection_refuses(change, status, text):
 
 PROCESS = dict(d_logits=A, dtype=1, rows=2, v=100, row_stride=100, rules=None, d_out=2 * A, out_stride=100)
 BAD_RULES = [(dict(d_bitmask=A), "v_mask"), (dict(d_tokens=A, d_n_tokens=A), "stride"), (dict(d_tokens=A, token_stride=8), "lengths"),
-             (dict(d_tokens=A, d_n_tokens=A, token_stride=1 << 31), "2\\^31"), (dict(d_repetition=A), "history"), (dict(d_presence=A), "history"),
+             (dict(d_tokens=A, d_n_tokens=A, token_stride=1 << 20), "XGM_MAX_HISTORY"), (dict(d_repetition=A), "history"), (dict(d_presence=A), "history"),
              (dict(d_frequency=A), "history"), (dict(d_bias_ids=A, d_bias=A), "offsets"), (dict(d_bias_ids=A, d_bias_offsets=A), "biases"),
              (dict(d_bias_ids=A, d_bias=A, d_bias_offsets=A, n_bias=-1), "number")]
 
