@@ -62,7 +62,7 @@ __device__ __forceinline__ void store_logit(const Head& h, Elem type, int64_t at
 }
 
 // ---------------------------------------------------------------- few rows in the batch
-// Up to 16 NB rows, whose hidden states fit LDS.  A wave takes 16 rows of the matrix (a tile) and all columns, so that waves need
+// Up to 16 NB rows, whose hidden states and their sums fit LDS.  A wave takes 16 rows of the matrix (a tile) and all columns, so that waves need
 // nothing of each other: it reads the codes a step of 512 columns (4 chunks of 128) at a time, the next ones while it multiplies
 // the last, 64 bytes of each row and chunk.  Hidden states lie in LDS in the order in which the products take them, zeros behind
 // the last column (what is read of the matrix there is some earlier part of the row); rows of the batch that are not there are read
@@ -74,7 +74,7 @@ constexpr int kFewMaxThreads = 1024;  // of NB = 1; two rows of products need th
 template <int NB> constexpr int kFewThreads = kFewMaxThreads / NB;
 constexpr int kFewRows = 1024;  // of the matrix at a time (a list of them lies in LDS)
 constexpr int kChunks = 4;      // of a step
-constexpr size_t kFewHiddenBytes = 128 * 1024;  // at most, of hidden states in LDS
+constexpr uint32_t kFewMaxLds = 160 * 1024;
 
 struct FewLayout {  // of dynamic LDS, bytes
   uint32_t sums, partial, list, end;
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void q4_many_kernel(Head h, Elem o
 constexpr int kComputeUnits = 256;
 
 template <Elem H, int NB, int P, bool Z> void launch_few(const Head& h, Elem out_type, hipStream_t stream) {
-  static const bool prepared = hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_few_kernel<H, NB, P, Z>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess;
+  static const bool prepared = hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_few_kernel<H, NB, P, Z>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kFewMaxLds) == hipSuccess;
   (void)prepared;
   const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), each = (tiles + kComputeUnits - 1) / kComputeUnits, steps = few_steps(h.K);
   int32_t threads = 64;  // waves for its tiles, or for the steps of the few that masks leave
@@ -584,6 +584,8 @@ template <Elem H, int NB, int P> void launch_few_zeros(const Head& h, Elem out_t
   if (h.zeros) launch_few<H, NB, P, true>(h, out_type, stream);
   else launch_few<H, NB, P, false>(h, out_type, stream);
 }
+int few_parts(int32_t group) { return group % 128 == 0 ? 4 : group == 64 ? 8 : 16; }
+bool few_fits(const Head& h, int nb) { return h.B <= 16 * nb && few_layout(h.K, h.B, few_parts(h.group), nb).end <= kFewMaxLds; }
 template <Elem H, int NB> void launch_few_groups(const Head& h, Elem out_type, hipStream_t stream) {
   if (h.group % 128 == 0) launch_few_zeros<H, NB, 4>(h, out_type, stream);
   else if (h.group == 64) launch_few_zeros<H, NB, 8>(h, out_type, stream);
@@ -606,9 +608,8 @@ template <Elem H, int MW, int WM> void launch_many_groups(const Head& h, Elem ou
   else launch_many_zeros<H, MW, WM, kLookedUp>(h, out_type, stream);
 }
 template <Elem H> void launch_head(const Head& h, Elem out_type, hipStream_t stream) {
-  const size_t row = (size_t)few_steps(h.K) * kChunks * 256;  // bytes of LDS for a row of hidden states
-  if (h.B <= 16 && row * h.B <= kFewHiddenBytes) return launch_few_groups<H, 1>(h, out_type, stream);
-  if (h.B <= 32 && row * h.B <= kFewHiddenBytes) return launch_few_groups<H, 2>(h, out_type, stream);
+  if (few_fits(h, 1)) return launch_few_groups<H, 1>(h, out_type, stream);
+  if (few_fits(h, 2)) return launch_few_groups<H, 2>(h, out_type, stream);
   if (h.B <= 32) return launch_many_groups<H, 2, 1>(h, out_type, stream);
   if (h.B <= 64) return launch_many_groups<H, 4, 1>(h, out_type, stream);
   launch_many_groups<H, 4, 2>(h, out_type, stream);

@@ -97,6 +97,14 @@ def test_projection_of_real_numbers(B, K, V, group, dtype, out):
     assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
 
 
+@pytest.mark.parametrize("B,K,V,group", [(1, 65536, 40, 32), (1, 65536, 40, 128), (1, 65536, 33, 64), (2, 32768, 20, 32), (3, 24576, 50, 96), (9, 8192, 70, 32),
+                                         (5, 12800, 30, 256), (17, 4096, 40, 32), (20, 3200, 50, 32)])
+def test_projection_of_columns_around_what_fits_lds(B, K, V, group):
+    p = Projection(B, K, V, group, "bf16", zeros=True, whole=True, seed=B)
+    want, _ = p.want()
+    assert np.array_equal(_np(p.run()), want)
+
+
 @pytest.mark.parametrize("B,K,V,group", [(1, 1024, 5000, 128), (4, 2080, 3001, 32), (20, 512, 2050, 64), (70, 384, 777, 32), (130, 256, 600, 128)])
 def test_projection_under_masks(B, K, V, group):
     rng = np.random.default_rng(B)
@@ -236,6 +244,22 @@ def test_rules_give_the_bits_of_the_definition(case, how):
         rest = torch.full_like(buf, 7.0)
         rest[k:k + c.rows * stride].view(c.rows, stride)[:, :c.V] = out
         assert torch.equal(buf.view(view), rest.view(view))
+
+
+def test_a_history_in_the_last_columns_of_a_wider_array():
+    xgm = _xgm()
+    c = Batch(3, 700, "f32", seed=2, history=90, bias=3)
+    wide = torch.full((3, 150), 5, dtype=torch.int32, device="cuda")     # tokens that would count if they were taken
+    wide[:, 60:] = c.d["tokens"]
+    c.h["n_tokens"] = np.array([90, 0, 71], np.int32)                   # within the array: the rows lie 150 apart
+    c.h["n_prompt"] = np.array([95, 3, 0], np.int32)
+    c.upload()
+    want = torch.from_numpy(c.want())
+    c.rules._s.d_tokens, c.rules._s.token_stride = wide[:, 60:].data_ptr(), 150
+    out = torch.empty((3, 700), device="cuda")
+    xgm.process_logits(c.address(), 0, 3, 700, c.stride, c.rules, out.data_ptr(), 700, _stream())
+    torch.cuda.synchronize()
+    assert torch.equal(out.cpu().view(torch.int32), want.view(torch.int32))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
