@@ -76,7 +76,7 @@ template <Elem E> __device__ __forceinline__ Group<E> load_group(const Row<E>& r
 // What the history and the biases of a row say about the tokens of a slice, a word each: how often the token was generated, a bit if it
 // occurs in the prompt, and which of the row's biases it has (one more; the highest number: one from there on, to be looked for).  Biases
 // are entered first, of those of a token the last wins; counts are whole numbers: the order of the atomics does not matter.
-// The first tokens of the history are read before its length is known (they lie in the row's memory whatever it is).
+// Nothing behind a history's length is read (the last row's memory may end there).
 constexpr uint32_t kInPrompt = 0x80000000u, kCount = 0xfffffu;  // (a history is shorter than 2^20)
 constexpr int kBiasShift = 20;
 constexpr uint32_t kBiasMask = 0x7ffu;
@@ -100,7 +100,7 @@ __device__ __forceinline__ History history_ahead(const LogitRules& r, int32_t b)
 #pragma unroll
   for (int k = 0; k < kHistoryAhead; ++k) {
     const int32_t i = (int32_t)threadIdx.x + k * kSliceThreads;
-    h.token[k] = i < r.token_stride ? tokens[i] : -1;
+    h.token[k] = i < h.n ? tokens[i] : -1;
   }
   return h;
 }
@@ -156,14 +156,21 @@ struct RowRules {
     return (float)y;
   }
 };
-// calls f(i, word) for those of the 8 tokens from `at` on that a rule touches
-template <class F> __device__ __forceinline__ void touched(const RuleTable& table, int32_t at, F&& f) {
-  const uint4 a = *reinterpret_cast<const uint4*>(table.word + at), b = *reinterpret_cast<const uint4*>(table.word + at + 4);
-  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  if (!(a.x | a.y | a.z | a.w | b.x | b.y | b.z | b.w)) return;
+// Which of the thread's tokens a rule touches.  They are few, and taken one by one in a loop: unrolled over the thread's tokens the rules
+// are 7000 instructions (a division in 64 bits each), which a kernel that runs once fetches from the L2.
+__device__ __forceinline__ int32_t place_of(int k) { return (k / 8 * kSliceThreads + (int32_t)threadIdx.x) * 8 + k % 8; }
+__device__ __forceinline__ uint32_t touched(const RuleTable& table, const uint32_t (&ok)[kGroups]) {
+  uint32_t hit = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (w[i]) f(i, w[i]);
+  for (int j = 0; j < kGroups; ++j) {
+    const uint4 a = *reinterpret_cast<const uint4*>(table.word + place_of(8 * j)), b = *reinterpret_cast<const uint4*>(table.word + place_of(8 * j) + 4);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t some = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) some |= w[i] ? 1u << i : 0u;
+    hit |= (some & ok[j]) << (8 * j);
+  }
+  return hit;
 }
 
 // One workgroup per slice.  Bound by the bytes where the batch is large (a logit that nothing touches is copied as it is, one that
@@ -191,11 +198,23 @@ __global__ __launch_bounds__(kSliceThreads) void process_logits_kernel(Logits in
   if (ruled) gather_rules(r, b, first, h, table);
   const RowRules rule(r, h, b);
   bits* const to = out + (int64_t)b * out_stride;
+  if (ruled) {
+#pragma unroll 1
+    for (uint32_t hit = touched(table, ok); hit; hit &= hit - 1) {
+      const int k = __builtin_ctz(hit);
+      bits v = 0;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i)
+        if (i == k) v = x[i / 8][i % 8];
+      v = narrowed<E>(rule(widened<E>(v), table.word[place_of(k)], first + place_of(k)));
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i)
+        if (i == k) x[i / 8].set(i % 8, v);
+    }
+  }
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
-    const int32_t at = (j * kSliceThreads + (int32_t)threadIdx.x) * 8, t = first + at;
-    if (ruled && ok[j])
-      touched(table, at, [&](int i, uint32_t word) { x[j].set(i, narrowed<E>(rule(widened<E>(x[j][i]), word, t + i))); });
+    const int32_t t = first + place_of(8 * j);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (!(ok[j] >> i & 1u)) x[j].set(i, narrowed<E>(-__builtin_inff()));
@@ -400,19 +419,26 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
   if (ruled) gather_rules(r, b, first, h, table);
   const RowRules rule(r, h, b);
 #pragma unroll
-  for (int j = 0; j < kGroups; ++j) {
+  for (int k = 0; k < kTokens; ++k) y[k] = ok[k / 8] >> (k % 8) & 1u ? widened<E>(x[k / 8][k % 8]) : -__builtin_inff();
+  if (ruled) {
+#pragma unroll 1
+    for (uint32_t hit = touched(table, ok); hit; hit &= hit - 1) {
+      const int k = __builtin_ctz(hit);
+      float v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[8 * j + i] = ok[j] >> i & 1u ? widened<E>(x[j][i]) : -__builtin_inff();
-    if (ruled && ok[j])
-      touched(table, (j * kSliceThreads + (int32_t)threadIdx.x) * 8, [&](int i, uint32_t word) {
-        if (ok[j] >> i & 1u) y[8 * j + i] = rule(y[8 * j + i], word, first + (j * kSliceThreads + (int32_t)threadIdx.x) * 8 + i);
-      });
+      for (int i = 0; i < kTokens; ++i)
+        if (i == k) v = y[i];
+      v = rule(v, table.word[place_of(k)], first + place_of(k));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[8 * j + i] = drawable(y[8 * j + i]);
+      for (int i = 0; i < kTokens; ++i)
+        if (i == k) y[i] = v;
+    }
   }
+#pragma unroll
+  for (int k = 0; k < kTokens; ++k) y[k] = drawable(y[k]);
   if (ruled) __syncthreads();  // (other things lie where the tables were)
 }
-__device__ __forceinline__ int32_t token_of(int32_t first, int k) { return first + (k / 8 * kSliceThreads + (int32_t)threadIdx.x) * 8 + k % 8; }
+__device__ __forceinline__ int32_t token_of(int32_t first, int k) { return first + place_of(k); }
 
 // Calls f(logit, token) for the thread's tokens of a slice in order of their ids.  The logits go round in their registers instead of the
 // loop being unrolled: what a single workgroup does once costs as much for fetching its instructions as for carrying them out.
@@ -672,7 +698,7 @@ __device__ uint32_t key_of_min(const RowDraw& d, float top) {
 }
 
 template <Elem E>
-__global__ __launch_bounds__(kSliceThreads) void draw_slices_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m, int32_t n_slices, int32_t* __restrict__ ids,
+__global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in, LogitRules r, DrawRules dr, DrawMemory m, int32_t n_slices, int32_t* __restrict__ ids,
                                                                     float* __restrict__ logprobs) {
   extern __shared__ __align__(16) char lds[];
   RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
@@ -817,10 +843,21 @@ template <Elem E, class F>
 __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRules& r, const RowDraw& d, const RowPlan& plan, int32_t b, int32_t n_slices, const u64* list,
                                                uint32_t listed, RuleTable& table, const Shared& s, const uint32_t* wanted, F&& f) {
   if (listed <= kMostCandidates) {
+    constexpr int kAhead = 4;
 #pragma unroll 1
-    for (uint32_t i = threadIdx.x; i < listed; i += kSliceThreads) {
-      const u64 x = listed <= kFew ? s.few[i] : take_in(list + i);
-      f((uint32_t)(x >> 32), (int32_t)(x >> 24 & 255u), (int32_t)(x & 0xffffffu));
+    for (uint32_t i = threadIdx.x; i < listed; i += kAhead * kSliceThreads) {
+      u64 x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const uint32_t at = min(i + k * kSliceThreads, listed - 1);
+        x[k] = listed <= kFew ? s.few[at] : list[at];
+      }
+#pragma unroll 1
+      for (uint32_t at = i; at < i + kAhead * kSliceThreads && at < listed; at += kSliceThreads) {
+        f((uint32_t)(x[0] >> 32), (int32_t)(x[0] >> 24 & 255u), (int32_t)(x[0] & 0xffffffu));
+#pragma unroll
+        for (int k = 1; k < kAhead; ++k) x[k - 1] = x[k];
+      }
     }
     return;
   }
