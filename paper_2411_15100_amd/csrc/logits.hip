@@ -159,6 +159,24 @@ struct RowRules {
 // Which of the thread's tokens a rule touches.  They are few, and taken one by one in a loop: unrolled over the thread's tokens the rules
 // are 7000 instructions (a division in 64 bits each), which a kernel that runs once fetches from the L2.
 __device__ __forceinline__ int32_t place_of(int k) { return (k / 8 * kSliceThreads + (int32_t)threadIdx.x) * 8 + k % 8; }
+// v[k], with the steps of a tree (the compiler's own way takes three instructions for each)
+template <class T> __device__ __forceinline__ T picked(const T (&v)[kTokens], int k) {
+  static_assert(kTokens == 16, "four steps");
+  T x[kTokens];
+#pragma unroll
+  for (int i = 0; i < kTokens; ++i) x[i] = v[i];
+#pragma unroll
+  for (int n = kTokens / 2; n; n >>= 1) {
+    const bool upper = k & n;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      T high = x[i + n];
+      asm("" : "+v"(high));  // (two elements of one vector are two values here)
+      x[i] = upper ? high : x[i];
+    }
+  }
+  return x[0];
+}
 __device__ __forceinline__ uint32_t touched(const RuleTable& table, const uint32_t (&ok)[kGroups]) {
   uint32_t hit = 0;
 #pragma unroll
@@ -195,18 +213,17 @@ __global__ __launch_bounds__(kSliceThreads) void process_logits_kernel(Logits in
     x[j] = Group<E>{};
     if (ok[j]) x[j] = load_group(row, t);
   }
+  const RowRules rule(r, h, b);  // (read before the barriers of the next)
   if (ruled) gather_rules(r, b, first, h, table);
-  const RowRules rule(r, h, b);
   bits* const to = out + (int64_t)b * out_stride;
   if (ruled) {
 #pragma unroll 1
     for (uint32_t hit = touched(table, ok); hit; hit &= hit - 1) {
       const int k = __builtin_ctz(hit);
-      bits v = 0;
+      uint32_t all[kTokens];
 #pragma unroll
-      for (int i = 0; i < kTokens; ++i)
-        if (i == k) v = x[i / 8][i % 8];
-      v = narrowed<E>(rule(widened<E>(v), table.word[place_of(k)], first + place_of(k)));
+      for (int i = 0; i < kTokens; ++i) all[i] = x[i / 8][i % 8];
+      const bits v = narrowed<E>(rule(widened<E>((bits)picked(all, k)), table.word[place_of(k)], first + place_of(k)));
 #pragma unroll
       for (int i = 0; i < kTokens; ++i)
         if (i == k) x[i / 8].set(i % 8, v);
@@ -270,40 +287,38 @@ __device__ __forceinline__ double octaves(float y, double per) {
 #pragma clang fp contract(off)
   return (double)y * per;
 }
-// 2^t as a whole octave and a number in [1, 2): the series of the exponential function around the middle of the octave, whose eleven
-// terms leave 2.2e-13 of it.
+// 2^t relative to 2^E, E a whole number: sixteenths of an octave come from a table in LDS (its 16 entries lie in different banks), the
+// rest from the series of the exponential function around the middle of a sixteenth, whose six terms leave 1.4e-13 of it.  (The
+// series over a whole octave takes eleven terms and as many instructions again.)
+__constant__ const double kRoots[16] = {1, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916,
+                                        1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927,
+                                        1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543,
+                                        1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
+__device__ __forceinline__ void fill_roots(double* roots) {
+  if (threadIdx.x < 16) roots[threadIdx.x] = kRoots[threadIdx.x];
+}
 struct Power {
-  double octave, number;
-  __device__ __forceinline__ explicit Power(double t) {
-    octave = floor(t);
-    const double x = (t - octave - 0.5) * 0.69314718055994530942;
-    double p = 1.0 / 3628800.0;
-    p = fma(p, x, 1.0 / 362880.0);
-    p = fma(p, x, 1.0 / 40320.0);
-    p = fma(p, x, 1.0 / 5040.0);
-    p = fma(p, x, 1.0 / 720.0);
-    p = fma(p, x, 1.0 / 120.0);
-    p = fma(p, x, 1.0 / 24.0);
-    p = fma(p, x, 1.0 / 6.0);
-    p = fma(p, x, 0.5);
-    p = fma(p, x, 1.0);
-    p = fma(p, x, 1.0);
-    number = p * 1.41421356237309504880;
+  int32_t i;      // whole sixteenths above E; far down: a large negative number
+  double number;  // 2^t relative to its own octave
+  __device__ __forceinline__ Power(double t, double E, const double* roots) {
+    const double sixteenths = t * 16.0, whole = floor(sixteenths), r = sixteenths - whole;
+    i = (int32_t)fmax(whole - E * 16.0, -1e6);
+    double p = 1.2994313288926215e-09;
+    p = fma(p, r, 1.467260724112997e-07);
+    p = fma(p, r, 1.3550831108683642e-05);
+    p = fma(p, r, 0.00093838478405108448);
+    p = fma(p, r, 0.043321698786749421);
+    p = fma(p, r, 0.99999999999985389);
+    number = p * roots[i & 15];
   }
-  // relative to 2^E
-  __device__ __forceinline__ double weight(double E) const {
-    const double d = octave - E;
-    return d > -1000.0 ? ldexp(number, (int)d) : 0.0;
-  }
+  __device__ __forceinline__ double weight() const { return ldexp(number, i >> 4); }
   __device__ __forceinline__ u64 mass() const {  // in 2^-kMassBits of the octave
     return (u64)__double_as_longlong(fma(number, (double)(1ull << kMassBits), 4503599627370496.0)) - (u64)__double_as_longlong(4503599627370496.0);
   }
   // the bin under the octave E, kBins or more: too far down
-  __device__ __forceinline__ int32_t bin(double t, double E) const {
-    const double d = E - octave;
-    return d < kBins / kBinsAnOctave ? (int32_t)d * kBinsAnOctave + (kBinsAnOctave - 1) - (int32_t)((t - octave) * kBinsAnOctave) : kBins;
-  }
+  __device__ __forceinline__ int32_t bin() const { return kBinsAnOctave - 1 - (i >> 2); }
 };
+static_assert(kBinsAnOctave == 4, "four sixteenths to a bin");
 
 struct Slot {  // what a slice leaves
   double E, sum;
@@ -378,6 +393,8 @@ struct Shared {
   int32_t found[2];
   double rest;
   int32_t slice;
+  int32_t pick;
+  float own[kTokens];  // logits of a thread
   u64 few[kFew];        // (not in the first kernel)
   u64 ranked[kRanked];  // (only in the third)
 };
@@ -416,19 +433,18 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
     x[j] = Group<E>{};
     if (ok[j]) x[j] = load_group(row, t);
   }
+  const RowRules rule(r, h, b);  // (read before the barriers of the next)
   if (ruled) gather_rules(r, b, first, h, table);
-  const RowRules rule(r, h, b);
 #pragma unroll
   for (int k = 0; k < kTokens; ++k) y[k] = ok[k / 8] >> (k % 8) & 1u ? widened<E>(x[k / 8][k % 8]) : -__builtin_inff();
   if (ruled) {
 #pragma unroll 1
     for (uint32_t hit = touched(table, ok); hit; hit &= hit - 1) {
       const int k = __builtin_ctz(hit);
-      float v = 0.0f;
+      float all[kTokens];
 #pragma unroll
-      for (int i = 0; i < kTokens; ++i)
-        if (i == k) v = y[i];
-      v = rule(v, table.word[place_of(k)], first + place_of(k));
+      for (int i = 0; i < kTokens; ++i) all[i] = y[i];
+      const float v = rule(picked(all, k), table.word[place_of(k)], first + place_of(k));
 #pragma unroll
       for (int i = 0; i < kTokens; ++i)
         if (i == k) y[i] = v;
@@ -452,18 +468,27 @@ template <class F> __device__ __forceinline__ void for_tokens(Tokens& y, int32_t
 }
 
 // The token of a slice at which the running sum of weights (w of a token's logit and id) first exceeds `rest`, and its logit; the
-// last one with a weight if rounding leaves none; -1 if none has any.
+// last one with a weight if rounding leaves none; -1 if none has any.  The thread in whose eight tokens it lies hands them to eight
+// lanes, a token each (one after the other they took 7000 clocks of 15000).
 template <class W> __device__ int32_t find_token(Tokens& y, int32_t first, double rest, float* logit, Shared& s, W&& w) {
   static_assert(kGroups == 2, "two groups a thread");
   const int32_t lane = (int32_t)threadIdx.x & 63, wave = (int32_t)threadIdx.x >> 6;
   double run0 = 0.0, run1 = 0.0;
   int32_t last = -1;
-  for_tokens(y, first, [&](float v, int32_t t, int j) {
-    const double x = w(v, t);
-    run0 += j ? 0.0 : x;
-    run1 += j ? x : 0.0;
-    if (x > 0.0) last = t;
-  });
+#pragma unroll 1
+  for (int h = 0; h < kTokens / 4; ++h) {
+    double x[4], run = h < 2 ? run0 : run1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = w(y[i], token_of(first, 4 * h + i));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      run += x[i];
+      if (x[i] > 0.0) last = token_of(first, 4 * h + i);
+    }
+    if (h < 2) run0 = run;
+    else run1 = run;
+    y = __builtin_shufflevector(y, y, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0, 1, 2, 3);
+  }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const double other0 = __shfl_up(run0, d), other1 = __shfl_up(run1, d);
@@ -488,19 +513,33 @@ template <class W> __device__ int32_t find_token(Tokens& y, int32_t first, doubl
   const double up0 = __shfl_up(run0, 1), up1 = __shfl_up(run1, 1);
   const double at0 = lane ? before0 + up0 : before0, at1 = lane ? before1 + up1 : before1;
   const bool in0 = at0 <= rest && rest < before0 + run0, in1 = at1 <= rest && rest < before1 + run1;
-  if (in0 || in1) {
-    int32_t token = -1;
-    double at = in0 ? at0 : at1;
-    for_tokens(y, first, [&](float v, int32_t t, int j) {
-      if ((j == 0) != in0) return;
-      const double x = w(v, t);
-      if (x > 0.0 && (token < 0 || at <= rest)) token = t;  // (the last whose stretch begins at or before)
-      at += x;
-    });
-    if (token >= 0) atomicMin(&s.found[0], token);
+  if (in0 || in1) {  // (one thread: each stretch ends where the next begins)
+    s.found[0] = token_of(first, in0 ? 0 : 8);
+    s.pick = in0 ? 0 : 8;
+    s.rest = in0 ? at0 : at1;
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) s.own[k] = y[k];
   }
   __syncthreads();
-  const int32_t id = s.found[0] != INT32_MAX ? s.found[0] : s.found[1];
+  const int32_t eight = s.found[0];
+  int32_t id = s.found[1];
+  if (eight != INT32_MAX) {
+    const float v = s.own[s.pick + (lane & 7)];
+    const double x = lane < 8 ? w(v, eight + lane) : 0.0;
+    double run = x;
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) {
+      const double other = __shfl_up(run, d);
+      if (lane >= d) run += other;
+    }
+    const double up = __shfl_up(run, 1), at = lane ? s.rest + up : s.rest;
+    const u64 some = __ballot(x > 0.0), begun = __ballot(x > 0.0 && at <= rest);  // the last whose stretch begins at or before
+    const int k = begun ? 63 - __builtin_clzll(begun) : __builtin_ctzll(some | 1ull << 63);
+    if (some) id = eight + k;
+    *logit = __shfl(v, k);
+    if (some) return id;
+  }
+  __syncthreads();
 #pragma unroll
   for (int k = 0; k < kTokens; ++k)
     if (token_of(first, k) == id) s.top[0] = y[k];
@@ -613,7 +652,7 @@ __device__ void row_bins(const u64* bins, int32_t n, double E, Shared& s) {
   __syncthreads();
   u64 mass = 0;
   uint32_t count = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int32_t i = tid / kBins; i < n; i += 2) {
     const double d = s.slots[i].top > -__builtin_inff() ? (E - s.slots[i].E) * kBinsAnOctave : (double)kBins;
     const bool some = d <= (double)bin;
@@ -703,6 +742,7 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
   extern __shared__ __align__(16) char lds[];
   RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   Shared& s = *reinterpret_cast<Shared*>(lds);
+  __shared__ double roots[16];
   const int32_t b = (int32_t)blockIdx.y, slice = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Row<E> row(in, b);
   const RowDraw d(dr, b, in.V);
@@ -710,6 +750,7 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
   u64* const bins = m.bins + (size_t)b * m.slices * kBins;
   int32_t first = row.first_token(slice);
   Tokens y;
+  fill_roots(roots);
   load_slice<E>(row, r, b, first, table, y);
 
   float top = -__builtin_inff();
@@ -736,10 +777,10 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
     auto add = [&](float v) {
       if (!(v > -__builtin_inff())) return;
       const double t = octaves(v, d.per);
-      const Power w(t);
-      sum += w.weight(slot.E);
+      const Power w(t, slot.E, roots);
+      sum += w.weight();
       if (d.cut) {
-        const int32_t bin = w.bin(t, slot.E);
+        const int32_t bin = w.bin();
         if (bin < kBins) atomicAdd(&s.bins[bin], w.mass() + (1ull << kCountShift));
       }
     };
@@ -768,7 +809,7 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
       const double rest = s.rest;
       first = row.first_token(s.slice);
       load_slice<E>(row, r, b, first, table, y);
-      id = find_token(y, first, rest, &logit, s, [&](float v, int32_t) { return v > -__builtin_inff() ? Power(octaves(v, d.per)).weight(total.E) : 0.0; });
+      id = find_token(y, first, rest, &logit, s, [&](float v, int32_t) { return v > -__builtin_inff() ? Power(octaves(v, d.per), total.E, roots).weight() : 0.0; });
     }
     if (tid == 0) {
       write_out(d, total, id, logit, ids + b, logprobs ? logprobs + b : nullptr);
@@ -804,8 +845,7 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
       from = min(from, to);
     }
     if (plan.min_key) {
-      const double t = octaves(value_of(plan.min_key), d.per);
-      low = Power(t).bin(t, total.E);
+      low = Power(octaves(value_of(plan.min_key), d.per), total.E, roots).bin();
     }
 #pragma unroll
     for (int k = 0; k < kBins / 64; ++k) {
@@ -841,7 +881,7 @@ __device__ KeyRange keys_of_bins(int32_t first, int32_t last, double E, double p
 // Goes through the tokens of the wanted bins: f(key, bin, id).  All threads; `listed` of them, a few in s.few, or more than the list holds.
 template <Elem E, class F>
 __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRules& r, const RowDraw& d, const RowPlan& plan, int32_t b, int32_t n_slices, const u64* list,
-                                               uint32_t listed, RuleTable& table, const Shared& s, const uint32_t* wanted, F&& f) {
+                                               uint32_t listed, RuleTable& table, const Shared& s, const uint32_t* wanted, const double* roots, F&& f) {
   if (listed <= kMostCandidates) {
     constexpr int kAhead = 4;
 #pragma unroll 1
@@ -868,8 +908,7 @@ __device__ __forceinline__ void for_candidates(const Row<E>& row, const LogitRul
     load_slice<E>(row, r, b, first, table, y);
     for_tokens(y, first, [&](float v, int32_t id, int) {
       if (!(v > -__builtin_inff())) return;
-      const double t = octaves(v, d.per);
-      const int32_t bin = Power(t).bin(t, plan.total.E);
+      const int32_t bin = Power(octaves(v, d.per), plan.total.E, roots).bin();
       if (bin < kBins && (wanted[bin / 32] >> (bin & 31) & 1u)) f(key_of(v), bin, id);
     });
   }
@@ -881,7 +920,7 @@ struct Cut {
   int32_t bin;
   uint32_t key;
   int32_t id;
-  __device__ __forceinline__ bool keeps(int32_t in, uint32_t k, int32_t i) const { return in < bin || (in == bin && (k > key || (k == key && i <= id))); }
+  __device__ __forceinline__ bool keeps(int32_t in, uint32_t k, int32_t i) const { return (in < bin) | ((in == bin) & ((k > key) | ((k == key) & (i <= id)))); }
 };
 
 template <Elem E>
@@ -889,6 +928,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, Log
   extern __shared__ __align__(16) char lds[];
   RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   __shared__ uint32_t wanted[kBins / 32];
+  __shared__ double roots[16];
   Shared& s = *reinterpret_cast<Shared*>(lds);
   const int32_t b = (int32_t)blockIdx.y, slice = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x;
   const RowPlan& plan = m.plans[b];
@@ -899,6 +939,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, Log
   Tokens y;
 
   // the tokens of the wanted bins, if the slice has any
+  fill_roots(roots);
   if (tid == 0) s.flag[1] = 0;
   if (tid < kBins / 32) wanted[tid] = reinterpret_cast<const uint32_t*>(plan.wanted)[tid];
   const double E_row = plan.total.E;
@@ -926,8 +967,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, Log
   for_tokens(y, first, [&](float v, int32_t id, int) {
     const uint32_t key = key_of(v);
     if (!(v > -__builtin_inff()) || key < range.lo || key > range.hi) return;
-    const double t = octaves(v, d.per);
-    const int32_t bin = Power(t).bin(t, E_row);
+    const int32_t bin = Power(octaves(v, d.per), E_row, roots).bin();
     if (bin >= kBins || !(wanted[bin / 32] >> (bin & 31) & 1u)) return;
     const u64 x = (u64)key << 32 | (u64)bin << 24 | (u64)(uint32_t)id;
     const uint32_t at = atomicAdd(&s.flag[0], 1u);
@@ -954,9 +994,9 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   __shared__ Shared s;
   __shared__ uint32_t wanted[kBins / 32];
+  __shared__ double roots[16];
   const int32_t b = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const RowPlan& plan = m.plans[b];
-  if (!plan.cut) return;
   const Row<E> row(in, b);
   const RowDraw d(dr, b, in.V);
   const Slot* const slots = m.slots + (size_t)b * m.slices;
@@ -964,12 +1004,20 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   const u64* const list = m.candidates + (size_t)b * kMostCandidates;
   const RowTotal total = plan.total;
   const uint32_t min_key = plan.min_key, listed = m.n_candidates[b];
+  const double in_front = plan.before[min(tid, kBins)];
+  const uint32_t some = reinterpret_cast<const uint32_t*>(plan.wanted)[min(tid, kBins / 32 - 1)];
+  const Slot slot = slots[min(tid, n_slices - 1)];
+  u64 few[kFew / kSliceThreads];  // (all are read, so that it need not be known how many there are)
+#pragma unroll
+  for (int k = 0; k < kFew / kSliceThreads; ++k) few[k] = list[k * kSliceThreads + tid];
+  if (!plan.cut) return;
   Tokens y;
-  if (tid <= kBins) s.before_mass[tid] = plan.before[tid];
-  if (tid < n_slices) s.slots[tid] = slots[tid];
-  if (tid < kBins / 32) wanted[tid] = reinterpret_cast<const uint32_t*>(plan.wanted)[tid];
-  if (listed <= kFew)
-    for (uint32_t i = (uint32_t)tid; i < listed; i += kSliceThreads) s.few[i] = list[i];
+  fill_roots(roots);
+  if (tid <= kBins) s.before_mass[tid] = in_front;
+  if (tid < n_slices) s.slots[tid] = slot;
+  if (tid < kBins / 32) wanted[tid] = some;
+#pragma unroll
+  for (int k = 0; k < kFew / kSliceThreads; ++k) s.few[k * kSliceThreads + tid] = few[k];
   int32_t k_bin = plan.k_bin, in_bin = plan.k_need ? k_bin : -1;  // in_bin: where the cut of a selection lies
   u64 need = (u64)plan.k_need;  // what the rest of the kept beginning has to reach there: tokens, or mass in the bin's whole numbers
   Cut cut{k_bin, 0, INT32_MAX};
@@ -977,9 +1025,8 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   if (tid == 0) m.n_candidates[b] = 0;
   double up_to = s.before_mass[min(k_bin, kBins - 1) + 1];
   k_bin = min(k_bin, kBins - 1);
-  const double t_low = octaves(value_of(min_key), d.per);
-  const int32_t low = min_key ? Power(t_low).bin(t_low, total.E) : kBins;
-  auto kept = [&](uint32_t key, int32_t bin, int32_t id) { return key >= min_key && cut.keeps(bin, key, id); };
+  const int32_t low = min_key ? Power(octaves(value_of(min_key), d.per), total.E, roots).bin() : kBins;
+  auto kept = [&](uint32_t key, int32_t bin, int32_t id) { return (key >= min_key) & cut.keeps(bin, key, id); };
 
   // Two selections, top-k and top-p of what it keeps, then the sums of the slices.  A selection goes through the tokens of its bin that
   // are kept so far: passes that sort them into 1024 stretches of their range of keys, and then of ids among the tokens with one
@@ -1031,6 +1078,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
     if (mode != kSums && left <= kRanked) {
       mode = kRank;
       if (tid == 0) { s.flag[0] = 0; s.found[0] = -1; }
+      if (tid < kRanked) { s.ranked[tid] = ~0ull; s.bins[tid] = 0; }
     } else if (mode != kSums) {
       s.bins[tid] = s.bins[tid + kSliceThreads] = 0;
       s.counts[tid] = s.counts[tid + kSliceThreads] = 0;
@@ -1038,13 +1086,13 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
       shift = width < 1024 ? 0 : 22 - __clz((int)width);
     }
     __syncthreads();
-    for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, table, s, wanted, [&](uint32_t key, int32_t bin, int32_t id) {
+    for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, table, s, wanted, roots, [&](uint32_t key, int32_t bin, int32_t id) {
       if (mode == kSums) {
-        if (bin == edge && kept(key, bin, id)) atomicAdd(&s.slice_more[(uint32_t)(id - row_first) / kSliceTokens], Power(octaves(value_of(key), d.per)).mass());
+        if (bin == edge && kept(key, bin, id)) atomicAdd(&s.slice_more[(uint32_t)(id - row_first) / kSliceTokens], Power(octaves(value_of(key), d.per), total.E, roots).mass());
         return;
       }
       if (bin != in_bin || !within.keeps(bin, key, id) || key > hi || key < lo || id < first_id || id > last_id) return;
-      const u64 mass = mode != kIds ? Power(octaves(value_of(key), d.per)).mass() : 0;
+      const u64 mass = mode != kIds ? Power(octaves(value_of(key), d.per), total.E, roots).mass() : 0;
       if (mode == kRank) {
         const uint32_t at = atomicAdd(&s.flag[0], 1u);
         s.ranked[at] = (u64)~key << 32 | (uint32_t)id;
@@ -1063,12 +1111,16 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
         const u64 mine = s.ranked[tid], own = s.bins[tid];
         u64 before = 0, whole = 0;
         uint32_t rank = 0;
-        for (uint32_t i = 0; i < n; ++i) {
-          const u64 x = s.bins[i];
-          const bool front = s.ranked[i] < mine;
-          before += front ? x : 0;
-          rank += front ? 1 : 0;
-          whole += x;
+#pragma unroll 1
+        for (uint32_t i = 0; i < n; i += 8) {
+#pragma unroll
+          for (uint32_t k = 0; k < 8; ++k) {
+            const u64 x = s.bins[i + k];
+            const bool front = s.ranked[i + k] < mine;
+            before += front ? x : 0;
+            rank += front ? 1 : 0;
+            whole += x;
+          }
         }
         // (rounding can leave a need above what there is: the last token then)
         const u64 wanted = min(max(need, (u64)1), what == 0 ? (u64)n : whole), at = what == 0 ? (u64)rank : before;
@@ -1150,20 +1202,30 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   }
   __syncthreads();
   const double up_to_bin = (double)(divided ? edge : min(edge + 1, kBins));
+  constexpr int kAtOnce = 3;  // slices of a wave whose bins are on their way together
 #pragma unroll 1
-  for (int32_t i = wave; i < n_slices; i += kWaves) {
-    double sum = 0.0;
-    if (s.slots[i].top > -__builtin_inff()) {
-      const double off = (total.E - s.slots[i].E) * kBinsAnOctave;  // of the slice's bins in the row's
+  for (int32_t begin = wave; begin < n_slices; begin += kAtOnce * kWaves) {
+    u64 x[kAtOnce][kBins / 64];
 #pragma unroll
-      for (int k = 0; k < kBins / 64; ++k) {
-        const int32_t bin = k * 64 + lane;  // of the slice
-        const double at = off + (double)bin;
-        if (at < up_to_bin) sum += ldexp((double)(bins[(size_t)i * kBins + bin] & kMassMask), -kMassBits - (int32_t)at / kBinsAnOctave);
+    for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+      for (int k = 0; k < kBins / 64; ++k) x[j][k] = bins[(size_t)min(begin + j * kWaves, n_slices - 1) * kBins + k * 64 + lane];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const int32_t i = begin + j * kWaves;
+      if (i >= n_slices) break;
+      double sum = 0.0;
+      if (s.slots[i].top > -__builtin_inff()) {
+        const double off = (total.E - s.slots[i].E) * kBinsAnOctave;  // of the slice's bins in the row's
+#pragma unroll
+        for (int k = 0; k < kBins / 64; ++k) {
+          const double at = off + (double)(k * 64 + lane);
+          if (at < up_to_bin) sum += ldexp((double)(x[j][k] & kMassMask), -kMassBits - (int32_t)at / kBinsAnOctave);
+        }
       }
+      sum = wave_sum(sum);
+      if (lane == 0) s.slice_sum[i] = sum + (divided ? ldexp((double)s.slice_more[i], -kMassBits - edge / kBinsAnOctave) : 0.0);
     }
-    sum = wave_sum(sum);
-    if (lane == 0) s.slice_sum[i] = sum + (divided ? ldexp((double)s.slice_more[i], -kMassBits - edge / kBinsAnOctave) : 0.0);
   }
   __syncthreads();
   find_slice(d.u, n_slices, s);
@@ -1172,13 +1234,17 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   __syncthreads();
   load_slice<E>(row, r, b, first, table, y);
   float logit = 0.0f;
-  const uint32_t least_key = max(max(min_key, cut.key), keys_of_bins(edge, min(edge, kBins - 1), total.E, d.per).lo);  // of what is kept
+  // of what is kept, all of which is above -inf
+  const uint32_t least_key = max(max(max(min_key, cut.key), keys_of_bins(edge, min(edge, kBins - 1), total.E, d.per).lo), key_of(-FLT_MAX));
   const int32_t id = find_token(y, first, rest, &logit, s, [&](float v, int32_t token) {
-    if (!(v > -__builtin_inff()) || key_of(v) < least_key) return 0.0;
-    const double t = octaves(v, d.per);
-    const Power w(t);
-    const int32_t bin = w.bin(t, total.E);
-    return bin < kBins && kept(key_of(v), bin, token) ? w.weight(total.E) : 0.0;
+    const uint32_t key = key_of(v);
+    double x = 0.0;
+    if (key >= least_key) {
+      const Power w(octaves(v, d.per), total.E, roots);
+      const int32_t bin = w.bin();
+      x = (bin < kBins) & kept(key, bin, token) ? w.weight() : 0.0;
+    }
+    return x;
   });
   if (tid == 0) write_out(d, total, id, logit, ids + b, logprobs ? logprobs + b : nullptr);
 }
