@@ -136,59 +136,61 @@ __device__ __forceinline__ void gather_rules(const LogitRules& r, int32_t b, int
 // What the rules make of a logit: in 64 bits, where neither the product of a factor and a count nor the order of a
 // compiler's contractions can change a bit of the 32 that are kept.
 struct RowRules {
-  double repetition, frequency, presence;
+  double repetition, inverse, frequency, presence;
   const LogitRules& r;
   int32_t begin, end;  // of the row's biases
   __device__ RowRules(const LogitRules& rules, const History& h, int32_t b)
-      : repetition(rules.repetition ? (double)rules.repetition[b] : 1.0), frequency(rules.frequency ? (double)rules.frequency[b] : 0.0),
+      : repetition(rules.repetition ? (double)rules.repetition[b] : 1.0), inverse(1.0 / repetition), frequency(rules.frequency ? (double)rules.frequency[b] : 0.0),
         presence(rules.presence ? (double)rules.presence[b] : 0.0), r(rules), begin(h.bias_begin), end(h.bias_end) {}
-  __device__ float operator()(float x, uint32_t word, int32_t token) const {
+  // The penalties alone.  A quotient is the product with the inverse and what that leaves of it, rounded as the division is; where the
+  // rest is none (infinite quotients, factors of 0) the product is the quotient.  frequency * count is exact.
+  __device__ __forceinline__ double penalised(float x, uint32_t word) const {
     double y = (double)x;
-    if (word & (kInPrompt | kCount)) y = y > 0.0 ? y / repetition : y * repetition;
-    if (word & kCount) y = y - frequency * (double)(word & kCount) - presence;
-    if (uint32_t entry = word >> kBiasShift & kBiasMask) {
-      int32_t e = begin + (int32_t)entry - 1;
-      if (entry == kBiasMask)
-        for (int32_t k = end - 1; k > e; --k)
-          if (r.bias_ids[k] == token) { e = k; break; }
-      y += (double)r.bias[e];
-    }
+    const bool divided = y > 0.0;
+    const double near = y * (divided ? inverse : repetition), rest = fma(-near, repetition, y);
+    y = divided && rest == rest ? fma(rest, inverse, near) : near;
+    return word & kCount ? y - frequency * (double)(word & kCount) - presence : y;
+  }
+  __device__ float biased(float x, uint32_t word, int32_t token) const {
+    double y = word & (kInPrompt | kCount) ? penalised(x, word) : (double)x;
+    const uint32_t entry = word >> kBiasShift & kBiasMask;
+    int32_t e = begin + (int32_t)entry - 1;
+    if (entry == kBiasMask)
+      for (int32_t k = end - 1; k > e; --k)
+        if (r.bias_ids[k] == token) { e = k; break; }
+    y += (double)r.bias[e];
     return (float)y;
   }
 };
-// Which of the thread's tokens a rule touches.  They are few, and taken one by one in a loop: unrolled over the thread's tokens the rules
-// are 7000 instructions (a division in 64 bits each), which a kernel that runs once fetches from the L2.
 __device__ __forceinline__ int32_t place_of(int k) { return (k / 8 * kSliceThreads + (int32_t)threadIdx.x) * 8 + k % 8; }
-// v[k], with the steps of a tree (the compiler's own way takes three instructions for each)
-template <class T> __device__ __forceinline__ T picked(const T (&v)[kTokens], int k) {
-  static_assert(kTokens == 16, "four steps");
-  T x[kTokens];
-#pragma unroll
-  for (int i = 0; i < kTokens; ++i) x[i] = v[i];
-#pragma unroll
-  for (int n = kTokens / 2; n; n >>= 1) {
-    const bool upper = k & n;
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      T high = x[i + n];
-      asm("" : "+v"(high));  // (two elements of one vector are two values here)
-      x[i] = upper ? high : x[i];
-    }
-  }
-  return x[0];
-}
-__device__ __forceinline__ uint32_t touched(const RuleTable& table, const uint32_t (&ok)[kGroups]) {
-  uint32_t hit = 0;
+// The rules on the thread's tokens: get(k) and set(k, logit) for those that a rule touches.  Tokens of a text lie close together where
+// ids are given out by frequency, so that many of a wave's are touched or none; biases are few and taken one by one.
+template <class Get, class Set> __device__ __forceinline__ void apply_rules(const RuleTable& table, const RowRules& rule, const uint32_t (&ok)[kGroups], int32_t first, Get&& get, Set&& set) {
+  uint32_t with_bias = 0;
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
     const uint4 a = *reinterpret_cast<const uint4*>(table.word + place_of(8 * j)), b = *reinterpret_cast<const uint4*>(table.word + place_of(8 * j) + 4);
     const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    uint32_t some = 0;
+    if (!ok[j] || !(a.x | a.y | a.z | a.w | b.x | b.y | b.z | b.w)) continue;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) some |= w[i] ? 1u << i : 0u;
-    hit |= (some & ok[j]) << (8 * j);
+    for (int i = 0; i < 8; ++i) {
+      if (!w[i] || !(ok[j] >> i & 1u)) continue;
+      if (w[i] >> kBiasShift & kBiasMask) with_bias |= 1u << (8 * j + i);
+      else set(8 * j + i, (float)rule.penalised(get(8 * j + i), w[i]));
+    }
   }
-  return hit;
+#pragma unroll 1
+  for (; with_bias; with_bias &= with_bias - 1) {
+    const int k = __builtin_ctz(with_bias);
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i)
+      if (i == k) v = get(i);
+    v = rule.biased(v, table.word[place_of(k)], first + place_of(k));
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i)
+      if (i == k) set(i, v);
+  }
 }
 
 // One workgroup per slice.  Bound by the bytes where the batch is large (a logit that nothing touches is copied as it is, one that
@@ -216,19 +218,8 @@ __global__ __launch_bounds__(kSliceThreads) void process_logits_kernel(Logits in
   const RowRules rule(r, h, b);  // (read before the barriers of the next)
   if (ruled) gather_rules(r, b, first, h, table);
   bits* const to = out + (int64_t)b * out_stride;
-  if (ruled) {
-#pragma unroll 1
-    for (uint32_t hit = touched(table, ok); hit; hit &= hit - 1) {
-      const int k = __builtin_ctz(hit);
-      uint32_t all[kTokens];
-#pragma unroll
-      for (int i = 0; i < kTokens; ++i) all[i] = x[i / 8][i % 8];
-      const bits v = narrowed<E>(rule(widened<E>((bits)picked(all, k)), table.word[place_of(k)], first + place_of(k)));
-#pragma unroll
-      for (int i = 0; i < kTokens; ++i)
-        if (i == k) x[i / 8].set(i % 8, v);
-    }
-  }
+  if (ruled)
+    apply_rules(table, rule, ok, first, [&](int k) { return widened<E>(x[k / 8][k % 8]); }, [&](int k, float v) { x[k / 8].set(k % 8, narrowed<E>(v)); });
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
     const int32_t t = first + place_of(8 * j);
@@ -437,19 +428,7 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
   if (ruled) gather_rules(r, b, first, h, table);
 #pragma unroll
   for (int k = 0; k < kTokens; ++k) y[k] = ok[k / 8] >> (k % 8) & 1u ? widened<E>(x[k / 8][k % 8]) : -__builtin_inff();
-  if (ruled) {
-#pragma unroll 1
-    for (uint32_t hit = touched(table, ok); hit; hit &= hit - 1) {
-      const int k = __builtin_ctz(hit);
-      float all[kTokens];
-#pragma unroll
-      for (int i = 0; i < kTokens; ++i) all[i] = y[i];
-      const float v = rule(picked(all, k), table.word[place_of(k)], first + place_of(k));
-#pragma unroll
-      for (int i = 0; i < kTokens; ++i)
-        if (i == k) y[i] = v;
-    }
-  }
+  if (ruled) apply_rules(table, rule, ok, first, [&](int k) { return y[k]; }, [&](int k, float v) { y[k] = v; });
 #pragma unroll
   for (int k = 0; k < kTokens; ++k) y[k] = drawable(y[k]);
   if (ruled) __syncthreads();  // (other things lie where the tables were)
