@@ -241,6 +241,7 @@ __global__ __launch_bounds__(kFewThreads<NB>) void q4_few_kernel(Head h, Elem ou
           if (next_t < tiles) load(next_v, next_step, next_codes, next_groups);
 #pragma unroll
           for (int j = 0; j < kChunks; ++j) {
+            if ((step * kChunks + j) * 128 >= h.K) break;
             const uint4v c = kAsTheyLie ? codes[j] : exchanged(codes[j]);
 #pragma unroll
             for (int r = 0; r < kParts; ++r) {
