@@ -62,13 +62,16 @@ __device__ __forceinline__ void store_logit(const Head& h, Elem type, int64_t at
 }
 
 // ---------------------------------------------------------------- few rows in the batch
-// Up to 16 NB rows, whose hidden states and their sums fit LDS.  A wave takes 16 rows of the matrix (a tile) and all columns, so that waves need
-// nothing of each other: it reads the codes a step of 512 columns (4 chunks of 128) at a time, the next ones while it multiplies
-// the last, 64 bytes of each row and chunk.  Hidden states lie in LDS in the order in which the products take them, zeros behind
-// the last column (what is read of the matrix there is some earlier part of the row); rows of the batch that are not there are read
-// from the last one and their sums dropped.
+// Shares of 16 NB rows, whose hidden states and their sums fit LDS.  A wave takes 16 rows of the matrix (a tile) and all columns, so
+// that waves need nothing of each other: it reads the codes a step of 512 columns (4 chunks of 128) at a time, the next ones while
+// it multiplies the last, 64 bytes of each row and chunk.  Hidden states lie in LDS in the order in which the products take them,
+// zeros behind the last column (what is read of the matrix there is some earlier part of the row); rows of the batch that are not
+// there are read from the last one and their sums dropped.
 // Under masks the workgroup lists the rows of its share that some request allows, and its waves take 16 of those at a time.
 // Where a workgroup has fewer tiles than waves, several waves take the steps of one in turn and their sums meet in LDS.
+// One row of the batch is bound by the bytes of the matrix: 128256 rows of 4096 columns take 55 us, 4.9 TB/s, as much as a large copy
+// moves.  24 rows (50001 x 2080, groups of 32, zero points: 51 us, 1.3 TB/s) are bound by what is done for each 32 columns of a tile
+// besides two products: unpacking, scale, zero point, and 4 KB out of LDS.
 // P: parts of a step that have a scale of their own: 4 (groups of 128 or a multiple), 8 (64) or 16 (32, or other multiples of it).
 constexpr int kFewMaxThreads = 1024;  // of NB = 1; two rows of products need the registers of half as many waves
 template <int NB> constexpr int kFewThreads = kFewMaxThreads / NB;
@@ -297,6 +300,9 @@ __global__ __launch_bounds__(kFewThreads<NB>) void q4_few_kernel(Head h, Elem ou
 // memory three chunks before they are needed, by all waves in equal parts, and go through two buffers in LDS, hidden states
 // through three; one barrier a chunk.
 // A workgroup's share is cut into passes of the tiles that its waves hold.
+// 128 rows (151936 x 4096, groups of 128) take 302 us, 0.53 PFLOP/s: the waves of a SIMD spend as long on unpacking codes, scaling sums and
+// on LDS as on products, and the barrier of a chunk leaves little of one under the other.  With eight waves for 64 x 64 logits each
+// instead of 32 x 32 it went from 565 to 441 us, with workgroups on different chunks to 303.
 constexpr int kManyThreads = 512, kManyTiles = 4;  // tiles of a wave
 
 // How the parts of a chunk find their scales: one for the chunk, looked up by its number; halves; quarters; quarters that are looked up.
@@ -586,7 +592,7 @@ template <Elem H, int NB, int P> void launch_few_zeros(const Head& h, Elem out_t
   else launch_few<H, NB, P, false>(h, out_type, stream);
 }
 int few_parts(int32_t group) { return group % 128 == 0 ? 4 : group == 64 ? 8 : 16; }
-bool few_fits(const Head& h, int nb) { return h.B <= 16 * nb && few_layout(h.K, h.B, few_parts(h.group), nb).end <= kFewMaxLds; }
+bool few_fits(const Head& h, int32_t rows, int nb) { return few_layout(h.K, rows, few_parts(h.group), nb).end <= kFewMaxLds; }
 template <Elem H, int NB> void launch_few_groups(const Head& h, Elem out_type, hipStream_t stream) {
   if (h.group % 128 == 0) launch_few_zeros<H, NB, 4>(h, out_type, stream);
   else if (h.group == 64) launch_few_zeros<H, NB, 8>(h, out_type, stream);
@@ -608,9 +614,13 @@ template <Elem H, int MW, int WM> void launch_many_groups(const Head& h, Elem ou
   else if (h.group == 32 && h.K >= 128) launch_many_zeros<H, MW, WM, kQuarters>(h, out_type, stream);
   else launch_many_zeros<H, MW, WM, kLookedUp>(h, out_type, stream);
 }
+// Up to 32 rows go through LDS as a whole where they fit: 24 rows of 50001 x 2080 in groups of 32 take 51 us that way and 63 as many
+// rows, 17 of 151936 x 2048 73 and 115.  Where 17 to 32 rows do not fit but 16 do, the matrix is read twice: 24 rows of 50001 x 4096 in
+// groups of 128 57 us, 70 as many rows; 32 of 151936 x 4096 150 and 158; under masks that leave 100 tokens a row 23 and 42.
 template <Elem H> void launch_head(const Head& h, Elem out_type, hipStream_t stream) {
-  if (few_fits(h, 1)) return launch_few_groups<H, 1>(h, out_type, stream);
-  if (few_fits(h, 2)) return launch_few_groups<H, 2>(h, out_type, stream);
+  if (h.B <= 16 && few_fits(h, h.B, 1)) return launch_few_groups<H, 1>(h, out_type, stream);
+  if (h.B <= 32 && few_fits(h, h.B, 2)) return launch_few_groups<H, 2>(h, out_type, stream);
+  if (h.B <= 32 && few_fits(h, 16, 1)) return launch_few_groups<H, 1>(h, out_type, stream);
   if (h.B <= 32) return launch_many_groups<H, 2, 1>(h, out_type, stream);
   if (h.B <= 64) return launch_many_groups<H, 4, 1>(h, out_type, stream);
   launch_many_groups<H, 4, 2>(h, out_type, stream);
