@@ -510,7 +510,9 @@ int xgm_apply_token_bitmask_inplace(void* d_logits, xgm_dtype dt, int32_t B, int
  * read):
  *   logits[b][v] = sum over k of hidden[b][k] * (code(v, k) - zero(v, k / group)) * scale(v, k / group),
  * summed in 32 bits and rounded once; -inf where bit (b, v) of d_bitmask is 0
- * (NULL: no mask), also where a hidden state is not finite.
+ * (NULL: no mask).  Codes are multiplied with 16 added to them and the sum taken
+ * off: a hidden state that is not finite, or beyond 2^122 (bf16), makes the
+ * allowed logits of its row inf or NaN, and the others' stay as they are.
  * d_hidden: [B, K] of hidden_dt (XGM_BF16 or XGM_F16), row stride
  * hidden_stride_elems.  d_codes: [V, K / 2] bytes, column 2 j in the low half of
  * byte j.  d_scales: [V, K / group] of hidden_dt.  d_zeros: [V, K / group] bytes
@@ -527,7 +529,7 @@ int xgm_q4_logits(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32_t 
  * call; what it points to is device memory with a value or a row for each row
  * b of the logits.  Any pointer may be NULL: the rule is off.
  *  - history: d_tokens[b][0 .. n) with n = d_n_tokens[b], row stride
- *    token_stride (n is cut off there); the first d_n_prompt[b] of them are
+ *    token_stride (n is cut off there; nothing behind n is read); the first d_n_prompt[b] of them are
  *    the prompt (NULL: none), the others were generated.  Ids outside the row of
  *    logits count for nothing.
  *  - a token that occurs in the history: x > 0 ? x / repetition : x * repetition;
