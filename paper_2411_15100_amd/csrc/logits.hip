@@ -433,6 +433,24 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
   for (int k = 0; k < kTokens; ++k) y[k] = drawable(y[k]);
   if (ruled) __syncthreads();  // (other things lie where the tables were)
 }
+// v[k], by the steps of a tree (the compiler's own way takes three instructions for each of the 16)
+__device__ __forceinline__ float picked(const float (&v)[kTokens], int k) {
+  static_assert(kTokens == 16, "four steps");
+  float x[kTokens];
+#pragma unroll
+  for (int i = 0; i < kTokens; ++i) x[i] = v[i];
+#pragma unroll
+  for (int n = kTokens / 2; n; n >>= 1) {
+    const bool upper = k & n;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      float high = x[i + n];
+      asm("" : "+v"(high));  // (two elements of one vector are two values here)
+      x[i] = upper ? high : x[i];
+    }
+  }
+  return x[0];
+}
 __device__ __forceinline__ int32_t token_of(int32_t first, int k) { return first + place_of(k); }
 
 // Calls f(logit, token) for the thread's tokens of a slice in order of their ids.  The logits go round in their registers instead of the
@@ -733,10 +751,11 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
   load_slice<E>(row, r, b, first, table, y);
 
   float top = -__builtin_inff();
-  int32_t top_id = -1;
+  int at = -1;
 #pragma unroll
   for (int k = 0; k < kTokens; ++k)
-    if (y[k] > top) { top = y[k]; top_id = token_of(first, k); }
+    if (y[k] > top) { top = y[k]; at = k; }
+  int32_t top_id = at < 0 ? -1 : token_of(first, at);
 #pragma unroll
   for (int k = 32; k; k >>= 1) {
     const float other = __shfl_xor(top, k);
@@ -943,11 +962,22 @@ __global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, Log
   load_slice<E>(row, r, b, first, table, y);
   if (tid == 0) s.flag[0] = 0;
   __syncthreads();
-  for_tokens(y, first, [&](float v, int32_t id, int) {
+  // (two comparisons a token; the few in the range one by one)
+  const float least = value_of(max(range.lo, key_of(-FLT_MAX))), most = value_of(min(range.hi, key_of(FLT_MAX)));
+  uint32_t in_range = 0;
+  float all[kTokens];
+#pragma unroll
+  for (int k = 0; k < kTokens; ++k) {
+    all[k] = y[k];
+    in_range |= (all[k] >= least) & (all[k] <= most) ? 1u << k : 0u;
+  }
+#pragma unroll 1
+  for (; in_range; in_range &= in_range - 1) {
+    const int k = __builtin_ctz(in_range);
+    const float v = picked(all, k);
     const uint32_t key = key_of(v);
-    if (!(v > -__builtin_inff()) || key < range.lo || key > range.hi) return;
-    const int32_t bin = Power(octaves(v, d.per), E_row, roots).bin();
-    if (bin >= kBins || !(wanted[bin / 32] >> (bin & 31) & 1u)) return;
+    const int32_t id = token_of(first, k), bin = Power(octaves(v, d.per), E_row, roots).bin();
+    if (bin >= kBins || !(wanted[bin / 32] >> (bin & 31) & 1u)) continue;
     const u64 x = (u64)key << 32 | (u64)bin << 24 | (u64)(uint32_t)id;
     const uint32_t at = atomicAdd(&s.flag[0], 1u);
     if (at < kFew) {
@@ -956,7 +986,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_list_kernel(Logits in, Log
       const uint32_t place = atomicAdd(m.n_candidates + b, 1u);
       if (place < kMostCandidates) list[place] = x;
     }
-  });
+  }
   __syncthreads();
   const uint32_t n = min(s.flag[0], (uint32_t)kFew);
   if (tid == 0 && n) s.counts[0] = atomicAdd(m.n_candidates + b, n);
