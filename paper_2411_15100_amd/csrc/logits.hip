@@ -330,6 +330,7 @@ struct RowPlan {  // what the first kernel leaves of a row for the others
   RowTotal total;
   int32_t cut;       // 0: the row is done
   uint32_t min_key;  // tokens with a smaller key weigh less than min_p
+  int32_t reach;     // kept tokens lie in no lighter bin than this one; -1: too many to list them all
   int32_t k_bin, k_need;  // where top-k ends and how many of its tokens there (0: all); k_bin = kBins: nowhere
   double before[kBins + 1];  // mass in front of each bin, in 2^E
 };
@@ -372,6 +373,7 @@ __device__ __forceinline__ Slot take_in(const Slot* from) { return Slot{take_in(
 constexpr int kMostSlices = (1 << 20) / kSliceTokens + 1;
 constexpr int kFew = 2048;    // candidates that are kept in LDS
 constexpr int kRanked = 256;  // and so many are compared each with each
+constexpr uint32_t kAtOnce = 1024;  // workgroups of slices that run at once, four to a compute unit
 struct Shared {
   double sum[kGroups][kWaves];
   u64 part[kWaves], mass_part[kWaves];
@@ -638,11 +640,12 @@ __device__ void find_slice(double u, int32_t n, Shared& s) {
   }
   __syncthreads();
 }
-__device__ __forceinline__ void write_out(const RowDraw& d, const RowTotal& r, int32_t id, float y, int32_t* to_id, float* to_logprob) {
+// (the sum is taken relative to the weight of the likeliest token as it went into the sum: a token that is alone has logprob 0)
+__device__ __forceinline__ void write_out(const RowDraw& d, const RowTotal& r, int32_t id, float y, const double* roots, int32_t* to_id, float* to_logprob) {
   *to_id = id;
   if (to_logprob)
     *to_logprob = id < 0 ? -__builtin_inff()
-                         : (float)(((double)y - (double)r.top) / (double)d.temperature - (log(r.sum) + (r.E - octaves(r.top, d.per)) * 0.69314718055994530942));
+                         : (float)(((double)y - (double)r.top) / (double)d.temperature - log(r.sum / Power(octaves(r.top, d.per), r.E, roots).weight()));
 }
 
 // The row's bins from its slices' into s.bins and s.counts, relative to the octave E, and what lies in front of each (s.before_*;
@@ -814,7 +817,7 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
       id = find_token(y, first, rest, &logit, s, [&](float v, int32_t) { return v > -__builtin_inff() ? Power(octaves(v, d.per), total.E, roots).weight() : 0.0; });
     }
     if (tid == 0) {
-      write_out(d, total, id, logit, ids + b, logprobs ? logprobs + b : nullptr);
+      write_out(d, total, id, logit, roots, ids + b, logprobs ? logprobs + b : nullptr);
       m.plans[b].cut = 0;
     }
     return;
@@ -849,10 +852,16 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
     if (plan.min_key) {
       low = Power(octaves(value_of(plan.min_key), d.per), total.E, roots).bin();
     }
+    // Where few tokens are kept they are listed, all of them, and one is drawn from the list: one row of 151936 with top-k 50 takes 37 us
+    // that way and 44 by the slices' sums.  Not where the batch has more slices than run at once: the list is then bound by how many slices
+    // have something to list (128 rows, top-p: 116 us and 111).
+    plan.reach = min(last, min(d.top_p < 1.0f ? to : kBins - 1, plan.min_key ? min(low, kBins - 1) : kBins - 1));
+    if (s.before_count[plan.reach + 1] > kRanked || gridDim.x * gridDim.y > kAtOnce) plan.reach = -1;
 #pragma unroll
     for (int k = 0; k < kBins / 64; ++k) {
       const int32_t lo = max(from - 64 * k, 0), hi = min(to - 64 * k, 63);
       u64 bits = lo <= hi ? (~0ull << lo) & (~0ull >> (63 - hi)) : 0;
+      if (plan.reach >= 64 * k) bits |= ~0ull >> (63 - min(plan.reach - 64 * k, 63));
       if (k_bin >= 0 && k_bin / 64 == k) bits |= 1ull << (k_bin & 63);
       if (low >= 0 && low / 64 == k) bits |= 1ull << (low & 63);
       plan.wanted[k] = bits;
@@ -865,6 +874,7 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
     out.min_key = plan.min_key;
     out.k_bin = plan.k_bin;
     out.k_need = plan.k_need;
+    out.reach = plan.reach;
   }
   if (tid <= kBins) m.plans[b].before[tid] = s.before_mass[tid];
 }
@@ -1031,6 +1041,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   if (tid < kBins / 32) wanted[tid] = some;
 #pragma unroll
   for (int k = 0; k < kFew / kSliceThreads; ++k) s.few[k * kSliceThreads + tid] = few[k];
+  const int32_t reach = plan.reach;
   int32_t k_bin = plan.k_bin, in_bin = plan.k_need ? k_bin : -1;  // in_bin: where the cut of a selection lies
   u64 need = (u64)plan.k_need;  // what the rest of the kept beginning has to reach there: tokens, or mass in the bin's whole numbers
   Cut cut{k_bin, 0, INT32_MAX};
@@ -1044,7 +1055,8 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
   // Two selections, top-k and top-p of what it keeps, then the sums of the slices.  A selection goes through the tokens of its bin that
   // are kept so far: passes that sort them into 1024 stretches of their range of keys, and then of ids among the tokens with one
   // key, and narrow the range to the stretch in which the need is reached, until few are left; each of those is then compared with all others.
-  enum { kKeys, kIds, kRank, kSums };
+  // (where few tokens are kept, they are collected and one of them drawn instead of the sums)
+  enum { kKeys, kIds, kRank, kSums, kKept };
   int mode = kKeys, what = 0;
   bool begins = true, divided = false;
   Cut within = cut;
@@ -1083,16 +1095,22 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
         // bins in front of the edge count as they are, the edge's tokens one by one if it is divided
         mode = kSums;
         edge = min(cut.bin, low);
-        divided = edge < kBins && (edge == low || cut.key != 0 || cut.id != INT32_MAX);
-        for (int32_t i = tid; i < n_slices; i += kSliceThreads) s.slice_more[i] = 0;
-        if (!divided) break;
+        if (reach >= 0) {
+          mode = kKept;
+          if (tid == 0) s.flag[0] = 0;
+          if (tid < kRanked) { s.ranked[tid] = ~0ull; s.bins[tid] = 0; }
+        } else {
+          divided = edge < kBins && (edge == low || cut.key != 0 || cut.id != INT32_MAX);
+          for (int32_t i = tid; i < n_slices; i += kSliceThreads) s.slice_more[i] = 0;
+          if (!divided) break;
+        }
       }
     }
-    if (mode != kSums && left <= kRanked) {
+    if (mode < kSums && left <= kRanked) {
       mode = kRank;
       if (tid == 0) { s.flag[0] = 0; s.found[0] = -1; }
       if (tid < kRanked) { s.ranked[tid] = ~0ull; s.bins[tid] = 0; }
-    } else if (mode != kSums) {
+    } else if (mode < kSums) {
       s.bins[tid] = s.bins[tid + kSliceThreads] = 0;
       s.counts[tid] = s.counts[tid + kSliceThreads] = 0;
       const uint32_t width = mode == kKeys ? hi - lo : (uint32_t)(last_id - first_id);
@@ -1100,6 +1118,14 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
     }
     __syncthreads();
     for_candidates<E>(row, r, d, plan, b, n_slices, list, listed, table, s, wanted, roots, [&](uint32_t key, int32_t bin, int32_t id) {
+      if (mode == kKept) {
+        if ((bin <= reach) & kept(key, bin, id)) {  // (kRanked of them at most: so many lie in these bins)
+          const uint32_t at = atomicAdd(&s.flag[0], 1u);
+          s.ranked[at] = (u64)(uint32_t)id << 32 | key;
+          s.bins[at] = (u64)(Power(octaves(value_of(key), d.per), total.E, roots).weight() * 4503599627370496.0);
+        }
+        return;
+      }
       if (mode == kSums) {
         if (bin == edge && kept(key, bin, id)) atomicAdd(&s.slice_more[(uint32_t)(id - row_first) / kSliceTokens], Power(octaves(value_of(key), d.per), total.E, roots).mass());
         return;
@@ -1116,7 +1142,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
       atomicAdd(&s.counts[at], 1u);
       if (mode == kKeys) atomicAdd(&s.bins[at], mass);
     });
-    if (mode == kSums) break;
+    if (mode >= kSums) break;
     __syncthreads();
     if (mode == kRank) {
       const uint32_t n = s.flag[0];
@@ -1214,17 +1240,47 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
     __syncthreads();
   }
   __syncthreads();
-  const double up_to_bin = (double)(divided ? edge : min(edge + 1, kBins));
-  constexpr int kAtOnce = 3;  // slices of a wave whose bins are on their way together
+  if (reach >= 0) {
+    // weights in whole numbers of 2^-52 of the octave, so that the order in which they were collected does not matter
+    const uint32_t n = s.flag[0];
+    if (tid == 0) s.found[0] = -1;
+    __syncthreads();
+    if ((uint32_t)tid < n) {
+      const u64 mine = s.ranked[tid], own = s.bins[tid];
+      u64 before = 0, whole = 0;
+      bool last = true;  // of those with a weight
 #pragma unroll 1
-  for (int32_t begin = wave; begin < n_slices; begin += kAtOnce * kWaves) {
-    u64 x[kAtOnce][kBins / 64];
+      for (uint32_t i = 0; i < n; i += 8) {
 #pragma unroll
-    for (int j = 0; j < kAtOnce; ++j)
+        for (uint32_t k = 0; k < 8; ++k) {
+          const u64 x = s.bins[i + k];
+          const bool front = s.ranked[i + k] < mine;
+          before += front ? x : 0;
+          whole += x;
+          last &= (s.ranked[i + k] <= mine) | (x == 0);
+        }
+      }
+      const u64 rest = (u64)(d.u * (double)whole);
+      if (own != 0 && before <= rest && (rest < before + own || last)) s.found[0] = tid;
+    }
+    __syncthreads();
+    if (tid == 0) {
+      const u64 it = s.found[0] >= 0 ? s.ranked[s.found[0]] : (u64)(uint32_t)total.top_id << 32 | key_of(total.top);
+      write_out(d, total, (int32_t)(it >> 32), value_of((uint32_t)it), roots, ids + b, logprobs ? logprobs + b : nullptr);
+    }
+    return;
+  }
+  const double up_to_bin = (double)(divided ? edge : min(edge + 1, kBins));
+  constexpr int kTogether = 3;  // slices of a wave whose bins are on their way together
+#pragma unroll 1
+  for (int32_t begin = wave; begin < n_slices; begin += kTogether * kWaves) {
+    u64 x[kTogether][kBins / 64];
+#pragma unroll
+    for (int j = 0; j < kTogether; ++j)
 #pragma unroll
       for (int k = 0; k < kBins / 64; ++k) x[j][k] = bins[(size_t)min(begin + j * kWaves, n_slices - 1) * kBins + k * 64 + lane];
 #pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
+    for (int j = 0; j < kTogether; ++j) {
       const int32_t i = begin + j * kWaves;
       if (i >= n_slices) break;
       double sum = 0.0;
@@ -1259,7 +1315,7 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
     }
     return x;
   });
-  if (tid == 0) write_out(d, total, id, logit, ids + b, logprobs ? logprobs + b : nullptr);
+  if (tid == 0) write_out(d, total, id, logit, roots, ids + b, logprobs ? logprobs + b : nullptr);
 }
 
 template <template <Elem> class Launch, class... Args>

@@ -418,6 +418,19 @@ def test_draws_follow_their_probabilities():
     assert np.abs(share - row.w / row.w.sum()).max() <= 1.0 / n
 
 
+@pytest.mark.parametrize("top_p", [None, 0.9])
+@pytest.mark.parametrize("V", [7, 2140, 20000])
+def test_a_token_that_is_alone_has_logprob_0(V, top_p):
+    rows = 24
+    c = Batch(rows, V, "bf16", seed=V, history=331, bias=194, mask="full")
+    only = np.random.default_rng(V).integers(0, V, rows)
+    c.allowed = np.zeros((rows, V), bool)
+    c.allowed[np.arange(rows), only] = True
+    c.upload()
+    ids, lp = _draw(c, np.linspace(0.3, 1.9, rows), top_p=None if top_p is None else [top_p] * rows, uniform=np.linspace(0.0, 0.999, rows))
+    assert ids.tolist() == only.tolist() and (lp == 0).all()
+
+
 def test_top_p_takes_lower_ids_first_among_equal_logits():
     c = Batch(4, 20000, "bf16", seed=0, sigma=0.0)                  # all equal
     n = [1, 2, 9999, 20000]
