@@ -259,7 +259,7 @@ template <Elem E> int32_t slices_of(const Logits& in) {
 // cuts among them (where there are too many for the list it goes through the row again each time), the slice and the token.
 // What workgroups of one kernel hand to each other goes through atomics of the device, which no cache of an XCD holds back.
 // 128 rows x 151936 (top-p, 5 rows of 13 open): 48, 22 and 41 us; instruction issue in 64 bits is 32 of the first's, and the third goes several
-// times through the tokens of bins that hold thousands.  One row: 18, 8 and 18 us, chains of loads, barriers and selections.  48 rows
+// times through the tokens of bins that hold thousands.  One row (top-k, top-p): 18, 8 and 10 us, chains of loads, barriers and selections.  48 rows
 // without a cut: 31 us, of which the last slice of a row is done after 17.
 constexpr int kWaves = kSliceThreads / 64;
 constexpr int kBins = 256, kBinsAnOctave = 4;
