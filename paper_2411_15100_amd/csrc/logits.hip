@@ -416,7 +416,8 @@ __device__ __forceinline__ double wave_sum(double x) {
   return x;
 }
 
-// The logits of a slice under the rules.
+// The logits of a slice under the rules, whose table may lie where other things of the workgroup lie: with rules it is called
+// only when all threads have read what they need of those, behind a barrier.
 template <Elem E>
 __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& r, int32_t b, int32_t first, RuleTable& table, Tokens& y) {
   const bool ruled = has_rules(r);
@@ -602,8 +603,13 @@ __device__ RowTotal row_total(const Slot* slots, int32_t n, Shared& s) {
   __syncthreads();
   return r;
 }
-// Which slice the random number falls into and what is left of it there: s.slice, s.rest.
-__device__ void find_slice(double u, int32_t n, Shared& s) {
+// Which slice the random number falls into and what is left of it there.  All threads have read it from `s` when it returns (a last
+// barrier sees to that): the tables of the rules may go over it.
+struct Place {
+  int32_t slice;
+  double rest;
+};
+__device__ Place find_slice(double u, int32_t n, Shared& s) {
   constexpr int kEach = (kMostSlices + 63) / 64;  // neighbours a lane
   const int32_t lane = (int32_t)threadIdx.x;
   if (lane < 64) {
@@ -639,6 +645,9 @@ __device__ void find_slice(double u, int32_t n, Shared& s) {
     }
   }
   __syncthreads();
+  const Place place{s.slice, s.rest};
+  __syncthreads();
+  return place;
 }
 // (the sum is taken relative to the weight of the likeliest token as it went into the sum: a token that is alone has logprob 0)
 __device__ __forceinline__ void write_out(const RowDraw& d, const RowTotal& r, int32_t id, float y, const double* roots, int32_t* to_id, float* to_logprob) {
@@ -810,11 +819,10 @@ __global__ __launch_bounds__(kSliceThreads, 8) void draw_slices_kernel(Logits in
     int32_t id = empty ? -1 : total.top_id;
     float logit = total.top;
     if (!empty && !d.greedy) {
-      find_slice(d.u, n_slices, s);
-      const double rest = s.rest;
-      first = row.first_token(s.slice);
+      const Place place = find_slice(d.u, n_slices, s);
+      first = row.first_token(place.slice);
       load_slice<E>(row, r, b, first, table, y);
-      id = find_token(y, first, rest, &logit, s, [&](float v, int32_t) { return v > -__builtin_inff() ? Power(octaves(v, d.per), total.E, roots).weight() : 0.0; });
+      id = find_token(y, first, place.rest, &logit, s, [&](float v, int32_t) { return v > -__builtin_inff() ? Power(octaves(v, d.per), total.E, roots).weight() : 0.0; });
     }
     if (tid == 0) {
       write_out(d, total, id, logit, roots, ids + b, logprobs ? logprobs + b : nullptr);
@@ -1297,15 +1305,13 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
     }
   }
   __syncthreads();
-  find_slice(d.u, n_slices, s);
-  const double rest = s.rest;
-  const int32_t first = row.first_token(s.slice);
-  __syncthreads();
+  const Place place = find_slice(d.u, n_slices, s);
+  const int32_t first = row.first_token(place.slice);
   load_slice<E>(row, r, b, first, table, y);
   float logit = 0.0f;
   // of what is kept, all of which is above -inf
   const uint32_t least_key = max(max(max(min_key, cut.key), keys_of_bins(edge, min(edge, kBins - 1), total.E, d.per).lo), key_of(-FLT_MAX));
-  const int32_t id = find_token(y, first, rest, &logit, s, [&](float v, int32_t token) {
+  const int32_t id = find_token(y, first, place.rest, &logit, s, [&](float v, int32_t token) {
     const uint32_t key = key_of(v);
     double x = 0.0;
     if (key >= least_key) {

@@ -442,6 +442,26 @@ def test_top_p_takes_lower_ids_first_among_equal_logits():
     assert ids.tolist() == [k - 1 for k in n]
 
 
+@pytest.mark.parametrize("rows,V,history,bias", [(128, 151936, 1500, 40), (48, 70001, 0, 3), (300, 9000, 200, 0), (2, 1000003, 3000, 9)])
+def test_draws_without_a_cut_under_rules_are_those_from_logits_that_went_through_the_rules_before(rows, V, history, bias):
+    xgm = _xgm()
+    c = Batch(rows, V, "f32", seed=V, history=history, bias=bias, mask="full")
+    done = torch.empty((rows, V), device="cuda")
+    xgm.process_logits(c.address(), 0, rows, V, c.stride, c.rules, done.data_ptr(), V, _stream())
+    ids, lp = torch.empty((2, rows), dtype=torch.int32, device="cuda"), torch.empty((2, rows), device="cuda")
+    temperature, sampler = torch.linspace(0.5, 1.6, rows, device="cuda"), xgm.Sampler(rows, V, _stream())
+    seen = set()
+    for turn in range(30):
+        u = torch.rand(rows, dtype=torch.float64, generator=torch.Generator().manual_seed(turn)).cuda()
+        draw = xgm.DrawRules(d_temperature=temperature.data_ptr(), d_uniform=u.data_ptr())
+        for k, (at, stride, rules) in enumerate([(c.address(), c.stride, c.rules), (done.data_ptr(), V, None)]):
+            sampler.sample(at, 0, rows, V, stride, rules, draw, ids[k].data_ptr(), lp[k].data_ptr(), _stream())
+        torch.cuda.synchronize()
+        assert torch.equal(ids[0], ids[1]) and torch.equal(lp[0], lp[1]), turn
+        seen |= set((ids[0] // 8192).tolist())
+    assert len(seen - {-1}) > 1                                     # (more than one slice was drawn from)
+
+
 # ------------------------------------------------------------------------------------------------ streams and graphs
 def test_the_chain_replays_from_a_graph_and_runs_on_another_stream():
     xgm = _xgm()
