@@ -509,8 +509,8 @@ int xgm_apply_token_bitmask_inplace(void* d_logits, xgm_dtype dt, int32_t B, int
  * whatever its value, so rows of the matrix that no request may take are not
  * read):
  *   logits[b][v] = sum over k of hidden[b][k] * (code(v, k) - zero(v, k / group)) * scale(v, k / group),
- * summed in 32 bits and rounded once; -inf where bit (b, v) of d_bitmask is 0
- * (NULL: no mask).  Codes are multiplied with 16 added to them and the sum taken
+ * summed in 32 bits and rounded once; -inf where bit (b, v) of d_bitmask
+ * ([B, xgm_bitmask_words(V)]; NULL: no mask) is 0.  Codes are multiplied with 16 added to them and the sum taken
  * off: a hidden state that is not finite, or beyond 2^122 (bf16), makes the
  * allowed logits of its row inf or NaN, and the others' stay as they are.
  * d_hidden: [B, K] of hidden_dt (XGM_BF16 or XGM_F16), row stride
@@ -524,6 +524,13 @@ int xgm_q4_logits(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32_t 
                   const uint8_t* d_codes, const void* d_scales, const uint8_t* d_zeros, int32_t V, int32_t group,
                   void* d_logits, xgm_dtype logits_dt, int64_t logits_stride_elems, const int32_t* d_bitmask,
                   void* hip_stream);
+/* The same with masks of another vocabulary than the matrix has rows: d_bitmask is [B, xgm_bitmask_words(v_mask)],
+ * and logits are -inf from v_mask on (a matrix that is padded behind the tokens).  A matrix with the rows from
+ * 32 i on of a larger one takes d_bitmask + i and the larger one's v_mask. */
+int xgm_q4_logits_ex(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32_t K, int64_t hidden_stride_elems,
+                     const uint8_t* d_codes, const void* d_scales, const uint8_t* d_zeros, int32_t V, int32_t group,
+                     void* d_logits, xgm_dtype logits_dt, int64_t logits_stride_elems, const int32_t* d_bitmask,
+                     int32_t v_mask, void* hip_stream);
 
 /* Rules on the logits of a batch.  The struct is host memory, read during the
  * call; what it points to is device memory with a value or a row for each row

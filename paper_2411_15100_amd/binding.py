@@ -108,6 +108,7 @@ SIGNATURES = {
     "xgm_overflow_total": (_i64, []),
     "xgm_apply_token_bitmask_inplace": (_i32, [_vp, _i32, _i32, _i32, _i64, _vp, _i32, _vp, _i32, _vp]),
     "xgm_q4_logits": (_i32, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _i64, _vp, _vp]),
+    "xgm_q4_logits_ex": (_i32, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _i32, _i32, _vp, _i32, _i64, _vp, _i32, _vp]),
     "xgm_process_logits": (_i32, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _i64, _vp]),
     "xgm_sampler_create": (_i32, [_i32, _i32, _vp, _pp]),
     "xgm_sampler_destroy": (None, [_vp]),
@@ -532,9 +533,10 @@ def apply_token_bitmask_inplace(d_logits: int, dtype: int, B: int, V_logits: int
 
 
 def q4_logits(d_hidden: int, dtype: int, rows: int, k: int, hidden_stride: int, d_codes: int, d_scales: int, d_zeros: int, v: int, group: int,
-              d_logits: int, logits_dtype: int, row_stride: int, d_bitmask: int = 0, stream: int = 0):
-    """Logits from hidden states and a 4-bit matrix, under the masks (xgm_q4_logits)."""
-    _fast.q4_logits(d_hidden, dtype, rows, k, hidden_stride, d_codes, d_scales, d_zeros, v, group, d_logits, logits_dtype, row_stride, d_bitmask, stream)
+              d_logits: int, logits_dtype: int, row_stride: int, d_bitmask: int = 0, stream: int = 0, v_mask: int = None):
+    """Logits from hidden states and a 4-bit matrix, under the masks (xgm_q4_logits_ex); v_mask: the masks' vocabulary, v if not given."""
+    _fast.q4_logits(d_hidden, dtype, rows, k, hidden_stride, d_codes, d_scales, d_zeros, v, group, d_logits, logits_dtype, row_stride, d_bitmask,
+                    v if v_mask is None else v_mask, stream)
 
 
 class _Struct:

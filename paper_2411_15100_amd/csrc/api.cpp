@@ -2309,6 +2309,12 @@ extern "C" {
 int xgm_q4_logits(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32_t K, int64_t hidden_stride_elems, const uint8_t* d_codes,
                   const void* d_scales, const uint8_t* d_zeros, int32_t V, int32_t group, void* d_logits, xgm_dtype logits_dt,
                   int64_t logits_stride_elems, const int32_t* d_bitmask, void* hip_stream) {
+  return xgm_q4_logits_ex(d_hidden, hidden_dt, B, K, hidden_stride_elems, d_codes, d_scales, d_zeros, V, group, d_logits, logits_dt, logits_stride_elems,
+                          d_bitmask, V, hip_stream);
+}
+int xgm_q4_logits_ex(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32_t K, int64_t hidden_stride_elems, const uint8_t* d_codes,
+                     const void* d_scales, const uint8_t* d_zeros, int32_t V, int32_t group, void* d_logits, xgm_dtype logits_dt,
+                     int64_t logits_stride_elems, const int32_t* d_bitmask, int32_t v_mask, void* hip_stream) {
   API_BEGIN
   if (!d_hidden || !d_codes || !d_scales) return fail(XGM_ERR_BAD_ARG, "q4_logits: null hidden states, codes or scales");
   Elem hidden, logits;
@@ -2322,9 +2328,10 @@ int xgm_q4_logits(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32_t 
   if (!aligned(d_hidden, 16) || hidden_stride_elems % 8 != 0 || !aligned(d_codes, 16))
     return fail(XGM_ERR_BAD_ARG, "q4_logits: hidden rows and codes must be 16-byte aligned");
   if (!aligned(d_scales, hidden_size)) return fail(XGM_ERR_BAD_ARG, "q4_logits: scales are not aligned to their element size");
+  if (d_bitmask && v_mask <= 0) return fail(XGM_ERR_BAD_ARG, "q4_logits: a bitmask without v_mask");
   require_device();
   Head h{d_hidden, hidden_stride_elems, d_codes, d_scales, d_zeros, d_logits, logits_stride_elems, reinterpret_cast<const uint32_t*>(d_bitmask),
-         B, K, V, group, xgm_bitmask_words(V)};
+         B, K, V, group, xgm_bitmask_words(v_mask), v_mask};
   launch_q4_logits(h, hidden, logits, static_cast<hipStream_t>(hip_stream));
   HIP_OK(hipGetLastError());
   return XGM_OK;

@@ -126,7 +126,8 @@ __device__ int32_t list_rows(const Head& h, Elem out_type, int32_t first_b, int3
   const int32_t w0 = (int32_t)(base >> 5), shift = (int32_t)(base & 31), words = (here + shift + 31) / 32;
   for (int32_t i = tid; i < words * rows; i += threads) {
     const int32_t b = i / words, w = i % words;
-    const uint32_t m = h.mask[(size_t)(first_b + b) * h.W_mask + w0 + w];
+    uint32_t m = w0 + w < h.W_mask ? h.mask[(size_t)(first_b + b) * h.W_mask + w0 + w] : 0u;
+    if (w0 + w == h.V_mask >> 5) m &= (1u << (h.V_mask & 31)) - 1u;  // (what lies behind the masks' vocabulary is not listed)
     if (m && shift) {
       if (w > 0) atomicOr(&any[w - 1], m << 16);
       if (w < kFewRows / 32) atomicOr(&any[w], m >> 16);

@@ -41,7 +41,7 @@ struct Head {
   void* logits;
   int64_t logits_stride;
   const uint32_t* mask;  // null: everything is allowed
-  int32_t B, K, V, group, W_mask;
+  int32_t B, K, V, group, W_mask, V_mask;
 };
 void launch_q4_logits(const Head& h, Elem hidden_type, Elem logits_type, hipStream_t stream);
 

@@ -28,7 +28,7 @@ struct {
   int (*batch_fork)(void*, const void*, void*);
   int (*batch_fill_next_token_bitmask)(void*, void*, void*);
   int (*batch_fill_and_apply)(void*, void*, void*, int, int32_t, int64_t, void*);
-  int (*q4_logits)(const void*, int, int32_t, int32_t, int64_t, const void*, const void*, const void*, int32_t, int32_t, void*, int, int64_t, const void*, void*);
+  int (*q4_logits_ex)(const void*, int, int32_t, int32_t, int64_t, const void*, const void*, const void*, int32_t, int32_t, void*, int, int64_t, const void*, int32_t, void*);
   int (*process_logits)(const void*, int, int32_t, int32_t, int64_t, const void*, void*, int64_t, void*);
   int (*sample)(void*, const void*, int, int32_t, int32_t, int64_t, const void*, const void*, void*, void*, void*);
 } api;
@@ -46,7 +46,7 @@ struct { const char* name; void** slot; } const kEntries[] = {
     {"xgm_batch_fork", (void**)&api.batch_fork},
     {"xgm_batch_fill_next_token_bitmask", (void**)&api.batch_fill_next_token_bitmask},
     {"xgm_batch_fill_and_apply", (void**)&api.batch_fill_and_apply},
-    {"xgm_q4_logits", (void**)&api.q4_logits},
+    {"xgm_q4_logits_ex", (void**)&api.q4_logits_ex},
     {"xgm_process_logits", (void**)&api.process_logits},
     {"xgm_sample", (void**)&api.sample},
 };
@@ -285,15 +285,15 @@ PyObject* apply(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return result(rc);
 }
 
-// q4_logits(d_hidden, dtype, rows, k, hidden_stride, d_codes, d_scales, d_zeros, v, group, d_logits, logits_dtype, row_stride, d_bitmask, stream)
+// q4_logits(d_hidden, dtype, rows, k, hidden_stride, d_codes, d_scales, d_zeros, v, group, d_logits, logits_dtype, row_stride, d_bitmask, v_mask, stream)
 PyObject* q4_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 15) return PyErr_Format(PyExc_TypeError, "q4_logits takes 15 arguments");
-  int64_t v[15];
-  if (!values(args, v, "aiiiiaaaiiaiiaa")) return nullptr;
+  if (n != 16) return PyErr_Format(PyExc_TypeError, "q4_logits takes 16 arguments");
+  int64_t v[16];
+  if (!values(args, v, "aiiiiaaaiiaiiaia")) return nullptr;
   int rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = api.q4_logits(pointer(v[0]), (int)v[1], (int32_t)v[2], (int32_t)v[3], v[4], pointer(v[5]), pointer(v[6]), pointer(v[7]), (int32_t)v[8], (int32_t)v[9],
-                     pointer(v[10]), (int)v[11], v[12], pointer(v[13]), pointer(v[14]));
+  rc = api.q4_logits_ex(pointer(v[0]), (int)v[1], (int32_t)v[2], (int32_t)v[3], v[4], pointer(v[5]), pointer(v[6]), pointer(v[7]), (int32_t)v[8], (int32_t)v[9],
+                        pointer(v[10]), (int)v[11], v[12], pointer(v[13]), (int32_t)v[14], pointer(v[15]));
   Py_END_ALLOW_THREADS
   return result(rc);
 }

@@ -122,6 +122,28 @@ def test_projection_under_masks(B, K, V, group):
         assert np.array_equal(got, np.where(allowed, want, -np.inf)), kind
 
 
+@pytest.mark.parametrize("B,K,V,group", [(1, 256, 1000, 128), (5, 128, 2049, 32), (20, 512, 2050, 64), (70, 384, 777, 32), (130, 256, 600, 128)])
+def test_projection_under_masks_of_another_vocabulary(B, K, V, group):
+    """A matrix that is padded behind the masks' tokens, and one that is a part of a larger one."""
+    xgm = _xgm()
+    rng = np.random.default_rng(V)
+    p = Projection(B, K, V, group, "bf16", whole=True, seed=4)
+    want, _ = p.want()
+    for v_mask, first in ((V - 1, 0), (V - 33, 0), (V - V // 3, 0), (1, 0), (V + 95, 0), (V + 3000, 0), (V + 3000, 64), (V + 640, 640)):
+        allowed = rng.random((B, v_mask)) < rng.choice([0.002, 0.5, 0.97], (B, 1))
+        words = plain.pack(allowed)
+        if v_mask % 32:
+            words[:, -1] |= np.int32(-1 << v_mask % 32)         # bits behind the vocabulary say nothing
+        d_mask = _dev(words)
+        out = torch.full((B, V + 3), 7.0, device="cuda")
+        xgm.q4_logits(p.hidden.data_ptr(), 1, B, K, K, p.codes.data_ptr(), p.scales.data_ptr(), 0, V, group, out.data_ptr(), 0, V + 3,
+                      d_mask.data_ptr() + first // 32 * 4, _stream(), v_mask=v_mask)
+        got = _np(out)
+        here = np.zeros((B, V), bool)
+        here[:, :v_mask - first] = allowed[:, first:first + V]
+        assert np.array_equal(got[:, :V], np.where(here, want, -np.inf)) and (got[:, V:] == 7).all(), (v_mask, first)
+
+
 def test_projection_of_what_is_not_finite():
     p = Projection(3, 256, 200, 32, "bf16", whole=True)
     p.hidden[1, 100] = float("inf")

@@ -27,6 +27,13 @@ def test_projection_refuses(change, status, text):
     assert e.value.status == status and "q4_logits" in str(e.value)
 
 
+@pytest.mark.parametrize("v_mask", [0, -5])
+def test_projection_refuses_masks_of_no_vocabulary(v_mask):
+    with pytest.raises(xgm.XgmError, match="v_mask") as e:
+        xgm.q4_logits(**PROJECT, d_bitmask=A, v_mask=v_mask)
+    assert e.value.status == -1
+
+
 PROCESS = dict(d_logits=A, dtype=1, rows=2, v=100, row_stride=100, rules=None, d_out=2 * A, out_stride=100)
 BAD_RULES = [(dict(d_bitmask=A), "v_mask"), (dict(d_tokens=A, d_n_tokens=A), "stride"), (dict(d_tokens=A, token_stride=8), "lengths"),
              (dict(d_tokens=A, d_n_tokens=A, token_stride=1 << 20), "XGM_MAX_HISTORY"), (dict(d_repetition=A), "history"), (dict(d_presence=A), "history"),
