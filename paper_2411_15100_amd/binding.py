@@ -164,7 +164,8 @@ def load_library():
         from . import _native
     except ImportError as e:
         raise ImportError("the extension _native is missing for this Python: build it with `python -m paper_2411_15100_amd.build`") from e
-    _native.install({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in SIGNATURES}, XgmError, Matcher, DeviceBatch)
+    _native.install({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in SIGNATURES}, XgmError, Matcher, DeviceBatch,
+                    LogitRules, DrawRules)
     _fast = _native
     _lib = lib
     _handles["lib"] = lib

@@ -51,6 +51,7 @@ struct { const char* name; void** slot; } const kEntries[] = {
     {"xgm_sample", (void**)&api.sample},
 };
 PyObject* g_error_class = nullptr;  // XgmError(status, message)
+PyObject *g_logit_rules = nullptr, *g_draw_rules = nullptr;
 PyObject *s_h, *s_addr, *s_matchers;
 
 PyObject* result(int rc) {
@@ -297,14 +298,17 @@ PyObject* q4_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_END_ALLOW_THREADS
   return result(rc);
 }
-// rules: an object with the address of its struct, or None; a reference to it is held for the call
+// an object of `type` with the address of its struct, or None; a reference to it is held for the call
 class Rules {
  public:
-  bool get(PyObject* o) {
+  bool get(PyObject* o, PyObject* type) {
     if (!o || o == Py_None) return true;
     Py_INCREF(o);
     kept_ = o;
-    return attribute(o, s_addr, &at_);
+    if (!attribute(o, s_addr, &at_)) return false;
+    const int is = PyObject_IsInstance(o, type);  // (the structs differ in size and meaning: one for the other would be read beyond its end)
+    if (is == 0) PyErr_Format(PyExc_TypeError, "%s where %s is expected", Py_TYPE(o)->tp_name, reinterpret_cast<PyTypeObject*>(type)->tp_name);
+    return is > 0;
   }
   ~Rules() { Py_XDECREF(kept_); }
   void* at() const { return at_; }
@@ -318,7 +322,7 @@ PyObject* process_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 9) return PyErr_Format(PyExc_TypeError, "process_logits takes 9 arguments");
   int64_t v[5], o[3];
   Rules r;
-  if (!values(args, v, "aiiii") || !r.get(args[5]) || !values(args + 6, o, "aia")) return nullptr;
+  if (!values(args, v, "aiiii") || !r.get(args[5], g_logit_rules) || !values(args + 6, o, "aia")) return nullptr;
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = api.process_logits(pointer(v[0]), (int)v[1], (int32_t)v[2], (int32_t)v[3], v[4], r.at(), pointer(o[0]), o[1], pointer(o[2]));
@@ -331,7 +335,7 @@ PyObject* sample(PyObject*, PyObject* const* args, Py_ssize_t n) {
   int64_t v[5], o[3];
   Rules r, d;
   void* h;
-  if (!attribute(args[0], s_h, &h) || !values(args + 1, v, "aiiii") || !r.get(args[6]) || !d.get(args[7]) || !values(args + 8, o, "aaa")) return nullptr;
+  if (!attribute(args[0], s_h, &h) || !values(args + 1, v, "aiiii") || !r.get(args[6], g_logit_rules) || !d.get(args[7], g_draw_rules) || !values(args + 8, o, "aaa")) return nullptr;
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = api.sample(h, pointer(v[0]), (int)v[1], (int32_t)v[2], (int32_t)v[3], v[4], r.at(), d.at(), pointer(o[0]), pointer(o[1]), pointer(o[2]));
@@ -364,10 +368,12 @@ bool put_methods(PyObject* cls, PyMethodDef (&defs)[N]) {
   }
   return true;
 }
-// install(addresses, XgmError, Matcher, DeviceBatch): addresses[name] = address of the entry point
+// install(addresses, XgmError, Matcher, DeviceBatch, LogitRules, DrawRules): addresses[name] = address of the entry point
 PyObject* install(PyObject*, PyObject* args) {
-  PyObject *addresses, *error, *matcher, *batch;
-  if (!PyArg_ParseTuple(args, "O!OO!O!", &PyDict_Type, &addresses, &error, &PyType_Type, &matcher, &PyType_Type, &batch)) return nullptr;
+  PyObject *addresses, *error, *matcher, *batch, *logit_rules, *draw_rules;
+  if (!PyArg_ParseTuple(args, "O!OO!O!O!O!", &PyDict_Type, &addresses, &error, &PyType_Type, &matcher, &PyType_Type, &batch, &PyType_Type, &logit_rules,
+                        &PyType_Type, &draw_rules))
+    return nullptr;
   for (auto& e : kEntries) {
     PyObject* a = PyDict_GetItemString(addresses, e.name);
     if (!a) return PyErr_Format(PyExc_KeyError, "no address of %s", e.name);
@@ -375,6 +381,10 @@ PyObject* install(PyObject*, PyObject* args) {
   }
   Py_INCREF(error);
   Py_XSETREF(g_error_class, error);
+  Py_INCREF(logit_rules);
+  Py_XSETREF(g_logit_rules, logit_rules);
+  Py_INCREF(draw_rules);
+  Py_XSETREF(g_draw_rules, draw_rules);
   if (!put_methods(matcher, kMatcherMethods) || !put_methods(batch, kBatchMethods)) return nullptr;
   Py_RETURN_NONE;
 }

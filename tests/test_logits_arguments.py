@@ -69,6 +69,25 @@ def test_unknown_names_and_what_is_no_struct():
         xgm.process_logits(**{**PROCESS, "rows": "2"})
 
 
+def test_one_struct_is_not_taken_for_the_other():
+    class AnotherSampler:
+        _h = 0
+
+    sampler, rules, draw = AnotherSampler(), xgm.LogitRules(), xgm.DrawRules(d_uniform=A)
+    for a, b, found, expected in ((draw, rules, "DrawRules", "LogitRules"), (draw, None, "DrawRules", "LogitRules"), (rules, rules, "LogitRules", "DrawRules"),
+                                  (None, rules, "LogitRules", "DrawRules"), (rules, AnotherStruct(), "AnotherStruct", "DrawRules")):
+        with pytest.raises(TypeError, match=f"{found} where .*{expected}"):
+            xgm.Sampler.sample(sampler, A, 1, 2, 100, 100, a, b, A)
+    with pytest.raises(TypeError, match="DrawRules where .*LogitRules"):
+        xgm.process_logits(**{**PROCESS, "rules": draw})
+    with pytest.raises(xgm.XgmError, match="null sampler"):         # in the right order they get as far as that
+        xgm.Sampler.sample(sampler, A, 1, 2, 100, 100, rules, draw, A)
+
+
+class AnotherStruct:
+    _addr = A
+
+
 def test_samplers_refuse():
     for rows, v, status in ((0, 10, -1), (4, 0, -1), (-1, 10, -1), (65536, 10, -9), (4, (1 << 20) + 1, -9)):
         with pytest.raises(xgm.XgmError, match="sampler_create") as e:
