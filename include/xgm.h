@@ -77,6 +77,7 @@ enum {
   XGM_BATCH_MAX_DEPTH = 128, /* frames per stack in an xgm_batch */
   XGM_BATCH_MAX_ROWS = 1024, /* rows of an xgm_batch */
   XGM_MAX_ROWS = 65535,      /* rows of a call below */
+  XGM_MAX_COLUMNS = 0x7fff0000, /* its logits a row, and the tokens of its masks (v_mask) */
   XGM_MAX_LOGITS = 1 << 20,  /* logits a row of an xgm_sampler (padding included) */
   XGM_MAX_HIDDEN = 1 << 16,  /* columns of xgm_q4_logits */
   XGM_MAX_HISTORY = 1 << 20  /* tokens of a history, and one more (xgm_logit_rules.token_stride is less) */

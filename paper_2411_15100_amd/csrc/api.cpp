@@ -2268,6 +2268,7 @@ const char* logits_fault(const void* d_logits, int size, int32_t B, int32_t V, i
   if (!d_logits) return "null logits";
   if (B <= 0 || V <= 0) return "sizes must be positive";
   if (B > XGM_MAX_ROWS) return "more than XGM_MAX_ROWS rows";
+  if (V > XGM_MAX_COLUMNS) return "more than XGM_MAX_COLUMNS logits a row";  // (places of a row and a slice behind it fit 32 bits)
   if (stride < V) return "row stride smaller than the row";
   if (!aligned(d_logits, size)) return "logits pointer is not aligned to its element size";
   return nullptr;
@@ -2278,6 +2279,7 @@ const char* rules_fault(const xgm_logit_rules* r, LogitRules* out) {
   if (!r) return nullptr;
   if (r->d_bitmask) {
     if (r->v_mask <= 0) return "a bitmask without v_mask";
+    if (r->v_mask > XGM_MAX_COLUMNS) return "v_mask is more than XGM_MAX_COLUMNS";
     out->mask = reinterpret_cast<const uint32_t*>(r->d_bitmask);
     out->W_mask = xgm_bitmask_words(r->v_mask);
     out->V_mask = r->v_mask;
@@ -2329,6 +2331,7 @@ int xgm_q4_logits_ex(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32
     return fail(XGM_ERR_BAD_ARG, "q4_logits: hidden rows and codes must be 16-byte aligned");
   if (!aligned(d_scales, hidden_size)) return fail(XGM_ERR_BAD_ARG, "q4_logits: scales are not aligned to their element size");
   if (d_bitmask && v_mask <= 0) return fail(XGM_ERR_BAD_ARG, "q4_logits: a bitmask without v_mask");
+  if (d_bitmask && v_mask > XGM_MAX_COLUMNS) return fail(XGM_ERR_BAD_ARG, "q4_logits: v_mask is more than XGM_MAX_COLUMNS");
   require_device();
   Head h{d_hidden, hidden_stride_elems, d_codes, d_scales, d_zeros, d_logits, logits_stride_elems, reinterpret_cast<const uint32_t*>(d_bitmask),
          B, K, V, group, xgm_bitmask_words(v_mask), v_mask};

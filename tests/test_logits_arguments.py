@@ -69,6 +69,18 @@ def test_unknown_names_and_what_is_no_struct():
         xgm.process_logits(**{**PROCESS, "rows": "2"})
 
 
+MOST = 0x7fff0000    # logits a row
+
+
+@pytest.mark.parametrize("v", [MOST + 1, 2 ** 31 - 8, 2 ** 31 - 1])
+def test_rows_whose_places_do_not_fit_32_bits_are_refused(v):
+    for call in (lambda: xgm.process_logits(**{**PROCESS, "v": v, "row_stride": v, "out_stride": v}), lambda: xgm.q4_logits(**{**PROJECT, "v": v, "row_stride": v}),
+                 lambda: xgm.process_logits(**{**PROCESS, "rules": xgm.LogitRules(d_bitmask=A, v_mask=v)}), lambda: xgm.q4_logits(**PROJECT, d_bitmask=A, v_mask=v)):
+        with pytest.raises(xgm.XgmError, match="XGM_MAX_COLUMNS") as e:
+            call()
+        assert e.value.status == -1
+
+
 def test_one_struct_is_not_taken_for_the_other():
     class AnotherSampler:
         _h = 0
