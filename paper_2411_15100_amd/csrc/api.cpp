@@ -2335,8 +2335,7 @@ int xgm_q4_logits_ex(const void* d_hidden, xgm_dtype hidden_dt, int32_t B, int32
   require_device();
   Head h{d_hidden, hidden_stride_elems, d_codes, d_scales, d_zeros, d_logits, logits_stride_elems, reinterpret_cast<const uint32_t*>(d_bitmask),
          B, K, V, group, xgm_bitmask_words(v_mask), v_mask};
-  launch_q4_logits(h, hidden, logits, static_cast<hipStream_t>(hip_stream));
-  HIP_OK(hipGetLastError());
+  hip_check(launch_q4_logits(h, hidden, logits, static_cast<hipStream_t>(hip_stream)), "q4_logits");
   return XGM_OK;
   API_END
 }
@@ -2354,8 +2353,8 @@ int xgm_process_logits(const void* d_logits, xgm_dtype dt, int32_t B, int32_t V,
   if (!what) what = rules_fault(rules, &r);
   if (what) return fail(XGM_ERR_BAD_ARG, std::string("process_logits: ") + what);
   require_device();
-  launch_process_logits(Logits{d_logits, row_stride_elems, V}, type, B, r, d_out, out_stride_elems, static_cast<hipStream_t>(hip_stream));
-  HIP_OK(hipGetLastError());
+  hip_check(launch_process_logits(Logits{d_logits, row_stride_elems, V}, type, B, r, d_out, out_stride_elems, static_cast<hipStream_t>(hip_stream)),
+            "process_logits");
   return XGM_OK;
   API_END
 }
@@ -2401,8 +2400,8 @@ int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, in
   if (B > s->max_rows || V > s->V) return fail(XGM_ERR_BAD_ARG, "sample: more rows or logits than the sampler was created for");
   require_device();
   const DrawRules d = draw ? DrawRules{draw->d_temperature, draw->d_top_k, draw->d_top_p, draw->d_min_p, draw->d_uniform} : DrawRules{};
-  launch_sample(Logits{d_logits, row_stride_elems, V}, type, B, r, d, s->memory, s->max_rows, s->V, d_ids, d_logprobs, static_cast<hipStream_t>(hip_stream));
-  HIP_OK(hipGetLastError());
+  hip_check(launch_sample(Logits{d_logits, row_stride_elems, V}, type, B, r, d, s->memory, s->max_rows, s->V, d_ids, d_logprobs,
+                          static_cast<hipStream_t>(hip_stream)), "sample");
   return XGM_OK;
   API_END
 }

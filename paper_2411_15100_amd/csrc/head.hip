@@ -579,59 +579,61 @@ __global__ __launch_bounds__(kManyThreads, 2) void q4_many_kernel(Head h, Elem o
 
 constexpr int kComputeUnits = 256;
 
-template <Elem H, int NB, int P, bool Z> void launch_few(const Head& h, Elem out_type, hipStream_t stream) {
-  static const bool prepared = hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_few_kernel<H, NB, P, Z>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kFewMaxLds) == hipSuccess;
-  (void)prepared;
+template <Elem H, int NB, int P, bool Z> hipError_t launch_few(const Head& h, Elem out_type, hipStream_t stream) {
+  static LdsRoom room;
+  if (const hipError_t e = room(reinterpret_cast<const void*>(&q4_few_kernel<H, NB, P, Z>), kFewMaxLds); e != hipSuccess) return e;
   const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), each = (tiles + kComputeUnits - 1) / kComputeUnits, steps = few_steps(h.K);
   int32_t threads = 64;  // waves for its tiles, or for the steps of the few that masks leave
   while (threads < kFewThreads<NB> && threads < 64 * (h.mask && steps > each ? steps : each * (each < 16 ? steps : 1))) threads *= 2;
   const dim3 grid((tiles + each - 1) / each, (h.B + 16 * NB - 1) / (16 * NB));
   hipLaunchKernelGGL((q4_few_kernel<H, NB, P, Z>), grid, dim3(threads), few_layout(h.K, h.B < 16 * NB ? h.B : 16 * NB, P, NB).end, stream, h, out_type, each);
+  return hipGetLastError();
 }
-template <Elem H, int NB, int P> void launch_few_zeros(const Head& h, Elem out_type, hipStream_t stream) {
-  if (h.zeros) launch_few<H, NB, P, true>(h, out_type, stream);
-  else launch_few<H, NB, P, false>(h, out_type, stream);
+template <Elem H, int NB, int P> hipError_t launch_few_zeros(const Head& h, Elem out_type, hipStream_t stream) {
+  if (h.zeros) return launch_few<H, NB, P, true>(h, out_type, stream);
+  return launch_few<H, NB, P, false>(h, out_type, stream);
 }
 int few_parts(int32_t group) { return group % 128 == 0 ? 4 : group == 64 ? 8 : 16; }
 bool few_fits(const Head& h, int32_t rows, int nb) { return few_layout(h.K, rows, few_parts(h.group), nb).end <= kFewMaxLds; }
-template <Elem H, int NB> void launch_few_groups(const Head& h, Elem out_type, hipStream_t stream) {
-  if (h.group % 128 == 0) launch_few_zeros<H, NB, 4>(h, out_type, stream);
-  else if (h.group == 64) launch_few_zeros<H, NB, 8>(h, out_type, stream);
-  else launch_few_zeros<H, NB, 16>(h, out_type, stream);
+template <Elem H, int NB> hipError_t launch_few_groups(const Head& h, Elem out_type, hipStream_t stream) {
+  if (h.group % 128 == 0) return launch_few_zeros<H, NB, 4>(h, out_type, stream);
+  if (h.group == 64) return launch_few_zeros<H, NB, 8>(h, out_type, stream);
+  return launch_few_zeros<H, NB, 16>(h, out_type, stream);
 }
-template <Elem H, int MW, int WM, int S, bool Z> void launch_many(const Head& h, Elem out_type, hipStream_t stream) {
+template <Elem H, int MW, int WM, int S, bool Z> hipError_t launch_many(const Head& h, Elem out_type, hipStream_t stream) {
   const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), each = (tiles + kComputeUnits - 1) / kComputeUnits;
   const dim3 grid((tiles + each - 1) / each, (h.B + 16 * MW * WM - 1) / (16 * MW * WM));
   const uint32_t parts = (uint32_t)(h.group / (128 / kPartsOf<S>));
   hipLaunchKernelGGL((q4_many_kernel<H, MW, WM, S, Z>), grid, dim3(kManyThreads), 0, stream, h, out_type, each, parts > 1 ? (uint32_t)(((1ull << 32) + parts - 1) / parts) : 0u);
+  return hipGetLastError();
 }
-template <Elem H, int MW, int WM, int S> void launch_many_zeros(const Head& h, Elem out_type, hipStream_t stream) {
-  if (h.zeros) launch_many<H, MW, WM, S, true>(h, out_type, stream);
-  else launch_many<H, MW, WM, S, false>(h, out_type, stream);
+template <Elem H, int MW, int WM, int S> hipError_t launch_many_zeros(const Head& h, Elem out_type, hipStream_t stream) {
+  if (h.zeros) return launch_many<H, MW, WM, S, true>(h, out_type, stream);
+  return launch_many<H, MW, WM, S, false>(h, out_type, stream);
 }
-template <Elem H, int MW, int WM> void launch_many_groups(const Head& h, Elem out_type, hipStream_t stream) {
-  if (h.group % 128 == 0) launch_many_zeros<H, MW, WM, kWhole>(h, out_type, stream);
-  else if (h.group == 64 && h.K >= 128) launch_many_zeros<H, MW, WM, kHalves>(h, out_type, stream);
-  else if (h.group == 32 && h.K >= 128) launch_many_zeros<H, MW, WM, kQuarters>(h, out_type, stream);
-  else launch_many_zeros<H, MW, WM, kLookedUp>(h, out_type, stream);
+template <Elem H, int MW, int WM> hipError_t launch_many_groups(const Head& h, Elem out_type, hipStream_t stream) {
+  if (h.group % 128 == 0) return launch_many_zeros<H, MW, WM, kWhole>(h, out_type, stream);
+  if (h.group == 64 && h.K >= 128) return launch_many_zeros<H, MW, WM, kHalves>(h, out_type, stream);
+  if (h.group == 32 && h.K >= 128) return launch_many_zeros<H, MW, WM, kQuarters>(h, out_type, stream);
+  return launch_many_zeros<H, MW, WM, kLookedUp>(h, out_type, stream);
 }
 // Up to 32 rows go through LDS as a whole where they fit: 24 rows of 50001 x 2080 in groups of 32 take 51 us that way and 63 as many
 // rows, 17 of 151936 x 2048 73 and 115.  Where 17 to 32 rows do not fit but 16 do, the matrix is read twice: 24 rows of 50001 x 4096 in
 // groups of 128 57 us, 70 as many rows; 32 of 151936 x 4096 150 and 158; under masks that leave 100 tokens a row 23 and 42.
-template <Elem H> void launch_head(const Head& h, Elem out_type, hipStream_t stream) {
+template <Elem H> hipError_t launch_head(const Head& h, Elem out_type, hipStream_t stream) {
   if (h.B <= 16 && few_fits(h, h.B, 1)) return launch_few_groups<H, 1>(h, out_type, stream);
   if (h.B <= 32 && few_fits(h, h.B, 2)) return launch_few_groups<H, 2>(h, out_type, stream);
   if (h.B <= 32 && few_fits(h, 16, 1)) return launch_few_groups<H, 1>(h, out_type, stream);
   if (h.B <= 32) return launch_many_groups<H, 2, 1>(h, out_type, stream);
   if (h.B <= 64) return launch_many_groups<H, 4, 1>(h, out_type, stream);
-  launch_many_groups<H, 4, 2>(h, out_type, stream);
+  return launch_many_groups<H, 4, 2>(h, out_type, stream);
 }
 
 }  // namespace
 
-void launch_q4_logits(const Head& h, Elem hidden_type, Elem logits_type, hipStream_t stream) {
-  if (hidden_type == Elem::kF16) launch_head<Elem::kF16>(h, logits_type, stream);
-  else launch_head<Elem::kBF16>(h, logits_type, stream);
+hipError_t launch_q4_logits(const Head& h, Elem hidden_type, Elem logits_type, hipStream_t stream) {
+  if (hidden_type == Elem::kF16) return launch_head<Elem::kF16>(h, logits_type, stream);
+  return launch_head<Elem::kBF16>(h, logits_type, stream);
 }
 
 }  // namespace xgm

@@ -1325,39 +1325,39 @@ __global__ __launch_bounds__(kSliceThreads) void draw_cut_kernel(Logits in, Logi
 }
 
 template <template <Elem> class Launch, class... Args>
-void by_type(Elem e, const Args&... args) {
-  if (e == Elem::kF32) Launch<Elem::kF32>::run(args...);
-  else if (e == Elem::kBF16) Launch<Elem::kBF16>::run(args...);
-  else Launch<Elem::kF16>::run(args...);
+hipError_t by_type(Elem e, const Args&... args) {
+  if (e == Elem::kF32) return Launch<Elem::kF32>::run(args...);
+  if (e == Elem::kBF16) return Launch<Elem::kBF16>::run(args...);
+  return Launch<Elem::kF16>::run(args...);
 }
 template <Elem E> struct Process {
-  static void run(const Logits& in, const int32_t& B, const LogitRules& r, void* const& out, const int64_t& out_stride, const hipStream_t& stream) {
+  static hipError_t run(const Logits& in, const int32_t& B, const LogitRules& r, void* const& out, const int64_t& out_stride, const hipStream_t& stream) {
     hipLaunchKernelGGL(process_logits_kernel<E>, dim3(slices_of<E>(in), B), dim3(kSliceThreads), rule_table_bytes(r), stream, in, r,
                        static_cast<typename Type<E>::bits*>(out), out_stride);
+    return hipGetLastError();
   }
 };
-template <class K> void more_lds(K kernel) {
-  (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RuleTable));
-}
 // LDS of a kernel that has no use for its tables any more when it needs the first `bytes` of Shared
 size_t lds_with(const LogitRules& r, size_t bytes) { return bytes < rule_table_bytes(r) ? rule_table_bytes(r) : bytes; }
 template <Elem E> struct Draw {
-  static void run(const Logits& in, const int32_t& B, const LogitRules& r, const DrawRules& d, const DrawMemory& m, int32_t* const& ids, float* const& logprobs,
-                  const hipStream_t& stream) {
-    static const bool prepared = (more_lds(&draw_slices_kernel<E>), more_lds(&draw_list_kernel<E>), more_lds(&draw_cut_kernel<E>), true);
-    (void)prepared;
+  static hipError_t run(const Logits& in, const int32_t& B, const LogitRules& r, const DrawRules& d, const DrawMemory& m, int32_t* const& ids, float* const& logprobs,
+                        const hipStream_t& stream) {
+    // (the only one of the three that takes a table and Shared at once, 70 KB)
+    static LdsRoom room;
+    if (const hipError_t e = room(reinterpret_cast<const void*>(&draw_cut_kernel<E>), sizeof(RuleTable)); e != hipSuccess) return e;
     const int32_t n = slices_of<E>(in);
     hipLaunchKernelGGL(draw_slices_kernel<E>, dim3(n, B), dim3(kSliceThreads), lds_with(r, offsetof(Shared, few)), stream, in, r, d, m, n, ids, logprobs);
-    if (!d.uniform || !(d.top_k || d.top_p || d.min_p)) return;
+    if (!d.uniform || !(d.top_k || d.top_p || d.min_p)) return hipGetLastError();
     hipLaunchKernelGGL(draw_list_kernel<E>, dim3(n, B), dim3(kSliceThreads), lds_with(r, offsetof(Shared, ranked)), stream, in, r, d, m);
     hipLaunchKernelGGL(draw_cut_kernel<E>, dim3(B), dim3(kSliceThreads), rule_table_bytes(r), stream, in, r, d, m, n, ids, logprobs);
+    return hipGetLastError();
   }
 };
 
 }  // namespace
 
-void launch_process_logits(const Logits& in, Elem type, int32_t B, const LogitRules& rules, void* out, int64_t out_stride, hipStream_t stream) {
-  by_type<Process>(type, in, B, rules, out, out_stride, stream);
+hipError_t launch_process_logits(const Logits& in, Elem type, int32_t B, const LogitRules& rules, void* out, int64_t out_stride, hipStream_t stream) {
+  return by_type<Process>(type, in, B, rules, out, out_stride, stream);
 }
 
 size_t sampler_bytes(int32_t max_rows, int32_t V) {
@@ -1366,10 +1366,10 @@ size_t sampler_bytes(int32_t max_rows, int32_t V) {
   return bytes;
 }
 
-void launch_sample(const Logits& in, Elem type, int32_t B, const LogitRules& rules, const DrawRules& draw, void* memory, int32_t max_rows, int32_t max_V, int32_t* ids,
-                   float* logprobs, hipStream_t stream) {
+hipError_t launch_sample(const Logits& in, Elem type, int32_t B, const LogitRules& rules, const DrawRules& draw, void* memory, int32_t max_rows, int32_t max_V,
+                         int32_t* ids, float* logprobs, hipStream_t stream) {
   size_t bytes = 0;
-  by_type<Draw>(type, in, B, rules, draw, memory_at(memory, max_rows, max_V, &bytes), ids, logprobs, stream);
+  return by_type<Draw>(type, in, B, rules, draw, memory_at(memory, max_rows, max_V, &bytes), ids, logprobs, stream);
 }
 
 }  // namespace xgm
