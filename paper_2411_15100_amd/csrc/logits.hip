@@ -283,8 +283,9 @@ __device__ __forceinline__ double octaves(float y, double per) {
   return (double)y * per;
 }
 // 2^t relative to 2^E, E a whole number: sixteenths of an octave come from a table in LDS (its 16 entries lie in different banks), the
-// rest from the series of the exponential function around the middle of a sixteenth, whose six terms leave 1.4e-13 of it.  (The
-// series over a whole octave takes eleven terms and as many instructions again.)
+// rest from the polynomial that meets the exponential function at the seven Chebyshev points of a sixteenth, which leaves less of it than
+// 64 bits hold: with the rounding of t a weight is off by (2 + |y| / temperature) 2^-52 of itself at most.  (A polynomial over a whole octave
+// takes eleven terms and as many instructions again.)
 __constant__ const double kRoots[16] = {1, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916,
                                         1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927,
                                         1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543,
@@ -298,12 +299,13 @@ struct Power {
   __device__ __forceinline__ Power(double t, double E, const double* roots) {
     const double sixteenths = t * 16.0, whole = floor(sixteenths), r = sixteenths - whole;
     i = (int32_t)fmax(whole - E * 16.0, -1e6);
-    double p = 1.2994313288926215e-09;
-    p = fma(p, r, 1.467260724112997e-07);
-    p = fma(p, r, 1.3550831108683642e-05);
-    p = fma(p, r, 0.00093838478405108448);
-    p = fma(p, r, 0.043321698786749421);
-    p = fma(p, r, 0.99999999999985389);
+    double p = 9.382399669764206e-12;
+    p = fma(p, r, 1.2713095335610576e-09);
+    p = fma(p, r, 1.467611928836712e-07);
+    p = fma(p, r, 1.3550807713052586e-05);
+    p = fma(p, r, 0.0009383847928200675);
+    p = fma(p, r, 0.043321698784995886);
+    p = fma(p, r, 1.0);
     number = p * roots[i & 15];
   }
   __device__ __forceinline__ double weight() const { return ldexp(number, i >> 4); }

@@ -440,6 +440,25 @@ def test_draws_follow_their_probabilities():
     assert np.abs(share - row.w / row.w.sum()).max() <= 1.0 / n
 
 
+@pytest.mark.parametrize("sigma", [0.3, 2.0])
+def test_weights_have_the_bits_of_64(sigma):
+    """A random number 1e-14 beside the border between two tokens falls on its side.  A weight is off by at most (2 + |logit|) 2^-52
+    of itself with logits below 12, the border by twice that, and four additions and the product with the number by 2^-53 each: 7e-15."""
+    rows, V = 8192, 4
+    rng = np.random.default_rng(8)
+    c = Batch(rows, V, "f32", sigma=sigma)
+    c.rules = None
+    y = c.logits.cpu().numpy().astype(np.longdouble)
+    assert np.abs(y).max() < 12 and np.finfo(np.longdouble).nmant >= 63
+    run = np.cumsum(np.exp(y - y.max(1, keepdims=True)), 1)
+    border = rng.integers(0, V - 1, rows)
+    upper = rng.random(rows) < 0.5
+    share = run[np.arange(rows), border] / run[:, -1]
+    u = (share * (1 + np.where(upper, 1, -1) * np.longdouble(1e-14))).astype(np.float64)
+    ids, _ = _draw(c, uniform=u)
+    assert (ids == border + upper).all(), int((ids != border + upper).sum())
+
+
 @pytest.mark.parametrize("top_p", [None, 0.9])
 @pytest.mark.parametrize("V", [7, 2140, 20000])
 def test_a_token_that_is_alone_has_logprob_0(V, top_p):
