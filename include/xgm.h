@@ -595,8 +595,13 @@ typedef struct {
  * sum of w over the kept ids up to it exceeds u times the sum over all kept
  * ids, and d_logprobs[b] (may be NULL) its logarithm of w / sum of w over all
  * tokens of the row, kept or not (at temperature 1 where the likeliest is taken).  A row without a logit above -inf (nothing is
- * allowed) gets -1 and -inf.  draw NULL: the likeliest token.  w and its sums are in 64
- * bits, and the same inputs give the same results; a token whose w is below 2^-43 may never be drawn. */
+ * allowed) gets -1 and -inf.  draw NULL: the likeliest token.  The same inputs
+ * give the same results.
+ * What it is exact to: a w is off by (2 + |y| / temperature) 2^-52 of itself at most, and sums of w are in 64 bits.  In a row that is
+ * cut off, sums in whole numbers take the place of some of them, each w to 2^-36 of itself: of those that decide where
+ * top_p ends and, where more than 256 tokens are kept or the batch is large, in which stretch of 8192 ids the token lies.  A
+ * top_p or a random number within 2^-35 of a border may fall on either side of it there, on another one in another
+ * batch; tokens with w below 2^-63 are not kept, and one with w below 2^-52 may never be drawn. */
 int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, int32_t V, int64_t row_stride_elems,
                const xgm_logit_rules* rules, const xgm_draw_rules* draw, int32_t* d_ids, float* d_logprobs,
                void* hip_stream);

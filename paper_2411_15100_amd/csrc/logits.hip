@@ -253,7 +253,8 @@ template <Elem E> int32_t slices_of(const Logits& in) {
 // First kernel, one workgroup per slice: logits are read once, the rules and the octave, the largest logit and the sum of the
 // slice go into the row's memory; where the row is cut off (top-k, top-p, min-p) also its bins: a quarter of an octave each, 64 octaves
 // down, with the number of tokens and the sum of their weights in whole numbers (2^-35 of the bin's octave), which do not depend on
-// the order of the atomics.  The workgroup that finishes last for its row puts the slices together.  Without a cut it then
+// the order of the atomics.  (That is 2^-36 of a weight at most; more bits, and 8192 tokens of them beside their number, would not fit one atomic of
+// 64 bits.)  The workgroup that finishes last for its row puts the slices together.  Without a cut it then
 // knows the slice of the drawn token and goes through that one again; with a cut it knows the few bins in which the cuts lie.
 // Second kernel, for rows with a cut, one workgroup per slice: the tokens of those bins are listed.  Third, one workgroup per row: it finds the
 // cuts among them (where there are too many for the list it goes through the row again each time), the slice and the token.

@@ -459,6 +459,22 @@ def test_weights_have_the_bits_of_64(sigma):
     assert (ids == border + upper).all(), int((ids != border + upper).sum())
 
 
+@pytest.mark.parametrize("V,sigma,top_p,rows", [(20000, 1.0, 0.999, 64), (40000, 2.0, 0.9, 48), (3000, 1.0, 0.06, 256), (3000, 1.0, 0.06, 1500), (16500, 1.0, 0.03, 500)])
+def test_a_cut_row_is_drawn_from_to_2_to_the_minus_35(V, sigma, top_p, rows):
+    """A random number 2^-34 of itself beside a border falls on its side (borders are off by 2^-35): by the sums of the slices, where
+    hundreds of tokens are kept or there are more than 1024 slices, and from a list of the kept ones."""
+    c = Batch(rows, V, "f32", seed=6, sigma=sigma)
+    rng = np.random.default_rng(6)
+    y, u, want = c.want(), np.zeros(rows), []
+    for b in range(rows):
+        row = plain.Row(y[b], 1.0, 0, float(np.float32(top_p)))
+        k, upper = int(rng.integers(0, len(row.kept) - 1)), bool(rng.random() < 0.5)
+        u[b] = row.run[k] / row.run[-1] * (1 + (2.0 ** -34 if upper else -2.0 ** -34))
+        want.append(int(row.kept[k + upper]))
+    ids, _ = _draw(c, top_p=[top_p] * rows, uniform=u)
+    assert ids.tolist() == want
+
+
 @pytest.mark.parametrize("top_p", [None, 0.9])
 @pytest.mark.parametrize("V", [7, 2140, 20000])
 def test_a_token_that_is_alone_has_logprob_0(V, top_p):
