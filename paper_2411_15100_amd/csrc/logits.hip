@@ -733,23 +733,28 @@ __device__ int32_t bin_of_mass(const Shared& s, double mass) {
   }
   return lo;
 }
-// The smallest key whose weight is min_p of the largest or more: the logarithm says about where, the exponential function where.
+// The smallest key whose weight is min_p of the largest or more: the logarithm says about where, the exponential function where.  The
+// first guess is a key or two off, unless the border lies near a logit of 0, where many keys have one weight: steps that
+// double, then halves.
 __device__ uint32_t key_of_min(const RowDraw& d, float top) {
   if (!(d.min_p > 0.0f)) return 0;
   const double t = (double)d.temperature;
-  uint32_t key = key_of((float)fmax((double)top + t * log((double)d.min_p), -(double)FLT_MAX));
+  auto enough = [&](uint32_t key) { return exp(((double)value_of(key) - (double)top) / t) >= (double)d.min_p; };
   const uint32_t most = key_of(top);
-  key = min(key, most);
-  int steps = 0;
+  const uint32_t guess = min(key_of((float)fmax((double)top + t * log((double)d.min_p), -(double)FLT_MAX)), most);
+  const bool down = enough(guess);
+  uint32_t good = down ? guess : most, bad = down ? key_of(-FLT_MAX) - 1 : guess, step = 1;
+  bool doubling = true;
 #pragma unroll 1
-  for (bool up = false; steps < 64; ++steps) {
-    const bool enough = exp(((double)value_of(key) - (double)top) / t) >= (double)d.min_p;
-    if (up && enough) break;
-    if (!up && !enough) up = true;
-    key = up ? min(key + 1, most) : key - 1;
-    if (key == most && up) break;
+  while (good - bad > 1) {
+    const uint32_t width = good - bad, at = !doubling || step >= width ? bad + width / 2 : down ? good - step : bad + step;
+    const bool is = enough(at);
+    if (is) good = at;
+    else bad = at;
+    doubling = doubling && is == down && step < width;
+    step *= 2;
   }
-  return key;
+  return good;
 }
 
 template <Elem E>

@@ -386,6 +386,26 @@ def test_the_likeliest_token_is_taken_without_random_numbers():
     assert ids.tolist() == [-1 if plain.Row(r).empty else int(plain.Row(r).order[0]) for r in y]
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_min_p_whose_border_lies_at_a_logit_of_0(dtype):
+    """Next to 0 thousands of floats have the same weight in 64 bits: those that weigh min_p are kept, all of them."""
+    tiny = [-1e-38, -1e-30, -1e-20, -1e-17, 0.0, 1e-20]
+    rows = [([0.0] + tiny, 1.0, 1.0), ([0.0] + tiny, 0.7, 1.0), ([1.0] + tiny, 1.0 / np.log(4.0), 0.25), ([0.5] + tiny, 0.5 / np.log(2.0), 0.5),
+            ([1e-30, -1.0] + tiny, 1.0, 1.0), ([-1e-25] + tiny[:2], 3.0, 1.0)]
+    c = Batch(len(rows), 64, dtype)
+    c.rules = None
+    x = torch.full((len(rows), 64), -50.0)
+    for b, (v, _, _) in enumerate(rows):
+        x[b, :len(v)] = torch.tensor(v)
+    c.buf[:] = x.reshape(-1).to(c.buf.dtype).cuda()
+    y, t, m = c.logits.float().cpu().numpy(), np.float32([r[1] for r in rows]), np.float32([r[2] for r in rows])
+    plains = [plain.Row(y[b], float(t[b]), 0, 1.0, float(m[b])) for b in range(len(rows))]
+    for k in range(64):
+        u = [(min(k, len(r.kept) - 1) + 0.5) / len(r.kept) if b in (0, 1, 4) else (k + 0.5) / 64 for b, r in enumerate(plains)]
+        ids, _ = _draw(c, t, None, None, m, u)
+        assert ids.tolist() == [r.pick(u[b]) for b, r in enumerate(plains)], k
+
+
 def test_random_numbers_and_settings_at_their_ends():
     c = Batch(8, 5003, "f32", seed=2, sigma=3.0)
     y = c.want()
