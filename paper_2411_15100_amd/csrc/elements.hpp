@@ -24,5 +24,11 @@ template <Elem E> __device__ __forceinline__ typename Type<E>::bits narrowed(flo
   if constexpr (E == Elem::kBF16) return __builtin_bit_cast(uint16_t, (__bf16)f);
   if constexpr (E == Elem::kF16) return __builtin_bit_cast(uint16_t, (_Float16)f);
 }
+// The same from 64 bits: one rounding, not one to 32 bits and another to the type.
+template <Elem E> __device__ __forceinline__ typename Type<E>::bits narrowed(double y) {
+  if constexpr (E == Elem::kF32) return __float_as_uint((float)y);
+  if constexpr (E == Elem::kBF16) return __builtin_bit_cast(uint16_t, (__bf16)y);
+  if constexpr (E == Elem::kF16) return __builtin_bit_cast(uint16_t, (_Float16)y);
+}
 
 }  // namespace xgm

@@ -133,8 +133,8 @@ __device__ __forceinline__ void gather_rules(const LogitRules& r, int32_t b, int
   }
   __syncthreads();
 }
-// What the rules make of a logit: in 64 bits, where neither the product of a factor and a count nor the order of a
-// compiler's contractions can change a bit of the 32 that are kept.
+// What the rules make of a logit: in 64 bits, rounded once where it is kept.  Neither the product of a factor and a count nor the order of a
+// compiler's contractions can change a bit of the 32 or fewer that are.
 struct RowRules {
   double repetition, inverse, frequency, presence;
   const LogitRules& r;
@@ -151,15 +151,14 @@ struct RowRules {
     y = divided && rest == rest ? fma(rest, inverse, near) : near;
     return word & kCount ? y - frequency * (double)(word & kCount) - presence : y;
   }
-  __device__ float biased(float x, uint32_t word, int32_t token) const {
+  __device__ double biased(float x, uint32_t word, int32_t token) const {
     double y = word & (kInPrompt | kCount) ? penalised(x, word) : (double)x;
     const uint32_t entry = word >> kBiasShift & kBiasMask;
     int32_t e = begin + (int32_t)entry - 1;
     if (entry == kBiasMask)
       for (int32_t k = end - 1; k > e; --k)
         if (r.bias_ids[k] == token) { e = k; break; }
-    y += (double)r.bias[e];
-    return (float)y;
+    return y + (double)r.bias[e];
   }
 };
 __device__ __forceinline__ int32_t place_of(int k) { return (k / 8 * kSliceThreads + (int32_t)threadIdx.x) * 8 + k % 8; }
@@ -176,7 +175,7 @@ template <class Get, class Set> __device__ __forceinline__ void apply_rules(cons
     for (int i = 0; i < 8; ++i) {
       if (!w[i] || !(ok[j] >> i & 1u)) continue;
       if (w[i] >> kBiasShift & kBiasMask) with_bias |= 1u << (8 * j + i);
-      else set(8 * j + i, (float)rule.penalised(get(8 * j + i), w[i]));
+      else set(8 * j + i, rule.penalised(get(8 * j + i), w[i]));
     }
   }
 #pragma unroll 1
@@ -186,10 +185,10 @@ template <class Get, class Set> __device__ __forceinline__ void apply_rules(cons
 #pragma unroll
     for (int i = 0; i < kTokens; ++i)
       if (i == k) v = get(i);
-    v = rule.biased(v, table.word[place_of(k)], first + place_of(k));
+    const double y = rule.biased(v, table.word[place_of(k)], first + place_of(k));
 #pragma unroll
     for (int i = 0; i < kTokens; ++i)
-      if (i == k) set(i, v);
+      if (i == k) set(i, y);
   }
 }
 
@@ -220,7 +219,7 @@ __global__ __launch_bounds__(kSliceThreads) void process_logits_kernel(Logits in
   if (ruled) gather_rules(r, b, first, h, table);
   bits* const to = out + (int64_t)b * out_stride;
   if (ruled)
-    apply_rules(table, rule, ok, first, [&](int k) { return widened<E>(x[k / 8][k % 8]); }, [&](int k, float v) { x[k / 8].set(k % 8, narrowed<E>(v)); });
+    apply_rules(table, rule, ok, first, [&](int k) { return widened<E>(x[k / 8][k % 8]); }, [&](int k, double v) { x[k / 8].set(k % 8, narrowed<E>(v)); });
 #pragma unroll
   for (int j = 0; j < kGroups; ++j) {
     const int32_t t = first + place_of(8 * j);
@@ -438,7 +437,7 @@ __device__ __forceinline__ void load_slice(const Row<E>& row, const LogitRules& 
   if (ruled) gather_rules(r, b, first, h, table);
 #pragma unroll
   for (int k = 0; k < kTokens; ++k) y[k] = ok[k / 8] >> (k % 8) & 1u ? widened<E>(x[k / 8][k % 8]) : -__builtin_inff();
-  if (ruled) apply_rules(table, rule, ok, first, [&](int k) { return y[k]; }, [&](int k, float v) { y[k] = v; });
+  if (ruled) apply_rules(table, rule, ok, first, [&](int k) { return y[k]; }, [&](int k, double v) { y[k] = (float)v; });
 #pragma unroll
   for (int k = 0; k < kTokens; ++k) y[k] = drawable(y[k]);
   if (ruled) __syncthreads();  // (other things lie where the tables were)

@@ -284,6 +284,35 @@ def test_a_history_in_the_last_columns_of_a_wider_array():
     assert torch.equal(out.cpu().view(torch.int32), want.view(torch.int32))
 
 
+@pytest.mark.parametrize("rule", ["bias", "presence"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_rules_round_once(dtype, rule):
+    """Sums that lie so close beside the middle of two neighbours of the type that 32 bits take them for the middle go to the nearer
+    neighbour, not to the even one."""
+    xgm = _xgm()
+    bits, V, t = {"bf16": 7, "f16": 10}[dtype], 4000, TYPES[dtype][0]
+    rng = np.random.default_rng(3)
+    low = (1 + rng.integers(0, 2 ** bits, V) * 2.0 ** -bits) * 2.0 ** rng.integers(5, 9, V)      # of the two neighbours, whose middle is
+    middle = low + 2.0 ** -(bits + 1) * 2.0 ** np.floor(np.log2(low))                            # exact in 32 bits
+    sign, side = rng.choice([-1.0, 1.0], V), rng.choice([-1.0, 1.0], V)
+    x = side * 2.0 ** -24                                                                        # less than 2^-25 of the sum
+    n = 1 if rule == "bias" else V
+    want = torch.from_numpy(np.where(sign * side > 0, 2 * middle - low, low) * sign).to(t)
+    assert (np.float32(sign * middle + x) == sign * middle).all() and (sign * middle + x != sign * middle).all()
+    if rule == "bias":
+        d = [_dev(np.arange(V, dtype=np.int32)), _dev((sign * middle).astype(np.float32)), _dev(np.array([0, V], np.int32))]
+        rules = xgm.LogitRules(d_bias_ids=_at(d[0]), d_bias=_at(d[1]), d_bias_offsets=_at(d[2]), n_bias=V)
+        logits = torch.from_numpy(x).to(t).cuda()[None]
+    else:       # row b generated token b
+        d = [torch.arange(V, dtype=torch.int32, device="cuda"), torch.ones(V, dtype=torch.int32, device="cuda"), _dev((-sign * middle).astype(np.float32))]
+        rules = xgm.LogitRules(d_tokens=_at(d[0]), token_stride=1, d_n_tokens=_at(d[1]), d_presence=_at(d[2]))
+        logits = torch.from_numpy(x).to(t).cuda()[None].expand(V, V).contiguous()
+    out = torch.empty((n, V), dtype=t, device="cuda")
+    xgm.process_logits(logits.data_ptr(), TYPES[dtype][1], n, V, V, rules, out.data_ptr(), V, _stream())
+    got = out[0] if rule == "bias" else out.diagonal().contiguous()
+    assert torch.equal(got.cpu().view(torch.int16), want.view(torch.int16))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_rules_on_what_is_not_finite(dtype):
     xgm = _xgm()
