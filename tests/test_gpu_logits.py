@@ -144,6 +144,42 @@ def test_projection_under_masks_of_another_vocabulary(B, K, V, group):
         assert np.array_equal(got[:, :V], np.where(here, want, -np.inf)) and (got[:, V:] == 7).all(), (v_mask, first)
 
 
+# (a workgroup of the projection of many rows takes ceil(tiles / 256) tiles of 16 rows of the matrix: 2, 5, 17, 19, 38 and 40)
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("B,K,V,group", [(40, 64, 5000, 64), (33, 160, 8179, 32), (128, 128, 20001, 128), (65, 96, 70000, 32), (100, 256, 77777, 64), (64, 192, 151936, 192),
+                                         (130, 64, 151936, 32), (50, 384, 160001, 128)])
+def test_projection_of_many_rows_with_many_tiles_a_workgroup(B, K, V, group, masked):
+    p = Projection(B, K, V, group, "bf16" if V % 2 else "f16", zeros=B % 2 == 0, whole=True, seed=B)
+    want = torch.from_numpy(p.want()[0]).float().cuda()             # (exact: small whole numbers)
+    mask = None
+    if masked:
+        rng = np.random.default_rng(V)
+        allowed = rng.random((B, V)) < rng.choice([0.0, 0.001, 0.4, 0.97], (B, 1))
+        allowed[:, V // 5:V // 2] = False                           # workgroups without a row, and some with few
+        allowed[B // 2, V // 3] = True
+        mask = _dev(plain.pack(allowed))
+        want.masked_fill_(_dev(~allowed), -float("inf"))
+    assert torch.equal(p.run("f32", mask, stride=V + 3), want)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("B,K,V,group", [(1, 128, 300001, 128), (3, 64, 600007, 32), (20, 128, 9000, 32), (32, 64, 70001, 64), (17, 256, 20000, 128), (24, 64, 300001, 32),
+                                         (40, 64, 300001, 64)])
+def test_projection_of_few_rows_with_many_tiles_or_long_lists(B, K, V, group, masked):
+    """Two times 16 rows with more than one tile a workgroup, and more than 1024 rows of the matrix, which are listed in parts."""
+    p = Projection(B, K, V, group, "f16" if V % 2 else "bf16", zeros=B % 2 == 1, whole=True, seed=B + 1)
+    want = torch.from_numpy(p.want()[0]).float().cuda()
+    mask = None
+    if masked:
+        rng = np.random.default_rng(V)
+        allowed = rng.random((B, V)) < rng.choice([0.002, 0.5, 1.0], (B, 1))
+        allowed[:, V // 5:V // 2] = False
+        allowed[B // 2, V // 3] = True
+        mask = _dev(plain.pack(allowed))
+        want.masked_fill_(_dev(~allowed), -float("inf"))
+    assert torch.equal(p.run("f32", mask), want)
+
+
 def test_projection_of_what_is_not_finite():
     p = Projection(3, 256, 200, 32, "bf16", whole=True)
     p.hidden[1, 100] = float("inf")
