@@ -437,6 +437,49 @@ def test_draws_are_those_of_the_definition(case, what):
             _check_logprob(got, w)
 
 
+@pytest.mark.parametrize("what", ["k", "p", "m", "kpm"])
+@pytest.mark.parametrize("case", [dict(rows=128, V=70000, dtype="bf16", history=300, bias=4, mask="full", sigma=3.0), dict(rows=1100, V=2000, dtype="f32", sigma=2.0),
+                                  dict(rows=200, V=50001, dtype="f16", sigma=0.0), dict(rows=64, V=151936, dtype="bf16", sigma=2.5, offset=3)],
+                         ids=lambda c: f"{c['rows']}x{c['V']}-{c['dtype']}")
+def test_large_batches_that_keep_few_tokens(case, what):
+    """More than 1024 slices, where no list of the kept tokens is made; in a small batch the same rows are drawn from a list."""
+    c = Batch(**case, seed=case["rows"])
+    rng = np.random.default_rng(len(what))
+    y, rows = c.want(), c.rows
+    assert rows * -(-c.V // 8192) > 1024
+    t = rng.choice([0.3, 0.7, 1.0, 1.7], rows).astype(np.float32)
+    k = rng.choice([1, 2, 5, 50], rows) if "k" in what else np.zeros(rows, int)
+    m = rng.choice([0.01, 0.2, 1.0], rows).astype(np.float32) if "m" in what else np.zeros(rows, np.float32)
+    p, u, want = np.ones(rows, np.float32), np.zeros(rows), []
+    for b in range(rows):
+        row = plain.Row(y[b], float(t[b]), int(k[b]))
+        if row.empty:
+            want.append((-1, -np.inf))
+            continue
+        if "p" in what:                     # the middle of the stretch of one of the first 60
+            share = row.run_sorted[:60] / row.run_sorted[-1]
+            at = int(rng.integers(0, share.size))
+            p[b] = np.float32(0.5 * (share[at] + (share[at - 1] if at else 0.0)))
+        row.__init__(y[b], float(t[b]), int(k[b]), float(p[b]), float(m[b]))
+        u[b], v = row.middle(rng)
+        want.append((v, row.logprob(v)))
+
+    def draw(n):
+        c.rows = n
+        ids, lp = _draw(c, t[:n], k[:n] if "k" in what else None, p[:n] if "p" in what else None, m[:n] if "m" in what else None, u[:n])
+        c.rows = rows
+        return ids, lp
+
+    buf, (ids, lp) = c.buf, draw(rows)
+    assert ids.tolist() == [v for v, _ in want]
+    for got, (_, w) in zip(lp, want):
+        _check_logprob(got, w)
+    few = 9
+    assert few * -(-c.V // 8192) <= 1024
+    some, some_lp = draw(few)
+    assert np.array_equal(some, ids[:few]) and np.array_equal(some_lp, lp[:few]) and c.buf is buf
+
+
 def test_the_likeliest_token_is_taken_without_random_numbers():
     c = Batch(6, 9001, "bf16", seed=5, mask="full", sigma=0.5)      # many equal logits at the top
     y = c.want()
