@@ -342,13 +342,12 @@ struct DrawMemory {
   Slot* slots;       // [rows][slices]
   u64* bins;         // [rows][slices][kBins]
   u64* candidates;   // [rows][kMostCandidates]: key, bin, id
-  int32_t rows, slices;
+  int32_t slices;
 };
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 int32_t most_slices(int32_t V) { return (V + 7 + kSliceTokens - 1) / kSliceTokens; }
 DrawMemory memory_at(void* at, int32_t rows, int32_t V, size_t* bytes) {
   DrawMemory m{};
-  m.rows = rows;
   m.slices = most_slices(V);
   char* p = static_cast<char*>(at);
   auto take = [&](size_t n) { char* q = p; p += rounded(n); return q; };
