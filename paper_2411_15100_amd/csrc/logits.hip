@@ -194,7 +194,7 @@ template <class Get, class Set> __device__ __forceinline__ void apply_rules(cons
 
 // One workgroup per slice.  A logit that nothing touches is copied as it is, one that is masked is not read; the table takes 32 KB of LDS, so
 // that four workgroups run on a compute unit.  128 rows x 151936 (bf16, histories to 2048, 5 rows of 13 open) take 20 us, 2.8 TB/s: half
-// of it instruction issue, half the chain length - history - table - logits in 2.4 rounds of workgroups.  One row of 32000: 6.4 us.
+// of it instruction issue, half the chain length - history - table - logits in 2.4 rounds of workgroups.  One row of 32000: 6.7 us.
 template <Elem E>
 __global__ __launch_bounds__(kSliceThreads) void process_logits_kernel(Logits in, LogitRules r, typename Type<E>::bits* out, int64_t out_stride) {
   typedef typename Type<E>::bits bits;
@@ -258,7 +258,7 @@ template <Elem E> int32_t slices_of(const Logits& in) {
 // Second kernel, for rows with a cut, one workgroup per slice: the tokens of those bins are listed.  Third, one workgroup per row: it finds the
 // cuts among them (where there are too many for the list it goes through the row again each time), the slice and the token.
 // What workgroups of one kernel hand to each other goes through atomics of the device, which no cache of an XCD holds back.
-// 128 rows x 151936 (top-p, 5 rows of 13 open): 48, 22 and 41 us; instruction issue in 64 bits is 32 of the first's, and the third goes several
+// 128 rows x 151936 (top-p, 5 rows of 13 open): 49, 22 and 42 us; instruction issue in 64 bits is 32 of the first's, and the third goes several
 // times through the tokens of bins that hold thousands.  One row (top-k, top-p): 18, 8 and 10 us, chains of loads, barriers and selections.  48 rows
 // without a cut: 31 us, of which the last slice of a row is done after 17.
 constexpr int kWaves = kSliceThreads / 64;
