@@ -193,8 +193,8 @@ __global__ __launch_bounds__(kFewThreads<NB>) void q4_few_kernel(Head h, Elem ou
       count = list_rows(h, out_type, first_b, rows, base, here, list, any, n_listed);
     }
     const int32_t tiles = (count + 15) / 16;
-    int32_t sharing = 1;  // waves to a tile
-    while (sharing * 2 <= n_steps && sharing * 2 * tiles <= waves) sharing *= 2;
+    int32_t sharing = 1;  // waves to a tile, no more than there are where masks leave no tile
+    while (sharing * 2 <= n_steps && sharing * 2 * max(tiles, 1) <= waves) sharing *= 2;
     const int32_t sub = wave & (sharing - 1), abreast = waves / sharing, rounds = (tiles + abreast - 1) / abreast;
     const uint8_t* const base_codes = h.codes + base * (h.K / 2);
     const uint16_t* const base_scales = static_cast<const uint16_t*>(h.scales) + base * per_row;

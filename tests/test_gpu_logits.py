@@ -144,6 +144,18 @@ def test_projection_under_masks_of_another_vocabulary(B, K, V, group):
         assert np.array_equal(got[:, :V], np.where(here, want, -np.inf)) and (got[:, V:] == 7).all(), (v_mask, first)
 
 
+@pytest.mark.parametrize("B,K,V,group", [(4, 16384, 700, 128), (3, 16384, 5000, 32), (1, 32768, 333, 128), (1, 40960, 200, 64), (1, 65536, 130, 65536)])
+def test_projection_of_many_columns_under_masks_that_leave_workgroups_nothing(B, K, V, group):
+    """More steps than a workgroup has waves, and no row of the matrix to share them out over."""
+    p = Projection(B, K, V, group, "bf16", whole=True, seed=7)
+    want, _ = p.want()
+    rng = np.random.default_rng(V)
+    for share in (0.0, 0.004, 0.3):
+        allowed = rng.random((B, V)) < share
+        allowed[:, V // 2:V // 2 + 64] = False
+        assert np.array_equal(_np(p.run(mask=_dev(plain.pack(allowed)))), np.where(allowed, want, -np.inf)), share
+
+
 # (a workgroup of the projection of many rows takes ceil(tiles / 256) tiles of 16 rows of the matrix: 2, 5, 17, 19, 38 and 40)
 @pytest.mark.parametrize("masked", [False, True])
 @pytest.mark.parametrize("B,K,V,group", [(40, 64, 5000, 64), (33, 160, 8179, 32), (128, 128, 20001, 128), (65, 96, 70000, 32), (100, 256, 77777, 64), (64, 192, 151936, 192),
