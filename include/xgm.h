@@ -578,7 +578,7 @@ void xgm_sampler_destroy(xgm_sampler* s);
 /* How a row is drawn; as above, device memory, a value a row, NULL: off.
  * d_temperature: NULL is 1; 0 or less takes the likeliest token (the lowest id
  * of several).  d_top_k: 0 or less is off; d_top_p: 1 or more is off; d_min_p: 0 or
- * less is off.  d_uniform: the random numbers, 0 <= u < 1 (NULL: the likeliest
+ * less is off, more than 1 is 1.  d_uniform: the random numbers, 0 <= u < 1 (NULL: the likeliest
  * token in every row). */
 typedef struct {
   const float* d_temperature;
