@@ -49,6 +49,7 @@ typedef struct xgm_cache xgm_cache;
 typedef struct xgm_matcher xgm_matcher;
 typedef struct xgm_batch xgm_batch;
 typedef struct xgm_sampler xgm_sampler;
+typedef struct xgm_beams xgm_beams;
 
 typedef enum {
   XGM_OK = 0,
@@ -65,7 +66,7 @@ typedef enum {
   XGM_ERR_INTERNAL = -11
 } xgm_status;
 
-typedef enum { XGM_F32 = 0, XGM_BF16 = 1, XGM_F16 = 2 } xgm_dtype;
+typedef enum { XGM_F32 = 0, XGM_BF16 = 1, XGM_F16 = 2, XGM_F8 = 3 /* e4m3, only where it is named */ } xgm_dtype;
 
 enum {
   XGM_MAX_STACKS = 64,       /* parallel stacks per matcher */
@@ -78,8 +79,11 @@ enum {
   XGM_BATCH_MAX_ROWS = 1024, /* rows of an xgm_batch */
   XGM_MAX_ROWS = 65535,      /* rows of a call below */
   XGM_MAX_COLUMNS = 0x7fff0000, /* its logits a row, and the tokens of its masks (v_mask) */
-  XGM_MAX_LOGITS = 1 << 20,  /* logits a row of an xgm_sampler (padding included) */
-  XGM_MAX_HIDDEN = 1 << 16,  /* columns of xgm_q4_logits */
+  XGM_MAX_LOGITS = 1 << 20,  /* logits a row of an xgm_sampler or xgm_beams (padding included) */
+  XGM_MAX_HIDDEN = 1 << 16,  /* columns of an output projection */
+  XGM_MAX_BEAMS = 64,        /* beams a request */
+  XGM_MAX_CONTINUATIONS = 128, /* of a request that xgm_beam_select returns */
+  XGM_MAX_ROW_DATA = 8,      /* entries of a call of xgm_reorder_rows */
   XGM_MAX_HISTORY = 1 << 20  /* tokens of a history, and one more (xgm_logit_rules.token_stride is less) */
 };
 
@@ -606,6 +610,88 @@ typedef struct {
 int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, int32_t V, int64_t row_stride_elems,
                const xgm_logit_rules* rules, const xgm_draw_rules* draw, int32_t* d_ids, float* d_logprobs,
                void* hip_stream);
+
+/* 9. The output projection (6) with a matrix in 8-bit floating point (e4m3: 4 bits of exponent, 3 of mantissa, up to 448, no
+ * infinities; 0x7f and 0xff are NaN) and a scale for each block of 128 rows and 128 columns:
+ *   logits[b][v] = sum over blocks j of 128 columns of
+ *                  hidden_scale(b, j) * scale(v / 128, j) * sum over k in j of hidden[b][k] * code(v, k),
+ * where hidden states are in 8 bits too; sums and scales in 32 bits, rounded once; -inf where bit (b, v) of d_bitmask
+ * ([B, xgm_bitmask_words(v_mask)]; NULL: no mask) is 0, and from v_mask on.
+ * d_hidden: [B, K], row stride hidden_stride_elems.  hidden_dt XGM_F8: codes, with d_hidden_scales: [B, ceil(K / 128)] floats.
+ * hidden_dt XGM_BF16 or XGM_F16: the call brings them to 8 bits itself, as xgm_f8_quantize does; d_hidden_scales is NULL,
+ * and d_work is xgm_f8_work_bytes(B, K) bytes of device memory (a multiple of 16 bytes as an address) for the call to work in; calls with one d_work
+ * must be ordered by the caller, as must replays of graphs that hold them.  (With XGM_F8 d_work is not looked at.)
+ * d_codes: [V, K] bytes.  d_scales: [ceil(V / 128), ceil(K / 128)] floats.  K is a multiple of 16, at most XGM_MAX_HIDDEN;
+ * B <= XGM_MAX_ROWS; d_hidden, its row pitch and d_codes must be multiples of 16 bytes.  d_logits: [B, V] of logits_dt (XGM_F32, XGM_BF16, XGM_F16),
+ * row stride logits_stride_elems.  A matrix with the rows from 128 i on of a larger one takes d_bitmask + 4 i and the larger one's v_mask,
+ * where that is no less than the larger one's rows. */
+int xgm_f8_logits(const void* d_hidden, xgm_dtype hidden_dt, const float* d_hidden_scales, int32_t B, int32_t K, int64_t hidden_stride_elems,
+                  const uint8_t* d_codes, const float* d_scales, int32_t V, void* d_logits, xgm_dtype logits_dt, int64_t logits_stride_elems,
+                  const int32_t* d_bitmask, int32_t v_mask, void* d_work, void* hip_stream);
+/* Bytes of d_work (B and K as above). */
+int64_t xgm_f8_work_bytes(int32_t B, int32_t K);
+/* Values in 8 bits: of each row and block of 128 columns (the last may be shorter) the scale is the smallest power of two 2^e,
+ * -126 <= e <= 120, for which no |x| is above 448 * 2^e, and a code is x / scale rounded to the nearest, ties to even: the only
+ * rounding there is.  A value that is not finite becomes NaN (and of an infinity's block the scale is 2^120).  d_x: [B, K] of dt
+ * (XGM_F32, XGM_BF16 or XGM_F16), row stride stride_elems; d_codes: [B, K] bytes, row stride codes_stride_elems; d_scales: [B, ceil(K / 128)].
+ * K is a multiple of 16; d_x, d_codes and their row pitches must be multiples of 16 bytes. */
+int xgm_f8_quantize(const void* d_x, xgm_dtype dt, int32_t B, int32_t K, int64_t stride_elems, uint8_t* d_codes, int64_t codes_stride_elems,
+                    float* d_scales, void* hip_stream);
+
+/* 10. Rows of an output matrix as the hidden states of tokens (a model whose input and output share one matrix):
+ *   out[i][k] = value(d_ids[i], k) * factor, in 64 bits, rounded once,
+ * where value is (code - zero) * scale of the 4-bit matrix of (6), or code * scale of the 8-bit one of (9).  A row whose id is
+ * negative (a text that has ended), or V or more, becomes zeros.  d_ids: [n]; d_out: [n, K] of out_dt, row stride out_stride_elems.
+ * K, group and the arrays of a matrix as above (scales_dt: XGM_BF16 or XGM_F16); d_codes must be a multiple of 16 bytes.  n <= 2^24. */
+int xgm_q4_embed(const int32_t* d_ids, int32_t n, const uint8_t* d_codes, const void* d_scales, xgm_dtype scales_dt, const uint8_t* d_zeros, int32_t V,
+                 int32_t K, int32_t group, float factor, void* d_out, xgm_dtype out_dt, int64_t out_stride_elems, void* hip_stream);
+int xgm_f8_embed(const int32_t* d_ids, int32_t n, const uint8_t* d_codes, const float* d_scales, int32_t V, int32_t K, float factor, void* d_out,
+                 xgm_dtype out_dt, int64_t out_stride_elems, void* hip_stream);
+
+/* 11. Several beams a request.  Rows come request by request: row r * n_beams + i is beam i of request r.  An xgm_beams holds the
+ * working memory of its calls, which must be ordered by the caller (one stream, or events), replays of graphs among them: rows up to
+ * max_rows, V <= XGM_MAX_LOGITS logits each; about 1 KB of device memory for each 8192 logits of a row.  xgm_beams_create synchronises hip_stream. */
+int xgm_beams_create(int32_t max_rows, int32_t V, void* hip_stream, xgm_beams** out);
+void xgm_beams_destroy(xgm_beams* s);
+/* The continuations with which a request's texts go on.  The logits ([requests * n_beams, V] of dt) go through the rules (NULL: none)
+ * in 32 bits; nothing is written back to them.  NaN counts as -inf there, +inf as the largest finite number.  A token v with y(v) > -inf
+ * continues row b with the sum
+ *   y(v) + (d_scores[b] - log(sum over the row of exp(y))),
+ * in 64 bits.  d_ended (NULL: none): a row with a value other than 0 has one continuation, itself, with token -1 and its score as the sum.  A row whose
+ * score is not finite has none (a beam without a text: -inf).
+ * The first n_out <= XGM_MAX_CONTINUATIONS continuations of a request, in falling order of the sum (among equal ones the lower row first;
+ * in a row the larger logit, then the lower id), become
+ *   d_rows[r][j], the row continued (of all rows, as xgm_batch_fork and xgm_reorder_rows take it),
+ *   d_ids[r][j], the token (as xgm_batch_accept_tokens takes it), d_out_scores[r][j], the sum, rounded to 32 bits,
+ * all [requests, n_out]; what is missing becomes -1, -1 and -inf.
+ * placed (n_out must be n_beams): not 0: the first continuation of a row takes the row's own place, and the others, in their order, the
+ * places that are left, lowest first: a text that goes on stays where it is, and whatever it keeps need not move.
+ * d_out_scores may be d_scores where n_out is n_beams.  n_beams <= XGM_MAX_BEAMS.  The same inputs give the same results; a sum is exact to
+ * (4 + |y| + |score|) 2^-50. */
+int xgm_beam_select(xgm_beams* s, const void* d_logits, xgm_dtype dt, int32_t requests, int32_t n_beams, int32_t V, int64_t row_stride_elems,
+                    const xgm_logit_rules* rules, const float* d_scores, const int32_t* d_ended, int32_t n_out, int32_t placed, int32_t* d_rows,
+                    int32_t* d_ids, float* d_out_scores, void* hip_stream);
+
+/* 12. What rows keep (caches, texts, penalties) moves with them, in place.  Row b of an array is, for each o < n_outer and p < n_parts, the
+ * part_bytes bytes at d_data + o * outer_stride + b * row_stride + p * part_stride (strides in bytes); of a part only the first
+ * d_used[row] * used_bytes are in use (d_used: a value a row, device memory; NULL: all of it). */
+typedef struct {
+  void* d_data;
+  int64_t row_stride;
+  int64_t outer_stride;
+  int64_t part_stride;
+  int64_t part_bytes;
+  const int32_t* d_used;
+  int64_t used_bytes;
+  int32_t n_outer;
+  int32_t n_parts;
+} xgm_row_data;
+/* Row b of each of the n <= XGM_MAX_ROW_DATA arrays (host memory, read during the call) takes over what is in use of row d_rows[b], as that was before the
+ * call, whatever goes where; behind that it stays as it is.  A row whose d_rows[b] is negative, b itself, or B or more stays.  B <= XGM_BATCH_MAX_ROWS.  Rows
+ * and parts of an array must not overlap each other, nor what lies from the first byte of an array to its last that of another array of the call, d_rows
+ * or a d_used (lengths are moved by a call of their own, behind this one).  Bytes are copied in units of up to 16, the largest power of two that divides
+ * the address, the strides and sizes of an array.  One launch. */
+int xgm_reorder_rows(const xgm_row_data* arrays, int32_t n, const int32_t* d_rows, int32_t B, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -32,7 +32,7 @@ class _NotLoaded:
 
 _fast = _NotLoaded()
 
-DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_F8 = 0, 1, 2, 3
 
 # name -> (restype, argtypes); must list every symbol include/xgm.h declares
 _vp, _cp, _i32, _i64, _sz = ctypes.c_void_p, ctypes.c_char_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
@@ -113,6 +113,15 @@ SIGNATURES = {
     "xgm_sampler_create": (_i32, [_i32, _i32, _vp, _pp]),
     "xgm_sampler_destroy": (None, [_vp]),
     "xgm_sample": (_i32, [_vp, _vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp]),
+    "xgm_f8_logits": (_i32, [_vp, _i32, _vp, _i32, _i32, _i64, _vp, _vp, _i32, _vp, _i32, _i64, _vp, _i32, _vp, _vp]),
+    "xgm_f8_work_bytes": (_i64, [_i32, _i32]),
+    "xgm_f8_quantize": (_i32, [_vp, _i32, _i32, _i32, _i64, _vp, _i64, _vp, _vp]),
+    "xgm_q4_embed": (_i32, [_vp, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _i32, ctypes.c_float, _vp, _i32, _i64, _vp]),
+    "xgm_f8_embed": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, ctypes.c_float, _vp, _i32, _i64, _vp]),
+    "xgm_beams_create": (_i32, [_i32, _i32, _vp, _pp]),
+    "xgm_beams_destroy": (None, [_vp]),
+    "xgm_beam_select": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "xgm_reorder_rows": (_i32, [_vp, _i32, _vp, _i32, _vp]),
 }
 
 STATUS_NAMES = {
@@ -590,3 +599,77 @@ class Sampler:
     def sample(self, d_logits: int, dtype: int, rows: int, v: int, row_stride: int, rules, draw, d_ids: int, d_logprobs: int = 0, stream: int = 0):
         """rules: a LogitRules, or None; draw: a DrawRules, or None (the likeliest token)."""
         _fast.sample(self, d_logits, dtype, rows, v, row_stride, rules, draw, d_ids, d_logprobs, stream)
+
+
+def f8_work_bytes(rows: int, k: int) -> int:
+    """Bytes of f8_logits' working memory for hidden states that are not in 8 bits (xgm_f8_work_bytes)."""
+    return _check(load_library().xgm_f8_work_bytes(int(rows), int(k)))
+
+
+def f8_quantize(d_x: int, dtype: int, rows: int, k: int, stride: int, d_codes: int, codes_stride: int, d_scales: int, stream: int = 0):
+    """Values in 8 bits with a scale for each 128 columns (xgm_f8_quantize)."""
+    _check(load_library().xgm_f8_quantize(ctypes.c_void_p(d_x), dtype, rows, k, stride, ctypes.c_void_p(d_codes), codes_stride,
+                                          ctypes.c_void_p(d_scales), ctypes.c_void_p(stream)))
+
+
+def f8_logits(d_hidden: int, dtype: int, d_hidden_scales: int, rows: int, k: int, hidden_stride: int, d_codes: int, d_scales: int, v: int,
+              d_logits: int, logits_dtype: int, row_stride: int, d_bitmask: int = 0, d_work: int = 0, stream: int = 0, v_mask: int = None):
+    """Logits from hidden states and an 8-bit matrix, under the masks (xgm_f8_logits); v_mask: the masks' vocabulary, v if not given."""
+    _fast.f8_logits(d_hidden, dtype, d_hidden_scales, rows, k, hidden_stride, d_codes, d_scales, v, d_logits, logits_dtype, row_stride, d_bitmask,
+                    v if v_mask is None else v_mask, d_work, stream)
+
+
+def q4_embed(d_ids: int, n: int, d_codes: int, d_scales: int, scales_dtype: int, d_zeros: int, v: int, k: int, group: int, factor: float,
+             d_out: int, out_dtype: int, out_stride: int, stream: int = 0):
+    """Rows of a 4-bit output matrix as hidden states (xgm_q4_embed)."""
+    _fast.q4_embed(d_ids, n, d_codes, d_scales, scales_dtype, d_zeros, v, k, group, factor, d_out, out_dtype, out_stride, stream)
+
+
+def f8_embed(d_ids: int, n: int, d_codes: int, d_scales: int, v: int, k: int, factor: float, d_out: int, out_dtype: int, out_stride: int,
+             stream: int = 0):
+    """Rows of an 8-bit output matrix as hidden states (xgm_f8_embed)."""
+    _fast.f8_embed(d_ids, n, d_codes, d_scales, v, k, factor, d_out, out_dtype, out_stride, stream)
+
+
+class BeamSearch:
+    """Continuations of several beams a request (xgm_beams): working memory for up to max_rows rows of v logits."""
+
+    def __init__(self, max_rows: int, v: int, stream: int = 0):
+        h = ctypes.c_void_p()
+        _check(load_library().xgm_beams_create(int(max_rows), int(v), ctypes.c_void_p(stream), ctypes.byref(h)))
+        self._h = h.value
+
+    def __del__(self, _destroy=_destroy):
+        _destroy("xgm_beams_destroy", self)
+
+    def select(self, d_logits: int, dtype: int, requests: int, beams: int, v: int, row_stride: int, rules, d_scores: int, d_ended: int, n_out: int,
+               placed: bool, d_rows: int, d_ids: int, d_out_scores: int, stream: int = 0):
+        """The n_out best continuations of each request (xgm_beam_select); rules: a LogitRules, or None."""
+        _fast.beam_select(self, d_logits, dtype, requests, beams, v, row_stride, rules, d_scores, d_ended, n_out, int(bool(placed)), d_rows, d_ids,
+                          d_out_scores, stream)
+
+
+class RowData(_Struct):
+    """What the rows of a batch keep in one array (xgm_row_data)."""
+
+    _pointers = ("d_data",)
+    _numbers = (("row_stride", _i64), ("outer_stride", _i64), ("part_stride", _i64), ("part_bytes", _i64), ("d_used", _vp), ("used_bytes", _i64),
+                ("n_outer", _i32), ("n_parts", _i32))
+
+
+class RowSet:
+    """The arrays that one call of reorder_rows moves, laid out once; they are the caller's and must outlive the calls."""
+
+    def __init__(self, *arrays: RowData):
+        if not all(isinstance(a, RowData) for a in arrays):
+            raise TypeError("RowSet takes RowData")
+        self._s = (RowData._type * len(arrays))(*[a._s for a in arrays])
+        self._addr = ctypes.addressof(self._s)
+        self.size = len(arrays)
+
+
+def reorder_rows(arrays: RowSet, d_rows: int, rows: int, stream: int = 0):
+    """Row b of every array takes over row d_rows[b], in place (xgm_reorder_rows)."""
+    if not isinstance(arrays, RowSet):
+        raise TypeError("reorder_rows takes a RowSet")
+    _fast.reorder_rows(arrays, arrays.size, d_rows, rows, stream)

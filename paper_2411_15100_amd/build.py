@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libxgm.so")
 EXT = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
 EXT_UNTAGGED = os.path.join(HERE, "_native.so")  # (any Python would load it)
 EXT_SOURCE = os.path.join(CSRC, "pybinding.cpp")
-SOURCES = ["automaton.cpp", "engine.cpp", "schema.cpp", "api.cpp", "kernels.hip", "head.hip", "logits.hip"]
+SOURCES = ["automaton.cpp", "engine.cpp", "schema.cpp", "api.cpp", "kernels.hip", "head.hip", "f8.hip", "logits.hip", "beam.hip"]
 HEADERS = ["automaton.hpp", "engine.hpp", "schema.hpp", "kernels.hpp", "logits.hpp", "elements.hpp", "slices.hpp", "walk.hpp", os.path.join("..", "..", "include", "xgm.h")]
 
 FLAGS = [

@@ -2253,12 +2253,17 @@ struct xgm_sampler {
   int32_t max_rows = 0, V = 0;
   void* memory = nullptr;
 };
+struct xgm_beams {
+  int32_t max_rows = 0, V = 0;
+  void* memory = nullptr;
+};
 namespace {
 bool elem_of(xgm_dtype dt, Elem* e, int* size) {
   switch (dt) {
     case XGM_F32: *e = Elem::kF32; *size = 4; return true;
     case XGM_BF16: *e = Elem::kBF16; *size = 2; return true;
     case XGM_F16: *e = Elem::kF16; *size = 2; return true;
+    case XGM_F8: break;  // (not a type of logits)
   }
   return false;
 }
@@ -2402,6 +2407,220 @@ int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, in
   const DrawRules d = draw ? DrawRules{draw->d_temperature, draw->d_top_k, draw->d_top_p, draw->d_min_p, draw->d_uniform} : DrawRules{};
   hip_check(launch_sample(Logits{d_logits, row_stride_elems, V}, type, B, r, d, s->memory, s->max_rows, s->V, d_ids, d_logprobs,
                           static_cast<hipStream_t>(hip_stream)), "sample");
+  return XGM_OK;
+  API_END
+}
+
+// --------------------------------------------------- the output matrix in 8 bits
+int64_t xgm_f8_work_bytes(int32_t B, int32_t K) {
+  API_BEGIN
+  if (B <= 0 || K <= 0) return fail(XGM_ERR_BAD_ARG, "f8_work_bytes: sizes must be positive");
+  if (B > XGM_MAX_ROWS || K > XGM_MAX_HIDDEN) return fail(XGM_ERR_TOO_LARGE, "f8_work_bytes: more than XGM_MAX_ROWS rows or XGM_MAX_HIDDEN columns");
+  return (int64_t)f8_work_bytes(B, K);
+  API_END
+}
+
+int xgm_f8_quantize(const void* d_x, xgm_dtype dt, int32_t B, int32_t K, int64_t stride_elems, uint8_t* d_codes, int64_t codes_stride_elems,
+                    float* d_scales, void* hip_stream) {
+  API_BEGIN
+  if (!d_x || !d_codes || !d_scales) return fail(XGM_ERR_BAD_ARG, "f8_quantize: null values, codes or scales");
+  Elem type;
+  int size;
+  if (!elem_of(dt, &type, &size)) return fail(XGM_ERR_BAD_ARG, "f8_quantize: unknown dtype");
+  if (B <= 0 || K <= 0 || K % 16 != 0) return fail(XGM_ERR_BAD_ARG, "f8_quantize: sizes must be positive, and columns a multiple of 16");
+  if (B > XGM_MAX_ROWS || K > XGM_MAX_HIDDEN) return fail(XGM_ERR_TOO_LARGE, "f8_quantize: more than XGM_MAX_ROWS rows or XGM_MAX_HIDDEN columns");
+  if (stride_elems < K || codes_stride_elems < K) return fail(XGM_ERR_BAD_ARG, "f8_quantize: stride smaller than the row");
+  if (!aligned(d_x, 16) || stride_elems * size % 16 != 0 || !aligned(d_codes, 16) || codes_stride_elems % 16 != 0)
+    return fail(XGM_ERR_BAD_ARG, "f8_quantize: rows of values and of codes must be 16-byte aligned");
+  if (!aligned(d_scales, 4)) return fail(XGM_ERR_BAD_ARG, "f8_quantize: scales are not aligned to their element size");
+  require_device();
+  hip_check(launch_f8_quantize(d_x, type, B, K, stride_elems, d_codes, codes_stride_elems, d_scales, static_cast<hipStream_t>(hip_stream)), "f8_quantize");
+  return XGM_OK;
+  API_END
+}
+
+int xgm_f8_logits(const void* d_hidden, xgm_dtype hidden_dt, const float* d_hidden_scales, int32_t B, int32_t K, int64_t hidden_stride_elems,
+                  const uint8_t* d_codes, const float* d_scales, int32_t V, void* d_logits, xgm_dtype logits_dt, int64_t logits_stride_elems,
+                  const int32_t* d_bitmask, int32_t v_mask, void* d_work, void* hip_stream) {
+  API_BEGIN
+  if (!d_hidden || !d_codes || !d_scales) return fail(XGM_ERR_BAD_ARG, "f8_logits: null hidden states, codes or scales");
+  Elem hidden = Elem::kBF16, logits;
+  int hidden_size = 1, logits_size;
+  if (hidden_dt != XGM_F8 && (!elem_of(hidden_dt, &hidden, &hidden_size) || hidden == Elem::kF32))
+    return fail(XGM_ERR_BAD_ARG, "f8_logits: hidden states are bf16, f16 or in 8 bits");
+  if (hidden_dt == XGM_F8 && !d_hidden_scales) return fail(XGM_ERR_BAD_ARG, "f8_logits: hidden states in 8 bits without their scales");
+  if (hidden_dt != XGM_F8 && d_hidden_scales) return fail(XGM_ERR_BAD_ARG, "f8_logits: scales of hidden states that are not in 8 bits");
+  if (hidden_dt != XGM_F8 && !d_work) return fail(XGM_ERR_BAD_ARG, "f8_logits: hidden states that are not in 8 bits, and no memory to bring them there");
+  if (!elem_of(logits_dt, &logits, &logits_size)) return fail(XGM_ERR_BAD_ARG, "f8_logits: unknown dtype");
+  if (const char* what = logits_fault(d_logits, logits_size, B, V, logits_stride_elems)) return fail(XGM_ERR_BAD_ARG, std::string("f8_logits: ") + what);
+  if (K <= 0 || K % 16 != 0) return fail(XGM_ERR_BAD_ARG, "f8_logits: columns must be a multiple of 16");
+  if (K > XGM_MAX_HIDDEN) return fail(XGM_ERR_TOO_LARGE, "f8_logits: more than XGM_MAX_HIDDEN columns");
+  if (hidden_stride_elems < K) return fail(XGM_ERR_BAD_ARG, "f8_logits: hidden stride smaller than the row");
+  if (!aligned(d_hidden, 16) || hidden_stride_elems * hidden_size % 16 != 0 || !aligned(d_codes, 16))
+    return fail(XGM_ERR_BAD_ARG, "f8_logits: hidden rows and codes must be 16-byte aligned");
+  if (!aligned(d_scales, 4) || !aligned(d_hidden_scales, 4)) return fail(XGM_ERR_BAD_ARG, "f8_logits: scales are not aligned to their element size");
+  if (hidden_dt != XGM_F8 && !aligned(d_work, 16)) return fail(XGM_ERR_BAD_ARG, "f8_logits: working memory must be 16-byte aligned");
+  if (d_bitmask && v_mask <= 0) return fail(XGM_ERR_BAD_ARG, "f8_logits: a bitmask without v_mask");
+  if (d_bitmask && v_mask > XGM_MAX_COLUMNS) return fail(XGM_ERR_BAD_ARG, "f8_logits: v_mask is more than XGM_MAX_COLUMNS");
+  require_device();
+  const F8Head h{F8States{d_hidden, hidden_stride_elems, d_hidden_scales}, d_codes, d_scales, d_logits, logits_stride_elems,
+                 reinterpret_cast<const uint32_t*>(d_bitmask), B, K, V, d_bitmask ? xgm_bitmask_words(v_mask) : 0, v_mask};
+  hip_check(launch_f8_logits(h, hidden, logits, d_work, static_cast<hipStream_t>(hip_stream)), "f8_logits");
+  return XGM_OK;
+  API_END
+}
+
+}  // extern "C"
+namespace {
+// what is wrong with the ids and the output of a lookup, or null
+const char* embed_fault(const Embed& e, int out_size) {
+  if (!e.ids || !e.codes || !e.scales || !e.out) return "null ids, codes, scales or output";
+  if (e.n <= 0 || e.V <= 0 || e.K <= 0) return "sizes must be positive";
+  if (e.n > 1 << 24) return "more than 2^24 ids";
+  if (e.V > XGM_MAX_COLUMNS || e.K > XGM_MAX_HIDDEN) return "more than XGM_MAX_COLUMNS rows or XGM_MAX_HIDDEN columns of the matrix";
+  if (e.out_stride < e.K) return "output stride smaller than the row";
+  if (!aligned(e.codes, 16)) return "codes must be 16-byte aligned";
+  if (!aligned(e.ids, 4) || !aligned(e.out, out_size)) return "ids or output are not aligned to their element size";
+  return nullptr;
+}
+}  // namespace
+extern "C" {
+int xgm_q4_embed(const int32_t* d_ids, int32_t n, const uint8_t* d_codes, const void* d_scales, xgm_dtype scales_dt, const uint8_t* d_zeros, int32_t V,
+                 int32_t K, int32_t group, float factor, void* d_out, xgm_dtype out_dt, int64_t out_stride_elems, void* hip_stream) {
+  API_BEGIN
+  Elem scales, out;
+  int scales_size, out_size;
+  if (!elem_of(scales_dt, &scales, &scales_size) || scales == Elem::kF32) return fail(XGM_ERR_BAD_ARG, "q4_embed: scales are bf16 or f16");
+  if (!elem_of(out_dt, &out, &out_size)) return fail(XGM_ERR_BAD_ARG, "q4_embed: unknown dtype");
+  const Embed e{d_ids, d_codes, d_scales, d_zeros, d_out, out_stride_elems, n, V, K, group, factor};
+  if (const char* what = embed_fault(e, out_size)) return fail(XGM_ERR_BAD_ARG, std::string("q4_embed: ") + what);
+  if (group <= 0 || group % 32 != 0 || K % group != 0) return fail(XGM_ERR_BAD_ARG, "q4_embed: group must be a multiple of 32 that divides K");
+  if (!aligned(d_scales, scales_size)) return fail(XGM_ERR_BAD_ARG, "q4_embed: scales are not aligned to their element size");
+  require_device();
+  hip_check(launch_q4_embed(e, scales, out, static_cast<hipStream_t>(hip_stream)), "q4_embed");
+  return XGM_OK;
+  API_END
+}
+int xgm_f8_embed(const int32_t* d_ids, int32_t n, const uint8_t* d_codes, const float* d_scales, int32_t V, int32_t K, float factor, void* d_out,
+                 xgm_dtype out_dt, int64_t out_stride_elems, void* hip_stream) {
+  API_BEGIN
+  Elem out;
+  int out_size;
+  if (!elem_of(out_dt, &out, &out_size)) return fail(XGM_ERR_BAD_ARG, "f8_embed: unknown dtype");
+  const Embed e{d_ids, d_codes, d_scales, nullptr, d_out, out_stride_elems, n, V, K, 128, factor};
+  if (const char* what = embed_fault(e, out_size)) return fail(XGM_ERR_BAD_ARG, std::string("f8_embed: ") + what);
+  if (K % 16 != 0) return fail(XGM_ERR_BAD_ARG, "f8_embed: columns must be a multiple of 16");
+  if (!aligned(d_scales, 4)) return fail(XGM_ERR_BAD_ARG, "f8_embed: scales are not aligned to their element size");
+  require_device();
+  hip_check(launch_f8_embed(e, out, static_cast<hipStream_t>(hip_stream)), "f8_embed");
+  return XGM_OK;
+  API_END
+}
+
+// --------------------------------------------------------------------- beams
+int xgm_beams_create(int32_t max_rows, int32_t V, void* hip_stream, xgm_beams** out) {
+  API_BEGIN
+  if (!out) return fail(XGM_ERR_BAD_ARG, "beams_create: out is null");
+  *out = nullptr;
+  if (max_rows <= 0 || V <= 0) return fail(XGM_ERR_BAD_ARG, "beams_create: sizes must be positive");
+  if (max_rows > XGM_MAX_ROWS || V > XGM_MAX_LOGITS) return fail(XGM_ERR_TOO_LARGE, "beams_create: more than XGM_MAX_ROWS rows or XGM_MAX_LOGITS logits");
+  require_device();
+  std::unique_ptr<xgm_beams> s(new xgm_beams());
+  s->max_rows = max_rows;
+  s->V = V;
+  const size_t bytes = beam_bytes(max_rows, V);
+  s->memory = dev_alloc<char>(bytes);
+  hipError_t e = hipMemsetAsync(s->memory, 0, bytes, static_cast<hipStream_t>(hip_stream));
+  if (e == hipSuccess) e = hipStreamSynchronize(static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) {
+    (void)hipFree(s->memory);
+    hip_check(e, "beams_create");
+  }
+  *out = s.release();
+  return XGM_OK;
+  API_END
+}
+void xgm_beams_destroy(xgm_beams* s) {
+  if (!s) return;
+  (void)hipFree(s->memory);
+  delete s;
+}
+int xgm_beam_select(xgm_beams* s, const void* d_logits, xgm_dtype dt, int32_t requests, int32_t n_beams, int32_t V, int64_t row_stride_elems,
+                    const xgm_logit_rules* rules, const float* d_scores, const int32_t* d_ended, int32_t n_out, int32_t placed, int32_t* d_rows,
+                    int32_t* d_ids, float* d_out_scores, void* hip_stream) {
+  API_BEGIN
+  if (!s || !d_scores || !d_rows || !d_ids || !d_out_scores) return fail(XGM_ERR_BAD_ARG, "beam_select: null beams, scores or results");
+  Elem type;
+  int size;
+  if (!elem_of(dt, &type, &size)) return fail(XGM_ERR_BAD_ARG, "beam_select: unknown dtype");
+  if (requests <= 0 || n_beams <= 0 || n_out <= 0) return fail(XGM_ERR_BAD_ARG, "beam_select: sizes must be positive");
+  if (n_beams > XGM_MAX_BEAMS || n_out > XGM_MAX_CONTINUATIONS)
+    return fail(XGM_ERR_TOO_LARGE, "beam_select: more than XGM_MAX_BEAMS beams or XGM_MAX_CONTINUATIONS continuations");
+  if ((int64_t)requests * n_beams > s->max_rows || V > s->V) return fail(XGM_ERR_BAD_ARG, "beam_select: more rows or logits than the beams were created for");
+  const char* what = logits_fault(d_logits, size, requests * n_beams, V, row_stride_elems);
+  LogitRules r;
+  if (!what) what = rules_fault(rules, &r);
+  if (!what && placed && n_out != n_beams) what = "placed, and not as many continuations as beams";
+  if (!what && (const float*)d_out_scores == d_scores && n_out != n_beams) what = "scores in place, and not as many continuations as beams";
+  if (what) return fail(XGM_ERR_BAD_ARG, std::string("beam_select: ") + what);
+  require_device();
+  const BeamSearch b{d_scores, d_ended, requests, n_beams, n_out, placed, d_rows, d_ids, d_out_scores};
+  hip_check(launch_beam_select(Logits{d_logits, row_stride_elems, V}, type, r, b, s->memory, s->max_rows, s->V, static_cast<hipStream_t>(hip_stream)), "beam_select");
+  return XGM_OK;
+  API_END
+}
+
+}  // extern "C"
+namespace {
+// What is wrong with an array of a reordering, or null.  Every address that rows below B have lies within *last bytes behind d_data.
+const char* row_data_fault(const xgm_row_data& d, int32_t B, uint64_t* last) {
+  if (!d.d_data) return "null data";
+  if (d.n_outer <= 0 || d.n_parts <= 0 || d.part_bytes <= 0) return "sizes must be positive";
+  if (d.row_stride < 0 || d.outer_stride < 0 || d.part_stride < 0) return "negative stride";
+  if (d.d_used && d.used_bytes <= 0) return "lengths without their unit";
+  if (d.d_used && !aligned(d.d_used, 4)) return "lengths are not aligned to their element size";
+  // rows, parts and outer repetitions, each beside the others: by falling strides what is inside one step fits it
+  struct Axis { int64_t n, stride; } axes[3] = {{B, d.row_stride}, {d.n_outer, d.outer_stride}, {d.n_parts, d.part_stride}};
+  std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+  __int128 extent = d.part_bytes;
+  for (const Axis& a : axes) {
+    if (a.n == 1) continue;
+    if (a.stride < extent) return "rows or parts overlap";
+    extent += (__int128)(a.n - 1) * a.stride;
+  }
+  if (extent > ((__int128)1 << 62)) return "strides beyond the address space";
+  *last = (uint64_t)extent;
+  return nullptr;
+}
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + b_bytes && y < x + a_bytes;
+}
+}  // namespace
+extern "C" {
+int xgm_reorder_rows(const xgm_row_data* arrays, int32_t n, const int32_t* d_rows, int32_t B, void* hip_stream) {
+  API_BEGIN
+  if (!arrays || !d_rows) return fail(XGM_ERR_BAD_ARG, "reorder_rows: null arrays or rows");
+  if (n <= 0 || B <= 0) return fail(XGM_ERR_BAD_ARG, "reorder_rows: sizes must be positive");
+  if (n > XGM_MAX_ROW_DATA || B > XGM_BATCH_MAX_ROWS) return fail(XGM_ERR_TOO_LARGE, "reorder_rows: more than XGM_MAX_ROW_DATA arrays or XGM_BATCH_MAX_ROWS rows");
+  if (!aligned(d_rows, 4)) return fail(XGM_ERR_BAD_ARG, "reorder_rows: rows are not aligned to their element size");
+  RowData data[XGM_MAX_ROW_DATA];
+  uint64_t extent[XGM_MAX_ROW_DATA];
+  for (int32_t i = 0; i < n; ++i) {
+    const xgm_row_data& d = arrays[i];
+    if (const char* what = row_data_fault(d, B, &extent[i])) return fail(XGM_ERR_BAD_ARG, std::string("reorder_rows: ") + what);
+    data[i] = RowData{d.d_data, d.row_stride, d.outer_stride, d.part_stride, d.part_bytes, d.d_used, d.used_bytes, d.n_outer, d.n_parts};
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    if (overlap(arrays[i].d_data, extent[i], d_rows, (uint64_t)B * 4)) return fail(XGM_ERR_BAD_ARG, "reorder_rows: an array overlaps the rows' sources");
+    for (int32_t k = 0; k < n; ++k) {
+      if (arrays[k].d_used && overlap(arrays[i].d_data, extent[i], arrays[k].d_used, (uint64_t)B * 4))
+        return fail(XGM_ERR_BAD_ARG, "reorder_rows: an array overlaps lengths of the same call");
+      if (k < i && overlap(arrays[i].d_data, extent[i], arrays[k].d_data, extent[k])) return fail(XGM_ERR_BAD_ARG, "reorder_rows: two arrays overlap");
+    }
+  }
+  require_device();
+  hip_check(launch_reorder_rows(data, n, d_rows, B, static_cast<hipStream_t>(hip_stream)), "reorder_rows");
   return XGM_OK;
   API_END
 }

@@ -1,0 +1,477 @@
+// Several beams a request: which continuations go on, and what the rows that go on keep.
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "elements.hpp"
+#include "logits.hpp"
+#include "slices.hpp"
+
+namespace xgm {
+
+namespace {
+
+// ------------------------------------------------------------- continuations of beams
+// A continuation of row b is worth logit + base, base = score - log(sum of exp of the row's logits), in 64 bits: two continuations of
+// different rows may be as near to each other as two numbers get, and the order of a sum in 32 bits would decide between them.
+// One launch, a workgroup per slice of a row: it reads the logits once, under the rules, and leaves the slice's sum of weights and its
+// n_out best tokens in order (a key: the logit as a whole number, then the id's complement, so that no two are alike).  The
+// workgroup that finishes last for its request knows every row's base and takes the n_out best of all lists.
+// A list begins with a bound: the threads form n groups, and no more than the least of their largest logits has to be looked
+// at, for every group has one as good.  The tokens above the bound (n ln n of them or so) are compared each with each.
+constexpr int kMostFound = 1024;   // tokens of a slice above its bound that are kept in LDS
+constexpr int kMostJoined = 2048;  // continuations of a request, likewise
+constexpr int kMostSlices = (1 << 20) / kSliceTokens + 1;
+
+struct BeamSlot {  // what a slice leaves beside its list
+  double E, sum;
+  float top;  // -inf: it has no list
+};
+struct BeamMemory {
+  uint32_t* arrived;  // [requests]: zero between calls
+  BeamSlot* slots;    // [rows][slices]
+  u64* lists;         // [rows][slices][n_out], 0 behind the last
+  int32_t slices;
+};
+size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+int32_t most_slices(int32_t V) { return (V + 7 + kSliceTokens - 1) / kSliceTokens; }
+BeamMemory memory_at(void* at, int32_t rows, int32_t V, size_t* bytes) {
+  BeamMemory m{};
+  m.slices = most_slices(V);
+  char* p = static_cast<char*>(at);
+  auto take = [&](size_t n) { char* q = p; p += rounded(n); return q; };
+  m.arrived = reinterpret_cast<uint32_t*>(take((size_t)rows * 4));
+  m.slots = reinterpret_cast<BeamSlot*>(take((size_t)rows * m.slices * sizeof(BeamSlot)));
+  m.lists = reinterpret_cast<u64*>(take((size_t)rows * m.slices * kMaxContinuations * 8));
+  *bytes = (size_t)(p - static_cast<char*>(at));
+  return m;
+}
+
+// A token in the order of its row: the larger logit first, then the lower id.  0 is none.
+__device__ __forceinline__ u64 token_key(float y, int32_t id) { return (u64)key_of(y) << 32 | (uint32_t)~id; }
+__device__ __forceinline__ int32_t id_of(u64 key) { return (int32_t)~(uint32_t)key; }
+__device__ __forceinline__ float logit_of(u64 key) { return value_of((uint32_t)(key >> 32)); }
+
+// A continuation in the order of its request: the larger sum first, then `place` falling: the lower row, the larger logit, the lower id.
+__device__ __forceinline__ u64 order_of(double x) {
+  const u64 u = (u64)__double_as_longlong(x == 0.0 ? 0.0 : x);
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double sum_of(u64 order) { return __longlong_as_double((long long)(order >> 63 ? order & ~(1ull << 63) : ~order)); }
+constexpr int kIdBits = 20;
+static_assert(kMaxBeams <= 64, "six bits of a place");
+__device__ __forceinline__ u64 place_in(int32_t beam, u64 key) {
+  return (u64)(kMaxBeams - 1 - beam) << (32 + kIdBits) | (key >> 32) << kIdBits | ((uint32_t)key & ((1u << kIdBits) - 1u));
+}
+__device__ __forceinline__ int32_t beam_of(u64 place) { return kMaxBeams - 1 - (int32_t)(place >> (32 + kIdBits)); }
+__device__ __forceinline__ int32_t id_at(u64 place) { return (int32_t)(~(uint32_t)place & ((1u << kIdBits) - 1u)); }
+
+struct BeamShared {
+  float top[kWaves];
+  double sum[kWaves];
+  float least[kWaves];
+  uint32_t n_found, flag;
+  u64 found[kMostFound];  // (in front of what the last workgroup needs)
+  uint32_t counts[kWaves];
+};
+struct JoinShared {
+  double base[kMaxBeams];
+  int32_t is_ended[kMaxBeams];
+  uint32_t n_joined;
+  uint32_t counts[kWaves];
+  u64 part[kWaves];
+  u64 order[kMostJoined], place[kMostJoined];
+  int32_t rows[kMaxContinuations], ids[kMaxContinuations], first[kMaxBeams], taken[kMaxBeams];
+  float scores[kMaxContinuations];
+};
+
+__device__ __forceinline__ bool is_live(const BeamSearch& s, int32_t b) { return s.scores[b] > -__builtin_inff() && s.scores[b] < __builtin_inff(); }
+__device__ __forceinline__ bool is_ended(const BeamSearch& s, int32_t b) { return s.ended && s.ended[b] != 0; }
+
+__device__ __forceinline__ uint32_t count_all(uint32_t mine, uint32_t (&counts)[kWaves]) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) mine += __shfl_xor(mine, d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  uint32_t all = 0;
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) all += counts[k];
+  return all;
+}
+
+// The least of the largest numbers of `groups` groups of threads (a power of two, at most one group a thread); all threads get it.
+__device__ __forceinline__ float least_of_groups(float mine, int groups, float (&least)[kWaves]) {
+  int d = 1;
+  for (; d < kSliceThreads / groups && d < 64; d *= 2) mine = fmaxf(mine, __shfl_xor(mine, d));
+  if (groups < kWaves) {  // a group is several waves
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) least[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    const int waves = kWaves / groups;
+    float r = __builtin_inff();
+    for (int g = 0; g < groups; ++g) {
+      float m = -__builtin_inff();
+      for (int k = 0; k < waves; ++k) m = fmaxf(m, least[g * waves + k]);
+      r = fminf(r, m);
+    }
+    return r;
+  }
+  for (; d < 64; d *= 2) mine = fminf(mine, __shfl_xor(mine, d));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) least[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  float r = least[0];
+#pragma unroll
+  for (int k = 1; k < kWaves; ++k) r = fminf(r, least[k]);
+  return r;
+}
+
+template <Elem E>
+__global__ __launch_bounds__(kSliceThreads) void beam_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m, int32_t n_slices, int groups) {
+  extern __shared__ __align__(16) char lds[];
+  RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
+  BeamShared& sh = *reinterpret_cast<BeamShared*>(lds);
+  JoinShared& join = *reinterpret_cast<JoinShared*>(lds);
+  __shared__ double roots[16];
+  __shared__ uint32_t is_last;
+  const int32_t slice = (int32_t)blockIdx.x, b = (int32_t)blockIdx.y, request = b / s.beams, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t n = s.n_out;
+  fill_roots(roots);
+  if (is_live(s, b) && !is_ended(s, b)) {
+    const Row<E> row(in, b);
+    const int32_t first = row.first_token(slice);
+    Tokens y;
+    load_slice<E>(row, r, b, first, table, y);
+    float mine = -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < kTokens; ++k) mine = fmaxf(mine, y[k]);
+    const float bound = least_of_groups(mine, groups, sh.least);
+    float top = mine;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) sh.top[wave] = top;
+    if (tid == 0) sh.n_found = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, sh.top[k]);
+    BeamSlot slot{0.0, 0.0, top};
+    u64* const list = m.lists + ((size_t)b * m.slices + slice) * n;
+    if (top > -__builtin_inff()) {
+      constexpr double per = 1.4426950408889634074;
+      slot.E = floor(octaves(top, per));
+      double sum = 0.0;
+#pragma unroll
+      for (int k = 0; k < kTokens; ++k)
+        if (y[k] > -__builtin_inff()) sum += Power(octaves(y[k], per), slot.E, roots).weight();
+      sum = wave_sum(sum);
+      if (lane == 0) sh.sum[wave] = sum;
+      uint32_t good = 0;
+#pragma unroll
+      for (int k = 0; k < kTokens; ++k) good |= (y[k] > -__builtin_inff() && y[k] >= bound ? 1u : 0u) << k;
+      uint32_t all = count_all((uint32_t)__builtin_popcount(good), sh.counts);
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) slot.sum += sh.sum[k];
+      if (all > kMostFound) {  // many equal ones: the key of the n-th best, bit by bit
+        u64 edge = 0;
+#pragma unroll 1
+        for (int bit = 63; bit >= 0; --bit) {
+          const u64 at = edge | 1ull << bit;
+          uint32_t above = 0;
+#pragma unroll
+          for (int k = 0; k < kTokens; ++k) above += y[k] > -__builtin_inff() && token_key(y[k], first + place_of(k)) >= at;
+          if (count_all(above, sh.counts) >= (uint32_t)n) edge = at;
+        }
+        good = 0;
+#pragma unroll
+        for (int k = 0; k < kTokens; ++k) good |= (y[k] > -__builtin_inff() && token_key(y[k], first + place_of(k)) >= edge ? 1u : 0u) << k;
+        all = (uint32_t)n;
+      }
+      if (good) {
+        uint32_t at = atomicAdd(&sh.n_found, (uint32_t)__builtin_popcount(good));
+#pragma unroll
+        for (int k = 0; k < kTokens; ++k)
+          if (good >> k & 1u) sh.found[at++] = token_key(y[k], first + place_of(k));
+      }
+      __syncthreads();
+      for (uint32_t i = (uint32_t)tid; i < all; i += kSliceThreads) {
+        const u64 key = sh.found[i];
+        uint32_t rank = 0;
+        for (uint32_t k = 0; k < all; ++k) rank += sh.found[k] > key;
+        if (rank < (uint32_t)n) put_out(list + rank, key);
+      }
+      if ((uint32_t)tid >= all && tid < n) put_out(list + tid, (u64)0);
+    }
+    if (tid == 0) {
+      BeamSlot& out = m.slots[(size_t)b * m.slices + slice];
+      put_out(&out.E, slot.E);
+      put_out(&out.sum, slot.sum);
+      put_out(&out.top, slot.top);
+    }
+  }
+  if (!last_of(m.arrived + request, (uint32_t)(n_slices * s.beams), is_last)) return;
+
+  // ---- the request's lists
+  const int32_t b0 = request * s.beams;
+  for (int32_t i = wave; i < s.beams; i += kWaves) {  // a wave a row
+    const BeamSlot* const slots = m.slots + (size_t)(b0 + i) * m.slices;
+    const bool ended = is_ended(s, b0 + i), live = is_live(s, b0 + i);
+    double base = -__builtin_inf();
+    if (live && !ended) {
+      float top = -__builtin_inff();
+      double most = -__builtin_inf();
+      for (int32_t k = lane; k < n_slices; k += 64) {
+        const float t = take_in(&slots[k].top);
+        top = fmaxf(top, t);
+        if (t > -__builtin_inff()) most = fmax(most, take_in(&slots[k].E));
+      }
+#pragma unroll
+      for (int d = 32; d; d >>= 1) {
+        top = fmaxf(top, __shfl_xor(top, d));
+        most = fmax(most, __shfl_xor(most, d));
+      }
+      double sum = 0.0;
+      for (int32_t k = lane; k < n_slices; k += 64) {
+        const bool some = take_in(&slots[k].top) > -__builtin_inff();
+        const double d = some ? take_in(&slots[k].E) - most : -2000.0;
+        if (d > -1100.0) sum += ldexp(take_in(&slots[k].sum), (int)d);
+      }
+      sum = wave_sum(sum);
+      // (relative to the largest logit's own weight: a token that is alone costs nothing)
+      constexpr double per = 1.4426950408889634074;
+      if (top > -__builtin_inff()) base = (double)s.scores[b0 + i] - ((double)top + log(sum / Power(octaves(top, per), most, roots).weight()));
+    } else if (live) {
+      base = (double)s.scores[b0 + i];
+    }
+    if (lane == 0) {
+      join.base[i] = base;
+      join.is_ended[i] = ended;
+    }
+  }
+  if (tid == 0) join.n_joined = 0;
+  __syncthreads();
+  const int32_t per_row = n_slices * n, entries = s.beams * per_row;
+  // f(entry's order, its place) for the thread's entries
+  auto for_entries = [&](auto&& f) {
+    for (int32_t e = tid; e < entries; e += kSliceThreads) {
+      const int32_t beam = e / per_row, in_row = e % per_row;
+      const double base = join.base[beam];
+      if (!(base > -__builtin_inf())) continue;
+      if (join.is_ended[beam]) {
+        if (in_row == 0) f(order_of(base), place_in(beam, (u64)key_of(0.0f) << 32));
+        continue;
+      }
+      const size_t at = (size_t)(b0 + beam) * m.slices + in_row / n;
+      if (!(take_in(&m.slots[at].top) > -__builtin_inff())) continue;
+      const u64 key = take_in(m.lists + at * n + in_row % n);
+      if (key) f(order_of((double)logit_of(key) + base), place_in(beam, key));
+    }
+  };
+  u64 edge = 0, edge_place = 0;  // what counts: more than edge, or edge itself with edge_place or more
+  uint32_t all = 0;
+  {
+    uint32_t mine = 0;
+    for_entries([&](u64, u64) { ++mine; });
+    all = count_all(mine, join.counts);
+  }
+  if (all > kMostJoined) {
+#pragma unroll 1
+    for (int bit = 63; bit >= 0; --bit) {
+      const u64 at = edge | 1ull << bit;
+      uint32_t mine = 0;
+      for_entries([&](u64 order, u64) { mine += order >= at; });
+      if (count_all(mine, join.counts) >= (uint32_t)n) edge = at;
+    }
+#pragma unroll 1
+    for (int bit = 63; bit >= 0; --bit) {
+      const u64 at = edge_place | 1ull << bit;
+      uint32_t mine = 0;
+      for_entries([&](u64 order, u64 place) { mine += order > edge || (order == edge && place >= at); });
+      if (count_all(mine, join.counts) >= (uint32_t)n) edge_place = at;
+    }
+    all = (uint32_t)n;
+  }
+  for_entries([&](u64 order, u64 place) {
+    if (order > edge || (order == edge && place >= edge_place)) {
+      const uint32_t at = atomicAdd(&join.n_joined, 1u);
+      join.order[at] = order;
+      join.place[at] = place;
+    }
+  });
+  if (tid < n) {
+    join.rows[tid] = join.ids[tid] = -1;
+    join.scores[tid] = -__builtin_inff();
+  }
+  __syncthreads();
+  for (uint32_t i = (uint32_t)tid; i < all; i += kSliceThreads) {
+    const u64 order = join.order[i], place = join.place[i];
+    uint32_t rank = 0;
+    for (uint32_t k = 0; k < all; ++k) rank += join.order[k] > order || (join.order[k] == order && join.place[k] > place);
+    if (rank < (uint32_t)n) {
+      const int32_t beam = beam_of(place);
+      join.rows[rank] = b0 + beam;
+      join.ids[rank] = join.is_ended[beam] ? -1 : id_at(place);
+      join.scores[rank] = (float)sum_of(order);
+    }
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  // one wave writes out; placed: a row's first continuation takes the row's own place, the others what is left, in order
+  for (int32_t i0 = 0; i0 < n; i0 += 64) {
+    const int32_t i = i0 + lane;
+    int32_t to = i;
+    if (s.placed) {  // (n is the number of beams, so that there is one round)
+      const int32_t parent = i < n ? join.rows[i] - b0 : -1;
+      bool is_first = i < n && join.rows[i] >= 0;
+      for (int32_t k = 0; k < i && k < n; ++k) is_first = is_first && join.rows[k] - b0 != parent;
+      uint64_t places = 0;
+      for (int32_t k = 0; k < n; ++k) {
+        const int f = __shfl((int)is_first, k), p = __shfl(parent, k);
+        if (f) places |= 1ull << p;
+      }
+      const uint64_t others = __ballot(i < n && !is_first);
+      if (is_first) to = parent;
+      else {
+        uint64_t left = ~places;
+        for (int k = __builtin_popcountll(others & ((1ull << lane) - 1ull)); k > 0; --k) left &= left - 1;
+        to = __builtin_ctzll(left | 1ull << 63);
+      }
+    }
+    if (i < n) {
+      s.rows[(size_t)request * n + to] = join.rows[i];
+      s.ids[(size_t)request * n + to] = join.ids[i];
+      s.out_scores[(size_t)request * n + to] = join.scores[i];
+    }
+  }
+}
+
+// ------------------------------------------------------------------ what rows keep
+// In place, whatever goes where: a workgroup takes the same region of every row that moves, in stretches that its registers hold at once:
+// it reads a stretch of all of them, and writes when all of it is read.  No workgroup's region is another's.
+constexpr int kMoveThreads = 256, kMoveUnits = 8;  // a thread's of a stretch
+constexpr int kMaxMoveRows = 1024;
+struct RowDataList {
+  RowData of[kMaxRowData];
+  int64_t first[kMaxRowData + 1];  // workgroup of each
+  int32_t unit[kMaxRowData];       // bytes: 1, 2, 4, 8 or 16
+  int32_t region;                  // units of a row that a workgroup takes, a power of two
+};
+template <class T>
+__device__ __forceinline__ void move_region(const RowData& d, char* base, int64_t begin, int64_t end, int32_t units, const int32_t* to, const int32_t* from, const int64_t* limit, int32_t moved) {
+  // stretches of 2^shift units
+  int shift = 0;
+  while ((2 << shift) * moved <= kMoveThreads * kMoveUnits && (2 << shift) <= units) ++shift;
+  // (more rows than that holds of a single unit: there are at most kMaxMoveRows)
+  static_assert(kMaxMoveRows <= kMoveThreads * kMoveUnits, "a unit of every row fits");
+  const int64_t stretch = (int64_t)sizeof(T) << shift;
+  for (int64_t at = begin; at < end; at += stretch) {
+    T x[kMoveUnits];
+    bool ok[kMoveUnits];
+#pragma unroll
+    for (int k = 0; k < kMoveUnits; ++k) {
+      const int32_t u = k * kMoveThreads + (int32_t)threadIdx.x, i = u >> shift;
+      const int64_t in = at + (int64_t)(u & ((1 << shift) - 1)) * (int64_t)sizeof(T);
+      ok[k] = i < moved && in < end && in < limit[i < moved ? i : 0];
+      if (ok[k]) x[k] = *reinterpret_cast<const T*>(base + from[i] * d.row_stride + in);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);  // (everything is read)
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kMoveUnits; ++k) {
+      const int32_t u = k * kMoveThreads + (int32_t)threadIdx.x, i = u >> shift;
+      const int64_t in = at + (int64_t)(u & ((1 << shift) - 1)) * (int64_t)sizeof(T);
+      if (ok[k]) *reinterpret_cast<T*>(base + to[i] * d.row_stride + in) = x[k];
+    }
+  }
+}
+__global__ __launch_bounds__(kMoveThreads) void reorder_kernel(RowDataList list, int n, const int32_t* __restrict__ source, int32_t B) {
+  __shared__ int32_t to[kMaxMoveRows], from[kMaxMoveRows];
+  __shared__ int64_t limit[kMaxMoveRows];
+  __shared__ int32_t n_moved;
+  int which = 0;
+  while (which + 1 < n && (int64_t)blockIdx.x >= list.first[which + 1]) ++which;
+  const RowData& d = list.of[which];
+  const int64_t region = (int64_t)list.region * list.unit[which], regions = (d.part_bytes + region - 1) / region;
+  const int64_t group = (int64_t)blockIdx.x - list.first[which], piece = group / regions, begin = group % regions * region;
+  const int64_t end = begin + region < d.part_bytes ? begin + region : d.part_bytes;
+  if (threadIdx.x == 0) n_moved = 0;
+  __syncthreads();
+  for (int32_t b = (int32_t)threadIdx.x; b < B; b += kMoveThreads) {
+    const int32_t a = source[b];
+    if (a < 0 || a >= B || a == b) continue;
+    const int64_t most = d.used ? (int64_t)d.used[a] * d.used_bytes : d.part_bytes;
+    if (most <= begin) continue;
+    const int32_t i = atomicAdd(&n_moved, 1);
+    to[i] = b;
+    from[i] = a;
+    limit[i] = most;
+  }
+  __syncthreads();
+  const int32_t moved = n_moved;
+  if (!moved) return;
+  char* const base = static_cast<char*>(d.data) + piece / d.n_parts * d.outer_stride + piece % d.n_parts * d.part_stride;
+  switch (list.unit[which]) {
+    case 16: move_region<uint4>(d, base, begin, end, list.region, to, from, limit, moved); break;
+    case 8: move_region<uint2>(d, base, begin, end, list.region, to, from, limit, moved); break;
+    case 4: move_region<uint32_t>(d, base, begin, end, list.region, to, from, limit, moved); break;
+    case 2: move_region<uint16_t>(d, base, begin, end, list.region, to, from, limit, moved); break;
+    default: move_region<uint8_t>(d, base, begin, end, list.region, to, from, limit, moved); break;
+  }
+}
+
+}  // namespace
+
+size_t beam_bytes(int32_t max_rows, int32_t V) {
+  size_t bytes = 0;
+  (void)memory_at(nullptr, max_rows, V, &bytes);
+  return bytes;
+}
+namespace {
+template <Elem E> hipError_t select(const Logits& in, const LogitRules& r, const BeamSearch& s, const BeamMemory& m, hipStream_t stream) {
+  const size_t lds = has_rules(r) && sizeof(RuleTable) > sizeof(JoinShared) ? sizeof(RuleTable) : sizeof(JoinShared) > sizeof(BeamShared) ? sizeof(JoinShared) : sizeof(BeamShared);
+  const int32_t n = slices_of<E>(in);
+  int groups = 1;
+  while (groups < s.n_out) groups *= 2;
+  hipLaunchKernelGGL(beam_kernel<E>, dim3(n, s.requests * s.beams), dim3(kSliceThreads), lds, stream, in, r, s, m, n, groups);
+  return hipGetLastError();
+}
+}  // namespace
+hipError_t launch_beam_select(const Logits& in, Elem type, const LogitRules& r, const BeamSearch& s, void* memory, int32_t max_rows, int32_t max_V, hipStream_t stream) {
+  size_t bytes;
+  const BeamMemory m = memory_at(memory, max_rows, max_V, &bytes);
+  if (type == Elem::kF32) return select<Elem::kF32>(in, r, s, m, stream);
+  if (type == Elem::kBF16) return select<Elem::kBF16>(in, r, s, m, stream);
+  return select<Elem::kF16>(in, r, s, m, stream);
+}
+
+hipError_t launch_reorder_rows(const RowData* data, int n, const int32_t* source, int32_t B, hipStream_t stream) {
+  RowDataList list{};
+  auto groups = [&](int32_t region) {
+    int64_t all = 0;
+    for (int i = 0; i < n; ++i) {
+      list.first[i] = all;
+      const int64_t bytes = (int64_t)region * list.unit[i];
+      all += (int64_t)data[i].n_outer * data[i].n_parts * ((data[i].part_bytes + bytes - 1) / bytes);
+    }
+    return all;
+  };
+  for (int i = 0; i < n; ++i) {
+    list.of[i] = data[i];
+    uint64_t all = 16 | reinterpret_cast<uintptr_t>(data[i].data) | (uint64_t)data[i].row_stride | (uint64_t)data[i].part_bytes;
+    if (data[i].n_outer > 1) all |= (uint64_t)data[i].outer_stride;
+    if (data[i].n_parts > 1) all |= (uint64_t)data[i].part_stride;
+    if (data[i].used) all |= (uint64_t)data[i].used_bytes;
+    list.unit[i] = (int32_t)(all & (~all + 1));
+  }
+  list.region = 1024;
+  while (list.region > 64 && groups(list.region) < 2048) list.region /= 2;
+  while (list.region < (1 << 20) && groups(list.region) > (1 << 20)) list.region *= 2;
+  const int64_t all = groups(list.region);
+  if (all > INT32_MAX) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(reorder_kernel, dim3((uint32_t)all), dim3(kMoveThreads), 0, stream, list, n, source, B);
+  return hipGetLastError();
+}
+
+}  // namespace xgm

@@ -30,6 +30,11 @@ struct {
   int (*batch_fill_and_apply)(void*, void*, void*, int, int32_t, int64_t, void*);
   int (*q4_logits_ex)(const void*, int, int32_t, int32_t, int64_t, const void*, const void*, const void*, int32_t, int32_t, void*, int, int64_t, const void*, int32_t, void*);
   int (*process_logits)(const void*, int, int32_t, int32_t, int64_t, const void*, void*, int64_t, void*);
+  int (*f8_logits)(const void*, int, const void*, int32_t, int32_t, int64_t, const void*, const void*, int32_t, void*, int, int64_t, const void*, int32_t, void*, void*);
+  int (*q4_embed)(const void*, int32_t, const void*, const void*, int, const void*, int32_t, int32_t, int32_t, float, void*, int, int64_t, void*);
+  int (*f8_embed)(const void*, int32_t, const void*, const void*, int32_t, int32_t, float, void*, int, int64_t, void*);
+  int (*beam_select)(void*, const void*, int, int32_t, int32_t, int32_t, int64_t, const void*, const void*, const void*, int32_t, int32_t, void*, void*, void*, void*);
+  int (*reorder_rows)(const void*, int32_t, const void*, int32_t, void*);
   int (*sample)(void*, const void*, int, int32_t, int32_t, int64_t, const void*, const void*, void*, void*, void*);
 } api;
 struct { const char* name; void** slot; } const kEntries[] = {
@@ -49,6 +54,11 @@ struct { const char* name; void** slot; } const kEntries[] = {
     {"xgm_q4_logits_ex", (void**)&api.q4_logits_ex},
     {"xgm_process_logits", (void**)&api.process_logits},
     {"xgm_sample", (void**)&api.sample},
+    {"xgm_f8_logits", (void**)&api.f8_logits},
+    {"xgm_q4_embed", (void**)&api.q4_embed},
+    {"xgm_f8_embed", (void**)&api.f8_embed},
+    {"xgm_beam_select", (void**)&api.beam_select},
+    {"xgm_reorder_rows", (void**)&api.reorder_rows},
 };
 PyObject* g_error_class = nullptr;  // XgmError(status, message)
 PyObject *g_logit_rules = nullptr, *g_draw_rules = nullptr;
@@ -342,6 +352,72 @@ PyObject* sample(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_END_ALLOW_THREADS
   return result(rc);
 }
+// f8_logits(d_hidden, dtype, d_hidden_scales, rows, k, hidden_stride, d_codes, d_scales, v, d_logits, logits_dtype, row_stride, d_bitmask, v_mask, d_work, stream)
+PyObject* f8_logits(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 16) return PyErr_Format(PyExc_TypeError, "f8_logits takes 16 arguments");
+  int64_t v[16];
+  if (!values(args, v, "aiaiiiaaiaiiaiaa")) return nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = api.f8_logits(pointer(v[0]), (int)v[1], pointer(v[2]), (int32_t)v[3], (int32_t)v[4], v[5], pointer(v[6]), pointer(v[7]), (int32_t)v[8], pointer(v[9]),
+                     (int)v[10], v[11], pointer(v[12]), (int32_t)v[13], pointer(v[14]), pointer(v[15]));
+  Py_END_ALLOW_THREADS
+  return result(rc);
+}
+// q4_embed(d_ids, n, d_codes, d_scales, scales_dtype, d_zeros, v, k, group, factor, d_out, out_dtype, out_stride, stream)
+PyObject* q4_embed(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 14) return PyErr_Format(PyExc_TypeError, "q4_embed takes 14 arguments");
+  int64_t v[9], o[4];
+  if (!values(args, v, "aiaaiaiii") || !values(args + 10, o, "aiia")) return nullptr;
+  const double factor = PyFloat_AsDouble(args[9]);
+  if (factor == -1.0 && PyErr_Occurred()) return nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = api.q4_embed(pointer(v[0]), (int32_t)v[1], pointer(v[2]), pointer(v[3]), (int)v[4], pointer(v[5]), (int32_t)v[6], (int32_t)v[7], (int32_t)v[8],
+                    (float)factor, pointer(o[0]), (int)o[1], o[2], pointer(o[3]));
+  Py_END_ALLOW_THREADS
+  return result(rc);
+}
+// f8_embed(d_ids, n, d_codes, d_scales, v, k, factor, d_out, out_dtype, out_stride, stream)
+PyObject* f8_embed(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 11) return PyErr_Format(PyExc_TypeError, "f8_embed takes 11 arguments");
+  int64_t v[6], o[4];
+  if (!values(args, v, "aiaaii") || !values(args + 7, o, "aiia")) return nullptr;
+  const double factor = PyFloat_AsDouble(args[6]);
+  if (factor == -1.0 && PyErr_Occurred()) return nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = api.f8_embed(pointer(v[0]), (int32_t)v[1], pointer(v[2]), pointer(v[3]), (int32_t)v[4], (int32_t)v[5], (float)factor, pointer(o[0]), (int)o[1], o[2],
+                    pointer(o[3]));
+  Py_END_ALLOW_THREADS
+  return result(rc);
+}
+// beam_select(beams, d_logits, dtype, requests, n_beams, v, row_stride, rules, d_scores, d_ended, n_out, placed, d_rows, d_ids, d_out_scores, stream)
+PyObject* beam_select(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 16) return PyErr_Format(PyExc_TypeError, "beam_select takes 16 arguments");
+  int64_t v[6], o[8];
+  Rules r;
+  void* h;
+  if (!attribute(args[0], s_h, &h) || !values(args + 1, v, "aiiiii") || !r.get(args[7], g_logit_rules) || !values(args + 8, o, "aaiiaaaa")) return nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = api.beam_select(h, pointer(v[0]), (int)v[1], (int32_t)v[2], (int32_t)v[3], (int32_t)v[4], v[5], r.at(), pointer(o[0]), pointer(o[1]), (int32_t)o[2],
+                       (int32_t)o[3], pointer(o[4]), pointer(o[5]), pointer(o[6]), pointer(o[7]));
+  Py_END_ALLOW_THREADS
+  return result(rc);
+}
+// reorder_rows(set, n, d_rows, rows, stream)
+PyObject* reorder_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 5) return PyErr_Format(PyExc_TypeError, "reorder_rows takes 5 arguments");
+  int64_t v[4];
+  void* at;
+  if (!attribute(args[0], s_addr, &at) || !values(args + 1, v, "iaia")) return nullptr;
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = api.reorder_rows(at, (int32_t)v[0], pointer(v[1]), (int32_t)v[2], pointer(v[3]));
+  Py_END_ALLOW_THREADS
+  return result(rc);
+}
 
 #define FAST(fn) (PyCFunction)(void (*)(void))(fn), METH_FASTCALL
 #define FAST_KW(fn) (PyCFunction)(void (*)(void))(fn), METH_FASTCALL | METH_KEYWORDS
@@ -396,6 +472,11 @@ PyMethodDef kFunctions[] = {
     {"q4_logits", FAST(q4_logits), nullptr},
     {"process_logits", FAST(process_logits), nullptr},
     {"sample", FAST(sample), nullptr},
+    {"f8_logits", FAST(f8_logits), nullptr},
+    {"q4_embed", FAST(q4_embed), nullptr},
+    {"f8_embed", FAST(f8_embed), nullptr},
+    {"beam_select", FAST(beam_select), nullptr},
+    {"reorder_rows", FAST(reorder_rows), nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "the per-step calls of binding.py", -1, kFunctions, nullptr, nullptr, nullptr, nullptr};
