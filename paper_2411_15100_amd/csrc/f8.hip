@@ -24,13 +24,16 @@ __device__ __forceinline__ f16x8 halves(uint32_t lo, uint32_t hi) {
   const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, true);
   return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+struct Halves {  // 32 numbers of a row
+  f16x8 of[4];
+  __device__ __forceinline__ Halves(uint4v lo, uint4v hi) : of{halves(lo[0], lo[1]), halves(lo[2], lo[3]), halves(hi[0], hi[1]), halves(hi[2], hi[3])} {}
+};
 // 16 x 16 sums over 128 columns, of which a lane holds 32 of its row: the same ones on both sides, whichever they are.
-__device__ __forceinline__ float4v products(uint4v a0, uint4v a1, uint4v b0, uint4v b1) {
+__device__ __forceinline__ float4v products(const Halves& a, const Halves& b) {
   float4v c = {0, 0, 0, 0};
-  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(a0[0], a0[1]), halves(b0[0], b0[1]), c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(a0[2], a0[3]), halves(b0[2], b0[3]), c, 0, 0, 0);
-  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(a1[0], a1[1]), halves(b1[0], b1[1]), c, 0, 0, 0);
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(a1[2], a1[3]), halves(b1[2], b1[3]), c, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.of[i], b.of[i], c, 0, 0, 0);
+  return c;
 }
 
 __device__ __forceinline__ void store_logit(const F8Head& h, Elem type, int64_t at, float y) {
@@ -94,7 +97,7 @@ __device__ __forceinline__ float most_of_16(float m) {
 }
 // 16 lanes to a block.  Columns behind K, up to `width`, become zeros.
 template <Elem E>
-__global__ __launch_bounds__(256) void f8_quantize_kernel(const void* x, int64_t stride, int32_t B, int32_t K, int32_t width, uint8_t* codes, int64_t codes_stride, float* scales) {
+__global__ __launch_bounds__(256) void f8_quantize_kernel(const void* x, int64_t stride, int32_t B, int32_t K, int32_t width, uint8_t* codes, int64_t codes_stride, float* scales, int64_t scales_row, int64_t scales_block) {
   const int32_t blocks = f8_blocks(K);
   const int64_t block = ((int64_t)blockIdx.x * 256 + threadIdx.x) / 16;
   if (block >= (int64_t)B * blocks) return;  // (16 lanes together)
@@ -104,44 +107,409 @@ __global__ __launch_bounds__(256) void f8_quantize_kernel(const void* x, int64_t
   else v.clear();
   const uint32_t e = exponent_of(most_of_16(v.most()));
   if (k < width) *reinterpret_cast<uint2*>(codes + b * codes_stride + k) = v.codes(__uint_as_float((254u - e) << 23));
-  if (((int32_t)threadIdx.x & 15) == 0) scales[block] = __uint_as_float(e << 23);
+  if (((int32_t)threadIdx.x & 15) == 0) scales[b * scales_row + kb * scales_block] = __uint_as_float(e << 23);
 }
 
 // ------------------------------------------------------------------- the projection
-// A wave takes 16 rows of the matrix and 16 of the batch.
-__global__ __launch_bounds__(256) void f8_logits_kernel(F8Head h, Elem out_type) {
-  const int32_t lane = (int32_t)threadIdx.x & 63, n = lane & 15, q = lane >> 4;
-  const int64_t v0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 16;
-  const int32_t b0 = (int32_t)blockIdx.y * 16;
-  if (v0 >= h.V) return;
-  const int64_t v = min(v0 + n, (int64_t)h.V - 1);
-  const int32_t b = min(b0 + n, h.B - 1), blocks = f8_blocks(h.K);
-  const uint8_t* const row = h.codes + v * h.K;
-  const uint8_t* const state = static_cast<const uint8_t*>(h.hidden.at) + b * h.hidden.stride;
-  const float* const row_scales = h.scales + (v0 >> 7) * blocks;  // (16 rows lie in one block)
-  const float* const state_scales = h.hidden.scales + (int64_t)b * blocks;
-  float4v acc = {0, 0, 0, 0};
-  for (int32_t kb = 0; kb < blocks; ++kb) {
-    const int32_t k0 = kb * 128 + q * 16, k1 = k0 + 64;
-    const uint4v none = {0, 0, 0, 0};
-    uint4v a0 = none, a1 = none, x0 = none, x1 = none;
-    if (k0 < h.K) {
-      a0 = *reinterpret_cast<const uint4v*>(row + k0);
-      x0 = *reinterpret_cast<const uint4v*>(state + k0);
+// Lists the rows of the matrix among the `here` <= kListed from `base` (a multiple of 16) on that some of the `rows` rows of the batch
+// from first_b on allows, as numbers behind base, and masks the logits of the others.  Returns how many.
+constexpr int kListed = 1024;
+struct List {
+  int32_t row[kListed];
+  uint32_t any[kListed / 32];
+  int32_t n;
+};
+__device__ __forceinline__ bool allowed(const F8Head& h, int32_t b, int64_t token) {
+  return !h.mask || (token < h.V_mask && (h.mask[(size_t)b * h.W_mask + (token >> 5)] >> (token & 31) & 1u));
+}
+__device__ int32_t list_rows(const F8Head& h, Elem out_type, int32_t first_b, int32_t rows, int64_t base, int32_t here, List& list) {
+  const int32_t tid = (int32_t)threadIdx.x, threads = (int32_t)blockDim.x;
+  __syncthreads();
+  if (tid < kListed / 32) list.any[tid] = 0;
+  if (tid == 0) list.n = 0;
+  __syncthreads();
+  const int32_t w0 = (int32_t)(base >> 5), shift = (int32_t)(base & 31), words = (here + shift + 31) / 32;
+  for (int32_t i = tid; i < words * rows; i += threads) {
+    const int32_t b = i / words, w = i % words;
+    uint32_t m = w0 + w < h.W_mask ? h.mask[(size_t)(first_b + b) * h.W_mask + w0 + w] : 0u;
+    if (w0 + w == h.V_mask >> 5) m &= (1u << (h.V_mask & 31)) - 1u;  // (what lies behind the masks' vocabulary is not listed)
+    if (m && shift) {
+      if (w > 0) atomicOr(&list.any[w - 1], m << 16);
+      if (w < kListed / 32) atomicOr(&list.any[w], m >> 16);
+    } else if (m) {
+      atomicOr(&list.any[w], m);
     }
-    if (k1 < h.K) {
-      a1 = *reinterpret_cast<const uint4v*>(row + k1);
-      x1 = *reinterpret_cast<const uint4v*>(state + k1);
-    }
-    acc += products(a0, a1, x0, x1) * (row_scales[kb] * state_scales[kb]);
   }
-  for (int i = 0; i < 4; ++i) {
-    const int64_t token = v0 + q * 4 + i;
-    if (token >= h.V || b0 + n >= h.B) continue;
-    const bool ok = !h.mask || (token < h.V_mask && (h.mask[(size_t)b * h.W_mask + (token >> 5)] >> (token & 31) & 1u));
-    store_logit(h, out_type, b * h.logits_stride + token, ok ? acc[i] : -__builtin_inff());
+  __syncthreads();
+  for (int32_t r = tid; r < here; r += threads) {
+    if (list.any[r >> 5] >> (r & 31) & 1u) {
+      int32_t place = __builtin_popcount(list.any[r >> 5] & ((1u << (r & 31)) - 1u));
+      for (int32_t w = 0; w < r >> 5; ++w) place += __builtin_popcount(list.any[w]);
+      list.row[place] = r;
+      atomicAdd(&list.n, 1);
+    } else {
+      for (int32_t b = 0; b < rows; ++b) store_logit(h, out_type, (int64_t)(first_b + b) * h.logits_stride + base + r, -__builtin_inff());
+    }
+  }
+  __syncthreads();
+  return list.n;
+}
+
+// ---------------------------------------------------------------- few rows in the batch
+// Shares of 16 NB rows, whose hidden states fit LDS in 8 bits; a workgroup brings them there itself.  A wave takes 16 rows of the matrix (a
+// tile) and all columns, so that waves need nothing of each other: it reads the codes a step of kStep blocks of 128 columns at a
+// time, the next ones while it multiplies the last.  Under masks the workgroup lists the rows of its share that some request
+// allows, and its waves take 16 of those at a time.  Where a workgroup has fewer tiles than waves, several waves take the steps of one
+// in turn and their sums meet in LDS.
+constexpr int kFewThreads = 1024;
+constexpr int kStep = 2;
+constexpr uint32_t kMaxLds = 160 * 1024;
+struct FewLayout {  // of dynamic LDS, bytes
+  uint32_t scales, partial, list, end;
+};
+__host__ __device__ inline FewLayout few_layout(int32_t K, int32_t rows, int nb) {
+  const uint32_t blocks = (uint32_t)f8_blocks(K);
+  FewLayout l;
+  l.scales = blocks * 128 * (uint32_t)rows;
+  l.partial = l.scales + (blocks * (uint32_t)rows * 4 + 15) / 16 * 16;
+  l.list = l.partial + kFewThreads * 16;
+  l.end = l.list + (uint32_t)sizeof(List);
+  (void)nb;
+  return l;
+}
+enum class States : int { kF8, kBF16, kF16 };
+
+template <States T, int NB, bool kMasked>
+__global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_type, int32_t tiles_each) {
+  extern __shared__ __align__(16) char lds[];
+  const int32_t tid = (int32_t)threadIdx.x, threads = (int32_t)blockDim.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = threads >> 6;
+  const int32_t n = lane & 15, q = lane >> 4;
+  const int32_t first_b = (int32_t)blockIdx.y * 16 * NB, rows = min(h.B - first_b, 16 * NB), blocks = f8_blocks(h.K);
+  const FewLayout at = few_layout(h.K, min(h.B, 16 * NB), NB);
+  uint4v* const hidden = reinterpret_cast<uint4v*>(lds);  // [block][16 columns][row]
+  float* const hidden_scales = reinterpret_cast<float*>(lds + at.scales);  // [block][row]
+  float4v* const partial = reinterpret_cast<float4v*>(lds + at.partial);
+  List& list = *reinterpret_cast<List*>(lds + at.list);
+
+  const int32_t n_steps = (blocks + kStep - 1) / kStep;
+  const int64_t row0 = (int64_t)blockIdx.x * tiles_each * 16, row1 = min((int64_t)h.V, row0 + (int64_t)tiles_each * 16);
+  struct Codes {
+    uint4v of[kStep][2];
+    float scale[kStep];
+  };
+  auto load = [&](const uint8_t* row, const float* scales, int32_t step, Codes& c) {
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      const int32_t block = min(step * kStep + j, blocks - 1);
+      // (behind the last column some earlier part of the row: hidden states are 0 there)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) c.of[j][i] = *reinterpret_cast<const uint4v*>(row + min(block * 128 + i * 64 + q * 16, h.K - 16));
+      c.scale[j] = scales[block];
+    }
+  };
+
+  bool brought = false;
+  for (int64_t base = row0; base < row1; base += kListed) {
+    const int32_t here = (int32_t)min((int64_t)kListed, row1 - base);
+    int32_t count = here;
+    if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, list);
+    const int32_t tiles = (count + 15) / 16;
+    int32_t sharing = 1;  // waves to a tile, no more than there are where masks leave no tile
+    while (sharing * 2 <= n_steps && sharing * 2 * max(tiles, 1) <= waves) sharing *= 2;
+    const int32_t sub = wave & (sharing - 1), abreast = waves / sharing, rounds = (tiles + abreast - 1) / abreast;
+    auto row_of = [&](int32_t t, int32_t i) -> int32_t {  // the i-th of a tile
+      const int32_t k = min(t * 16 + i, count - 1);
+      return kMasked ? list.row[k] : k;
+    };
+    Codes codes, next_codes;
+    int32_t t = wave / sharing;
+    const uint8_t *row = nullptr, *next_row = nullptr;
+    const float *scales = nullptr, *next_scales = nullptr;
+    auto point = [&](int32_t tile, const uint8_t*& r, const float*& s) {
+      const int64_t v = base + row_of(tile, n);
+      r = h.codes + v * h.K;
+      s = h.scales + (v >> 7) * blocks;
+    };
+    if (t < tiles) {
+      point(t, row, scales);
+      load(row, scales, sub, codes);
+      next_row = row;
+      next_scales = scales;
+    }
+    if (!brought) {  // (the first codes are on their way meanwhile)
+      brought = true;
+      const int32_t units = blocks * rows * 16;  // 8 columns each, 16 neighbouring threads to a block
+      for (int32_t u0 = 0; u0 < units; u0 += threads) {
+        const int32_t u = u0 + tid, k8 = u & 15, b = (u >> 4) % rows, block = (u >> 4) / rows, k = block * 128 + k8 * 8;
+        if (u >= units) break;
+        uint2 w = {0, 0};
+        float scale;
+        if constexpr (T == States::kF8) {
+          if (k < h.K) w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(h.hidden.at) + (first_b + b) * h.hidden.stride + k);
+          scale = h.hidden.scales[(int64_t)(first_b + b) * blocks + block];
+        } else {
+          Eight<T == States::kF16 ? Elem::kF16 : Elem::kBF16> x;
+          if (k < h.K) x.load(static_cast<const uint16_t*>(h.hidden.at) + (first_b + b) * h.hidden.stride + k);
+          else x.clear();
+          const uint32_t e = exponent_of(most_of_16(x.most()));
+          w = x.codes(__uint_as_float((254u - e) << 23));
+          scale = __uint_as_float(e << 23);
+        }
+        reinterpret_cast<uint2*>(hidden)[((block * 8 + (k8 >> 1)) * rows + b) * 2 + (k8 & 1)] = w;
+        if (k8 == 0) hidden_scales[block * rows + b] = scale;
+      }
+      __syncthreads();
+    }
+    for (int32_t round = 0; round < rounds; ++round) {
+      float4v acc[NB];
+      for (int nb = 0; nb < NB; ++nb) acc[nb] = float4v{0, 0, 0, 0};
+      if (t < tiles) {
+        for (int32_t step = sub; step < n_steps; step += sharing) {
+          int32_t next_step = step + sharing;
+          bool more = true;
+          if (next_step >= n_steps) {
+            next_step = sub;
+            more = t + abreast < tiles;
+            if (more) point(t + abreast, next_row, next_scales);
+          }
+          if (more) load(next_row, next_scales, next_step, next_codes);
+#pragma unroll
+          for (int j = 0; j < kStep; ++j) {
+            const int32_t block = step * kStep + j;
+            if (block >= blocks) break;
+            const Halves a(codes.of[j][0], codes.of[j][1]);
+            // the scale of a row lies with the lane that holds its codes; the sums of rows 4 q .. lie elsewhere
+            float4v scale;
+            if constexpr (kMasked) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) scale[i] = __shfl(codes.scale[j], q * 4 + i);
+            } else {
+              scale[0] = codes.scale[j];  // (16 rows lie in one block of the matrix)
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              const int32_t b = min(nb * 16 + n, rows - 1);
+              const Halves x(hidden[(block * 8 + q) * rows + b], hidden[(block * 8 + 4 + q) * rows + b]);
+              const float4v sum = products(a, x);
+              const float state_scale = hidden_scales[block * rows + b];
+              if constexpr (kMasked) acc[nb] += sum * (scale * state_scale);
+              else acc[nb] += sum * (scale[0] * state_scale);
+            }
+          }
+          codes = next_codes;
+        }
+      }
+      for (int nb = 0; nb < NB; ++nb) {
+        if (sharing > 1) {
+          partial[tid] = acc[nb];
+          __syncthreads();
+          if (sub == 0)
+            for (int32_t w = 1; w < sharing; ++w) acc[nb] += partial[tid + w * 64];
+          __syncthreads();
+        }
+        if (sub == 0 && t < tiles && nb * 16 + n < rows) {
+          const int32_t b = first_b + nb * 16 + n;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (t * 16 + q * 4 + i >= count) continue;
+            const int64_t token = base + row_of(t, q * 4 + i);
+            store_logit(h, out_type, b * h.logits_stride + token, !kMasked || allowed(h, b, token) ? acc[nb][i] : -__builtin_inff());
+          }
+        }
+      }
+      t += abreast;
+      row = next_row;
+      scales = next_scales;
+    }
   }
 }
+
+// --------------------------------------------------------------- many rows in the batch
+// Up to 16 MW WM rows and any number of columns, both sides in 8 bits through LDS, a block of 128 columns at a time in two buffers.  The eight
+// waves of a workgroup form WM groups that share the rows of the batch, and in each 8 / WM waves that share the matrix, up to TW tiles
+// each.  While a block is multiplied, the next one goes from registers to the other buffer and the one after is read from memory; one
+// barrier a block.  16 bytes of a row lie in LDS at their place in the row with the row's last three bits exchanged into it: eight rows
+// of one place, as a wave reads them, lie in different banks.
+constexpr int kManyThreads = 512, kManyWaves = kManyThreads / 64;
+template <int MW, int WM, int TW> struct ManyShape {
+  static constexpr int kRows = 16 * MW * WM, kWide = kManyWaves / WM, kPass = kWide * TW, kMatrix = 16 * kPass;
+  static constexpr int kStateUnits = (kRows * 8 + kManyThreads - 1) / kManyThreads, kCodeUnits = kMatrix * 8 / kManyThreads;
+};
+template <int MW, int WM, int TW> struct ManyShared {
+  typedef ManyShape<MW, WM, TW> Shape;
+  uint4v states[2][Shape::kRows * 8];
+  uint4v codes[2][Shape::kMatrix * 8];
+  float state_scales[2][Shape::kRows];
+  float scales[2][Shape::kMatrix];
+  List list;
+};
+struct StateScales {  // where the scale of a row and a block lies
+  int64_t row, block;
+};
+template <int MW, int WM, int TW, bool kMasked>
+__global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, StateScales strides, Elem out_type, int32_t batch_tiles, int32_t shares, int32_t tiles_each, bool wide) {
+  typedef ManyShape<MW, WM, TW> Shape;
+  extern __shared__ __align__(16) char lds[];
+  ManyShared<MW, WM, TW>& s = *reinterpret_cast<ManyShared<MW, WM, TW>*>(lds);
+  const int32_t tid = (int32_t)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t n = lane & 15, q = lane >> 4, wm = wave % WM, wn = wave / WM;
+  // workgroups that share a part of the matrix follow each other on one XCD
+  int32_t share, batch_tile;
+  {
+    const int32_t id = (int32_t)blockIdx.x, whole = shares / 8 * 8 * batch_tiles;
+    if (id < whole) {
+      share = id / 8 / batch_tiles * 8 + id % 8;
+      batch_tile = id / 8 % batch_tiles;
+    } else {
+      share = shares / 8 * 8 + (id - whole) / batch_tiles;
+      batch_tile = (id - whole) % batch_tiles;
+    }
+  }
+  const int32_t first_b = batch_tile * Shape::kRows, rows = min(h.B - first_b, Shape::kRows), blocks = f8_blocks(h.K);
+
+  // Rows of the matrix and of the hidden states lie a power of two apart as a rule, so that the same columns of all of them are on few
+  // channels of the L2: the workgroups of an XCD begin with different blocks.
+  const int32_t begin = share / 8 % blocks;
+  auto turned = [&](int32_t block) { return block + begin < blocks ? block + begin : block + begin - blocks; };
+  const int32_t unit = tid & 7, unit_row = tid >> 3, unit_to = unit_row * 8 + (unit ^ (unit_row & 7));  // and 64 rows further on
+  const uint8_t* const all_states = static_cast<const uint8_t*>(h.hidden.at) + first_b * h.hidden.stride;
+  const float* const all_state_scales = h.hidden.scales + first_b * strides.row;
+  struct Brought {
+    uint4v states[Shape::kStateUnits], codes[Shape::kCodeUnits];
+    float state_scale, scale;
+  };
+  const int64_t row0 = (int64_t)share * tiles_each * 16, row1 = min((int64_t)h.V, row0 + (int64_t)tiles_each * 16);
+  for (int64_t base = row0; base < row1; base += kListed) {
+    const int32_t here = (int32_t)min((int64_t)kListed, row1 - base);
+    int32_t count = here;
+    if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, s.list);
+    const int32_t tiles = (count + 15) / 16;
+    auto row_of = [&](int32_t i) -> int32_t {
+      const int32_t k = min(i, count - 1);
+      return kMasked ? s.list.row[k] : k;
+    };
+    const uint8_t* const base_codes = h.codes + base * h.K;
+    const int32_t passes = (tiles + Shape::kPass - 1) / Shape::kPass, even = passes ? (tiles + passes - 1) / passes : 0;
+    for (int32_t pass = 0; pass < tiles; pass += even) {
+      const int32_t pass_tiles = min(even, tiles - pass), each = (pass_tiles + Shape::kWide - 1) / Shape::kWide;
+      const int32_t first = wn * each, mine = max(0, min(each, pass_tiles - first));
+      uint32_t code_at[Shape::kCodeUnits];
+#pragma unroll
+      for (int u = 0; u < Shape::kCodeUnits; ++u) code_at[u] = (uint32_t)row_of(pass * 16 + min(u * 64 + unit_row, pass_tiles * 16 - 1)) * (uint32_t)h.K;
+      const float* const my_scales = h.scales + ((base + row_of(pass * 16 + min(tid, pass_tiles * 16 - 1))) >> 7) * blocks;
+      auto load = [&](int32_t turn, Brought& to) {
+        const int32_t block = turned(turn), k = block * 128 + unit * 16;
+        const bool there = k < h.K;
+#pragma unroll
+        for (int u = 0; u < Shape::kStateUnits; ++u) {
+          to.states[u] = uint4v{0, 0, 0, 0};
+          if (there) to.states[u] = *reinterpret_cast<const uint4v*>(all_states + min(u * 64 + unit_row, rows - 1) * h.hidden.stride + k);
+        }
+        const uint32_t in_row = (uint32_t)min(k, h.K - 16);  // (hidden states are 0 behind the last column)
+#pragma unroll
+        for (int u = 0; u < Shape::kCodeUnits; ++u)
+          if (u * 64 < pass_tiles * 16) to.codes[u] = *reinterpret_cast<const uint4v*>(base_codes + code_at[u] + in_row);
+        to.state_scale = all_state_scales[min(tid, rows - 1) * strides.row + block * strides.block];
+        to.scale = my_scales[block];
+      };
+      auto put = [&](const Brought& from, int buffer) {
+#pragma unroll
+        for (int u = 0; u < Shape::kStateUnits; ++u)
+          if (Shape::kStateUnits * kManyThreads == Shape::kRows * 8 || u * 64 + unit_row < Shape::kRows) s.states[buffer][u * 512 + unit_to] = from.states[u];
+#pragma unroll
+        for (int u = 0; u < Shape::kCodeUnits; ++u) s.codes[buffer][u * 512 + unit_to] = from.codes[u];
+        if (tid < Shape::kRows) s.state_scales[buffer][tid] = from.state_scale;
+        if (tid < Shape::kMatrix) s.scales[buffer][tid] = from.scale;
+      };
+      float4v acc[TW][MW];
+#pragma unroll
+      for (int c = 0; c < TW; ++c)
+        for (int m = 0; m < MW; ++m) acc[c][m] = float4v{0, 0, 0, 0};
+      auto multiply = [&](int buffer, auto&& refill) {
+        const int place = q ^ (n & 7);
+#pragma unroll
+        for (int c0 = 0; c0 < TW; c0 += 2) {
+          const uint4v* const at0 = &s.codes[buffer][((first + c0) * 16 + n) * 8];
+          const uint4v* const at1 = &s.codes[buffer][((first + c0 + 1) * 16 + n) * 8];
+          const Halves a[2] = {Halves(at0[place], at0[place ^ 4]), Halves(at1[place], at1[place ^ 4])};
+          float4v scale[2];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if constexpr (kMasked) scale[c] = *reinterpret_cast<const float4v*>(&s.scales[buffer][(first + c0 + c) * 16 + q * 4]);
+            else scale[c][0] = s.scales[buffer][(first + c0 + c) * 16];
+          }
+          if (c0 == 0) refill();
+          uint4v lo = s.states[buffer][(wm * MW * 16 + n) * 8 + place], hi = s.states[buffer][(wm * MW * 16 + n) * 8 + (place ^ 4)];
+          float state_scale = s.state_scales[buffer][wm * MW * 16 + n];
+#pragma unroll
+          for (int m = 0; m < MW; ++m) {
+            const Halves x(lo, hi);
+            const float scale_now = state_scale;
+            if (m + 1 < MW) {
+              const int32_t b = (wm * MW + m + 1) * 16 + n;
+              lo = s.states[buffer][b * 8 + place];
+              hi = s.states[buffer][b * 8 + (place ^ 4)];
+              state_scale = s.state_scales[buffer][b];
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const float4v sum = products(a[c], x);
+              if constexpr (kMasked) acc[c0 + c][m] += sum * (scale[c] * scale_now);
+              else acc[c0 + c][m] += sum * (scale[c][0] * scale_now);
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (what belongs to all rows at once would not fit the registers)
+          }
+        }
+      };
+      Brought next;
+      load(0, next);
+      __syncthreads();  // (the last pass has read its last block)
+      put(next, 0);
+      if (blocks > 1) load(1, next);
+      __syncthreads();
+#pragma unroll 1
+      for (int32_t block = 0; block < blocks; ++block) {
+        const int buffer = block & 1;
+        multiply(buffer, [&] {
+          if (block + 1 < blocks) put(next, buffer ^ 1);
+          if (block + 2 < blocks) load(block + 2, next);
+        });
+        __syncthreads();
+      }
+      auto store = [&](auto type) {
+        constexpr Elem O = decltype(type)::value;
+        typedef typename Type<O>::bits bits;
+#pragma unroll
+        for (int c = 0; c < TW; ++c) {
+          if (c >= mine) continue;
+          const int32_t i0 = (pass + first + c) * 16 + q * 4;
+#pragma unroll
+          for (int m = 0; m < MW; ++m) {
+            const int32_t in = (wm * MW + m) * 16 + n, b = first_b + in;
+            if (in >= rows) continue;
+            bits* const out = static_cast<bits*>(h.logits) + b * h.logits_stride + base;
+            bits y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = narrowed<O>(!kMasked || (i0 + i < count && allowed(h, b, base + row_of(i0 + i))) ? acc[c][m][i] : -__builtin_inff());
+            if (!kMasked && wide && i0 + 4 <= count) {
+              typedef bits bits4 __attribute__((ext_vector_type(4)));
+              *reinterpret_cast<bits4*>(out + i0) = bits4{y[0], y[1], y[2], y[3]};
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (i0 + i < count) out[row_of(i0 + i)] = y[i];
+            }
+          }
+        }
+      };
+      if (out_type == Elem::kF32) store(std::integral_constant<Elem, Elem::kF32>());
+      else if (out_type == Elem::kBF16) store(std::integral_constant<Elem, Elem::kBF16>());
+      else store(std::integral_constant<Elem, Elem::kF16>());
+    }
+  }
+}
+
+constexpr int kComputeUnits = 256;
 
 int64_t padded(int32_t K) { return (int64_t)f8_blocks(K) * 128; }
 
@@ -182,15 +550,59 @@ template <Elem S, bool Q4> hipError_t launch_embed(const Embed& e, Elem out_type
   return hipGetLastError();
 }
 
-template <Elem E> hipError_t quantize(const void* x, int32_t B, int32_t K, int64_t stride, int32_t width, uint8_t* codes, int64_t codes_stride, float* scales, hipStream_t stream) {
+struct Quantized {
+  uint8_t* codes;
+  int64_t stride;
+  int32_t width;  // columns of it
+  float* scales;
+  StateScales strides;
+};
+template <Elem E> hipError_t quantize(const void* x, int32_t B, int32_t K, int64_t stride, const Quantized& to, hipStream_t stream) {
   const int64_t groups = ((int64_t)B * f8_blocks(K) + 15) / 16;
-  hipLaunchKernelGGL(f8_quantize_kernel<E>, dim3((uint32_t)groups), dim3(256), 0, stream, x, stride, B, K, width, codes, codes_stride, scales);
+  hipLaunchKernelGGL(f8_quantize_kernel<E>, dim3((uint32_t)groups), dim3(256), 0, stream, x, stride, B, K, to.width, to.codes, to.stride, to.scales, to.strides.row,
+                     to.strides.block);
   return hipGetLastError();
 }
-hipError_t quantize_any(const void* x, Elem type, int32_t B, int32_t K, int64_t stride, int32_t width, uint8_t* codes, int64_t codes_stride, float* scales, hipStream_t stream) {
-  if (type == Elem::kF32) return quantize<Elem::kF32>(x, B, K, stride, width, codes, codes_stride, scales, stream);
-  if (type == Elem::kBF16) return quantize<Elem::kBF16>(x, B, K, stride, width, codes, codes_stride, scales, stream);
-  return quantize<Elem::kF16>(x, B, K, stride, width, codes, codes_stride, scales, stream);
+hipError_t quantize_any(const void* x, Elem type, int32_t B, int32_t K, int64_t stride, const Quantized& to, hipStream_t stream) {
+  if (type == Elem::kF32) return quantize<Elem::kF32>(x, B, K, stride, to, stream);
+  if (type == Elem::kBF16) return quantize<Elem::kBF16>(x, B, K, stride, to, stream);
+  return quantize<Elem::kF16>(x, B, K, stride, to, stream);
+}
+
+template <States T, int NB, bool kMasked> hipError_t launch_few(const F8Head& h, Elem out_type, hipStream_t stream) {
+  static LdsRoom room;
+  if (const hipError_t e = room(reinterpret_cast<const void*>(&f8_few_kernel<T, NB, kMasked>), kMaxLds); e != hipSuccess) return e;
+  const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), each = (tiles + kComputeUnits - 1) / kComputeUnits, steps = (f8_blocks(h.K) + kStep - 1) / kStep;
+  int32_t threads = 64;  // waves for its tiles, or for the steps of the few that masks leave
+  while (threads < kFewThreads && threads < 64 * (kMasked && steps > each ? steps : each * (each < 16 ? steps : 1))) threads *= 2;
+  const dim3 grid((tiles + each - 1) / each, (h.B + 16 * NB - 1) / (16 * NB));
+  hipLaunchKernelGGL((f8_few_kernel<T, NB, kMasked>), grid, dim3(threads), few_layout(h.K, h.B < 16 * NB ? h.B : 16 * NB, NB).end, stream, h, out_type, each);
+  return hipGetLastError();
+}
+template <States T, int NB> hipError_t launch_few_masked(const F8Head& h, Elem out_type, hipStream_t stream) {
+  return h.mask ? launch_few<T, NB, true>(h, out_type, stream) : launch_few<T, NB, false>(h, out_type, stream);
+}
+template <int NB> hipError_t launch_few_states(const F8Head& h, Elem hidden_type, Elem out_type, hipStream_t stream) {
+  if (h.hidden.scales) return launch_few_masked<States::kF8, NB>(h, out_type, stream);
+  if (hidden_type == Elem::kF16) return launch_few_masked<States::kF16, NB>(h, out_type, stream);
+  return launch_few_masked<States::kBF16, NB>(h, out_type, stream);
+}
+bool few_fits(const F8Head& h, int32_t rows, int nb) { return few_layout(h.K, rows, nb).end <= kMaxLds; }
+
+template <int MW, int WM, int TW, bool kMasked> hipError_t launch_many(const F8Head& h, const StateScales& strides, Elem out_type, hipStream_t stream) {
+  typedef ManyShape<MW, WM, TW> Shape;
+  static LdsRoom room;
+  if (const hipError_t e = room(reinterpret_cast<const void*>(&f8_many_kernel<MW, WM, TW, kMasked>), sizeof(ManyShared<MW, WM, TW>)); e != hipSuccess) return e;
+  const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), batch_tiles = (h.B + Shape::kRows - 1) / Shape::kRows;
+  const int32_t most = batch_tiles < kComputeUnits ? kComputeUnits / batch_tiles : 1, each = (tiles + most - 1) / most, shares = (tiles + each - 1) / each;
+  const int size = out_type == Elem::kF32 ? 4 : 2;
+  const bool wide = reinterpret_cast<uintptr_t>(h.logits) % (4 * size) == 0 && h.logits_stride % 4 == 0;
+  hipLaunchKernelGGL((f8_many_kernel<MW, WM, TW, kMasked>), dim3((uint32_t)(shares * batch_tiles)), dim3(kManyThreads), sizeof(ManyShared<MW, WM, TW>), stream, h, strides, out_type,
+                     batch_tiles, shares, each, wide);
+  return hipGetLastError();
+}
+template <int MW, int WM, int TW> hipError_t launch_many_masked(const F8Head& h, const StateScales& strides, Elem out_type, hipStream_t stream) {
+  return h.mask ? launch_many<MW, WM, TW, true>(h, strides, out_type, stream) : launch_many<MW, WM, TW, false>(h, strides, out_type, stream);
 }
 
 }  // namespace
@@ -198,20 +610,26 @@ hipError_t quantize_any(const void* x, Elem type, int32_t B, int32_t K, int64_t 
 size_t f8_work_bytes(int32_t B, int32_t K) { return (size_t)B * (size_t)(padded(K) + f8_blocks(K) * 4); }
 
 hipError_t launch_f8_quantize(const void* x, Elem type, int32_t B, int32_t K, int64_t stride, uint8_t* codes, int64_t codes_stride, float* scales, hipStream_t stream) {
-  return quantize_any(x, type, B, K, stride, K, codes, codes_stride, scales, stream);
+  return quantize_any(x, type, B, K, stride, Quantized{codes, codes_stride, K, scales, StateScales{f8_blocks(K), 1}}, stream);
 }
 
 hipError_t launch_f8_logits(const F8Head& head, Elem hidden_type, Elem logits_type, void* work, hipStream_t stream) {
   F8Head h = head;
+  if (h.B <= 16 && few_fits(h, h.B, 1)) return launch_few_states<1>(h, hidden_type, logits_type, stream);
+  if (h.B <= 32 && few_fits(h, h.B, 2)) return launch_few_states<2>(h, hidden_type, logits_type, stream);
+  StateScales strides{f8_blocks(h.K), 1};
   if (!h.hidden.scales) {
     uint8_t* const codes = static_cast<uint8_t*>(work);
     float* const scales = reinterpret_cast<float*>(codes + h.B * padded(h.K));
-    if (const hipError_t e = quantize_any(h.hidden.at, hidden_type, h.B, h.K, h.hidden.stride, (int32_t)padded(h.K), codes, padded(h.K), scales, stream); e != hipSuccess) return e;
+    strides = StateScales{1, h.B};
+    if (const hipError_t e = quantize_any(h.hidden.at, hidden_type, h.B, h.K, h.hidden.stride, Quantized{codes, padded(h.K), (int32_t)padded(h.K), scales, strides}, stream);
+        e != hipSuccess)
+      return e;
     h.hidden = F8States{codes, padded(h.K), scales};
   }
-  const dim3 grid((uint32_t)(((int64_t)h.V + 63) / 64), (uint32_t)((h.B + 15) / 16));
-  hipLaunchKernelGGL(f8_logits_kernel, grid, dim3(256), 0, stream, h, logits_type);
-  return hipGetLastError();
+  if (h.B <= 32) return launch_many_masked<2, 1, 4>(h, strides, logits_type, stream);
+  if (h.B <= 64) return launch_many_masked<4, 1, 4>(h, strides, logits_type, stream);
+  return launch_many_masked<4, 2, 4>(h, strides, logits_type, stream);
 }
 
 hipError_t launch_q4_embed(const Embed& e, Elem scales_type, Elem out_type, hipStream_t stream) {
