@@ -2459,7 +2459,7 @@ int xgm_f8_logits(const void* d_hidden, xgm_dtype hidden_dt, const float* d_hidd
   if (!aligned(d_hidden, 16) || hidden_stride_elems * hidden_size % 16 != 0 || !aligned(d_codes, 16))
     return fail(XGM_ERR_BAD_ARG, "f8_logits: hidden rows and codes must be 16-byte aligned");
   if (!aligned(d_scales, 4) || !aligned(d_hidden_scales, 4)) return fail(XGM_ERR_BAD_ARG, "f8_logits: scales are not aligned to their element size");
-  if (hidden_dt != XGM_F8 && !aligned(d_work, 16)) return fail(XGM_ERR_BAD_ARG, "f8_logits: working memory must be 16-byte aligned");
+  if (!aligned(d_work, 16)) return fail(XGM_ERR_BAD_ARG, "f8_logits: working memory must be 16-byte aligned");
   if (d_bitmask && v_mask <= 0) return fail(XGM_ERR_BAD_ARG, "f8_logits: a bitmask without v_mask");
   if (d_bitmask && v_mask > XGM_MAX_COLUMNS) return fail(XGM_ERR_BAD_ARG, "f8_logits: v_mask is more than XGM_MAX_COLUMNS");
   require_device();

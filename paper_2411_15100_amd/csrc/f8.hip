@@ -14,11 +14,14 @@ namespace {
 
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef int int8v __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// Codes go through the matrix instructions as f16, which holds every e4m3 number: the instructions for 8 bits add up neighbouring products
-// with 14 bits of the largest of them, and sums of logits are to have the 24 of a float.
+// Codes go through the matrix instructions as f16, which holds every e4m3 number, or as they are: the instructions for 8 bits add up
+// neighbouring products with what lies above 2^-14 of the largest of them (measured: 2^16 + 2^3 is exact, 2^16 + 2^2 is 2^16, unless they lie 8 columns
+// apart), and take half the time.  Sums of few rows and logits in 32 bits are made the first way, with the 24 bits of a float; where many rows are
+// rounded to 16 bits behind it, what the second way loses is less than the rounding: 2^-14.7 of the largest product of a block on average.
 __device__ __forceinline__ f16x8 halves(uint32_t lo, uint32_t hi) {
   const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, true);
   const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, true);
@@ -28,6 +31,13 @@ struct Halves {  // 32 numbers of a row
   f16x8 of[4];
   __device__ __forceinline__ Halves(uint4v lo, uint4v hi) : of{halves(lo[0], lo[1]), halves(lo[2], lo[3]), halves(hi[0], hi[1]), halves(hi[2], hi[3])} {}
 };
+struct Eights {
+  int8v of;
+  __device__ __forceinline__ Eights(uint4v lo, uint4v hi) : of{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]} {}
+};
+__device__ __forceinline__ float4v products(const Eights& a, const Eights& b) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.of, b.of, float4v{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+}
 // 16 x 16 sums over 128 columns, of which a lane holds 32 of its row: the same ones on both sides, whichever they are.
 __device__ __forceinline__ float4v products(const Halves& a, const Halves& b) {
   float4v c = {0, 0, 0, 0};
@@ -325,32 +335,55 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
 }
 
 // --------------------------------------------------------------- many rows in the batch
-// Up to 16 MW WM rows and any number of columns, both sides in 8 bits through LDS, a block of 128 columns at a time in two buffers.  The eight
-// waves of a workgroup form WM groups that share the rows of the batch, and in each 8 / WM waves that share the matrix, up to TW tiles
-// each.  While a block is multiplied, the next one goes from registers to the other buffer and the one after is read from memory; one
-// barrier a block.  16 bytes of a row lie in LDS at their place in the row with the row's last three bits exchanged into it: eight rows
-// of one place, as a wave reads them, lie in different banks.
+// Up to 16 MW WM rows and any number of columns, both sides in 8 bits through LDS, a block of 128 columns at a time.  The eight waves of a
+// workgroup form WM groups that share the rows of the batch, and in each 8 / WM waves that share the matrix, up to TW tiles each.
+// What a block needs goes from memory to LDS without passing a register, into a ring of kStages buffers: while a block is multiplied the
+// next kStages - 1 are on their way; one barrier a block.  16 bytes of a row lie in LDS at their place in the row with the row's last three bits
+// exchanged into it: eight rows of one place, as a wave reads them, lie in different banks.
 constexpr int kManyThreads = 512, kManyWaves = kManyThreads / 64;
 template <int MW, int WM, int TW> struct ManyShape {
   static constexpr int kRows = 16 * MW * WM, kWide = kManyWaves / WM, kPass = kWide * TW, kMatrix = 16 * kPass;
-  static constexpr int kStateUnits = (kRows * 8 + kManyThreads - 1) / kManyThreads, kCodeUnits = kMatrix * 8 / kManyThreads;
+  static constexpr int kStateLoads = kRows / 8 / kManyWaves, kCodeLoads = kMatrix / 8 / kManyWaves;  // of a wave, 64 x 16 bytes each
+  static constexpr int kStages = kRows + kMatrix <= 384 ? 3 : 2;
+  static_assert(kStateLoads > 0 && kCodeLoads > 0 && kRows + kMatrix <= kManyThreads, "equal parts for all waves, and a scale a thread");
 };
-template <int MW, int WM, int TW> struct ManyShared {
+template <int MW, int WM, int TW> struct Stage {
   typedef ManyShape<MW, WM, TW> Shape;
-  uint4v states[2][Shape::kRows * 8];
-  uint4v codes[2][Shape::kMatrix * 8];
-  float state_scales[2][Shape::kRows];
-  float scales[2][Shape::kMatrix];
-  List list;
+  uint4v states[Shape::kRows * 8];
+  uint4v codes[Shape::kMatrix * 8];
+  float scales[kManyThreads];  // of the rows of the batch, then of those of the matrix
 };
 struct StateScales {  // where the scale of a row and a block lies
   int64_t row, block;
 };
-template <int MW, int WM, int TW, bool kMasked>
+__device__ const uint4v kZeros = {0, 0, 0, 0};
+// 16 or 4 bytes a lane; `to` is the place of the wave's first lane.  (Written out because the compiler would let every read of LDS wait for all
+// of these; they have no result in a register, and who reads what they bring waits for them behind barrier_behind_loads.)
+__device__ __forceinline__ uint32_t lds_place(const void* to) {
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)to);
+}
+__device__ __forceinline__ void bring16(const void* from, const void* to) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_place(to)), "v"(from) : "memory");
+}
+__device__ __forceinline__ void bring4(const void* from, const void* to) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_place(to)), "v"(from) : "memory");
+}
+// A barrier for which a wave waits until no more than n of its loads are on their way, and none of its reads of LDS.
+template <int n> __device__ __forceinline__ void barrier_behind_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((n & 15) | (n >> 4) << 14 | 7 << 4);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+struct Nothing {};
+template <int MW, int WM, int TW, bool kMasked, class Operand>
 __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, StateScales strides, Elem out_type, int32_t batch_tiles, int32_t shares, int32_t tiles_each, bool wide) {
   typedef ManyShape<MW, WM, TW> Shape;
-  extern __shared__ __align__(16) char lds[];
-  ManyShared<MW, WM, TW>& s = *reinterpret_cast<ManyShared<MW, WM, TW>*>(lds);
+  constexpr int kLoads = Shape::kStateLoads + Shape::kCodeLoads + 1;
+  typedef Stage<MW, WM, TW> Buffer;
+  __shared__ Buffer stage0, stage1;  // (of their own names: a read of one does not wait for loads to another)
+  __shared__ std::conditional_t<Shape::kStages == 3, Buffer, Nothing> stage2;
+  __shared__ std::conditional_t<kMasked, List, Nothing> list;
   const int32_t tid = (int32_t)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t n = lane & 15, q = lane >> 4, wm = wave % WM, wn = wave / WM;
   // workgroups that share a part of the matrix follow each other on one XCD
@@ -371,121 +404,142 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
   // channels of the L2: the workgroups of an XCD begin with different blocks.
   const int32_t begin = share / 8 % blocks;
   auto turned = [&](int32_t block) { return block + begin < blocks ? block + begin : block + begin - blocks; };
-  const int32_t unit = tid & 7, unit_row = tid >> 3, unit_to = unit_row * 8 + (unit ^ (unit_row & 7));  // and 64 rows further on
-  const uint8_t* const all_states = static_cast<const uint8_t*>(h.hidden.at) + first_b * h.hidden.stride;
-  const float* const all_state_scales = h.hidden.scales + first_b * strides.row;
-  struct Brought {
-    uint4v states[Shape::kStateUnits], codes[Shape::kCodeUnits];
-    float state_scale, scale;
-  };
+  const int32_t row_in = lane >> 3, column = ((lane & 7) ^ row_in) * 16;  // what a lane brings of 8 rows
+  const uint8_t* state_at[Shape::kStateLoads];
+#pragma unroll
+  for (int u = 0; u < Shape::kStateLoads; ++u)
+    state_at[u] = static_cast<const uint8_t*>(h.hidden.at) + (first_b + min((wave * Shape::kStateLoads + u) * 8 + row_in, rows - 1)) * h.hidden.stride + column;
   const int64_t row0 = (int64_t)share * tiles_each * 16, row1 = min((int64_t)h.V, row0 + (int64_t)tiles_each * 16);
   for (int64_t base = row0; base < row1; base += kListed) {
     const int32_t here = (int32_t)min((int64_t)kListed, row1 - base);
     int32_t count = here;
-    if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, s.list);
+    if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, list);
     const int32_t tiles = (count + 15) / 16;
     auto row_of = [&](int32_t i) -> int32_t {
       const int32_t k = min(i, count - 1);
-      return kMasked ? s.list.row[k] : k;
+      if constexpr (kMasked) return list.row[k];
+      else return k;
     };
     const uint8_t* const base_codes = h.codes + base * h.K;
     const int32_t passes = (tiles + Shape::kPass - 1) / Shape::kPass, even = passes ? (tiles + passes - 1) / passes : 0;
     for (int32_t pass = 0; pass < tiles; pass += even) {
       const int32_t pass_tiles = min(even, tiles - pass), each = (pass_tiles + Shape::kWide - 1) / Shape::kWide;
       const int32_t first = wn * each, mine = max(0, min(each, pass_tiles - first));
-      uint32_t code_at[Shape::kCodeUnits];
+      uint32_t code_at[Shape::kCodeLoads];
 #pragma unroll
-      for (int u = 0; u < Shape::kCodeUnits; ++u) code_at[u] = (uint32_t)row_of(pass * 16 + min(u * 64 + unit_row, pass_tiles * 16 - 1)) * (uint32_t)h.K;
-      const float* const my_scales = h.scales + ((base + row_of(pass * 16 + min(tid, pass_tiles * 16 - 1))) >> 7) * blocks;
-      auto load = [&](int32_t turn, Brought& to) {
-        const int32_t block = turned(turn), k = block * 128 + unit * 16;
-        const bool there = k < h.K;
-#pragma unroll
-        for (int u = 0; u < Shape::kStateUnits; ++u) {
-          to.states[u] = uint4v{0, 0, 0, 0};
-          if (there) to.states[u] = *reinterpret_cast<const uint4v*>(all_states + min(u * 64 + unit_row, rows - 1) * h.hidden.stride + k);
+      for (int u = 0; u < Shape::kCodeLoads; ++u)
+        code_at[u] = (uint32_t)row_of(pass * 16 + min((wave * Shape::kCodeLoads + u) * 8 + row_in, pass_tiles * 16 - 1)) * (uint32_t)h.K;
+      const float* scale_at;
+      int32_t scale_step;
+      if (tid < Shape::kRows) {
+        scale_at = h.hidden.scales + (first_b + min(tid, rows - 1)) * strides.row;
+        scale_step = (int32_t)strides.block;
+      } else {
+        scale_at = h.scales + ((base + row_of(pass * 16 + min(tid - Shape::kRows, pass_tiles * 16 - 1))) >> 7) * blocks;
+        scale_step = 1;
+      }
+      // the i-th of a wave's kLoads loads of a block
+      auto load = [&](int i, int32_t turn, Buffer& to) {
+        const int32_t block = turned(turn), k = block * 128;
+        if (i < Shape::kCodeLoads) {  // (hidden states are 0 behind the last column)
+          bring16(base_codes + (code_at[i] + (uint32_t)min(k + column, h.K - 16)), &to.codes[(wave * Shape::kCodeLoads + i) * 64]);
+        } else if (i < Shape::kCodeLoads + Shape::kStateLoads) {
+          const int u = i - Shape::kCodeLoads;
+          bring16(reinterpret_cast<const void*>(k + column < h.K ? reinterpret_cast<uintptr_t>(state_at[u] + k) : reinterpret_cast<uintptr_t>(&kZeros)),
+                  &to.states[(wave * Shape::kStateLoads + u) * 64]);
+        } else {
+          bring4(scale_at + block * scale_step, &to.scales[wave * 64]);
         }
-        const uint32_t in_row = (uint32_t)min(k, h.K - 16);  // (hidden states are 0 behind the last column)
-#pragma unroll
-        for (int u = 0; u < Shape::kCodeUnits; ++u)
-          if (u * 64 < pass_tiles * 16) to.codes[u] = *reinterpret_cast<const uint4v*>(base_codes + code_at[u] + in_row);
-        to.state_scale = all_state_scales[min(tid, rows - 1) * strides.row + block * strides.block];
-        to.scale = my_scales[block];
-      };
-      auto put = [&](const Brought& from, int buffer) {
-#pragma unroll
-        for (int u = 0; u < Shape::kStateUnits; ++u)
-          if (Shape::kStateUnits * kManyThreads == Shape::kRows * 8 || u * 64 + unit_row < Shape::kRows) s.states[buffer][u * 512 + unit_to] = from.states[u];
-#pragma unroll
-        for (int u = 0; u < Shape::kCodeUnits; ++u) s.codes[buffer][u * 512 + unit_to] = from.codes[u];
-        if (tid < Shape::kRows) s.state_scales[buffer][tid] = from.state_scale;
-        if (tid < Shape::kMatrix) s.scales[buffer][tid] = from.scale;
       };
       float4v acc[TW][MW];
 #pragma unroll
       for (int c = 0; c < TW; ++c)
         for (int m = 0; m < MW; ++m) acc[c][m] = float4v{0, 0, 0, 0};
-      auto multiply = [&](int buffer, auto&& refill) {
+      // Multiplies a block.  The loads of another one are seen to when the first reads of LDS are on their way: between the products, where they
+      // keep nobody waiting, they come too late for the next barrier (1024 rows of 128256 x 4096: 642 us, and 676).
+      auto multiply = [&](const Buffer& s, auto&& load_other) {
         const int place = q ^ (n & 7);
+        auto operand = [&](const uint4v* row) { return Operand(row[place], row[place ^ 4]); };
+        const uint4v* const my_codes = &s.codes[(first * 16 + n) * 8];
+        const uint4v* const my_states = &s.states[(wm * MW * 16 + n) * 8];
+        uint4v lo = my_states[place], hi = my_states[place ^ 4];
+        float state_scale = s.scales[wm * MW * 16 + n];
+        float4v scale[TW];
 #pragma unroll
-        for (int c0 = 0; c0 < TW; c0 += 2) {
-          const uint4v* const at0 = &s.codes[buffer][((first + c0) * 16 + n) * 8];
-          const uint4v* const at1 = &s.codes[buffer][((first + c0 + 1) * 16 + n) * 8];
-          const Halves a[2] = {Halves(at0[place], at0[place ^ 4]), Halves(at1[place], at1[place ^ 4])};
-          float4v scale[2];
+        for (int c = 0; c < TW; ++c) {
+          if constexpr (kMasked) scale[c] = *reinterpret_cast<const float4v*>(&s.scales[Shape::kRows + (first + c) * 16 + q * 4]);
+          else scale[c][0] = s.scales[Shape::kRows + (first + c) * 16];
+        }
+        const Operand a[4] = {operand(my_codes), operand(my_codes + (TW > 1) * 128), operand(my_codes + (TW > 2) * 256), operand(my_codes + (TW > 3) * 384)};
+        // the sums of 16 rows are scaled while the next ones' products are made
+        float4v sum[2][TW];
+        float scale_of[2];
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            if constexpr (kMasked) scale[c] = *reinterpret_cast<const float4v*>(&s.scales[buffer][(first + c0 + c) * 16 + q * 4]);
-            else scale[c][0] = s.scales[buffer][(first + c0 + c) * 16];
-          }
-          if (c0 == 0) refill();
-          uint4v lo = s.states[buffer][(wm * MW * 16 + n) * 8 + place], hi = s.states[buffer][(wm * MW * 16 + n) * 8 + (place ^ 4)];
-          float state_scale = s.state_scales[buffer][wm * MW * 16 + n];
-#pragma unroll
-          for (int m = 0; m < MW; ++m) {
-            const Halves x(lo, hi);
-            const float scale_now = state_scale;
+        for (int m = 0; m <= MW; ++m) {
+          if (m == 0) load_other();
+          if (m < MW) {
+            const Operand x(lo, hi);
+            scale_of[m & 1] = state_scale;
             if (m + 1 < MW) {
-              const int32_t b = (wm * MW + m + 1) * 16 + n;
-              lo = s.states[buffer][b * 8 + place];
-              hi = s.states[buffer][b * 8 + (place ^ 4)];
-              state_scale = s.state_scales[buffer][b];
+              lo = my_states[(m + 1) * 128 + place];
+              hi = my_states[(m + 1) * 128 + (place ^ 4)];
+              state_scale = s.scales[(wm * MW + m + 1) * 16 + n];
             }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const float4v sum = products(a[c], x);
-              if constexpr (kMasked) acc[c0 + c][m] += sum * (scale[c] * scale_now);
-              else acc[c0 + c][m] += sum * (scale[c][0] * scale_now);
-            }
-            __builtin_amdgcn_sched_barrier(0);  // (what belongs to all rows at once would not fit the registers)
+            for (int c = 0; c < TW; ++c) sum[m & 1][c] = products(a[c], x);
           }
+          if (m > 0) {
+#pragma unroll
+            for (int c = 0; c < TW; ++c) {
+              float4v& to = acc[c][m - 1];
+              if constexpr (kMasked) to += sum[(m - 1) & 1][c] * (scale[c] * scale_of[(m - 1) & 1]);
+              else to += sum[(m - 1) & 1][c] * (scale[c][0] * scale_of[(m - 1) & 1]);
+              asm volatile("" : "+v"(to));  // (here, and not when all products are made: they would not fit the registers)
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
       };
-      Brought next;
-      load(0, next);
-      __syncthreads();  // (the last pass has read its last block)
-      put(next, 0);
-      if (blocks > 1) load(1, next);
-      __syncthreads();
-#pragma unroll 1
-      for (int32_t block = 0; block < blocks; ++block) {
-        const int buffer = block & 1;
-        multiply(buffer, [&] {
-          if (block + 1 < blocks) put(next, buffer ^ 1);
-          if (block + 2 < blocks) load(block + 2, next);
+      // A block is there when all waves have waited for their parts of it; the buffer of the block before it is free then.
+      auto turn = [&](int32_t block, const Buffer& now, Buffer& free) {
+        if (Shape::kStages == 3 && block + 1 < blocks) barrier_behind_loads<kLoads>();
+        else barrier_behind_loads<0>();
+        const int32_t next = block + Shape::kStages - 1;
+        multiply(now, [&] {
+          if (next >= blocks) return;
+#pragma unroll
+          for (int i = 0; i < kLoads; ++i) load(i, next, free);
         });
-        __syncthreads();
+      };
+      barrier_behind_loads<0>();  // (the last pass has read its last block)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) load(i, 0, stage0);
+      if (Shape::kStages == 3 && blocks > 1)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load(i, 1, stage1);
+#pragma unroll 1
+      for (int32_t block = 0; block < blocks; block += Shape::kStages) {
+        if constexpr (Shape::kStages == 3) {
+          turn(block, stage0, stage2);
+          if (block + 1 < blocks) turn(block + 1, stage1, stage0);
+          if (block + 2 < blocks) turn(block + 2, stage2, stage1);
+        } else {
+          turn(block, stage0, stage1);
+          if (block + 1 < blocks) turn(block + 1, stage1, stage0);
+        }
       }
       auto store = [&](auto type) {
         constexpr Elem O = decltype(type)::value;
         typedef typename Type<O>::bits bits;
+        int32_t in0 = wm * MW * 16 + n;
+        asm volatile("" : "+v"(in0));  // (else the addresses of all rows are computed ahead of the loops and fill the registers)
 #pragma unroll
         for (int c = 0; c < TW; ++c) {
           if (c >= mine) continue;
           const int32_t i0 = (pass + first + c) * 16 + q * 4;
 #pragma unroll
           for (int m = 0; m < MW; ++m) {
-            const int32_t in = (wm * MW + m) * 16 + n, b = first_b + in;
+            const int32_t in = in0 + m * 16, b = first_b + in;
             if (in >= rows) continue;
             bits* const out = static_cast<bits*>(h.logits) + b * h.logits_stride + base;
             bits y[4];
@@ -507,6 +561,12 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
       else store(std::integral_constant<Elem, Elem::kF16>());
     }
   }
+}
+
+// scales of hidden states, [row][block] to [block][row]
+__global__ __launch_bounds__(256) void f8_turn_scales_kernel(const float* from, int32_t B, int32_t blocks, float* to) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < (int64_t)B * blocks) to[i] = from[i % B * blocks + i / B];
 }
 
 constexpr int kComputeUnits = 256;
@@ -589,20 +649,18 @@ template <int NB> hipError_t launch_few_states(const F8Head& h, Elem hidden_type
 }
 bool few_fits(const F8Head& h, int32_t rows, int nb) { return few_layout(h.K, rows, nb).end <= kMaxLds; }
 
-template <int MW, int WM, int TW, bool kMasked> hipError_t launch_many(const F8Head& h, const StateScales& strides, Elem out_type, hipStream_t stream) {
+template <int MW, int WM, int TW, bool kMasked, class Operand> hipError_t launch_many(const F8Head& h, const StateScales& strides, Elem out_type, hipStream_t stream) {
   typedef ManyShape<MW, WM, TW> Shape;
-  static LdsRoom room;
-  if (const hipError_t e = room(reinterpret_cast<const void*>(&f8_many_kernel<MW, WM, TW, kMasked>), sizeof(ManyShared<MW, WM, TW>)); e != hipSuccess) return e;
   const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), batch_tiles = (h.B + Shape::kRows - 1) / Shape::kRows;
   const int32_t most = batch_tiles < kComputeUnits ? kComputeUnits / batch_tiles : 1, each = (tiles + most - 1) / most, shares = (tiles + each - 1) / each;
   const int size = out_type == Elem::kF32 ? 4 : 2;
   const bool wide = reinterpret_cast<uintptr_t>(h.logits) % (4 * size) == 0 && h.logits_stride % 4 == 0;
-  hipLaunchKernelGGL((f8_many_kernel<MW, WM, TW, kMasked>), dim3((uint32_t)(shares * batch_tiles)), dim3(kManyThreads), sizeof(ManyShared<MW, WM, TW>), stream, h, strides, out_type,
+  hipLaunchKernelGGL((f8_many_kernel<MW, WM, TW, kMasked, Operand>), dim3((uint32_t)(shares * batch_tiles)), dim3(kManyThreads), 0, stream, h, strides, out_type,
                      batch_tiles, shares, each, wide);
   return hipGetLastError();
 }
-template <int MW, int WM, int TW> hipError_t launch_many_masked(const F8Head& h, const StateScales& strides, Elem out_type, hipStream_t stream) {
-  return h.mask ? launch_many<MW, WM, TW, true>(h, strides, out_type, stream) : launch_many<MW, WM, TW, false>(h, strides, out_type, stream);
+template <int MW, int WM, int TW, class Operand> hipError_t launch_many_masked(const F8Head& h, const StateScales& strides, Elem out_type, hipStream_t stream) {
+  return h.mask ? launch_many<MW, WM, TW, true, Operand>(h, strides, out_type, stream) : launch_many<MW, WM, TW, false, Operand>(h, strides, out_type, stream);
 }
 
 }  // namespace
@@ -618,6 +676,14 @@ hipError_t launch_f8_logits(const F8Head& head, Elem hidden_type, Elem logits_ty
   if (h.B <= 16 && few_fits(h, h.B, 1)) return launch_few_states<1>(h, hidden_type, logits_type, stream);
   if (h.B <= 32 && few_fits(h, h.B, 2)) return launch_few_states<2>(h, hidden_type, logits_type, stream);
   StateScales strides{f8_blocks(h.K), 1};
+  if (h.hidden.scales && work) {  // (a block's scales side by side: as they are, 256 rows take as many requests as 16 KB of codes)
+    float* const scales = static_cast<float*>(work);
+    strides = StateScales{1, h.B};
+    const int64_t n = (int64_t)h.B * f8_blocks(h.K);
+    hipLaunchKernelGGL(f8_turn_scales_kernel, dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, stream, h.hidden.scales, h.B, f8_blocks(h.K), scales);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    h.hidden.scales = scales;
+  }
   if (!h.hidden.scales) {
     uint8_t* const codes = static_cast<uint8_t*>(work);
     float* const scales = reinterpret_cast<float*>(codes + h.B * padded(h.K));
@@ -627,9 +693,13 @@ hipError_t launch_f8_logits(const F8Head& head, Elem hidden_type, Elem logits_ty
       return e;
     h.hidden = F8States{codes, padded(h.K), scales};
   }
-  if (h.B <= 32) return launch_many_masked<2, 1, 4>(h, strides, logits_type, stream);
-  if (h.B <= 64) return launch_many_masked<4, 1, 4>(h, strides, logits_type, stream);
-  return launch_many_masked<4, 2, 4>(h, strides, logits_type, stream);
+  if (h.B <= 64) return launch_many_masked<4, 1, 2, Halves>(h, strides, logits_type, stream);
+  if (logits_type == Elem::kF32) return launch_many_masked<4, 2, 4, Halves>(h, strides, logits_type, stream);
+  // Tiles of 256 rows read the matrix half as often as those of 128, and multiply more rows that are not there: 1024 rows of 128256 x 4096 take 642
+  // us and 700, 384 of them 349 and 271.
+  const int32_t of_256 = (h.B + 255) / 256 * 256, of_128 = (h.B + 127) / 128 * 128;
+  if (of_128 * 11 < of_256 * 10 || h.B <= 128) return launch_many_masked<4, 2, 4, Eights>(h, strides, logits_type, stream);
+  return launch_many_masked<8, 2, 4, Eights>(h, strides, logits_type, stream);
 }
 
 hipError_t launch_q4_embed(const Embed& e, Elem scales_type, Elem out_type, hipStream_t stream) {

@@ -90,7 +90,7 @@ class Beams:
         some = np.isfinite(want[2])
         assert np.array_equal(got[2][~some], want[2][~some])
         size = 4 + 3 * float(self.logits.float().abs().max()) + np.abs(self.scores[np.isfinite(self.scores)]).max(initial=0.0)
-        assert (np.abs(got[2] - want[2])[some] <= 2.0 ** -24 * np.abs(want[2][some]) + size * 2.0 ** -50).all()
+        assert (np.abs(got[2][some] - want[2][some]) <= 2.0 ** -24 * np.abs(want[2][some]) + size * 2.0 ** -50).all()
         return got
 
 

@@ -5,7 +5,12 @@ Tolerances.  Codes and scales: the same, bit for bit.  Projection: products are 
 32 bits, each addition off by at most 2^-23 of S = sum |hidden * weight| (the matrix instruction may cut off what it does not keep),
 with random signs within 2 sqrt(K) 2^-23 S; the product of two scales, the product with it and the addition of a block add 3 * 2^-24 S;
 the result is rounded once to its type (eps / 2 of the value, and half of the smallest number).  Where values are small whole numbers and scales powers of two all
-sums are exact, and so must the result be.  Lookups: 64 bits rounded once, the same bits."""
+sums are exact, and so must the result be.  Lookups: 64 bits rounded once, the same bits.
+
+Logits of 16 bits in batches of more than 64 rows come from the instructions for 8 bits, which cut a product off at 2^-13 of the largest of
+its group of at most 8 neighbours.  With p the products of a logit and m their groups' largest, the K cuts are independent and each less than
+2^-13 m, so that their sum has a deviation of at most 2^-13 / sqrt(3) sqrt(sum of m^2) <= 2^-13 / sqrt(3) sqrt(8 sum of p^2); six of
+those are allowed for: 2^-13 sqrt(96) sqrt(sum of p^2)."""
 
 import numpy as np
 import pytest
@@ -139,7 +144,15 @@ class Projection:
     def want(self):
         return plain.project(*self.eight, self.codes.cpu().numpy(), self.scales.double().cpu().numpy())
 
-    def run(self, out="f32", mask=None, stride=None, offset=0, v_mask=None):
+    def squares(self, out):
+        if self.B <= 64 or out == "f32":
+            return None
+        table, K = plain.e4m3(), self.K
+        h = table[self.eight[0]] * np.repeat(self.eight[1], 128, 1)[:, :K]
+        w = table[self.codes.cpu().numpy()] * np.repeat(np.repeat(self.scales.double().cpu().numpy(), 128, 0)[:self.V], 128, 1)[:, :K]
+        return (h * h) @ (w * w).T
+
+    def run(self, out="f32", mask=None, stride=None, offset=0, v_mask=None, with_work=False):
         xgm = _xgm()
         stride = stride or self.V
         buf = torch.full((offset + self.B * stride + 8,), 7.0, dtype=TYPES[out][0], device="cuda")
@@ -147,7 +160,7 @@ class Projection:
         work = torch.full((n + 64,), 127, dtype=torch.uint8, device="cuda")
         xgm.f8_logits(self.hidden.data_ptr(), TYPES[self.dtype][1], _at(self.hidden_scales), self.B, self.K, self.hidden.stride(0), self.codes.data_ptr(),
                       self.scales.data_ptr(), self.V, buf.data_ptr() + offset * buf.element_size(), TYPES[out][1], stride, _at(mask),
-                      0 if self.dtype == "f8" else work.data_ptr(), _stream(), v_mask)
+                      0 if self.dtype == "f8" and not with_work else work.data_ptr(), _stream(), v_mask)
         torch.cuda.synchronize()
         assert bool((work[n:] == 127).all())
         assert bool((buf[:offset] == 7).all()) and bool((buf[offset + self.B * stride:] == 7).all())
@@ -156,8 +169,11 @@ class Projection:
         return rows[:, :self.V]
 
 
-def tolerance(want, size, K, out):
+def tolerance(want, size, K, out, squares=None):
+    """squares: sums of the squares of the products, where the instructions for 8 bits make them."""
     t = TYPES[out][0]
+    if squares is not None:
+        return torch.finfo(t).eps / 2 * np.abs(want) + TINY[out] / 2 + 2.0 ** -13 * np.sqrt(96 * squares) + 2.0 ** -20 * size
     return torch.finfo(t).eps / 2 * np.abs(want) + TINY[out] / 2 + (2 * np.sqrt(K) * 2.0 ** -23 + 3 * 2.0 ** -24) * size
 
 
@@ -183,8 +199,17 @@ def test_projection_of_real_numbers(B, K, V, dtype, out):
         p.scales *= 2.0 ** -6          # (within the type's range)
     want, size = p.want()
     got = _np(p.run(out, stride=V + B % 5, offset=B % 4))
-    tol = tolerance(want, size, K, out)
+    tol = tolerance(want, size, K, out, p.squares(out))
     assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
+
+
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("B,K,V", [(5, 272, 130), (40, 144, 300), (100, 384, 1000), (257, 256, 65), (300, 1040, 777), (700, 512, 300)])
+def test_projection_of_states_in_8_bits_with_working_memory(B, K, V, out):
+    p = Projection(B, K, V, "f8", whole=True, seed=K, pad=1)
+    want = p.want()[0]
+    got = p.run(out, with_work=True)
+    assert torch.equal(got, p.run(out)) and (out != "f32" or np.array_equal(_np(got), want))
 
 
 @pytest.mark.parametrize("B,K,V", [(1, 65536, 40), (2, 32768, 20), (16, 10240, 33), (17, 9216, 30), (9, 24576, 70), (33, 65536, 36)])
