@@ -15,9 +15,10 @@ namespace {
 // ------------------------------------------------------------- continuations of beams
 // A continuation of row b is worth logit + base, base = score - log(sum of exp of the row's logits), in 64 bits: two continuations of
 // different rows may be as near to each other as two numbers get, and the order of a sum in 32 bits would decide between them.
-// One launch, a workgroup per slice of a row: it reads the logits once, under the rules, and leaves the slice's sum of weights and its
-// n_out best tokens in order (a key: the logit as a whole number, then the id's complement, so that no two are alike).  The
-// workgroup that finishes last for its request knows every row's base and takes the n_out best of all lists.
+// First kernel, a workgroup per slice of a row: it reads the logits once, under the rules, and leaves the slice's sum of weights and its
+// n_out best tokens in order (a key: the logit as a whole number, then the id's complement, so that no two are alike).  Second
+// kernel, a workgroup per request: it knows every row's base and takes the n_out best of all lists.  (As one kernel whose last workgroup of a
+// request goes on, what the second needs of registers and LDS keeps waves of the first from running: 128 rows of 151936 took 70 us.)
 // A list begins with a bound: the threads form n groups, and no more than the least of their largest logits has to be looked
 // at, for every group has one as good.  The tokens above the bound (n ln n of them or so) are compared each with each.
 constexpr int kMostFound = 1024;   // tokens of a slice above its bound that are kept in LDS
@@ -29,9 +30,8 @@ struct BeamSlot {  // what a slice leaves beside its list
   float top;  // -inf: it has no list
 };
 struct BeamMemory {
-  uint32_t* arrived;  // [requests]: zero between calls
-  BeamSlot* slots;    // [rows][slices]
-  u64* lists;         // [rows][slices][n_out], 0 behind the last
+  BeamSlot* slots;  // [rows][slices]
+  u64* lists;       // [rows][slices][n_out], 0 behind the last
   int32_t slices;
 };
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -41,7 +41,6 @@ BeamMemory memory_at(void* at, int32_t rows, int32_t V, size_t* bytes) {
   m.slices = most_slices(V);
   char* p = static_cast<char*>(at);
   auto take = [&](size_t n) { char* q = p; p += rounded(n); return q; };
-  m.arrived = reinterpret_cast<uint32_t*>(take((size_t)rows * 4));
   m.slots = reinterpret_cast<BeamSlot*>(take((size_t)rows * m.slices * sizeof(BeamSlot)));
   m.lists = reinterpret_cast<u64*>(take((size_t)rows * m.slices * kMaxContinuations * 8));
   *bytes = (size_t)(p - static_cast<char*>(at));
@@ -68,21 +67,17 @@ __device__ __forceinline__ int32_t beam_of(u64 place) { return kMaxBeams - 1 - (
 __device__ __forceinline__ int32_t id_at(u64 place) { return (int32_t)(~(uint32_t)place & ((1u << kIdBits) - 1u)); }
 
 struct BeamShared {
-  float top[kWaves];
+  float top[kWaves], most[kSliceThreads];
   double sum[kWaves];
-  float least[kWaves];
-  uint32_t n_found, flag;
-  u64 found[kMostFound];  // (in front of what the last workgroup needs)
-  uint32_t counts[kWaves];
+  uint32_t n_found, counts[kWaves];
+  u64 found[kMostFound], better[kMostFound];
 };
 struct JoinShared {
-  double base[kMaxBeams];
+  double base[kMaxBeams], most[kSliceThreads];
   int32_t is_ended[kMaxBeams];
-  uint32_t n_joined;
-  uint32_t counts[kWaves];
-  u64 part[kWaves];
+  uint32_t n_joined, counts[kWaves];
   u64 order[kMostJoined], place[kMostJoined];
-  int32_t rows[kMaxContinuations], ids[kMaxContinuations], first[kMaxBeams], taken[kMaxBeams];
+  int32_t rows[kMaxContinuations], ids[kMaxContinuations];
   float scores[kMaxContinuations];
 };
 
@@ -101,45 +96,45 @@ __device__ __forceinline__ uint32_t count_all(uint32_t mine, uint32_t (&counts)[
   return all;
 }
 
-// The least of the largest numbers of `groups` groups of threads (a power of two, at most one group a thread); all threads get it.
-__device__ __forceinline__ float least_of_groups(float mine, int groups, float (&least)[kWaves]) {
-  int d = 1;
-  for (; d < kSliceThreads / groups && d < 64; d *= 2) mine = fmaxf(mine, __shfl_xor(mine, d));
-  if (groups < kWaves) {  // a group is several waves
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) least[threadIdx.x >> 6] = mine;
-    __syncthreads();
-    const int waves = kWaves / groups;
-    float r = __builtin_inff();
-    for (int g = 0; g < groups; ++g) {
-      float m = -__builtin_inff();
-      for (int k = 0; k < waves; ++k) m = fmaxf(m, least[g * waves + k]);
-      r = fminf(r, m);
-    }
-    return r;
-  }
-  for (; d < 64; d *= 2) mine = fminf(mine, __shfl_xor(mine, d));
+// The least of the largest numbers of `groups` groups of threads (a power of two up to kMaxContinuations); all threads get it.  Threads of a group lie
+// `groups` apart: where a row ends in the slice every group still has some of its tokens.
+constexpr int kMaxGroups = 128;
+static_assert(kMaxContinuations <= kMaxGroups && kMaxGroups == 128, "two waves of groups at most");
+template <class T> __device__ __forceinline__ T least_of_groups(T mine, int groups, T (&most)[kSliceThreads]) {
+  const int lane = (int)threadIdx.x & 63, tid = (int)threadIdx.x;
+  for (int d = 32; d >= groups; d >>= 1) mine = max(mine, (T)__shfl_xor(mine, d));
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) least[threadIdx.x >> 6] = mine;
+  most[tid] = mine;
   __syncthreads();
-  float r = least[0];
+  T r = most[lane];  // groups of all waves, or of the even ones
+  if (groups <= 64) {
 #pragma unroll
-  for (int k = 1; k < kWaves; ++k) r = fminf(r, least[k]);
+    for (int k = 1; k < kWaves; ++k) r = max(r, most[k * 64 + lane]);
+  } else {
+    T odd = most[64 + lane];
+#pragma unroll
+    for (int k = 2; k < kWaves; k += 2) {
+      r = max(r, most[k * 64 + lane]);
+      odd = max(odd, most[k * 64 + 64 + lane]);
+    }
+    r = min(r, odd);
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) r = min(r, (T)__shfl_xor(r, d));
   return r;
 }
 
 template <Elem E>
-__global__ __launch_bounds__(kSliceThreads) void beam_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m, int32_t n_slices, int groups) {
+__global__ __launch_bounds__(kSliceThreads, 5) void beam_slices_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m, int groups) {
   extern __shared__ __align__(16) char lds[];
   RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   BeamShared& sh = *reinterpret_cast<BeamShared*>(lds);
-  JoinShared& join = *reinterpret_cast<JoinShared*>(lds);
   __shared__ double roots[16];
-  __shared__ uint32_t is_last;
-  const int32_t slice = (int32_t)blockIdx.x, b = (int32_t)blockIdx.y, request = b / s.beams, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t slice = (int32_t)blockIdx.x, b = (int32_t)blockIdx.y, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t n = s.n_out;
+  if (!is_live(s, b) || is_ended(s, b)) return;
   fill_roots(roots);
-  if (is_live(s, b) && !is_ended(s, b)) {
+  {
     const Row<E> row(in, b);
     const int32_t first = row.first_token(slice);
     Tokens y;
@@ -147,7 +142,7 @@ __global__ __launch_bounds__(kSliceThreads) void beam_kernel(Logits in, LogitRul
     float mine = -__builtin_inff();
 #pragma unroll
     for (int k = 0; k < kTokens; ++k) mine = fmaxf(mine, y[k]);
-    const float bound = least_of_groups(mine, groups, sh.least);
+    const float bound = least_of_groups(mine, groups, sh.most);
     float top = mine;
 #pragma unroll
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -162,9 +157,14 @@ __global__ __launch_bounds__(kSliceThreads) void beam_kernel(Logits in, LogitRul
       constexpr double per = 1.4426950408889634074;
       slot.E = floor(octaves(top, per));
       double sum = 0.0;
-#pragma unroll
-      for (int k = 0; k < kTokens; ++k)
-        if (y[k] > -__builtin_inff()) sum += Power(octaves(y[k], per), slot.E, roots).weight();
+      auto add = [&](float v) {
+        if (v > -__builtin_inff()) sum += Power(octaves(v, per), slot.E, roots).weight();
+      };
+#pragma unroll 1
+      for (int k = 0; k < kTokens / 4; ++k) {  // (instructions that are fetched once cost as much as carrying them out)
+        add(y[0]); add(y[1]); add(y[2]); add(y[3]);
+        y = __builtin_shufflevector(y, y, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0, 1, 2, 3);
+      }
       sum = wave_sum(sum);
       if (lane == 0) sh.sum[wave] = sum;
       uint32_t good = 0;
@@ -174,57 +174,105 @@ __global__ __launch_bounds__(kSliceThreads) void beam_kernel(Logits in, LogitRul
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) slot.sum += sh.sum[k];
       if (all > kMostFound) {  // many equal ones: the key of the n-th best, bit by bit
+        // (the logits go round in their registers: 16 keys at once would take twice as many)
+        auto above = [&](u64 least) {
+          uint32_t bits = 0;
+#pragma unroll 1
+          for (int k = 0; k < kTokens; ++k) {
+            const float v = y[0];
+            y = __builtin_shufflevector(y, y, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0);
+            bits |= (v > -__builtin_inff() && token_key(v, first + place_of(k)) >= least ? 1u : 0u) << k;
+          }
+          return bits;
+        };
         u64 edge = 0;
 #pragma unroll 1
         for (int bit = 63; bit >= 0; --bit) {
           const u64 at = edge | 1ull << bit;
-          uint32_t above = 0;
-#pragma unroll
-          for (int k = 0; k < kTokens; ++k) above += y[k] > -__builtin_inff() && token_key(y[k], first + place_of(k)) >= at;
-          if (count_all(above, sh.counts) >= (uint32_t)n) edge = at;
+          if (count_all((uint32_t)__builtin_popcount(above(at)), sh.counts) >= (uint32_t)n) edge = at;
         }
-        good = 0;
-#pragma unroll
-        for (int k = 0; k < kTokens; ++k) good |= (y[k] > -__builtin_inff() && token_key(y[k], first + place_of(k)) >= edge ? 1u : 0u) << k;
+        good = above(edge);
         all = (uint32_t)n;
       }
       if (good) {
         uint32_t at = atomicAdd(&sh.n_found, (uint32_t)__builtin_popcount(good));
-#pragma unroll
-        for (int k = 0; k < kTokens; ++k)
-          if (good >> k & 1u) sh.found[at++] = token_key(y[k], first + place_of(k));
+#pragma unroll 1
+        for (int k = 0; k < kTokens; ++k) {
+          const float v = y[0];
+          y = __builtin_shufflevector(y, y, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0);
+          if (good >> k & 1u) sh.found[at++] = token_key(v, first + place_of(k));
+        }
       }
       __syncthreads();
-      for (uint32_t i = (uint32_t)tid; i < all; i += kSliceThreads) {
-        const u64 key = sh.found[i];
-        uint32_t rank = 0;
-        for (uint32_t k = 0; k < all; ++k) rank += sh.found[k] > key;
-        if (rank < (uint32_t)n) put_out(list + rank, key);
+      const u64* found = sh.found;
+      // Where masks leave tokens in a few places a bound says little; another one among what was found, which lies in no order, says more.
+      if (all > (uint32_t)(4 * groups + 64)) {
+        static_assert(kMostFound == 2 * kSliceThreads, "two tokens a thread");
+        const u64 none = 0;
+        const u64 one = (uint32_t)tid < all ? sh.found[tid] : none, two = (uint32_t)tid + kSliceThreads < all ? sh.found[tid + kSliceThreads] : none;
+        const float next = least_of_groups(max(one, two) ? logit_of(max(one, two)) : -__builtin_inff(), groups, sh.most);
+        if (tid == 0) sh.n_found = 0;
+        __syncthreads();
+        if (one && logit_of(one) >= next) sh.better[atomicAdd(&sh.n_found, 1u)] = one;
+        if (two && logit_of(two) >= next) sh.better[atomicAdd(&sh.n_found, 1u)] = two;
+        __syncthreads();
+        all = sh.n_found;
+        found = sh.better;
       }
-      if ((uint32_t)tid >= all && tid < n) put_out(list + tid, (u64)0);
+      for (uint32_t i = (uint32_t)tid; i < all; i += kSliceThreads) {
+        const u64 key = found[i];
+        uint32_t rank = 0;
+        for (uint32_t k = 0; k < all; ++k) rank += found[k] > key;
+        if (rank < (uint32_t)n) list[rank] = key;
+      }
+      if ((uint32_t)tid >= all && tid < n) list[tid] = 0;
+    } else if (tid < n) {
+      list[tid] = 0;
     }
-    if (tid == 0) {
-      BeamSlot& out = m.slots[(size_t)b * m.slices + slice];
-      put_out(&out.E, slot.E);
-      put_out(&out.sum, slot.sum);
-      put_out(&out.top, slot.top);
-    }
+    if (tid == 0) m.slots[(size_t)b * m.slices + slice] = slot;
   }
-  if (!last_of(m.arrived + request, (uint32_t)(n_slices * s.beams), is_last)) return;
+}
 
-  // ---- the request's lists
+__global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, BeamMemory m, int32_t n_slices, int groups) {
+  __shared__ JoinShared join;
+  __shared__ double roots[16];
+  const int32_t request = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6, n = s.n_out;
+  fill_roots(roots);
+  // What is needed first is read at once: the thread's first entries of the lists, and what the slices left.
   const int32_t b0 = request * s.beams;
+  // (the lists' first entries come first, then the second ones: the bound below is taken from them)
+  const int32_t n_lists = s.beams * n_slices, entries = n_lists * n;
+  constexpr int kHeld = 4;  // entries of a thread
+  const u64* const lists = m.lists + (size_t)b0 * m.slices * n;
+  u64 held[kHeld];
+  auto key_at = [&](int32_t e) -> u64 {
+    const int32_t rank = e / n_lists, list = e - rank * n_lists, beam = list / n_slices;
+    return lists[((size_t)beam * m.slices + (list - beam * n_slices)) * n + rank];
+  };
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int32_t e = k * kSliceThreads + tid;
+    held[k] = e < entries ? key_at(e) : 0;
+  }
+  __syncthreads();
   for (int32_t i = wave; i < s.beams; i += kWaves) {  // a wave a row
     const BeamSlot* const slots = m.slots + (size_t)(b0 + i) * m.slices;
     const bool ended = is_ended(s, b0 + i), live = is_live(s, b0 + i);
     double base = -__builtin_inf();
     if (live && !ended) {
+      constexpr int kEach = (kMostSlices + 63) / 64;
       float top = -__builtin_inff();
-      double most = -__builtin_inf();
-      for (int32_t k = lane; k < n_slices; k += 64) {
-        const float t = take_in(&slots[k].top);
+      double most = -__builtin_inf(), octave[kEach], x[kEach];
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const int32_t k = lane + 64 * j;
+        const bool there = k < n_slices;
+        const float t = there ? slots[k].top : -__builtin_inff();
+        octave[j] = there ? slots[k].E : 0.0;
+        x[j] = there ? slots[k].sum : 0.0;
+        if (!(t > -__builtin_inff())) octave[j] = -__builtin_inf();
         top = fmaxf(top, t);
-        if (t > -__builtin_inff()) most = fmax(most, take_in(&slots[k].E));
+        most = fmax(most, octave[j]);
       }
 #pragma unroll
       for (int d = 32; d; d >>= 1) {
@@ -232,11 +280,9 @@ __global__ __launch_bounds__(kSliceThreads) void beam_kernel(Logits in, LogitRul
         most = fmax(most, __shfl_xor(most, d));
       }
       double sum = 0.0;
-      for (int32_t k = lane; k < n_slices; k += 64) {
-        const bool some = take_in(&slots[k].top) > -__builtin_inff();
-        const double d = some ? take_in(&slots[k].E) - most : -2000.0;
-        if (d > -1100.0) sum += ldexp(take_in(&slots[k].sum), (int)d);
-      }
+#pragma unroll
+      for (int j = 0; j < kEach; ++j)
+        if (octave[j] - most > -1100.0) sum += ldexp(x[j], (int)(octave[j] - most));
       sum = wave_sum(sum);
       // (relative to the largest logit's own weight: a token that is alone costs nothing)
       constexpr double per = 1.4426950408889634074;
@@ -251,49 +297,54 @@ __global__ __launch_bounds__(kSliceThreads) void beam_kernel(Logits in, LogitRul
   }
   if (tid == 0) join.n_joined = 0;
   __syncthreads();
-  const int32_t per_row = n_slices * n, entries = s.beams * per_row;
-  // f(entry's order, its place) for the thread's entries
-  auto for_entries = [&](auto&& f) {
-    for (int32_t e = tid; e < entries; e += kSliceThreads) {
-      const int32_t beam = e / per_row, in_row = e % per_row;
-      const double base = join.base[beam];
-      if (!(base > -__builtin_inf())) continue;
-      if (join.is_ended[beam]) {
-        if (in_row == 0) f(order_of(base), place_in(beam, (u64)key_of(0.0f) << 32));
-        continue;
-      }
-      const size_t at = (size_t)(b0 + beam) * m.slices + in_row / n;
-      if (!(take_in(&m.slots[at].top) > -__builtin_inff())) continue;
-      const u64 key = take_in(m.lists + at * n + in_row % n);
-      if (key) f(order_of((double)logit_of(key) + base), place_in(beam, key));
+  // f(entry's sum, its place) for the thread's entries.  (A row that is not live has what an earlier call left there.)
+  auto with = [&](int32_t e, u64 key, auto&& f) {
+    const int32_t list = e % n_lists, beam = list / n_slices;
+    const double base = join.base[beam];
+    if (!(base > -__builtin_inf())) return;
+    if (join.is_ended[beam]) {
+      if (e == beam * n_slices) f(base, place_in(beam, (u64)key_of(0.0f) << 32));
+    } else if (key) {
+      f((double)logit_of(key) + base, place_in(beam, key));
     }
   };
-  u64 edge = 0, edge_place = 0;  // what counts: more than edge, or edge itself with edge_place or more
+  auto for_entries = [&](auto&& f) {
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (k * kSliceThreads + tid < entries) with(k * kSliceThreads + tid, held[k], f);
+    for (int32_t e = kHeld * kSliceThreads + tid; e < entries; e += kSliceThreads) with(e, key_at(e), f);
+  };
+  double mine = -__builtin_inf();
+  for_entries([&](double sum, u64) { mine = max(mine, sum); });
+  const double bound = least_of_groups(mine, groups, join.most);
+  auto joins = [&](double sum) { return sum >= bound; };
   uint32_t all = 0;
   {
-    uint32_t mine = 0;
-    for_entries([&](u64, u64) { ++mine; });
-    all = count_all(mine, join.counts);
+    uint32_t some = 0;
+    for_entries([&](double sum, u64) { some += joins(sum); });
+    all = count_all(some, join.counts);
   }
-  if (all > kMostJoined) {
+  u64 edge = 0, edge_place = 0;  // what counts: more than edge, or edge itself with edge_place or more
+  if (all > kMostJoined) {  // many equal ones: the n-th best, bit by bit
 #pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const u64 at = edge | 1ull << bit;
-      uint32_t mine = 0;
-      for_entries([&](u64 order, u64) { mine += order >= at; });
-      if (count_all(mine, join.counts) >= (uint32_t)n) edge = at;
+      uint32_t some = 0;
+      for_entries([&](double sum, u64) { some += order_of(sum) >= at; });
+      if (count_all(some, join.counts) >= (uint32_t)n) edge = at;
     }
 #pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const u64 at = edge_place | 1ull << bit;
-      uint32_t mine = 0;
-      for_entries([&](u64 order, u64 place) { mine += order > edge || (order == edge && place >= at); });
-      if (count_all(mine, join.counts) >= (uint32_t)n) edge_place = at;
+      uint32_t some = 0;
+      for_entries([&](double sum, u64 place) { some += order_of(sum) > edge || (order_of(sum) == edge && place >= at); });
+      if (count_all(some, join.counts) >= (uint32_t)n) edge_place = at;
     }
     all = (uint32_t)n;
   }
-  for_entries([&](u64 order, u64 place) {
-    if (order > edge || (order == edge && place >= edge_place)) {
+  for_entries([&](double sum, u64 place) {
+    const u64 order = order_of(sum);
+    if (joins(sum) && (order > edge || (order == edge && place >= edge_place))) {
       const uint32_t at = atomicAdd(&join.n_joined, 1u);
       join.order[at] = order;
       join.place[at] = place;
@@ -430,11 +481,13 @@ size_t beam_bytes(int32_t max_rows, int32_t V) {
 }
 namespace {
 template <Elem E> hipError_t select(const Logits& in, const LogitRules& r, const BeamSearch& s, const BeamMemory& m, hipStream_t stream) {
-  const size_t lds = has_rules(r) && sizeof(RuleTable) > sizeof(JoinShared) ? sizeof(RuleTable) : sizeof(JoinShared) > sizeof(BeamShared) ? sizeof(JoinShared) : sizeof(BeamShared);
+  const size_t lds = has_rules(r) && sizeof(RuleTable) > sizeof(BeamShared) ? sizeof(RuleTable) : sizeof(BeamShared);
   const int32_t n = slices_of<E>(in);
   int groups = 1;
   while (groups < s.n_out) groups *= 2;
-  hipLaunchKernelGGL(beam_kernel<E>, dim3(n, s.requests * s.beams), dim3(kSliceThreads), lds, stream, in, r, s, m, n, groups);
+  hipLaunchKernelGGL(beam_slices_kernel<E>, dim3(n, s.requests * s.beams), dim3(kSliceThreads), lds, stream, in, r, s, m, groups);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(beam_join_kernel, dim3(s.requests), dim3(kSliceThreads), 0, stream, s, m, n, groups);
   return hipGetLastError();
 }
 }  // namespace
