@@ -406,7 +406,7 @@ __global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, 
 // sources, lengths, the data.
 typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
-constexpr int kMoveThreads = 256, kMoveUnits = 8;  // a thread's of a stretch
+constexpr int kMoveThreads = 256, kMoveUnits = 8, kFewUnits = 4;  // a thread's at a time, of rows row after row, of stretches of all rows
 constexpr int kMaxMoveRows = 1024;
 struct RowDataList {
   RowData of[kMaxRowData];
@@ -428,15 +428,15 @@ struct Moves {
 // the other: 32 KB lie side by side and not 512 bytes of each row.
 template <class T, bool kTangled> __device__ __forceinline__ void move_region(const Region& r, int32_t units, const Moves& m) {
   int shift = 0;  // 2^shift units of a row at a time
-  while ((2 << shift) <= units && (!kTangled || (2 << shift) * m.n <= kMoveThreads * kMoveUnits)) ++shift;
-  static_assert(kMaxMoveRows <= kMoveThreads * kMoveUnits, "a unit of every row fits");
+  while ((2 << shift) <= units && (!kTangled || (2 << shift) * m.n <= kMoveThreads * kFewUnits)) ++shift;
+  static_assert(kMaxMoveRows <= kMoveThreads * kFewUnits, "a unit of every row fits");
   const int32_t all = m.n << shift;
   for (int64_t at = r.begin; at < r.end; at += (int64_t)sizeof(T) << shift)
-    for (int32_t u0 = 0; u0 < all; u0 += kMoveThreads * kMoveUnits) {
-      T x[kMoveUnits];
-      bool ok[kMoveUnits];
+    for (int32_t u0 = 0; u0 < all; u0 += kMoveThreads * kFewUnits) {
+      T x[kFewUnits];
+      bool ok[kFewUnits];
 #pragma unroll
-      for (int k = 0; k < kMoveUnits; ++k) {
+      for (int k = 0; k < kFewUnits; ++k) {
         const int32_t u = u0 + k * kMoveThreads + (int32_t)threadIdx.x, i = u >> shift;
         const int64_t in = at + (int64_t)(u & ((1 << shift) - 1)) * (int64_t)sizeof(T);
         ok[k] = u < all && in < r.end && in < m.limit[u < all ? i : 0];
@@ -448,7 +448,7 @@ template <class T, bool kTangled> __device__ __forceinline__ void move_region(co
         __syncthreads();
       }
 #pragma unroll
-      for (int k = 0; k < kMoveUnits; ++k) {
+      for (int k = 0; k < kFewUnits; ++k) {
         const int32_t u = u0 + k * kMoveThreads + (int32_t)threadIdx.x, i = u >> shift;
         const int64_t in = at + (int64_t)(u & ((1 << shift) - 1)) * (int64_t)sizeof(T);
         if (ok[k]) *reinterpret_cast<T*>(r.base + m.to[i] * r.row_stride + in) = x[k];
