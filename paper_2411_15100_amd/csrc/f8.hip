@@ -574,39 +574,69 @@ constexpr int kComputeUnits = 256;
 int64_t padded(int32_t K) { return (int64_t)f8_blocks(K) * 128; }
 
 // ------------------------------------------------------ rows of the matrix as hidden states
-// value * scale * factor in 64 bits, rounded once.
-template <Elem S, Elem O, bool Q4> __global__ __launch_bounds__(256) void embed_kernel(Embed e) {
+// A thread takes 16 columns at a time, 2^shift threads a row.  value * (scale * factor) in 64 bits, where both products are exact, rounded once.
+constexpr int kEmbedThreads = 256;
+template <Elem S, Elem O, bool Q4> __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(Embed e, int shift, bool wide) {
   typedef typename Type<O>::bits bits;
-  const int32_t units = e.K / 8;
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < (int64_t)e.n * units; u += (int64_t)gridDim.x * 256) {
-    const int32_t i = (int32_t)(u / units), k = (int32_t)(u % units) * 8, id = e.ids[i];
-    const bool there = id >= 0 && id < e.V;
-    float x[8];
-    double scale = 0.0;
+  const int32_t i = (int32_t)blockIdx.x * (kEmbedThreads >> shift) + ((int32_t)threadIdx.x >> shift), t = (int32_t)threadIdx.x & ((1 << shift) - 1);
+  if (i >= e.n) return;
+  const int32_t id = e.ids[i];
+  const bool there = id >= 0 && id < e.V;
+  const int64_t v = there ? id : 0;
+  const double factor = (double)e.factor;
+  bits* const out = static_cast<bits*>(e.out) + (int64_t)i * e.out_stride;
+#pragma unroll 2
+  for (int32_t k = t * 16; k < e.K; k += 16 << shift) {
+    float x[16];
+    double scale;
     if constexpr (Q4) {
-      const int64_t g = (int64_t)(there ? id : 0) * (e.K / e.group) + k / e.group;
-      const uint32_t w = there ? *reinterpret_cast<const uint32_t*>(e.codes + ((int64_t)id * e.K + k) / 2) : 0u;
+      const int64_t g = v * (e.K / e.group) + k / e.group;  // (a group is a multiple of 32)
+      const uint2 w = *reinterpret_cast<const uint2*>(e.codes + (v * e.K + k) / 2);
       const int zero = e.zeros ? e.zeros[g] : 8;
       scale = (double)widened<S>(static_cast<const typename Type<S>::bits*>(e.scales)[g]);
-      for (int j = 0; j < 8; ++j) x[j] = (float)((int)(w >> (4 * j) & 15u) - zero);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] = (float)((int)(w.x >> (4 * j) & 15u) - zero);
+        x[8 + j] = (float)((int)(w.y >> (4 * j) & 15u) - zero);
+      }
     } else {
-      const uint2 w = there ? *reinterpret_cast<const uint2*>(e.codes + (int64_t)id * e.K + k) : uint2{0, 0};
-      scale = (double)static_cast<const float*>(e.scales)[(int64_t)((there ? id : 0) >> 7) * f8_blocks(e.K) + (k >> 7)];
-      x[0] = __builtin_amdgcn_cvt_f32_fp8((int)w.x, 0); x[1] = __builtin_amdgcn_cvt_f32_fp8((int)w.x, 1);
-      x[2] = __builtin_amdgcn_cvt_f32_fp8((int)w.x, 2); x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w.x, 3);
-      x[4] = __builtin_amdgcn_cvt_f32_fp8((int)w.y, 0); x[5] = __builtin_amdgcn_cvt_f32_fp8((int)w.y, 1);
-      x[6] = __builtin_amdgcn_cvt_f32_fp8((int)w.y, 2); x[7] = __builtin_amdgcn_cvt_f32_fp8((int)w.y, 3);
+      const uint4v w = *reinterpret_cast<const uint4v*>(e.codes + v * e.K + k);
+      scale = (double)static_cast<const float*>(e.scales)[(v >> 7) * f8_blocks(e.K) + (k >> 7)];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[4 * j] = __builtin_amdgcn_cvt_f32_fp8((int)w[j], 0);
+        x[4 * j + 1] = __builtin_amdgcn_cvt_f32_fp8((int)w[j], 1);
+        x[4 * j + 2] = __builtin_amdgcn_cvt_f32_fp8((int)w[j], 2);
+        x[4 * j + 3] = __builtin_amdgcn_cvt_f32_fp8((int)w[j], 3);
+      }
     }
-    bits* const out = static_cast<bits*>(e.out) + (int64_t)i * e.out_stride + k;
-    for (int j = 0; j < 8; ++j) out[j] = there ? narrowed<O>((double)x[j] * scale * (double)e.factor) : narrowed<O>(0.0f);
+    scale *= factor;
+    uint32_t y[4 * sizeof(bits)];  // as it goes to memory
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const uint32_t one = there ? (uint32_t)narrowed<O>((double)x[j] * scale) : 0u;
+      if constexpr (sizeof(bits) == 4) y[j] = one;
+      else y[j / 2] = j & 1 ? y[j / 2] | one << 16 : one;
+    }
+    if (wide) {
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(bits); ++j) reinterpret_cast<uint4v*>(out + k)[j] = uint4v{y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) out[k + j] = (bits)(sizeof(bits) == 4 ? y[j] : y[j / 2] >> (16 * (j & 1)));
+    }
   }
 }
 template <Elem S, bool Q4> hipError_t launch_embed(const Embed& e, Elem out_type, hipStream_t stream) {
-  const int64_t units = (int64_t)e.n * (e.K / 8), groups = (units + 255) / 256;
-  const dim3 grid((uint32_t)(groups < (1 << 30) ? groups : 1 << 30));
-  if (out_type == Elem::kF32) hipLaunchKernelGGL((embed_kernel<S, Elem::kF32, Q4>), grid, dim3(256), 0, stream, e);
-  else if (out_type == Elem::kBF16) hipLaunchKernelGGL((embed_kernel<S, Elem::kBF16, Q4>), grid, dim3(256), 0, stream, e);
-  else hipLaunchKernelGGL((embed_kernel<S, Elem::kF16, Q4>), grid, dim3(256), 0, stream, e);
+  int shift = 0;
+  while (shift < 8 && (16 << shift) < e.K) ++shift;
+  const int32_t rows = kEmbedThreads >> shift;
+  const int size = out_type == Elem::kF32 ? 4 : 2;
+  const bool wide = reinterpret_cast<uintptr_t>(e.out) % 16 == 0 && e.out_stride * size % 16 == 0;
+  const dim3 grid((uint32_t)((e.n + rows - 1) / rows));
+  if (out_type == Elem::kF32) hipLaunchKernelGGL((embed_kernel<S, Elem::kF32, Q4>), grid, dim3(kEmbedThreads), 0, stream, e, shift, wide);
+  else if (out_type == Elem::kBF16) hipLaunchKernelGGL((embed_kernel<S, Elem::kBF16, Q4>), grid, dim3(kEmbedThreads), 0, stream, e, shift, wide);
+  else hipLaunchKernelGGL((embed_kernel<S, Elem::kF16, Q4>), grid, dim3(kEmbedThreads), 0, stream, e, shift, wide);
   return hipGetLastError();
 }
 
