@@ -249,24 +249,36 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
     if (!brought) {  // (the first codes are on their way meanwhile)
       brought = true;
       const int32_t units = blocks * rows * 16;  // 8 columns each, 16 neighbouring threads to a block
-      for (int32_t u0 = 0; u0 < units; u0 += threads) {
-        const int32_t u = u0 + tid, k8 = u & 15, b = (u >> 4) % rows, block = (u >> 4) / rows, k = block * 128 + k8 * 8;
-        if (u >= units) break;
-        uint2 w = {0, 0};
-        float scale;
-        if constexpr (T == States::kF8) {
-          if (k < h.K) w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(h.hidden.at) + (first_b + b) * h.hidden.stride + k);
-          scale = h.hidden.scales[(int64_t)(first_b + b) * blocks + block];
-        } else {
-          Eight<T == States::kF16 ? Elem::kF16 : Elem::kBF16> x;
-          if (k < h.K) x.load(static_cast<const uint16_t*>(h.hidden.at) + (first_b + b) * h.hidden.stride + k);
-          else x.clear();
-          const uint32_t e = exponent_of(most_of_16(x.most()));
-          w = x.codes(__uint_as_float((254u - e) << 23));
-          scale = __uint_as_float(e << 23);
+      constexpr int kAtOnce = 4;                 // of a thread
+      for (int32_t u0 = tid; u0 < units; u0 += threads * kAtOnce) {
+        Eight<T == States::kF16 ? Elem::kF16 : Elem::kBF16> x[kAtOnce];
+        uint2 w[kAtOnce];
+        float scale[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int32_t u = u0 + i * threads, b = (u >> 4) % rows, block = (u >> 4) / rows, k = block * 128 + (u & 15) * 8;
+          const bool there = u < units && k < h.K;
+          if constexpr (T == States::kF8) {
+            w[i] = uint2{0, 0};
+            if (there) w[i] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(h.hidden.at) + (first_b + b) * h.hidden.stride + k);
+            if (u < units) scale[i] = h.hidden.scales[(int64_t)(first_b + b) * blocks + block];
+          } else {
+            x[i].clear();
+            if (there) x[i].load(static_cast<const uint16_t*>(h.hidden.at) + (first_b + b) * h.hidden.stride + k);
+          }
         }
-        reinterpret_cast<uint2*>(hidden)[((block * 8 + (k8 >> 1)) * rows + b) * 2 + (k8 & 1)] = w;
-        if (k8 == 0) hidden_scales[block * rows + b] = scale;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int32_t u = u0 + i * threads, b = (u >> 4) % rows, block = (u >> 4) / rows, k8 = u & 15;
+          if constexpr (T != States::kF8) {
+            const uint32_t e = exponent_of(most_of_16(x[i].most()));
+            w[i] = x[i].codes(__uint_as_float((254u - e) << 23));
+            scale[i] = __uint_as_float(e << 23);
+          }
+          if (u >= units) break;
+          reinterpret_cast<uint2*>(hidden)[((block * 8 + (k8 >> 1)) * rows + b) * 2 + (k8 & 1)] = w[i];
+          if (k8 == 0) hidden_scales[block * rows + b] = scale[i];
+        }
       }
       __syncthreads();
     }
@@ -410,8 +422,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
   for (int u = 0; u < Shape::kStateLoads; ++u)
     state_at[u] = static_cast<const uint8_t*>(h.hidden.at) + (first_b + min((wave * Shape::kStateLoads + u) * 8 + row_in, rows - 1)) * h.hidden.stride + column;
   const int64_t row0 = (int64_t)share * tiles_each * 16, row1 = min((int64_t)h.V, row0 + (int64_t)tiles_each * 16);
-  for (int64_t base = row0; base < row1; base += kListed) {
-    const int32_t here = (int32_t)min((int64_t)kListed, row1 - base);
+  constexpr int64_t kTogether = kMasked ? kListed : 32768;  // (rows of the matrix, whose codes begin within 32 bits of each other)
+  for (int64_t base = row0; base < row1; base += kTogether) {
+    const int32_t here = (int32_t)min(kTogether, row1 - base);
     int32_t count = here;
     if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, list);
     const int32_t tiles = (count + 15) / 16;
@@ -422,22 +435,18 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
     };
     const uint8_t* const base_codes = h.codes + base * h.K;
     const int32_t passes = (tiles + Shape::kPass - 1) / Shape::kPass, even = passes ? (tiles + passes - 1) / passes : 0;
-    for (int32_t pass = 0; pass < tiles; pass += even) {
-      const int32_t pass_tiles = min(even, tiles - pass), each = (pass_tiles + Shape::kWide - 1) / Shape::kWide;
-      const int32_t first = wn * each, mine = max(0, min(each, pass_tiles - first));
-      uint32_t code_at[Shape::kCodeLoads];
+    if (tiles == 0) continue;
+    uint32_t code_at[Shape::kCodeLoads];
+    const float* scale_at;
+    const int32_t scale_step = tid < Shape::kRows ? (int32_t)strides.block : 1;
+    auto point = [&](int32_t pass) {  // at what the wave brings of a pass
+      const int32_t last = min(even, tiles - pass) * 16 - 1;
 #pragma unroll
       for (int u = 0; u < Shape::kCodeLoads; ++u)
-        code_at[u] = (uint32_t)row_of(pass * 16 + min((wave * Shape::kCodeLoads + u) * 8 + row_in, pass_tiles * 16 - 1)) * (uint32_t)h.K;
-      const float* scale_at;
-      int32_t scale_step;
-      if (tid < Shape::kRows) {
-        scale_at = h.hidden.scales + (first_b + min(tid, rows - 1)) * strides.row;
-        scale_step = (int32_t)strides.block;
-      } else {
-        scale_at = h.scales + ((base + row_of(pass * 16 + min(tid - Shape::kRows, pass_tiles * 16 - 1))) >> 7) * blocks;
-        scale_step = 1;
-      }
+        code_at[u] = (uint32_t)row_of(pass * 16 + min((wave * Shape::kCodeLoads + u) * 8 + row_in, last)) * (uint32_t)h.K;
+      if (tid < Shape::kRows) scale_at = h.hidden.scales + (first_b + min(tid, rows - 1)) * strides.row;
+      else scale_at = h.scales + ((base + row_of(pass * 16 + min(tid - Shape::kRows, last))) >> 7) * blocks;
+    };
       // the i-th of a wave's kLoads loads of a block
       auto load = [&](int i, int32_t turn, Buffer& to) {
         const int32_t block = turned(turn), k = block * 128;
@@ -451,6 +460,19 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
           bring4(scale_at + block * scale_step, &to.scales[wave * 64]);
         }
       };
+    auto begin_pass = [&](int32_t pass) {
+      point(pass);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) load(i, 0, stage0);
+      if (Shape::kStages == 3 && blocks > 1)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load(i, 1, stage1);
+    };
+    barrier_behind_loads<0>();  // (what was there before has been read)
+    begin_pass(0);
+    for (int32_t pass = 0; pass < tiles; pass += even) {
+      const int32_t pass_tiles = min(even, tiles - pass), each = (pass_tiles + Shape::kWide - 1) / Shape::kWide;
+      const int32_t first = wn * each, mine = max(0, min(each, pass_tiles - first));
       float4v acc[TW][MW];
 #pragma unroll
       for (int c = 0; c < TW; ++c)
@@ -511,12 +533,6 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
           for (int i = 0; i < kLoads; ++i) load(i, next, free);
         });
       };
-      barrier_behind_loads<0>();  // (the last pass has read its last block)
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) load(i, 0, stage0);
-      if (Shape::kStages == 3 && blocks > 1)
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load(i, 1, stage1);
 #pragma unroll 1
       for (int32_t block = 0; block < blocks; block += Shape::kStages) {
         if constexpr (Shape::kStages == 3) {
@@ -527,6 +543,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
           turn(block, stage0, stage1);
           if (block + 1 < blocks) turn(block + 1, stage1, stage0);
         }
+      }
+      if (pass + even < tiles) {  // the next pass's first blocks come while this one's logits go
+        barrier_behind_loads<0>();
+        begin_pass(pass + even);
       }
       auto store = [&](auto type) {
         constexpr Elem O = decltype(type)::value;
