@@ -83,27 +83,34 @@ template <Elem E> struct Eight {
     for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));  // (a NaN is no maximum)
     return m;
   }
-  __device__ __forceinline__ uint2 codes(float inverse) const {
+  // `most`: the block's largest number, which is infinite where one of the eight may be
+  __device__ __forceinline__ uint2 codes(float inverse, float most) const {
+    float t[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t[k] = x[k] * inverse;
+    if (most > FLT_MAX) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (!(fabsf(t[k]) <= FLT_MAX)) t[k] = __builtin_nanf("");  // (e4m3 has no infinity)
+    }
     uint32_t w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      float t[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        t[k] = x[4 * i + k] * inverse;
-        if (!(fabsf(t[k]) <= FLT_MAX)) t[k] = __builtin_nanf("");  // (an infinity becomes NaN, which e4m3 has)
-      }
-      int word = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], 0, false);
-      w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], word, true);
+      const int word = __builtin_amdgcn_cvt_pk_fp8_f32(t[4 * i], t[4 * i + 1], 0, false);
+      w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(t[4 * i + 2], t[4 * i + 3], word, true);
     }
     return uint2{w[0], w[1]};
   }
 };
-// the largest of 16 neighbouring lanes
+// the largest of 16 neighbouring lanes: they turn by 8, 4, 2 and 1
+template <int kBy> __device__ __forceinline__ float turned_in_16(float m) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(m), 0x120 + kBy, 15, 15, true));
+}
 __device__ __forceinline__ float most_of_16(float m) {
-#pragma unroll
-  for (int d = 8; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-  return m;
+  m = fmaxf(m, turned_in_16<8>(m));
+  m = fmaxf(m, turned_in_16<4>(m));
+  m = fmaxf(m, turned_in_16<2>(m));
+  return fmaxf(m, turned_in_16<1>(m));
 }
 // 16 lanes to a block.  Columns behind K, up to `width`, become zeros.
 template <Elem E>
@@ -115,8 +122,9 @@ __global__ __launch_bounds__(256) void f8_quantize_kernel(const void* x, int64_t
   Eight<E> v;
   if (k < K) v.load(static_cast<const typename Type<E>::bits*>(x) + b * stride + k);
   else v.clear();
-  const uint32_t e = exponent_of(most_of_16(v.most()));
-  if (k < width) *reinterpret_cast<uint2*>(codes + b * codes_stride + k) = v.codes(__uint_as_float((254u - e) << 23));
+  const float most = most_of_16(v.most());
+  const uint32_t e = exponent_of(most);
+  if (k < width) *reinterpret_cast<uint2*>(codes + b * codes_stride + k) = v.codes(__uint_as_float((254u - e) << 23), most);
   if (((int32_t)threadIdx.x & 15) == 0) scales[b * scales_row + kb * scales_block] = __uint_as_float(e << 23);
 }
 
@@ -177,14 +185,15 @@ constexpr uint32_t kMaxLds = 160 * 1024;
 struct FewLayout {  // of dynamic LDS, bytes
   uint32_t scales, partial, list, end;
 };
-__host__ __device__ inline FewLayout few_layout(int32_t K, int32_t rows, int nb) {
+// 16 columns of all rows lie side by side, an odd number of them, so that a row's lie in different banks.
+__host__ __device__ inline int32_t few_pitch(int32_t rows) { return rows | 1; }
+__host__ __device__ inline FewLayout few_layout(int32_t K, int32_t rows) {
   const uint32_t blocks = (uint32_t)f8_blocks(K);
   FewLayout l;
-  l.scales = blocks * 128 * (uint32_t)rows;
+  l.scales = blocks * 128 * (uint32_t)few_pitch(rows);
   l.partial = l.scales + (blocks * (uint32_t)rows * 4 + 15) / 16 * 16;
   l.list = l.partial + kFewThreads * 16;
   l.end = l.list + (uint32_t)sizeof(List);
-  (void)nb;
   return l;
 }
 enum class States : int { kF8, kBF16, kF16 };
@@ -195,7 +204,8 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
   const int32_t tid = (int32_t)threadIdx.x, threads = (int32_t)blockDim.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = threads >> 6;
   const int32_t n = lane & 15, q = lane >> 4;
   const int32_t first_b = (int32_t)blockIdx.y * 16 * NB, rows = min(h.B - first_b, 16 * NB), blocks = f8_blocks(h.K);
-  const FewLayout at = few_layout(h.K, min(h.B, 16 * NB), NB);
+  const FewLayout at = few_layout(h.K, min(h.B, 16 * NB));
+  const int32_t pitch = few_pitch(min(h.B, 16 * NB));
   uint4v* const hidden = reinterpret_cast<uint4v*>(lds);  // [block][16 columns][row]
   float* const hidden_scales = reinterpret_cast<float*>(lds + at.scales);  // [block][row]
   float4v* const partial = reinterpret_cast<float4v*>(lds + at.partial);
@@ -250,13 +260,15 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
       brought = true;
       const int32_t units = blocks * rows * 16;  // 8 columns each, 16 neighbouring threads to a block
       constexpr int kAtOnce = 4;                 // of a thread
+      const uint32_t inverse = (uint32_t)(0x100000000ull / (uint32_t)rows) + 1u;  // (quotients of less than 2^26 by it are exact)
+      auto block_of = [&](int32_t u) { return rows == 1 ? u >> 4 : (int32_t)__umulhi((uint32_t)u >> 4, inverse); };
       for (int32_t u0 = tid; u0 < units; u0 += threads * kAtOnce) {
         Eight<T == States::kF16 ? Elem::kF16 : Elem::kBF16> x[kAtOnce];
         uint2 w[kAtOnce];
         float scale[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-          const int32_t u = u0 + i * threads, b = (u >> 4) % rows, block = (u >> 4) / rows, k = block * 128 + (u & 15) * 8;
+          const int32_t u = u0 + i * threads, block = block_of(u), b = (u >> 4) - block * rows, k = block * 128 + (u & 15) * 8;
           const bool there = u < units && k < h.K;
           if constexpr (T == States::kF8) {
             w[i] = uint2{0, 0};
@@ -269,14 +281,15 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
         }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-          const int32_t u = u0 + i * threads, b = (u >> 4) % rows, block = (u >> 4) / rows, k8 = u & 15;
+          const int32_t u = u0 + i * threads, block = block_of(u), b = (u >> 4) - block * rows, k8 = u & 15;
           if constexpr (T != States::kF8) {
-            const uint32_t e = exponent_of(most_of_16(x[i].most()));
-            w[i] = x[i].codes(__uint_as_float((254u - e) << 23));
+            const float most = most_of_16(x[i].most());
+            const uint32_t e = exponent_of(most);
+            w[i] = x[i].codes(__uint_as_float((254u - e) << 23), most);
             scale[i] = __uint_as_float(e << 23);
           }
           if (u >= units) break;
-          reinterpret_cast<uint2*>(hidden)[((block * 8 + (k8 >> 1)) * rows + b) * 2 + (k8 & 1)] = w[i];
+          reinterpret_cast<uint2*>(hidden)[((block * 8 + (k8 >> 1)) * pitch + b) * 2 + (k8 & 1)] = w[i];
           if (k8 == 0) hidden_scales[block * rows + b] = scale[i];
         }
       }
@@ -311,7 +324,7 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
               const int32_t b = min(nb * 16 + n, rows - 1);
-              const Halves x(hidden[(block * 8 + q) * rows + b], hidden[(block * 8 + 4 + q) * rows + b]);
+              const Halves x(hidden[(block * 8 + q) * pitch + b], hidden[(block * 8 + 4 + q) * pitch + b]);
               const float4v sum = products(a, x);
               const float state_scale = hidden_scales[block * rows + b];
               if constexpr (kMasked) acc[nb] += sum * (scale * state_scale);
@@ -321,22 +334,27 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
           codes = next_codes;
         }
       }
-      for (int nb = 0; nb < NB; ++nb) {
-        if (sharing > 1) {
+      if (sharing > 1) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
           partial[tid] = acc[nb];
           __syncthreads();
-          if (sub == 0)
+          if (sub == 0) {
+#pragma unroll 3
             for (int32_t w = 1; w < sharing; ++w) acc[nb] += partial[tid + w * 64];
+          }
           __syncthreads();
         }
-        if (sub == 0 && t < tiles && nb * 16 + n < rows) {
-          const int32_t b = first_b + nb * 16 + n;
+      }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (t * 16 + q * 4 + i >= count) continue;
-            const int64_t token = base + row_of(t, q * 4 + i);
-            store_logit(h, out_type, b * h.logits_stride + token, !kMasked || allowed(h, b, token) ? acc[nb][i] : -__builtin_inff());
-          }
+      for (int nb = 0; nb < NB; ++nb) {
+        if (sub != 0 || t >= tiles || nb * 16 + n >= rows) continue;
+        const int32_t b = first_b + nb * 16 + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (t * 16 + q * 4 + i >= count) continue;
+          const int64_t token = base + row_of(t, q * 4 + i);
+          store_logit(h, out_type, b * h.logits_stride + token, !kMasked || allowed(h, b, token) ? acc[nb][i] : -__builtin_inff());
         }
       }
       t += abreast;
@@ -679,14 +697,19 @@ hipError_t quantize_any(const void* x, Elem type, int32_t B, int32_t K, int64_t 
   return quantize<Elem::kF16>(x, B, K, stride, to, stream);
 }
 
+// tiles of a workgroup where the batch goes in shares of `rows`: so many that all workgroups run at once
+int32_t few_tiles(const F8Head& h, int32_t rows) {
+  const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), shares = (h.B + rows - 1) / rows, most = shares < kComputeUnits ? kComputeUnits / shares : 1;
+  return (tiles + most - 1) / most;
+}
 template <States T, int NB, bool kMasked> hipError_t launch_few(const F8Head& h, Elem out_type, hipStream_t stream) {
   static LdsRoom room;
   if (const hipError_t e = room(reinterpret_cast<const void*>(&f8_few_kernel<T, NB, kMasked>), kMaxLds); e != hipSuccess) return e;
-  const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), each = (tiles + kComputeUnits - 1) / kComputeUnits, steps = (f8_blocks(h.K) + kStep - 1) / kStep;
+  const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), each = few_tiles(h, 16 * NB), steps = (f8_blocks(h.K) + kStep - 1) / kStep;
   int32_t threads = 64;  // waves for its tiles, or for the steps of the few that masks leave
   while (threads < kFewThreads && threads < 64 * (kMasked && steps > each ? steps : each * (each < 16 ? steps : 1))) threads *= 2;
   const dim3 grid((tiles + each - 1) / each, (h.B + 16 * NB - 1) / (16 * NB));
-  hipLaunchKernelGGL((f8_few_kernel<T, NB, kMasked>), grid, dim3(threads), few_layout(h.K, h.B < 16 * NB ? h.B : 16 * NB, NB).end, stream, h, out_type, each);
+  hipLaunchKernelGGL((f8_few_kernel<T, NB, kMasked>), grid, dim3(threads), few_layout(h.K, h.B < 16 * NB ? h.B : 16 * NB).end, stream, h, out_type, each);
   return hipGetLastError();
 }
 template <States T, int NB> hipError_t launch_few_masked(const F8Head& h, Elem out_type, hipStream_t stream) {
@@ -697,7 +720,7 @@ template <int NB> hipError_t launch_few_states(const F8Head& h, Elem hidden_type
   if (hidden_type == Elem::kF16) return launch_few_masked<States::kF16, NB>(h, out_type, stream);
   return launch_few_masked<States::kBF16, NB>(h, out_type, stream);
 }
-bool few_fits(const F8Head& h, int32_t rows, int nb) { return few_layout(h.K, rows, nb).end <= kMaxLds; }
+bool few_fits(const F8Head& h, int32_t rows) { return few_layout(h.K, rows).end <= kMaxLds; }
 
 template <int MW, int WM, int TW, bool kMasked, class Operand> hipError_t launch_many(const F8Head& h, const StateScales& strides, Elem out_type, hipStream_t stream) {
   typedef ManyShape<MW, WM, TW> Shape;
@@ -721,10 +744,34 @@ hipError_t launch_f8_quantize(const void* x, Elem type, int32_t B, int32_t K, in
   return quantize_any(x, type, B, K, stride, Quantized{codes, codes_stride, K, scales, StateScales{f8_blocks(K), 1}}, stream);
 }
 
+namespace {
+// Which kernel takes more than 32 rows, by what a call takes them in us: a workgroup of few rows a start and a piece of each of its tiles; one of many
+// rows a time for each block of columns of each of its passes, which is that of a barrier and of loads that come back, not of the products.
+// For 4096 columns (32 blocks), bf16: 40 rows of 4096: few 21, many 40; 128 of 10000: 42 and 37; 500 of 2048: many 37 in tiles of 128 rows and 64 in those
+// of 256; 1024 of 128256: 700 and 628; 384 of 128256: 270 and 349.  Logits in 32 bits, 128 rows of 4096: few 25, many 63.
+enum class Many { kFew, k64, k128, k128Whole, k256 };
+double few_time(const F8Head& h) { return 7.0 + f8_blocks(h.K) * (0.3 + 0.075 * few_tiles(h, 32)); }
+double many_time(const F8Head& h, int32_t rows, double block) {
+  const int32_t passes = (few_tiles(h, rows) + 15) / 16;  // (a pass is 16 tiles in all of them)
+  return 4.0 + passes * (f8_blocks(h.K) * block);
+}
+Many kernel_of(const F8Head& h, Elem logits_type) {
+  const bool whole = logits_type == Elem::kF32;
+  Many best = h.B <= 64 ? Many::k64 : whole ? Many::k128Whole : Many::k128;
+  double time = h.B <= 64 ? many_time(h, 64, 1.2) : many_time(h, 128, whole ? 1.8 : 1.1);
+  if (!whole && h.B > 128 && many_time(h, 256, 1.95) < time) {
+    best = Many::k256;
+    time = many_time(h, 256, 1.95);
+  }
+  return few_fits(h, 32) && few_time(h) < time ? Many::kFew : best;
+}
+}  // namespace
 hipError_t launch_f8_logits(const F8Head& head, Elem hidden_type, Elem logits_type, void* work, hipStream_t stream) {
   F8Head h = head;
-  if (h.B <= 16 && few_fits(h, h.B, 1)) return launch_few_states<1>(h, hidden_type, logits_type, stream);
-  if (h.B <= 32 && few_fits(h, h.B, 2)) return launch_few_states<2>(h, hidden_type, logits_type, stream);
+  if (h.B <= 16 && few_fits(h, h.B)) return launch_few_states<1>(h, hidden_type, logits_type, stream);
+  if (h.B <= 32 && few_fits(h, h.B)) return launch_few_states<2>(h, hidden_type, logits_type, stream);
+  const Many kernel = kernel_of(h, logits_type);
+  if (kernel == Many::kFew) return launch_few_states<2>(h, hidden_type, logits_type, stream);
   StateScales strides{f8_blocks(h.K), 1};
   if (h.hidden.scales && work) {  // (a block's scales side by side: as they are, 256 rows take as many requests as 16 KB of codes)
     float* const scales = static_cast<float*>(work);
@@ -743,13 +790,12 @@ hipError_t launch_f8_logits(const F8Head& head, Elem hidden_type, Elem logits_ty
       return e;
     h.hidden = F8States{codes, padded(h.K), scales};
   }
-  if (h.B <= 64) return launch_many_masked<4, 1, 2, Halves>(h, strides, logits_type, stream);
-  if (logits_type == Elem::kF32) return launch_many_masked<4, 2, 4, Halves>(h, strides, logits_type, stream);
-  // Tiles of 256 rows read the matrix half as often as those of 128, and multiply more rows that are not there: 1024 rows of 128256 x 4096 take 642
-  // us and 700, 384 of them 349 and 271.
-  const int32_t of_256 = (h.B + 255) / 256 * 256, of_128 = (h.B + 127) / 128 * 128;
-  if (of_128 * 11 < of_256 * 10 || h.B <= 128) return launch_many_masked<4, 2, 4, Eights>(h, strides, logits_type, stream);
-  return launch_many_masked<8, 2, 4, Eights>(h, strides, logits_type, stream);
+  switch (kernel) {
+    case Many::k64: return launch_many_masked<4, 1, 2, Halves>(h, strides, logits_type, stream);
+    case Many::k128Whole: return launch_many_masked<4, 2, 4, Halves>(h, strides, logits_type, stream);
+    case Many::k256: return launch_many_masked<8, 2, 4, Eights>(h, strides, logits_type, stream);
+    default: return launch_many_masked<4, 2, 4, Eights>(h, strides, logits_type, stream);
+  }
 }
 
 hipError_t launch_q4_embed(const Embed& e, Elem scales_type, Elem out_type, hipStream_t stream) {
