@@ -67,7 +67,7 @@ __device__ __forceinline__ int32_t beam_of(u64 place) { return kMaxBeams - 1 - (
 __device__ __forceinline__ int32_t id_at(u64 place) { return (int32_t)(~(uint32_t)place & ((1u << kIdBits) - 1u)); }
 
 struct BeamShared {
-  float top[kWaves], most[kSliceThreads];
+  float most[kSliceThreads];
   double sum[kWaves];
   uint32_t n_found, counts[kWaves];
   u64 found[kMostFound], better[kMostFound];
@@ -96,36 +96,51 @@ __device__ __forceinline__ uint32_t count_all(uint32_t mine, uint32_t (&counts)[
   return all;
 }
 
-// The least of the largest numbers of `groups` groups of threads (a power of two up to kMaxContinuations); all threads get it.  Threads of a group lie
+// What bounds the largest numbers of `groups` groups of threads (a power of two up to kMaxContinuations); all threads get it.  Threads of a group lie
 // `groups` apart: where a row ends in the slice every group still has some of its tokens.
 constexpr int kMaxGroups = 128;
 static_assert(kMaxContinuations <= kMaxGroups && kMaxGroups == 128, "two waves of groups at most");
-template <class T> __device__ __forceinline__ T least_of_groups(T mine, int groups, T (&most)[kSliceThreads]) {
+template <class T> struct Bounds {
+  T least, top;  // of the groups' largest numbers: the least, and the largest of all
+};
+template <class T> __device__ __forceinline__ Bounds<T> bounds_of_groups(T mine, int groups, T (&most)[kSliceThreads]) {
   const int lane = (int)threadIdx.x & 63, tid = (int)threadIdx.x;
   for (int d = 32; d >= groups; d >>= 1) mine = max(mine, (T)__shfl_xor(mine, d));
   __syncthreads();
   most[tid] = mine;
   __syncthreads();
-  T r = most[lane];  // groups of all waves, or of the even ones
-  if (groups <= 64) {
+  T r = most[lane], odd = most[64 + lane];  // groups of the even waves, and of the odd ones
 #pragma unroll
-    for (int k = 1; k < kWaves; ++k) r = max(r, most[k * 64 + lane]);
-  } else {
-    T odd = most[64 + lane];
-#pragma unroll
-    for (int k = 2; k < kWaves; k += 2) {
-      r = max(r, most[k * 64 + lane]);
-      odd = max(odd, most[k * 64 + 64 + lane]);
-    }
-    r = min(r, odd);
+  for (int k = 2; k < kWaves; k += 2) {
+    r = max(r, most[k * 64 + lane]);
+    odd = max(odd, most[k * 64 + 64 + lane]);
   }
+  Bounds<T> b{groups <= 64 ? max(r, odd) : min(r, odd), max(r, odd)};
 #pragma unroll
-  for (int d = 32; d; d >>= 1) r = min(r, (T)__shfl_xor(r, d));
-  return r;
+  for (int d = 32; d; d >>= 1) {
+    b.least = min(b.least, (T)__shfl_xor(b.least, d));
+    b.top = max(b.top, (T)__shfl_xor(b.top, d));
+  }
+  return b;
+}
+// y[k], by the steps of a tree
+__device__ __forceinline__ float token_at(const Tokens& y, int k) {
+  float x[kTokens];
+#pragma unroll
+  for (int i = 0; i < kTokens; ++i) x[i] = y[i];
+#pragma unroll
+  for (int n = kTokens / 2; n; n >>= 1)
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      float upper = x[i + n];
+      asm("" : "+v"(upper));  // (else the compiler makes it one access by a number that differs between lanes, in a loop over them: 13 us of 47)
+      x[i] = k & n ? upper : x[i];
+    }
+  return x[0];
 }
 
 template <Elem E>
-__global__ __launch_bounds__(kSliceThreads, 5) void beam_slices_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m, int groups) {
+__global__ __launch_bounds__(kSliceThreads, 8) void beam_slices_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m, int groups) {
   extern __shared__ __align__(16) char lds[];
   RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   BeamShared& sh = *reinterpret_cast<BeamShared*>(lds);
@@ -142,15 +157,9 @@ __global__ __launch_bounds__(kSliceThreads, 5) void beam_slices_kernel(Logits in
     float mine = -__builtin_inff();
 #pragma unroll
     for (int k = 0; k < kTokens; ++k) mine = fmaxf(mine, y[k]);
-    const float bound = least_of_groups(mine, groups, sh.most);
-    float top = mine;
-#pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane == 0) sh.top[wave] = top;
-    if (tid == 0) sh.n_found = 0;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, sh.top[k]);
+    if (tid == 0) sh.n_found = 0;  // (read behind the next barriers)
+    const Bounds<float> bounds = bounds_of_groups(mine, groups, sh.most);
+    const float top = bounds.top;
     BeamSlot slot{0.0, 0.0, top};
     u64* const list = m.lists + ((size_t)b * m.slices + slice) * n;
     if (top > -__builtin_inff()) {
@@ -169,18 +178,27 @@ __global__ __launch_bounds__(kSliceThreads, 5) void beam_slices_kernel(Logits in
       if (lane == 0) sh.sum[wave] = sum;
       uint32_t good = 0;
 #pragma unroll
-      for (int k = 0; k < kTokens; ++k) good |= (y[k] > -__builtin_inff() && y[k] >= bound ? 1u : 0u) << k;
-      uint32_t all = count_all((uint32_t)__builtin_popcount(good), sh.counts);
+      for (int k = 0; k < kTokens; ++k) good |= (y[k] > -__builtin_inff() && y[k] >= bounds.least ? 1u : 0u) << k;
+      auto collect = [&] {
+        if (!good) return;
+        uint32_t at = atomicAdd(&sh.n_found, (uint32_t)__builtin_popcount(good));
+#pragma unroll 1
+        for (uint32_t left = good; left; left &= left - 1, ++at) {
+          const int k = __builtin_ctz(left);
+          if (at < kMostFound) sh.found[at] = token_key(token_at(y, k), first + place_of(k));
+        }
+      };
+      collect();
+      __syncthreads();
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) slot.sum += sh.sum[k];
+      uint32_t all = sh.n_found;
       if (all > kMostFound) {  // many equal ones: the key of the n-th best, bit by bit
-        // (the logits go round in their registers: 16 keys at once would take twice as many)
         auto above = [&](u64 least) {
           uint32_t bits = 0;
 #pragma unroll 1
           for (int k = 0; k < kTokens; ++k) {
-            const float v = y[0];
-            y = __builtin_shufflevector(y, y, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0);
+            const float v = token_at(y, k);
             bits |= (v > -__builtin_inff() && token_key(v, first + place_of(k)) >= least ? 1u : 0u) << k;
           }
           return bits;
@@ -192,26 +210,20 @@ __global__ __launch_bounds__(kSliceThreads, 5) void beam_slices_kernel(Logits in
           if (count_all((uint32_t)__builtin_popcount(above(at)), sh.counts) >= (uint32_t)n) edge = at;
         }
         good = above(edge);
+        if (tid == 0) sh.n_found = 0;
+        __syncthreads();
+        collect();
+        __syncthreads();
         all = (uint32_t)n;
       }
-      if (good) {
-        uint32_t at = atomicAdd(&sh.n_found, (uint32_t)__builtin_popcount(good));
-#pragma unroll 1
-        for (int k = 0; k < kTokens; ++k) {
-          const float v = y[0];
-          y = __builtin_shufflevector(y, y, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15, 0);
-          if (good >> k & 1u) sh.found[at++] = token_key(v, first + place_of(k));
-        }
-      }
-      __syncthreads();
       const u64* found = sh.found;
       // Where masks leave tokens in a few places a bound says little; another one among what was found, which lies in no order, says more.
       if (all > (uint32_t)(4 * groups + 64)) {
         static_assert(kMostFound == 2 * kSliceThreads, "two tokens a thread");
         const u64 none = 0;
         const u64 one = (uint32_t)tid < all ? sh.found[tid] : none, two = (uint32_t)tid + kSliceThreads < all ? sh.found[tid + kSliceThreads] : none;
-        const float next = least_of_groups(max(one, two) ? logit_of(max(one, two)) : -__builtin_inff(), groups, sh.most);
-        if (tid == 0) sh.n_found = 0;
+        const float next = bounds_of_groups(max(one, two) ? logit_of(max(one, two)) : -__builtin_inff(), groups, sh.most).least;
+        if (tid == 0) sh.n_found = 0;  // (all have read it: they have met behind that)
         __syncthreads();
         if (one && logit_of(one) >= next) sh.better[atomicAdd(&sh.n_found, 1u)] = one;
         if (two && logit_of(two) >= next) sh.better[atomicAdd(&sh.n_found, 1u)] = two;
@@ -316,16 +328,23 @@ __global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, 
   };
   double mine = -__builtin_inf();
   for_entries([&](double sum, u64) { mine = max(mine, sum); });
-  const double bound = least_of_groups(mine, groups, join.most);
-  auto joins = [&](double sum) { return sum >= bound; };
-  uint32_t all = 0;
-  {
-    uint32_t some = 0;
-    for_entries([&](double sum, u64) { some += joins(sum); });
-    all = count_all(some, join.counts);
-  }
-  u64 edge = 0, edge_place = 0;  // what counts: more than edge, or edge itself with edge_place or more
+  const double bound = bounds_of_groups(mine, groups, join.most).least;
+  auto collect = [&](auto&& joins) {
+    for_entries([&](double sum, u64 place) {
+      const u64 order = order_of(sum);
+      if (!joins(sum, order, place)) return;
+      const uint32_t at = atomicAdd(&join.n_joined, 1u);
+      if (at < kMostJoined) {
+        join.order[at] = order;
+        join.place[at] = place;
+      }
+    });
+  };
+  collect([&](double sum, u64, u64) { return sum >= bound; });
+  __syncthreads();
+  uint32_t all = join.n_joined;
   if (all > kMostJoined) {  // many equal ones: the n-th best, bit by bit
+    u64 edge = 0, edge_place = 0;  // what counts: more than edge, or edge itself with edge_place or more
 #pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const u64 at = edge | 1ull << bit;
@@ -340,16 +359,12 @@ __global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, 
       for_entries([&](double sum, u64 place) { some += order_of(sum) > edge || (order_of(sum) == edge && place >= at); });
       if (count_all(some, join.counts) >= (uint32_t)n) edge_place = at;
     }
+    if (tid == 0) join.n_joined = 0;
+    __syncthreads();
+    collect([&](double, u64 order, u64 place) { return order > edge || (order == edge && place >= edge_place); });
+    __syncthreads();
     all = (uint32_t)n;
   }
-  for_entries([&](double sum, u64 place) {
-    const u64 order = order_of(sum);
-    if (joins(sum) && (order > edge || (order == edge && place >= edge_place))) {
-      const uint32_t at = atomicAdd(&join.n_joined, 1u);
-      join.order[at] = order;
-      join.place[at] = place;
-    }
-  });
   if (tid < n) {
     join.rows[tid] = join.ids[tid] = -1;
     join.scores[tid] = -__builtin_inff();
