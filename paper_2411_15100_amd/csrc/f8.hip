@@ -478,13 +478,23 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
           bring4(scale_at + block * scale_step, &to.scales[wave * 64]);
         }
       };
+    // all of a block, or its codes, or the rest
+    auto load_codes = [&](int32_t turn, Buffer& to) {
+#pragma unroll
+      for (int i = 0; i < Shape::kCodeLoads; ++i) load(i, turn, to);
+    };
+    auto load_others = [&](int32_t turn, Buffer& to) {
+#pragma unroll
+      for (int i = Shape::kCodeLoads; i < kLoads; ++i) load(i, turn, to);
+    };
     auto begin_pass = [&](int32_t pass) {
       point(pass);
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) load(i, 0, stage0);
-      if (Shape::kStages == 3 && blocks > 1)
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) load(i, 1, stage1);
+      load_others(0, stage0);
+      load_codes(0, stage0);
+      if (blocks > 1) {
+        if (Shape::kStages == 3) load_others(1, stage1);
+        load_codes(1, stage1);
+      }
     };
     barrier_behind_loads<0>();  // (what was there before has been read)
     begin_pass(0);
@@ -540,16 +550,28 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
           __builtin_amdgcn_sched_barrier(0);
         }
       };
-      // A block is there when all waves have waited for their parts of it; the buffer of the block before it is free then.
-      auto turn = [&](int32_t block, const Buffer& now, Buffer& free) {
-        if (Shape::kStages == 3 && block + 1 < blocks) barrier_behind_loads<kLoads>();
-        else barrier_behind_loads<0>();
-        const int32_t next = block + Shape::kStages - 1;
-        multiply(now, [&] {
-          if (next >= blocks) return;
-#pragma unroll
-          for (int i = 0; i < kLoads; ++i) load(i, next, free);
-        });
+      // A block is there when all waves have waited for their parts of it.  Of three buffers the one of the block before it is free then.  Of two,
+      // codes are in registers before the first product: behind a barrier more, those of the block after the next come to the same place, and are
+      // on their way for two blocks, as memory asks; hidden states, which come from the L2, for one (1024 rows of 128256 x 4096: 611 us, and 627
+      // where all of the next block comes at once).
+      auto turn = [&](int32_t block, Buffer& now, Buffer& other) {
+        if constexpr (Shape::kStages == 3) {
+          if (block + 1 < blocks) barrier_behind_loads<kLoads>();
+          else barrier_behind_loads<0>();
+          multiply(now, [&] {
+            if (block + 2 >= blocks) return;
+            load_others(block + 2, other);
+            load_codes(block + 2, other);
+          });
+        } else {
+          if (block + 1 < blocks) barrier_behind_loads<Shape::kCodeLoads>();
+          else barrier_behind_loads<0>();
+          multiply(now, [&] {
+            barrier_behind_loads<63>();  // (for reads of LDS alone)
+            if (block + 1 < blocks) load_others(block + 1, other);
+            if (block + 2 < blocks) load_codes(block + 2, now);
+          });
+        }
       };
 #pragma unroll 1
       for (int32_t block = 0; block < blocks; block += Shape::kStages) {
