@@ -611,7 +611,9 @@ int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, in
                const xgm_logit_rules* rules, const xgm_draw_rules* draw, int32_t* d_ids, float* d_logprobs,
                void* hip_stream);
 
-/* 9. The output projection (6) with a matrix in 8-bit floating point (e4m3: 4 bits of exponent, 3 of mantissa, up to 448, no
+/* (As those above, the calls of 9 to 12 but for create and destroy are asynchronous, allocate nothing and may be captured into a graph.)
+ *
+ * 9. The output projection (6) with a matrix in 8-bit floating point (e4m3: 4 bits of exponent, 3 of mantissa, up to 448, no
  * infinities; 0x7f and 0xff are NaN) and a scale for each block of 128 rows and 128 columns:
  *   logits[b][v] = sum over blocks j of 128 columns of
  *                  hidden_scale(b, j) * scale(v / 128, j) * sum over k in j of hidden[b][k] * code(v, k),
@@ -691,7 +693,7 @@ typedef struct {
 /* Row b of each of the n <= XGM_MAX_ROW_DATA arrays (host memory, read during the call) takes over what is in use of row d_rows[b], as that was before the
  * call, whatever goes where; behind that it stays as it is.  A row whose d_rows[b] is negative, b itself, or B or more stays.  B <= XGM_BATCH_MAX_ROWS.  Rows
  * and parts of an array must not overlap each other, nor what lies from the first byte of an array to its last that of another array of the call, d_rows
- * or a d_used (lengths are moved by a call of their own, behind this one).  Bytes are copied in units of up to 16, the largest power of two that divides
+ * or a d_used (lengths are moved by a call of their own, behind this one).  n_outer * n_parts <= 2^27.  Bytes are copied in units of up to 16, the largest power of two that divides
  * the address, the strides and sizes of an array.  One launch. */
 int xgm_reorder_rows(const xgm_row_data* arrays, int32_t n, const int32_t* d_rows, int32_t B, void* hip_stream);
 

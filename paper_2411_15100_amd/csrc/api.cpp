@@ -2588,7 +2588,7 @@ const char* row_data_fault(const xgm_row_data& d, int32_t B, uint64_t* last) {
     if (a.stride < extent) return "rows or parts overlap";
     extent += (__int128)(a.n - 1) * a.stride;
   }
-  if (extent > ((__int128)1 << 62)) return "strides beyond the address space";
+  if (extent > ((__int128)1 << 62) || (d.d_used && d.used_bytes > (int64_t)1 << 62)) return "strides beyond the address space";
   *last = (uint64_t)extent;
   return nullptr;
 }
@@ -2609,6 +2609,7 @@ int xgm_reorder_rows(const xgm_row_data* arrays, int32_t n, const int32_t* d_row
   for (int32_t i = 0; i < n; ++i) {
     const xgm_row_data& d = arrays[i];
     if (const char* what = row_data_fault(d, B, &extent[i])) return fail(XGM_ERR_BAD_ARG, std::string("reorder_rows: ") + what);
+    if ((int64_t)d.n_outer * d.n_parts > 1 << 27) return fail(XGM_ERR_TOO_LARGE, "reorder_rows: more than 2^27 parts of a row");
     data[i] = RowData{d.d_data, d.row_stride, d.outer_stride, d.part_stride, d.part_bytes, d.d_used, d.used_bytes, d.n_outer, d.n_parts};
   }
   for (int32_t i = 0; i < n; ++i) {

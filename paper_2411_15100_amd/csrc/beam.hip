@@ -517,14 +517,15 @@ __global__ __launch_bounds__(kMoveThreads) void reorder_kernel(RowDataList list,
   r.row_stride = d.row_stride;
   r.base = static_cast<char*>(d.data) + piece / d.n_parts * d.outer_stride + piece % d.n_parts * d.part_stride;
   const int32_t* const used = d.used;
-  const int64_t used_bytes = d.used_bytes;
+  const int64_t used_bytes = d.used_bytes, units_of_part = used ? (part_bytes + used_bytes - 1) / used_bytes : 0;
   if (threadIdx.x < kMaxMoveRows / 32) m.moves[threadIdx.x] = 0;
   if (threadIdx.x == 0) m.n = m.tangled = 0;
   __syncthreads();
   for (int32_t b = (int32_t)threadIdx.x; b < B; b += kMoveThreads) {
     const int32_t a = source[b];
     if (a < 0 || a >= B || a == b) continue;
-    const int64_t most = used ? (int64_t)used[a] * used_bytes : part_bytes;
+    // (a length beyond the part is all of it, however large)
+    const int64_t most = used ? min((int64_t)used[a], units_of_part) * used_bytes : part_bytes;
     if (most <= r.begin) continue;
     const int32_t i = atomicAdd(&m.n, 1);
     m.to[i] = b;

@@ -118,7 +118,8 @@ ROWS = dict(d_data=A, row_stride=64, outer_stride=64 * 8, part_stride=16, part_b
     (dict(d_data=0), "null"), (dict(n_outer=0), "positive"), (dict(n_parts=-1), "positive"), (dict(part_bytes=0), "positive"), (dict(row_stride=-64), "negative"),
     (dict(outer_stride=-1), "negative"), (dict(part_stride=-16), "negative"), (dict(d_used=8 * A), "unit"), (dict(d_used=8 * A, used_bytes=-4), "unit"),
     (dict(d_used=8 * A + 2, used_bytes=4), "aligned"), (dict(row_stride=63), "overlap"), (dict(part_stride=15), "overlap"), (dict(outer_stride=511), "overlap"),
-    (dict(row_stride=0), "overlap"), (dict(row_stride=1 << 62), "address space")])
+    (dict(row_stride=0), "overlap"), (dict(row_stride=1 << 62), "address space"),
+    (dict(d_used=8 * A, used_bytes=(1 << 62) + 1), "address space")])
 def test_moving_rows_refuses(change, text):
     with pytest.raises(xgm.XgmError, match=text) as e:
         xgm.reorder_rows(xgm.RowSet(xgm.RowData(**{**ROWS, **change})), 4 * A, 8)
@@ -136,6 +137,10 @@ def test_moving_rows_refuses_what_overlaps_and_too_many():
         with pytest.raises(xgm.XgmError, match=text) as e:
             xgm.reorder_rows(xgm.RowSet(*arrays), d_rows, rows)
         assert e.value.status == status
+    with pytest.raises(xgm.XgmError, match="2\\^27") as e:
+        xgm.reorder_rows(xgm.RowSet(xgm.RowData(d_data=1 << 40, row_stride=1, part_bytes=1, n_outer=1 << 14, outer_stride=1 << 20, n_parts=(1 << 13) + 1, part_stride=8)),
+                         4 * A, 8)
+    assert e.value.status == -9
     with pytest.raises(TypeError):
         xgm.RowSet(dict(ROWS))
     with pytest.raises(TypeError):

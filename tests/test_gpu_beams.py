@@ -288,6 +288,22 @@ def test_several_arrays_move_at_once_with_strides_and_odd_addresses():
         assert torch.equal(g, w)
 
 
+def test_lengths_at_their_ends_and_units_that_do_not_divide_a_part():
+    xgm = _xgm()
+    B, part = 6, 100
+    for unit in (1, 3, 7, 100, 160, 2 ** 40):
+        for value in (0, -1, -2 ** 31, 1, 13, 2 ** 31 - 1):
+            t = torch.randint(0, 256, (B, 2, part), dtype=torch.uint8, device="cuda")
+            want = t.clone()
+            n = max(0, min(part, value * unit))
+            want[:, :, :n] = t[[1, 2, 3, 4, 5, 0], :, :n]
+            on, used = torch.tensor([1, 2, 3, 4, 5, 0], dtype=torch.int32, device="cuda"), torch.full((B,), value, dtype=torch.int32, device="cuda")
+            xgm.reorder_rows(xgm.RowSet(xgm.RowData(d_data=t.data_ptr(), row_stride=2 * part, part_bytes=part, part_stride=part, n_outer=1, n_parts=2,
+                                                    d_used=used.data_ptr(), used_bytes=unit)), on.data_ptr(), B, _stream())
+            torch.cuda.synchronize()
+            assert torch.equal(t, want), (unit, value)
+
+
 def test_rows_beyond_2_to_the_31_bytes():
     xgm = _xgm()
     t = torch.zeros((3, 1 << 30), dtype=torch.int32, device="cuda")      # 4 GiB a row

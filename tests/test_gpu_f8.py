@@ -263,6 +263,28 @@ def test_a_part_of_a_larger_matrix_under_its_masks():
     assert np.array_equal(got, np.where(allowed, want, -np.inf)[:, first:])
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("B,K,V", [(2000, 128, 1000), (1100, 272, 20001), (40000, 16, 64), (66000 - 465, 32, 17), (129, 512, 30001), (257, 1024, 9000), (48, 640, 70001)])
+def test_projection_of_large_batches_and_large_matrices(B, K, V, masked, out):
+    p = Projection(B, K, V, "f16", whole=True, seed=V)
+    mask, allowed = None, None
+    if masked:
+        allowed = torch.rand((B, V), generator=torch.Generator().manual_seed(1)) < 0.3
+        allowed[:, V // 4:V // 2] = False
+        allowed[B // 2:] = False
+        mask = torch.from_numpy(plain_logits.pack(allowed.numpy())).cuda()
+    got = p.run(out, mask=mask)
+    table = torch.from_numpy(plain.e4m3()).float().cuda()
+    h = table[torch.from_numpy(p.eight[0]).cuda().int()] * torch.from_numpy(p.eight[1]).float().cuda().repeat_interleave(128, 1)[:, :K]
+    w = table[p.codes.int()] * p.scales.repeat_interleave(128, 0)[:V].repeat_interleave(128, 1)[:, :K]
+    for b in range(0, B, 8192):          # (exact: whole numbers below 2^24)
+        want = h[b:b + 8192] @ w.T
+        if masked:
+            want.masked_fill_(~allowed[b:b + 8192].cuda(), -float("inf"))
+        assert torch.equal(got[b:b + 8192], want.to(got.dtype)), b
+
+
 def test_projection_of_what_is_not_finite():
     p = Projection(40, 256, 300, "bf16", seed=1)
     p.hidden[3, 5], p.hidden[39, 200] = float("inf"), float("nan")
