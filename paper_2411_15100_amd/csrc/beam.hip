@@ -140,7 +140,7 @@ __device__ __forceinline__ float token_at(const Tokens& y, int k) {
 }
 
 template <Elem E>
-__global__ __launch_bounds__(kSliceThreads, 8) void beam_slices_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m, int groups) {
+__global__ __launch_bounds__(kSliceThreads, 6) void beam_slices_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m, int groups) {
   extern __shared__ __align__(16) char lds[];
   RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   BeamShared& sh = *reinterpret_cast<BeamShared*>(lds);

@@ -141,7 +141,9 @@ __device__ __forceinline__ bool allowed(const F8Head& h, int32_t b, int64_t toke
   return !h.mask || (token < h.V_mask && (h.mask[(size_t)b * h.W_mask + (token >> 5)] >> (token & 31) & 1u));
 }
 __device__ int32_t list_rows(const F8Head& h, Elem out_type, int32_t first_b, int32_t rows, int64_t base, int32_t here, List& list) {
-  const int32_t tid = (int32_t)threadIdx.x, threads = (int32_t)blockDim.x;
+  int32_t tid = (int32_t)threadIdx.x;
+  const int32_t threads = (int32_t)blockDim.x;
+  asm volatile("" : "+v"(tid));  // (else places in the list are kept in registers while the matrix goes by)
   __syncthreads();
   if (tid < kListed / 32) list.any[tid] = 0;
   if (tid == 0) list.n = 0;
@@ -262,7 +264,9 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
       constexpr int kAtOnce = 4;                 // of a thread
       const uint32_t inverse = (uint32_t)(0x100000000ull / (uint32_t)rows) + 1u;  // (quotients of less than 2^26 by it are exact)
       auto block_of = [&](int32_t u) { return rows == 1 ? u >> 4 : (int32_t)__umulhi((uint32_t)u >> 4, inverse); };
-      for (int32_t u0 = tid; u0 < units; u0 += threads * kAtOnce) {
+      int32_t begin = tid;
+      asm volatile("" : "+v"(begin));  // (as in list_rows)
+      for (int32_t u0 = begin; u0 < units; u0 += threads * kAtOnce) {
         Eight<T == States::kF16 ? Elem::kF16 : Elem::kBF16> x[kAtOnce];
         uint2 w[kAtOnce];
         float scale[kAtOnce];
@@ -395,6 +399,10 @@ __device__ __forceinline__ uint32_t lds_place(const void* to) {
 __device__ __forceinline__ void bring16(const void* from, const void* to) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_place(to)), "v"(from) : "memory");
 }
+// the same from an address that all lanes share and an offset each
+__device__ __forceinline__ void bring16(const void* from, uint32_t offset, const void* to) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_place(to)), "v"(offset), "s"(from) : "memory");
+}
 __device__ __forceinline__ void bring4(const void* from, const void* to) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_place(to)), "v"(from) : "memory");
 }
@@ -434,11 +442,21 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
   // channels of the L2: the workgroups of an XCD begin with different blocks.
   const int32_t begin = share / 8 % blocks;
   auto turned = [&](int32_t block) { return block + begin < blocks ? block + begin : block + begin - blocks; };
-  const int32_t row_in = lane >> 3, column = ((lane & 7) ^ row_in) * 16;  // what a lane brings of 8 rows
-  const uint8_t* state_at[Shape::kStateLoads];
+  const uint8_t* const all_states = static_cast<const uint8_t*>(h.hidden.at) + first_b * h.hidden.stride;
+  const uint32_t in_row = (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);  // what a lane brings of 8 rows
+  // Addresses of all that a wave brings lie in registers, where there are enough.  kLean: the sums need them; 8 rows come from one address and an
+  // offset that stays the same, and those past the last one, or columns around the last one, from an address each that is computed anew every time
+  // (which the asm below sees to).
+  constexpr bool kLean = Shape::kStages == 2;
+  static_assert(!kLean || !kMasked, "rows of a list do not follow each other");
+  const bool near = h.hidden.stride < 1 << 28;  // (offsets within 8 rows fit 32 bits)
+  [[maybe_unused]] const uint32_t code_offset = (uint32_t)(lane >> 3) * (uint32_t)h.K + in_row, state_offset = (uint32_t)(lane >> 3) * (uint32_t)h.hidden.stride + in_row;
+  [[maybe_unused]] const uint8_t* state_at[Shape::kStateLoads];
+  if constexpr (!kLean) {
 #pragma unroll
-  for (int u = 0; u < Shape::kStateLoads; ++u)
-    state_at[u] = static_cast<const uint8_t*>(h.hidden.at) + (first_b + min((wave * Shape::kStateLoads + u) * 8 + row_in, rows - 1)) * h.hidden.stride + column;
+    for (int u = 0; u < Shape::kStateLoads; ++u)
+      state_at[u] = all_states + min((wave * Shape::kStateLoads + u) * 8 + (lane >> 3), rows - 1) * h.hidden.stride + in_row;
+  }
   const int64_t row0 = (int64_t)share * tiles_each * 16, row1 = min((int64_t)h.V, row0 + (int64_t)tiles_each * 16);
   constexpr int64_t kTogether = kMasked ? kListed : 32768;  // (rows of the matrix, whose codes begin within 32 bits of each other)
   for (int64_t base = row0; base < row1; base += kTogether) {
@@ -454,30 +472,59 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
     const uint8_t* const base_codes = h.codes + base * h.K;
     const int32_t passes = (tiles + Shape::kPass - 1) / Shape::kPass, even = passes ? (tiles + passes - 1) / passes : 0;
     if (tiles == 0) continue;
-    uint32_t code_at[Shape::kCodeLoads];
-    const float* scale_at;
-    const int32_t scale_step = tid < Shape::kRows ? (int32_t)strides.block : 1;
-    auto point = [&](int32_t pass) {  // at what the wave brings of a pass
-      const int32_t last = min(even, tiles - pass) * 16 - 1;
+    // What a wave brings of a pass, from_row .. last_row of the rows here, 8 rows at a time.
+    int32_t from_row = 0, last_row = 0;
+    [[maybe_unused]] uint32_t code_at[Shape::kCodeLoads];
+    const float* scale_at = nullptr;
+    auto point = [&](int32_t pass) {
+      from_row = pass * 16;
+      last_row = min(from_row + even * 16, count) - 1;
+      if constexpr (!kLean) {
 #pragma unroll
-      for (int u = 0; u < Shape::kCodeLoads; ++u)
-        code_at[u] = (uint32_t)row_of(pass * 16 + min((wave * Shape::kCodeLoads + u) * 8 + row_in, last)) * (uint32_t)h.K;
+        for (int u = 0; u < Shape::kCodeLoads; ++u)
+          code_at[u] = (uint32_t)row_of(min(from_row + (wave * Shape::kCodeLoads + u) * 8 + (lane >> 3), last_row)) * (uint32_t)h.K;
+      }
       if (tid < Shape::kRows) scale_at = h.hidden.scales + (first_b + min(tid, rows - 1)) * strides.row;
-      else scale_at = h.scales + ((base + row_of(pass * 16 + min(tid - Shape::kRows, last))) >> 7) * blocks;
+      else scale_at = h.scales + ((base + row_of(min(from_row + tid - Shape::kRows, last_row))) >> 7) * blocks;
     };
-      // the i-th of a wave's kLoads loads of a block
-      auto load = [&](int i, int32_t turn, Buffer& to) {
-        const int32_t block = turned(turn), k = block * 128;
-        if (i < Shape::kCodeLoads) {  // (hidden states are 0 behind the last column)
-          bring16(base_codes + (code_at[i] + (uint32_t)min(k + column, h.K - 16)), &to.codes[(wave * Shape::kCodeLoads + i) * 64]);
-        } else if (i < Shape::kCodeLoads + Shape::kStateLoads) {
-          const int u = i - Shape::kCodeLoads;
-          bring16(reinterpret_cast<const void*>(k + column < h.K ? reinterpret_cast<uintptr_t>(state_at[u] + k) : reinterpret_cast<uintptr_t>(&kZeros)),
-                  &to.states[(wave * Shape::kStateLoads + u) * 64]);
+    // the i-th of a wave's kLoads loads of a block
+    auto load = [&](int i, int32_t turn, Buffer& to) {
+      const int32_t block = turned(turn);
+      const bool whole = (block + 1) * 128 <= h.K;
+      int32_t thread = tid;
+      if (i < Shape::kCodeLoads) {  // (behind the last column some earlier part of the row: hidden states are 0 there)
+        const int32_t first = (wave * Shape::kCodeLoads + i) * 8;
+        uint4v* const place = &to.codes[first * 8];
+        if constexpr (!kLean) {
+          bring16(base_codes + (code_at[i] + (uint32_t)min(block * 128 + (int32_t)in_row, h.K - 16)), place);
+        } else if (whole && from_row + first + 7 <= last_row) {
+          bring16(base_codes + ((int64_t)(from_row + first) * h.K + block * 128), code_offset, place);
         } else {
-          bring4(scale_at + block * scale_step, &to.scales[wave * 64]);
+          asm volatile("" : "+v"(thread));
+          const int32_t in = thread >> 3 & 7, k = block * 128 + ((thread & 7) ^ in) * 16;
+          bring16(base_codes + ((uint32_t)min(from_row + first + in, last_row) * (uint32_t)h.K + (uint32_t)min(k, h.K - 16)), place);
         }
-      };
+      } else if (i < Shape::kCodeLoads + Shape::kStateLoads) {
+        const int u = i - Shape::kCodeLoads;
+        const int32_t first = (wave * Shape::kStateLoads + u) * 8;
+        uint4v* const place = &to.states[first * 8];
+        const auto or_zeros = [&](const uint8_t* at, int32_t k) {
+          return reinterpret_cast<const void*>(k < h.K ? reinterpret_cast<uintptr_t>(at) : reinterpret_cast<uintptr_t>(&kZeros));
+        };
+        if constexpr (!kLean) {
+          bring16(or_zeros(state_at[u] + block * 128, block * 128 + (int32_t)in_row), place);
+        } else if (whole && near && first + 8 <= rows) {
+          bring16(all_states + (first * h.hidden.stride + block * 128), state_offset, place);
+        } else {
+          asm volatile("" : "+v"(thread));
+          const int32_t in = thread >> 3 & 7, k = block * 128 + ((thread & 7) ^ in) * 16;
+          bring16(or_zeros(all_states + min(first + in, rows - 1) * h.hidden.stride + k, k), place);
+        }
+      } else {
+        asm volatile("" : "+v"(thread));
+        bring4(scale_at + block * (thread < Shape::kRows ? (int32_t)strides.block : 1), &to.scales[wave * 64]);
+      }
+    };
     // all of a block, or its codes, or the rest
     auto load_codes = [&](int32_t turn, Buffer& to) {
 #pragma unroll
@@ -521,29 +568,31 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
           else scale[c][0] = s.scales[Shape::kRows + (first + c) * 16];
         }
         const Operand a[4] = {operand(my_codes), operand(my_codes + (TW > 1) * 128), operand(my_codes + (TW > 2) * 256), operand(my_codes + (TW > 3) * 384)};
-        // the sums of 16 rows are scaled while the next ones' products are made
-        float4v sum[2][TW];
-        float scale_of[2];
+        // the sums of a tile are scaled while the next ones' products are made
+        // (1024 rows of 128256 x 4096: one behind 643 us, two 639, four 617)
+        constexpr int kBehind = kMasked && sizeof(Operand) > 32 ? 2 : 4;  // (registers)
+        constexpr int kRoundsBehind = (kBehind + TW - 1) / TW;
+        float4v sum[kBehind + 1];
+        float scale_of[kRoundsBehind + 1];
+        load_other();
 #pragma unroll
-        for (int m = 0; m <= MW; ++m) {
-          if (m == 0) load_other();
-          if (m < MW) {
-            const Operand x(lo, hi);
-            scale_of[m & 1] = state_scale;
-            if (m + 1 < MW) {
-              lo = my_states[(m + 1) * 128 + place];
-              hi = my_states[(m + 1) * 128 + (place ^ 4)];
-              state_scale = s.scales[(wm * MW + m + 1) * 16 + n];
-            }
-#pragma unroll
-            for (int c = 0; c < TW; ++c) sum[m & 1][c] = products(a[c], x);
+        for (int m = 0; m < MW + kRoundsBehind; ++m) {
+          const Operand x(lo, hi);
+          scale_of[m % (kRoundsBehind + 1)] = state_scale;
+          if (m + 1 < MW) {
+            lo = my_states[(m + 1) * 128 + place];
+            hi = my_states[(m + 1) * 128 + (place ^ 4)];
+            state_scale = s.scales[(wm * MW + m + 1) * 16 + n];
           }
-          if (m > 0) {
 #pragma unroll
-            for (int c = 0; c < TW; ++c) {
-              float4v& to = acc[c][m - 1];
-              if constexpr (kMasked) to += sum[(m - 1) & 1][c] * (scale[c] * scale_of[(m - 1) & 1]);
-              else to += sum[(m - 1) & 1][c] * (scale[c][0] * scale_of[(m - 1) & 1]);
+          for (int c = 0; c < TW; ++c) {
+            const int t = m * TW + c, was = t - kBehind;
+            if (m < MW) sum[t % (kBehind + 1)] = products(a[c], x);
+            if (was >= 0 && was < MW * TW) {
+              float4v& to = acc[was % TW][was / TW];
+              const float state = scale_of[was / TW % (kRoundsBehind + 1)];
+              if constexpr (kMasked) to += sum[was % (kBehind + 1)] * (scale[was % TW] * state);
+              else to += sum[was % (kBehind + 1)] * (scale[was % TW][0] * state);
               asm volatile("" : "+v"(to));  // (here, and not when all products are made: they would not fit the registers)
             }
           }
@@ -781,7 +830,7 @@ Many kernel_of(const F8Head& h, Elem logits_type) {
   const bool whole = logits_type == Elem::kF32;
   Many best = h.B <= 64 ? Many::k64 : whole ? Many::k128Whole : Many::k128;
   double time = h.B <= 64 ? many_time(h, 64, 1.2) : many_time(h, 128, whole ? 1.8 : 1.1);
-  if (!whole && h.B > 128 && many_time(h, 256, 1.95) < time) {
+  if (!whole && !h.mask && h.B > 128 && many_time(h, 256, 1.95) < time) {  // (with lists of rows its registers would not do)
     best = Many::k256;
     time = many_time(h, 256, 1.95);
   }
@@ -815,7 +864,7 @@ hipError_t launch_f8_logits(const F8Head& head, Elem hidden_type, Elem logits_ty
   switch (kernel) {
     case Many::k64: return launch_many_masked<4, 1, 2, Halves>(h, strides, logits_type, stream);
     case Many::k128Whole: return launch_many_masked<4, 2, 4, Halves>(h, strides, logits_type, stream);
-    case Many::k256: return launch_many_masked<8, 2, 4, Eights>(h, strides, logits_type, stream);
+    case Many::k256: return launch_many<8, 2, 4, false, Eights>(h, strides, logits_type, stream);
     default: return launch_many_masked<4, 2, 4, Eights>(h, strides, logits_type, stream);
   }
 }
