@@ -2545,6 +2545,14 @@ void xgm_beams_destroy(xgm_beams* s) {
   (void)hipFree(s->memory);
   delete s;
 }
+}  // extern "C"
+namespace {
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + b_bytes && y < x + a_bytes;
+}
+}  // namespace
+extern "C" {
 int xgm_beam_select(xgm_beams* s, const void* d_logits, xgm_dtype dt, int32_t requests, int32_t n_beams, int32_t V, int64_t row_stride_elems,
                     const xgm_logit_rules* rules, const float* d_scores, const int32_t* d_ended, int32_t n_out, int32_t placed, int32_t* d_rows,
                     int32_t* d_ids, float* d_out_scores, void* hip_stream) {
@@ -2562,6 +2570,17 @@ int xgm_beam_select(xgm_beams* s, const void* d_logits, xgm_dtype dt, int32_t re
   if (!what) what = rules_fault(rules, &r);
   if (!what && placed && n_out != n_beams) what = "placed, and not as many continuations as beams";
   if (!what && (const float*)d_out_scores == d_scores && n_out != n_beams) what = "scores in place, and not as many continuations as beams";
+  if (!what && (!aligned(d_scores, 4) || !aligned(d_ended, 4) || !aligned(d_rows, 4) || !aligned(d_ids, 4) || !aligned(d_out_scores, 4)))
+    what = "scores, ended or results are not aligned to their element size";
+  // a request's results are written while other requests' rows are read
+  const uint64_t read = (uint64_t)requests * n_beams * 4, written = (uint64_t)requests * n_out * 4;
+  for (const void* out : {(const void*)d_rows, (const void*)d_ids, (const void*)d_out_scores}) {
+    const bool in_place = out == d_out_scores && d_out_scores == d_scores;
+    if (!what && ((!in_place && overlap(out, written, d_scores, read)) || (d_ended && overlap(out, written, d_ended, read))))
+      what = "results overlap scores or ended";
+  }
+  if (!what && (overlap(d_rows, written, d_ids, written) || overlap(d_rows, written, d_out_scores, written) || overlap(d_ids, written, d_out_scores, written)))
+    what = "results overlap each other";
   if (what) return fail(XGM_ERR_BAD_ARG, std::string("beam_select: ") + what);
   require_device();
   const BeamSearch b{d_scores, d_ended, requests, n_beams, n_out, placed, d_rows, d_ids, d_out_scores};
@@ -2591,10 +2610,6 @@ const char* row_data_fault(const xgm_row_data& d, int32_t B, uint64_t* last) {
   if (extent > ((__int128)1 << 62) || (d.d_used && d.used_bytes > (int64_t)1 << 62)) return "strides beyond the address space";
   *last = (uint64_t)extent;
   return nullptr;
-}
-bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + b_bytes && y < x + a_bytes;
 }
 }  // namespace
 extern "C" {

@@ -84,8 +84,8 @@ def _search(max_rows=16, v=1000):
     return s
 
 
-SELECT = dict(d_logits=A, dtype=1, requests=4, beams=4, v=1000, row_stride=1000, rules=None, d_scores=A, d_ended=0, n_out=4, placed=False, d_rows=A, d_ids=A,
-              d_out_scores=2 * A)
+SELECT = dict(d_logits=A, dtype=1, requests=4, beams=4, v=1000, row_stride=1000, rules=None, d_scores=A, d_ended=0, n_out=4, placed=False, d_rows=3 * A,
+              d_ids=4 * A, d_out_scores=2 * A)
 
 
 @pytest.mark.parametrize("change,status,text", [
@@ -93,7 +93,12 @@ SELECT = dict(d_logits=A, dtype=1, requests=4, beams=4, v=1000, row_stride=1000,
     (dict(dtype=3), -1, "dtype"), (dict(requests=0), -1, "positive"), (dict(beams=0), -1, "positive"), (dict(n_out=0), -1, "positive"), (dict(v=0), -1, "positive"),
     (dict(beams=65), -9, "XGM_MAX_BEAMS"), (dict(n_out=129), -9, "XGM_MAX_CONTINUATIONS"), (dict(requests=5), -1, "created"), (dict(v=1001), -1, "created"),
     (dict(requests=1 << 30, beams=4), -1, "created"), (dict(row_stride=999), -1, "stride"), (dict(d_logits=A + 1), -1, "aligned"), (dict(n_out=8, placed=True), -1, "placed"),
-    (dict(n_out=8, d_out_scores=A), -1, "in place"), (dict(rules=xgm.LogitRules(d_bitmask=A)), -1, "v_mask")])
+    (dict(n_out=8, d_out_scores=A), -1, "in place"), (dict(d_scores=A + 2), -1, "aligned"), (dict(d_ended=A + 1), -1, "aligned"), (dict(d_rows=3 * A + 2), -1, "aligned"),
+    (dict(d_ids=4 * A + 1), -1, "aligned"), (dict(d_out_scores=2 * A + 2), -1, "aligned"), (dict(d_out_scores=A + 4), -1, "overlap scores"),
+    (dict(d_rows=A + 60), -1, "overlap scores"), (dict(d_ids=A), -1, "overlap scores"), (dict(d_out_scores=A, d_ids=A), -1, "overlap"),
+    (dict(d_ended=3 * A - 60), -1, "overlap scores or ended"), (dict(d_ended=2 * A), -1, "overlap scores or ended"),
+    (dict(d_rows=4 * A), -1, "overlap each other"), (dict(d_ids=2 * A + 32), -1, "overlap each other"), (dict(d_out_scores=3 * A - 4), -1, "overlap each other"),
+    (dict(rules=xgm.LogitRules(d_bitmask=A)), -1, "v_mask")])
 def test_continuations_refuse(change, status, text):
     s = _search()
     try:
