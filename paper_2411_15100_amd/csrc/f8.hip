@@ -51,6 +51,22 @@ __device__ __forceinline__ void store_logit(const F8Head& h, Elem type, int64_t 
   else if (type == Elem::kBF16) static_cast<uint16_t*>(h.logits)[at] = narrowed<Elem::kBF16>(y);
   else static_cast<uint16_t*>(h.logits)[at] = narrowed<Elem::kF16>(y);
 }
+// of four neighbouring tokens, the first of which lies at a multiple of four elements
+template <Elem E> __device__ __forceinline__ void store_four(const F8Head& h, int64_t at, const float (&y)[4]) {
+  typedef typename Type<E>::bits bits;
+  typedef bits bits4 __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<bits4*>(static_cast<bits*>(h.logits) + at) = bits4{narrowed<E>(y[0]), narrowed<E>(y[1]), narrowed<E>(y[2]), narrowed<E>(y[3])};
+}
+__device__ __forceinline__ void store_logits(const F8Head& h, Elem type, int64_t at, const float (&y)[4]) {
+  if (type == Elem::kF32) store_four<Elem::kF32>(h, at, y);
+  else if (type == Elem::kBF16) store_four<Elem::kBF16>(h, at, y);
+  else store_four<Elem::kF16>(h, at, y);
+}
+// whether rows of logits begin at such a multiple
+bool in_fours(const F8Head& h, Elem type) {
+  const uintptr_t size = type == Elem::kF32 ? 4 : 2;
+  return reinterpret_cast<uintptr_t>(h.logits) % (4 * size) == 0 && h.logits_stride % 4 == 0;
+}
 
 // ---------------------------------------------------------- hidden states to 8 bits
 // A power of two as the scale of a block: no value loses bits in the division, so that the only rounding is that to e4m3, and the range that a
@@ -137,8 +153,9 @@ struct List {
   uint32_t any[kListed / 32];
   int32_t n;
 };
-__device__ __forceinline__ bool allowed(const F8Head& h, int32_t b, int64_t token) {
-  return !h.mask || (token < h.V_mask && (h.mask[(size_t)b * h.W_mask + (token >> 5)] >> (token & 31) & 1u));
+// (a load whatever the token is: many of them are on their way at once)
+__device__ __forceinline__ uint32_t allowed(const F8Head& h, int32_t b, int64_t token) {
+  return h.mask[(size_t)b * h.W_mask + (min(token, (int64_t)h.V_mask - 1) >> 5)] >> (token & 31) & (uint32_t)(token < h.V_mask);
 }
 __device__ int32_t list_rows(const F8Head& h, Elem out_type, int32_t first_b, int32_t rows, int64_t base, int32_t here, List& list) {
   int32_t tid = (int32_t)threadIdx.x;
@@ -181,9 +198,9 @@ __device__ int32_t list_rows(const F8Head& h, Elem out_type, int32_t first_b, in
 // time, the next ones while it multiplies the last.  Under masks the workgroup lists the rows of its share that some request
 // allows, and its waves take 16 of those at a time.  Where a workgroup has fewer tiles than waves, several waves take the steps of one
 // in turn and their sums meet in LDS.
-// One row of 128256 x 4096 takes 103 us, 5.1 TB/s: the bytes of the matrix.  24 rows of 50001 x 2080 under masks take 37 us: one tile a wave, whose 9 steps
-// follow each other, and 20 us more than one row for conversions (58 VALU instructions a block beside 8 matrix instructions) and lists.
-// 32 rows of 4096 x 4096 take 19 us, 11 of them to bring hidden states to 8 bits in every workgroup.
+// One row of 32000 x 2048 takes 15 us, 4.4 TB/s, 16 rows 18: conversions (58 VALU instructions a block and 16 rows beside 4 matrix instructions) and hidden
+// states, which every workgroup brings to 8 bits by itself: 11 us of the 20 that 32 rows of 4096 x 4096 take.  Sums go out four at a time: one by one
+// 32 rows of 151936 x 1024 took 46 us, and 41.
 constexpr int kFewThreads = 1024;
 constexpr int kStep = 2;
 constexpr uint32_t kMaxLds = 160 * 1024;
@@ -204,7 +221,7 @@ __host__ __device__ inline FewLayout few_layout(int32_t K, int32_t rows) {
 enum class States : int { kF8, kBF16, kF16 };
 
 template <States T, int NB, bool kMasked>
-__global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_type, int32_t tiles_each) {
+__global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_type, int32_t tiles_each, bool wide) {
   extern __shared__ __align__(16) char lds[];
   const int32_t tid = (int32_t)threadIdx.x, threads = (int32_t)blockDim.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = threads >> 6;
   const int32_t n = lane & 15, q = lane >> 4;
@@ -353,15 +370,23 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
           __syncthreads();
         }
       }
+      int32_t in = n, i0 = q * 4;
+      asm volatile("" : "+v"(in), "+v"(i0));  // (as in list_rows)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        if (sub != 0 || t >= tiles || nb * 16 + n >= rows) continue;
-        const int32_t b = first_b + nb * 16 + n;
+        if (sub != 0 || t >= tiles || nb * 16 + in >= rows) continue;
+        const int32_t b = first_b + nb * 16 + in;
+        float y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (t * 16 + q * 4 + i >= count) continue;
-          const int64_t token = base + row_of(t, q * 4 + i);
-          store_logit(h, out_type, b * h.logits_stride + token, !kMasked || allowed(h, b, token) ? acc[nb][i] : -__builtin_inff());
+        for (int i = 0; i < 4; ++i) y[i] = !kMasked || allowed(h, b, base + row_of(t, i0 + i)) ? acc[nb][i] : -__builtin_inff();
+        const int64_t at = b * h.logits_stride + base;
+        const int32_t r0 = row_of(t, i0);
+        if (wide && t * 16 + i0 + 4 <= count && (!kMasked || (r0 % 4 == 0 && row_of(t, i0 + 3) == r0 + 3))) {
+          store_logits(h, out_type, at + r0, y);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (t * 16 + i0 + i < count) store_logit(h, out_type, at + row_of(t, i0 + i), y[i]);
         }
       }
       t += abreast;
@@ -377,19 +402,22 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
 // What a block needs goes from memory to LDS without passing a register, into a ring of kStages buffers: while a block is multiplied the
 // next kStages - 1 are on their way; one barrier a block.  16 bytes of a row lie in LDS at their place in the row with the row's last three bits
 // exchanged into it: eight rows of one place, as a wave reads them, lie in different banks.
+// One row of 128256 x 4096 takes 95 us, 5.5 TB/s, 32 rows 101: the bytes of the matrix.  (Of 32 rows and less a block without them takes 0.5 to 0.6 us, for
+// conversions and the barrier: four buffers instead of three take 1 us more a call.)
 // 128 rows of 151936 x 4096 take 153 us, 4.3 TB/s: memory, of which two blocks are on their way to each compute unit; through registers, a block ahead, it
 // took 264.  1024 rows of 128256 x 4096 take 611 us, 1.76 PFLOP/s; without its loads 456, at which clock and power hold the matrix instructions
 // (8192 x 8192 x 8192 in a library reach 2.67 PFLOP/s, and this product without scales of blocks 544 us).
 constexpr int kManyThreads = 512, kManyWaves = kManyThreads / 64;
 template <int MW, int WM, int TW> struct ManyShape {
   static constexpr int kRows = 16 * MW * WM, kWide = kManyWaves / WM, kPass = kWide * TW, kMatrix = 16 * kPass;
-  static constexpr int kStateLoads = kRows / 8 / kManyWaves, kCodeLoads = kMatrix / 8 / kManyWaves;  // of a wave, 64 x 16 bytes each
-  static constexpr int kStages = kRows + kMatrix <= 384 ? 3 : 2;
-  static_assert(kStateLoads > 0 && kCodeLoads > 0 && kRows + kMatrix <= kManyThreads, "equal parts for all waves, and a scale a thread");
+  static constexpr int kBrought = kRows < 64 ? 64 : kRows;  // (fewer rows come with copies of the last one)
+  static constexpr int kStateLoads = kBrought / 8 / kManyWaves, kCodeLoads = kMatrix / 8 / kManyWaves;  // of a wave, 64 x 16 bytes each
+  static constexpr int kStages = kBrought + kMatrix <= 384 ? 3 : 2;
+  static_assert(kBrought % 64 == 0 && kCodeLoads > 0 && kRows + kMatrix <= kManyThreads, "equal parts for all waves, and a scale a thread");
 };
 template <int MW, int WM, int TW> struct Stage {
   typedef ManyShape<MW, WM, TW> Shape;
-  uint4v states[Shape::kRows * 8];
+  uint4v states[Shape::kBrought * 8];
   uint4v codes[Shape::kMatrix * 8];
   float scales[kManyThreads];  // of the rows of the batch, then of those of the matrix
 };
@@ -652,21 +680,31 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
         for (int c = 0; c < TW; ++c) {
           if (c >= mine) continue;
           const int32_t i0 = (pass + first + c) * 16 + q * 4;
+          int32_t r[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[i] = row_of(i0 + i);
+          [[maybe_unused]] uint32_t open = 0;  // bit 4 m + i
+          if constexpr (kMasked) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int m = 0; m < MW; ++m) open |= allowed(h, first_b + min(in0 + m * 16, rows - 1), base + r[i]) << (4 * m + i);
+          }
+          const bool in_one = wide && i0 + 4 <= count && (!kMasked || (r[0] % 4 == 0 && r[3] == r[0] + 3));
 #pragma unroll
           for (int m = 0; m < MW; ++m) {
             const int32_t in = in0 + m * 16, b = first_b + in;
             if (in >= rows) continue;
-            bits* const out = static_cast<bits*>(h.logits) + b * h.logits_stride + base;
-            bits y[4];
+            const int64_t at = b * h.logits_stride + base;
+            float y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = narrowed<O>(!kMasked || (i0 + i < count && allowed(h, b, base + row_of(i0 + i))) ? acc[c][m][i] : -__builtin_inff());
-            if (!kMasked && wide && i0 + 4 <= count) {
-              typedef bits bits4 __attribute__((ext_vector_type(4)));
-              *reinterpret_cast<bits4*>(out + i0) = bits4{y[0], y[1], y[2], y[3]};
+            for (int i = 0; i < 4; ++i) y[i] = !kMasked || (open >> (4 * m + i) & 1u) ? acc[c][m][i] : -__builtin_inff();
+            if (in_one) {
+              store_four<O>(h, at + r[0], y);
             } else {
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                if (i0 + i < count) out[row_of(i0 + i)] = y[i];
+                if (i0 + i < count) static_cast<bits*>(h.logits)[at + r[i]] = narrowed<O>(y[i]);
             }
           }
         }
@@ -787,7 +825,7 @@ template <States T, int NB, bool kMasked> hipError_t launch_few(const F8Head& h,
   int32_t threads = 64;  // waves for its tiles, or for the steps of the few that masks leave
   while (threads < kFewThreads && threads < 64 * (kMasked && steps > each ? steps : each * (each < 16 ? steps : 1))) threads *= 2;
   const dim3 grid((tiles + each - 1) / each, (h.B + 16 * NB - 1) / (16 * NB));
-  hipLaunchKernelGGL((f8_few_kernel<T, NB, kMasked>), grid, dim3(threads), few_layout(h.K, h.B < 16 * NB ? h.B : 16 * NB).end, stream, h, out_type, each);
+  hipLaunchKernelGGL((f8_few_kernel<T, NB, kMasked>), grid, dim3(threads), few_layout(h.K, h.B < 16 * NB ? h.B : 16 * NB).end, stream, h, out_type, each, in_fours(h, out_type));
   return hipGetLastError();
 }
 template <States T, int NB> hipError_t launch_few_masked(const F8Head& h, Elem out_type, hipStream_t stream) {
@@ -804,10 +842,8 @@ template <int MW, int WM, int TW, bool kMasked, class Operand> hipError_t launch
   typedef ManyShape<MW, WM, TW> Shape;
   const int32_t tiles = (int32_t)(((int64_t)h.V + 15) / 16), batch_tiles = (h.B + Shape::kRows - 1) / Shape::kRows;
   const int32_t most = batch_tiles < kComputeUnits ? kComputeUnits / batch_tiles : 1, each = (tiles + most - 1) / most, shares = (tiles + each - 1) / each;
-  const int size = out_type == Elem::kF32 ? 4 : 2;
-  const bool wide = reinterpret_cast<uintptr_t>(h.logits) % (4 * size) == 0 && h.logits_stride % 4 == 0;
   hipLaunchKernelGGL((f8_many_kernel<MW, WM, TW, kMasked, Operand>), dim3((uint32_t)(shares * batch_tiles)), dim3(kManyThreads), 0, stream, h, strides, out_type,
-                     batch_tiles, shares, each, wide);
+                     batch_tiles, shares, each, in_fours(h, out_type));
   return hipGetLastError();
 }
 template <int MW, int WM, int TW, class Operand> hipError_t launch_many_masked(const F8Head& h, const StateScales& strides, Elem out_type, hipStream_t stream) {
@@ -823,35 +859,51 @@ hipError_t launch_f8_quantize(const void* x, Elem type, int32_t B, int32_t K, in
 }
 
 namespace {
-// Which kernel takes more than 32 rows, by what a call takes them in us: a workgroup of few rows a start and a piece of each of its tiles; one of many
-// rows a time for each block of columns of each of its passes, which is that of a barrier and of loads that come back, not of the products.
-// For 4096 columns (32 blocks), bf16: 40 rows of 4096: few 21, many 40; 128 of 10000: 42 and 37; 500 of 2048: many 37 in tiles of 128 rows and 64 in those
-// of 256; 1024 of 128256: 700 and 628; 384 of 128256: 270 and 349.  Logits in 32 bits, 128 rows of 4096: few 25, many 63.
-enum class Many { kFew, k64, k128, k128Whole, k256 };
-double few_time(const F8Head& h) { return 7.0 + f8_blocks(h.K) * (0.3 + 0.075 * few_tiles(h, 32)); }
-double many_time(const F8Head& h, int32_t rows, double block) {
-  const int32_t passes = (few_tiles(h, rows) + 15) / 16;  // (a pass is 16 tiles in all of them)
-  return 4.0 + passes * (f8_blocks(h.K) * block);
+// Which kernel takes a batch, by what a call takes them in us: a workgroup of few rows a start, its hidden states and its tiles; one of many rows (which
+// waits for a launch that brings hidden states to 8 bits) a time for each block of columns of each of its passes, which is that of a barrier and of
+// loads that come back, or where that is more the bytes of its tiles.  For bf16, few and many, us:
+//   4096 x 4096: 1 row 7 and 24, 16 rows 13 and 25, 32 rows 20 and 30, 40 rows 21 and 40
+//   50001 x 2080: 1 row 25.5 and 26.3, 16 rows 29.5 and 27.6, 32 rows 36.5 and 31.6
+//   128256 x 4096: 1 row 103 and 95, 16 rows 115 and 96, 32 rows 128 and 101; 151936 x 1024: 31 and 33, 36 and 37, 41 and 41
+// of many 500 rows of 2048 x 4096 37 in tiles of 128 rows and 64 in those of 256, 1024 of 128256 x 4096 700 and 628, 384 of them 270 and 349.
+// Logits in 32 bits, 128 rows of 4096 x 4096: few 25, many 63.
+enum class Many { kFew, k16, k32, k64, k128, k128Whole, k256 };
+int32_t few_rows(const F8Head& h) { return h.B <= 16 ? 16 : 32; }
+double few_time(const F8Head& h) {
+  const int32_t each = few_tiles(h, few_rows(h)), rows = h.B < 32 ? h.B : 32;
+  return 5.0 + f8_blocks(h.K) * (0.09 * each + rows * (0.0115 + 0.0005 * each));
+}
+double many_time(const F8Head& h, int32_t rows, double start, double block, double tile) {
+  const int32_t each = few_tiles(h, rows), passes = (each + 15) / 16;  // (a pass is 16 tiles in all of them)
+  const double latency = passes * block, bytes = each * tile;
+  return start + f8_blocks(h.K) * (latency > bytes ? latency : bytes);
 }
 Many kernel_of(const F8Head& h, Elem logits_type) {
   const bool whole = logits_type == Elem::kF32;
-  Many best = h.B <= 64 ? Many::k64 : whole ? Many::k128Whole : Many::k128;
-  double time = h.B <= 64 ? many_time(h, 64, 1.2) : many_time(h, 128, whole ? 1.8 : 1.1);
-  if (!whole && !h.mask && h.B > 128 && many_time(h, 256, 1.95) < time) {  // (with lists of rows its registers would not do)
-    best = Many::k256;
-    time = many_time(h, 256, 1.95);
-  }
-  return few_fits(h, 32) && few_time(h) < time ? Many::kFew : best;
+  Many best = Many::k16;
+  double time = 0.0;
+  auto offer = [&](Many kernel, double t) {
+    if (time == 0.0 || t < time) best = kernel, time = t;
+  };
+  const double start = h.hidden.scales ? 6.0 : 10.0;
+  if (h.B <= 16) offer(Many::k16, many_time(h, 16, start, 0.46, 0.083));
+  else if (h.B <= 32) offer(Many::k32, many_time(h, 32, start, 0.63, 0.09));
+  else if (h.B <= 64) offer(Many::k64, many_time(h, 64, start, 0.95, 0.09));
+  else if (whole) offer(Many::k128Whole, many_time(h, 128, 4.0, 1.8, 0.0));
+  else offer(Many::k128, many_time(h, 128, 4.0, 1.1, 0.0));
+  if (!whole && !h.mask && h.B > 128) offer(Many::k256, many_time(h, 256, 4.0, 1.95, 0.0));  // (with lists of rows its registers would not do)
+  if (few_fits(h, h.B < 32 ? h.B : 32)) offer(Many::kFew, few_time(h));
+  return best;
 }
 }  // namespace
 hipError_t launch_f8_logits(const F8Head& head, Elem hidden_type, Elem logits_type, void* work, hipStream_t stream) {
   F8Head h = head;
-  if (h.B <= 16 && few_fits(h, h.B)) return launch_few_states<1>(h, hidden_type, logits_type, stream);
-  if (h.B <= 32 && few_fits(h, h.B)) return launch_few_states<2>(h, hidden_type, logits_type, stream);
   const Many kernel = kernel_of(h, logits_type);
-  if (kernel == Many::kFew) return launch_few_states<2>(h, hidden_type, logits_type, stream);
+  if (kernel == Many::kFew) return few_rows(h) == 16 ? launch_few_states<1>(h, hidden_type, logits_type, stream) : launch_few_states<2>(h, hidden_type, logits_type, stream);
   StateScales strides{f8_blocks(h.K), 1};
-  if (h.hidden.scales && work) {  // (a block's scales side by side: as they are, 256 rows take as many requests as 16 KB of codes)
+  // A block's scales side by side: as they are, 256 rows take as many requests as 16 KB of codes.  (Of 64 rows and less, as they are: 64 rows of
+  // 128256 x 4096 take 105 us and 106 with the launch for it, 32 of 50001 x 2080 29.2 and 30.8.)
+  if (h.hidden.scales && work && h.B > 64) {
     float* const scales = static_cast<float*>(work);
     strides = StateScales{1, h.B};
     const int64_t n = (int64_t)h.B * f8_blocks(h.K);
@@ -869,6 +921,8 @@ hipError_t launch_f8_logits(const F8Head& head, Elem hidden_type, Elem logits_ty
     h.hidden = F8States{codes, padded(h.K), scales};
   }
   switch (kernel) {
+    case Many::k16: return launch_many_masked<1, 1, 2, Halves>(h, strides, logits_type, stream);
+    case Many::k32: return launch_many_masked<2, 1, 2, Halves>(h, strides, logits_type, stream);
     case Many::k64: return launch_many_masked<4, 1, 2, Halves>(h, strides, logits_type, stream);
     case Many::k128Whole: return launch_many_masked<4, 2, 4, Halves>(h, strides, logits_type, stream);
     case Many::k256: return launch_many<8, 2, 4, false, Eights>(h, strides, logits_type, stream);

@@ -219,6 +219,32 @@ def test_projection_of_columns_around_what_fits_lds(B, K, V):
     assert np.array_equal(_np(p.run()), p.want()[0])
 
 
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dtype", ["f16", "f8"])
+@pytest.mark.parametrize("B,K,V", [(3, 49152, 130), (16, 16400, 2049), (9, 24576, 300), (17, 9232, 777), (32, 8208, 4100), (30, 16384, 64)])
+def test_projection_of_few_rows_and_many_columns(B, K, V, dtype, masked):
+    mask, allowed = None, np.ones((B, V), bool)
+    if masked:
+        allowed = np.random.default_rng(V).random((B, V)) < 0.2
+        allowed[:, V // 3:V // 2] = False
+        allowed[0, V // 2:] = V % 2 == 0
+        mask = torch.from_numpy(plain_logits.pack(allowed)).cuda()
+    p = Projection(B, K, V, dtype, whole=True, seed=K, pad=B % 2)
+    p.scales.clamp_(max=0.25)
+    want = np.where(allowed, p.want()[0], -np.inf)
+    for stride, offset in ((V, 0), (V + 4 - V % 4, 0), (V + 3, 1)):
+        assert np.array_equal(_np(p.run("f32", mask=mask, stride=stride, offset=offset)), want), stride
+    if dtype == "f8":
+        assert np.array_equal(_np(p.run("f32", mask=mask, with_work=True)), want)
+    p = Projection(B, K, V, dtype, seed=B)
+    if dtype == "f16":
+        p.scales *= 2.0 ** -6
+    want, size = p.want()
+    got = _np(p.run("f16" if dtype == "f16" else "bf16", mask=mask, stride=V + 8 - V % 8))
+    tol = tolerance(want, size, K, "f16" if dtype == "f16" else "bf16", None)
+    assert (got[~allowed] == -np.inf).all() and (np.abs(got - want) <= tol)[allowed].all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f8"])
 @pytest.mark.parametrize("B,K,V", [(1, 1024, 5000), (4, 2080, 3001), (20, 512, 2050), (70, 384, 777), (130, 256, 600), (300, 128, 3000)])
 def test_projection_under_masks(B, K, V, dtype):
@@ -265,7 +291,7 @@ def test_a_part_of_a_larger_matrix_under_its_masks():
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("masked", [False, True])
-@pytest.mark.parametrize("B,K,V", [(2000, 128, 1000), (1100, 272, 20001), (40000, 16, 64), (66000 - 465, 32, 17), (129, 512, 30001), (257, 1024, 9000), (48, 640, 70001)])
+@pytest.mark.parametrize("B,K,V", [(2000, 128, 1000), (1100, 272, 20001), (40000, 16, 64), (66000 - 465, 32, 17), (129, 512, 30001), (257, 1024, 9000), (48, 640, 70001), (11, 2080, 50001), (16, 1040, 151936), (27, 2080, 50001)])
 def test_projection_of_large_batches_and_large_matrices(B, K, V, masked, out):
     p = Projection(B, K, V, "f16", whole=True, seed=V)
     mask, allowed = None, None
