@@ -68,14 +68,18 @@ __device__ __forceinline__ u64 place_in(int32_t beam, u64 key) {
 __device__ __forceinline__ int32_t beam_of(u64 place) { return kMaxBeams - 1 - (int32_t)(place >> (32 + kIdBits)); }
 __device__ __forceinline__ int32_t id_at(u64 place) { return (int32_t)(~(uint32_t)place & ((1u << kIdBits) - 1u)); }
 
+template <class T> struct Maxima {  // of threads; of groups of them
+  T of[kSliceThreads], least[kWaves], top[kWaves];
+};
 struct BeamShared {
-  float most[kSliceThreads];
+  Maxima<float> most;
   double sum[kWaves];
   uint32_t n_found, counts[kWaves];
   u64 found[kMostFound], better[kMostFound];
 };
 struct JoinShared {
-  double base[kMaxBeams], most[kSliceThreads];
+  double base[kMaxBeams];
+  Maxima<double> most;
   int32_t is_ended[kMaxBeams];
   uint32_t n_joined, counts[kWaves];
   u64 order[kMostJoined], place[kMostJoined];
@@ -98,30 +102,49 @@ __device__ __forceinline__ uint32_t count_all(uint32_t mine, uint32_t (&counts)[
   return all;
 }
 
-// What bounds the largest numbers of `groups` groups of threads (a power of two up to kMaxContinuations); all threads get it.  Threads of a group lie
-// `groups` apart: where a row ends in the slice every group still has some of its tokens.
-constexpr int kMaxGroups = 128;
-static_assert(kMaxContinuations <= kMaxGroups && kMaxGroups == 128, "two waves of groups at most");
+// A bound that n numbers of the workgroup reach, or -inf, by the largest number of every thread.  Up to kWaves of them: threads form as many groups (a power of
+// two), and the bound is the least of the groups' largest.  More: of kWaves groups the bound is the least of the ceil(n / kWaves)-th largest ones, which
+// few others reach (of 8192 tokens 150 to 200 for n = 128; with n groups and their largest it was 600).  A group's threads lie evenly over all: where a
+// row ends in the slice every group still has some of its tokens.
+static_assert(kMaxContinuations <= kSliceThreads, "a thread each");
 template <class T> struct Bounds {
-  T least, top;  // of the groups' largest numbers: the least, and the largest of all
+  T least, top;  // the bound, and the largest number of all
 };
-template <class T> __device__ __forceinline__ Bounds<T> bounds_of_groups(T mine, int groups, T (&most)[kSliceThreads]) {
-  const int lane = (int)threadIdx.x & 63, tid = (int)threadIdx.x;
-  for (int d = 32; d >= groups; d >>= 1) mine = max(mine, (T)__shfl_xor(mine, d));
+template <class T> __device__ __forceinline__ Bounds<T> bounds_of(T mine, int n, Maxima<T>& m) {
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
   __syncthreads();
-  most[tid] = mine;
+  m.of[threadIdx.x] = mine;
   __syncthreads();
-  T r = most[lane], odd = most[64 + lane];  // groups of the even waves, and of the odd ones
+  if (n <= kWaves) {  // (every wave finds all of it: no barrier more)
+    int groups = 1;
+    while (groups < n) groups *= 2;
+    T r = m.of[lane];  // lanes that lie `groups` apart are of one
 #pragma unroll
-  for (int k = 2; k < kWaves; k += 2) {
-    r = max(r, most[k * 64 + lane]);
-    odd = max(odd, most[k * 64 + 64 + lane]);
+    for (int k = 1; k < kWaves; ++k) r = max(r, m.of[k * 64 + lane]);
+    for (int d = 32; d >= groups; d >>= 1) r = max(r, (T)__shfl_xor(r, d));
+    Bounds<T> b{r, r};
+    for (int d = groups / 2; d; d >>= 1) {
+      b.least = min(b.least, (T)__shfl_xor(b.least, d));
+      b.top = max(b.top, (T)__shfl_xor(b.top, d));
+    }
+    return b;
   }
-  Bounds<T> b{groups <= 64 ? max(r, odd) : min(r, odd), max(r, odd)};
+  T x = m.of[lane * kWaves + wave];
 #pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    b.least = min(b.least, (T)__shfl_xor(b.least, d));
-    b.top = max(b.top, (T)__shfl_xor(b.top, d));
+  for (int size = 2; size <= 64; size *= 2)  // in falling order
+#pragma unroll
+    for (int d = size / 2; d; d >>= 1) {
+      const T other = (T)__shfl_xor(x, d);
+      x = ((lane & size) == 0) == ((lane & d) == 0) ? max(x, other) : min(x, other);
+    }
+  if (lane == (n + kWaves - 1) / kWaves - 1) m.least[wave] = x;
+  if (lane == 0) m.top[wave] = x;
+  __syncthreads();
+  Bounds<T> b{m.least[0], m.top[0]};
+#pragma unroll
+  for (int k = 1; k < kWaves; ++k) {
+    b.least = min(b.least, m.least[k]);
+    b.top = max(b.top, m.top[k]);
   }
   return b;
 }
@@ -142,7 +165,7 @@ __device__ __forceinline__ float token_at(const Tokens& y, int k) {
 }
 
 template <Elem E>
-__global__ __launch_bounds__(kSliceThreads, 6) void beam_slices_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m, int groups) {
+__global__ __launch_bounds__(kSliceThreads, 6) void beam_slices_kernel(Logits in, LogitRules r, BeamSearch s, BeamMemory m) {
   extern __shared__ __align__(16) char lds[];
   RuleTable& table = *reinterpret_cast<RuleTable*>(lds);
   BeamShared& sh = *reinterpret_cast<BeamShared*>(lds);
@@ -160,7 +183,7 @@ __global__ __launch_bounds__(kSliceThreads, 6) void beam_slices_kernel(Logits in
 #pragma unroll
     for (int k = 0; k < kTokens; ++k) mine = fmaxf(mine, y[k]);
     if (tid == 0) sh.n_found = 0;  // (read behind the next barriers)
-    const Bounds<float> bounds = bounds_of_groups(mine, groups, sh.most);
+    const Bounds<float> bounds = bounds_of(mine, n, sh.most);
     const float top = bounds.top;
     BeamSlot slot{0.0, 0.0, top};
     u64* const list = m.lists + ((size_t)b * m.slices + slice) * n;
@@ -220,11 +243,11 @@ __global__ __launch_bounds__(kSliceThreads, 6) void beam_slices_kernel(Logits in
       }
       const u64* found = sh.found;
       // Where masks leave tokens in a few places a bound says little; another one among what was found, which lies in no order, says more.
-      if (all > (uint32_t)(4 * groups + 64)) {
+      if (all > (uint32_t)(2 * n + 80)) {
         static_assert(kMostFound == 2 * kSliceThreads, "two tokens a thread");
         const u64 none = 0;
         const u64 one = (uint32_t)tid < all ? sh.found[tid] : none, two = (uint32_t)tid + kSliceThreads < all ? sh.found[tid + kSliceThreads] : none;
-        const float next = bounds_of_groups(max(one, two) ? logit_of(max(one, two)) : -__builtin_inff(), groups, sh.most).least;
+        const float next = bounds_of(max(one, two) ? logit_of(max(one, two)) : -__builtin_inff(), n, sh.most).least;
         if (tid == 0) sh.n_found = 0;  // (all have read it: they have met behind that)
         __syncthreads();
         if (one && logit_of(one) >= next) sh.better[atomicAdd(&sh.n_found, 1u)] = one;
@@ -247,7 +270,7 @@ __global__ __launch_bounds__(kSliceThreads, 6) void beam_slices_kernel(Logits in
   }
 }
 
-__global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, BeamMemory m, int32_t n_slices, int groups) {
+__global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, BeamMemory m, int32_t n_slices) {
   __shared__ JoinShared join;
   __shared__ double roots[16];
   const int32_t request = (int32_t)blockIdx.x, tid = (int32_t)threadIdx.x, lane = tid & 63, wave = tid >> 6, n = s.n_out;
@@ -269,42 +292,41 @@ __global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, 
     held[k] = e < entries ? key_at(e) : 0;
   }
   __syncthreads();
-  for (int32_t i = wave; i < s.beams; i += kWaves) {  // a wave a row
-    const BeamSlot* const slots = m.slots + (size_t)(b0 + i) * m.slices;
-    const bool ended = is_ended(s, b0 + i), live = is_live(s, b0 + i);
-    double base = -__builtin_inf();
-    if (live && !ended) {
-      constexpr int kEach = (kMostSlices + 63) / 64;
-      float top = -__builtin_inff();
-      double most = -__builtin_inf(), octave[kEach], x[kEach];
+  // A row's slices lie with 16, 32 or 64 lanes, as many as it has.
+  const int part = n_slices <= 16 ? 16 : n_slices <= 32 ? 32 : 64;
+  for (int32_t i0 = wave * (64 / part); i0 < s.beams; i0 += kWaves * (64 / part)) {
+    const int32_t i = i0 + lane / part, b = b0 + min(i, s.beams - 1);
+    const BeamSlot* const slots = m.slots + (size_t)b * m.slices;
+    const bool ended = is_ended(s, b), live = is_live(s, b), open = live && !ended;
+    constexpr int kEach = (kMostSlices + 63) / 64;
+    float top = -__builtin_inff();
+    double most = -__builtin_inf(), octave[kEach], x[kEach];
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int32_t k = lane + 64 * j;
-        const bool there = k < n_slices;
-        const float t = there ? slots[k].top : -__builtin_inff();
-        octave[j] = there ? slots[k].E : 0.0;
-        x[j] = there ? slots[k].sum : 0.0;
-        if (!(t > -__builtin_inff())) octave[j] = -__builtin_inf();
-        top = fmaxf(top, t);
-        most = fmax(most, octave[j]);
-      }
+    for (int j = 0; j < kEach; ++j) {
+      const int32_t k = lane % part + part * j;
+      const bool there = open && k < n_slices;
+      const float t = there ? slots[k].top : -__builtin_inff();
+      octave[j] = there ? slots[k].E : 0.0;
+      x[j] = there ? slots[k].sum : 0.0;
+      if (!(t > -__builtin_inff())) octave[j] = -__builtin_inf();
+      top = fmaxf(top, t);
+      most = fmax(most, octave[j]);
+    }
+    for (int d = part / 2; d; d >>= 1) {
+      top = fmaxf(top, __shfl_xor(top, d));
+      most = fmax(most, __shfl_xor(most, d));
+    }
+    double sum = 0.0;
 #pragma unroll
-      for (int d = 32; d; d >>= 1) {
-        top = fmaxf(top, __shfl_xor(top, d));
-        most = fmax(most, __shfl_xor(most, d));
-      }
-      double sum = 0.0;
-#pragma unroll
-      for (int j = 0; j < kEach; ++j)
-        if (octave[j] - most > -1100.0) sum += ldexp(x[j], (int)(octave[j] - most));
-      sum = wave_sum(sum);
+    for (int j = 0; j < kEach; ++j)
+      if (octave[j] - most > -1100.0) sum += ldexp(x[j], (int)(octave[j] - most));
+    for (int d = part / 2; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane % part == 0 && i < s.beams) {
+      const double score = (double)s.scores[b];
+      double base = live && ended ? score : -__builtin_inf();
       // (relative to the largest logit's own weight: a token that is alone costs nothing)
       constexpr double per = 1.4426950408889634074;
-      if (top > -__builtin_inff()) base = (double)s.scores[b0 + i] - ((double)top + log(sum / Power(octaves(top, per), most, roots).weight()));
-    } else if (live) {
-      base = (double)s.scores[b0 + i];
-    }
-    if (lane == 0) {
+      if (top > -__builtin_inff()) base = score - ((double)top + log(sum / Power(octaves(top, per), most, roots).weight()));
       join.base[i] = base;
       join.is_ended[i] = ended;
     }
@@ -322,50 +344,101 @@ __global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, 
       f((double)logit_of(key) + base, place_in(beam, key));
     }
   };
-  auto for_entries = [&](auto&& f) {
+  auto for_held = [&](auto&& f) {
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
       if (k * kSliceThreads + tid < entries) with(k * kSliceThreads + tid, held[k], f);
-    for (int32_t e = kHeld * kSliceThreads + tid; e < entries; e += kSliceThreads) with(e, key_at(e), f);
   };
+  // All entries, beam after beam as they lie in memory: what a request needs only where its bounds say too little.
+  auto for_all = [&](auto&& f) {
+    for (int32_t beam = 0; beam < s.beams; ++beam) {
+      if (!(join.base[beam] > -__builtin_inf())) continue;
+      const u64* const own = lists + (size_t)beam * m.slices * n;
+      const int32_t all = join.is_ended[beam] ? 1 : n_slices * n;
+      for (int32_t i = tid; i < all; i += kSliceThreads) with(i % n * n_lists + beam * n_slices + i / n, own[i], f);
+    }
+  };
+  auto join_in = [&](u64 order, u64 place) {
+    const uint32_t at = atomicAdd(&join.n_joined, 1u);
+    if (at < kMostJoined) {
+      join.order[at] = order;
+      join.place[at] = place;
+    }
+  };
+  auto joined = [&] {
+    __syncthreads();
+    return join.n_joined;
+  };
+  auto again = [&] {  // (all have read how many there are)
+    __syncthreads();
+    if (tid == 0) join.n_joined = 0;
+    __syncthreads();
+  };
+  // The bound by the entries held, the first ones of the lists; behind them a list has more of its kind only if its next one is.
   double mine = -__builtin_inf();
-  for_entries([&](double sum, u64) { mine = max(mine, sum); });
-  const double bound = bounds_of_groups(mine, groups, join.most).least;
-  auto collect = [&](auto&& joins) {
-    for_entries([&](double sum, u64 place) {
-      const u64 order = order_of(sum);
-      if (!joins(sum, order, place)) return;
-      const uint32_t at = atomicAdd(&join.n_joined, 1u);
-      if (at < kMostJoined) {
-        join.order[at] = order;
-        join.place[at] = place;
-      }
-    });
-  };
-  collect([&](double sum, u64, u64) { return sum >= bound; });
-  __syncthreads();
-  uint32_t all = join.n_joined;
+  for_held([&](double sum, u64) { mine = max(mine, sum); });
+  const double bound = bounds_of(mine, n, join.most).least;
+  for_held([&](double sum, u64 place) { if (sum >= bound) join_in(order_of(sum), place); });
+  for (int32_t list = tid; list < n_lists; list += kSliceThreads) {
+    int32_t rank = kHeld * kSliceThreads > list ? (kHeld * kSliceThreads - list + n_lists - 1) / n_lists : 0;
+    const int32_t beam = list / n_slices;
+    const u64* const own = lists + ((size_t)beam * m.slices + (list - beam * n_slices)) * n;
+    for (bool more = true; more && rank < n; ++rank) {
+      more = false;
+      with(rank * n_lists + list, own[rank], [&](double sum, u64 place) {
+        if (!(sum >= bound)) return;
+        join_in(order_of(sum), place);
+        more = true;
+      });
+    }
+  }
+  uint32_t all = joined();
+  if (all > kMostJoined) {  // few rows that have all of it
+    mine = -__builtin_inf();
+    for_all([&](double sum, u64) { mine = max(mine, sum); });
+    const double next = bounds_of(mine, n, join.most).least;
+    again();
+    for_all([&](double sum, u64 place) { if (sum >= next) join_in(order_of(sum), place); });
+    all = joined();
+  }
   if (all > kMostJoined) {  // many equal ones: the n-th best, bit by bit
     u64 edge = 0, edge_place = 0;  // what counts: more than edge, or edge itself with edge_place or more
 #pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const u64 at = edge | 1ull << bit;
       uint32_t some = 0;
-      for_entries([&](double sum, u64) { some += order_of(sum) >= at; });
+      for_all([&](double sum, u64) { some += order_of(sum) >= at; });
       if (count_all(some, join.counts) >= (uint32_t)n) edge = at;
     }
 #pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const u64 at = edge_place | 1ull << bit;
       uint32_t some = 0;
-      for_entries([&](double sum, u64 place) { some += order_of(sum) > edge || (order_of(sum) == edge && place >= at); });
+      for_all([&](double sum, u64 place) { some += order_of(sum) > edge || (order_of(sum) == edge && place >= at); });
       if (count_all(some, join.counts) >= (uint32_t)n) edge_place = at;
     }
-    if (tid == 0) join.n_joined = 0;
-    __syncthreads();
-    collect([&](double, u64 order, u64 place) { return order > edge || (order == edge && place >= edge_place); });
-    __syncthreads();
-    all = (uint32_t)n;
+    again();
+    for_all([&](double sum, u64 place) {
+      if (order_of(sum) > edge || (order_of(sum) == edge && place >= edge_place)) join_in(order_of(sum), place);
+    });
+    all = joined();  // n
+  }
+  if (all > (uint32_t)(2 * n + 80)) {  // as in a slice: another bound, of what has joined
+    constexpr int kEach = kMostJoined / kSliceThreads;
+    u64 order[kEach], place[kEach], best = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const uint32_t i = (uint32_t)(k * kSliceThreads + tid);
+      order[k] = i < all ? join.order[i] : 0;  // (0 is no number's)
+      place[k] = i < all ? join.place[i] : 0;
+      best = max(best, order[k]);
+    }
+    const double next = bounds_of(best ? sum_of(best) : -__builtin_inf(), n, join.most).least;
+    again();
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (order[k] && sum_of(order[k]) >= next) join_in(order[k], place[k]);
+    all = joined();
   }
   if (tid < n) {
     join.rows[tid] = join.ids[tid] = -1;
@@ -392,11 +465,10 @@ __global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, 
     if (s.placed) {  // (n is the number of beams, so that there is one round)
       const int32_t parent = i < n ? join.rows[i] - b0 : -1;
       bool is_first = i < n && join.rows[i] >= 0;
-      for (int32_t k = 0; k < i && k < n; ++k) is_first = is_first && join.rows[k] - b0 != parent;
+      for (int32_t k = 0; k < n; ++k) is_first = is_first & (k >= i || join.rows[k] - b0 != parent);
       uint64_t places = 0;
       for (int32_t k = 0; k < n; ++k) {
-        const int f = __shfl((int)is_first, k), p = __shfl(parent, k);
-        if (f) places |= 1ull << p;
+        if (__builtin_amdgcn_readlane((int)is_first, k)) places |= 1ull << (__builtin_amdgcn_readlane(parent, k) & 63);
       }
       const uint64_t others = __ballot(i < n && !is_first);
       if (is_first) to = parent;
@@ -560,11 +632,9 @@ namespace {
 template <Elem E> hipError_t select(const Logits& in, const LogitRules& r, const BeamSearch& s, const BeamMemory& m, hipStream_t stream) {
   const size_t lds = has_rules(r) && sizeof(RuleTable) > sizeof(BeamShared) ? sizeof(RuleTable) : sizeof(BeamShared);
   const int32_t n = slices_of<E>(in);
-  int groups = 1;
-  while (groups < s.n_out) groups *= 2;
-  hipLaunchKernelGGL(beam_slices_kernel<E>, dim3(n, s.requests * s.beams), dim3(kSliceThreads), lds, stream, in, r, s, m, groups);
+  hipLaunchKernelGGL(beam_slices_kernel<E>, dim3(n, s.requests * s.beams), dim3(kSliceThreads), lds, stream, in, r, s, m);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  hipLaunchKernelGGL(beam_join_kernel, dim3(s.requests), dim3(kSliceThreads), 0, stream, s, m, n, groups);
+  hipLaunchKernelGGL(beam_join_kernel, dim3(s.requests), dim3(kSliceThreads), 0, stream, s, m, n);
   return hipGetLastError();
 }
 }  // namespace

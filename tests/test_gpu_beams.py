@@ -123,6 +123,32 @@ def test_continuations_under_rules(requests, beams, V, dtype):
         b.check(2 * beams)
 
 
+@pytest.mark.parametrize("beams,V,n_out", [(64, 128256, 128), (32, 151936, 64), (19, 77650, 38), (64, 300000, 128), (9, 40000, 20)])
+def test_wide_searches(beams, V, n_out):
+    b = Beams(1, beams, V, "bf16", seed=n_out, ended=beams == 32)
+    b.check(n_out)
+    scores = b.scores.copy()
+    for live in ([0], [beams - 1], [beams // 2, 3], list(range(0, beams, 5))):          # a first step, and texts that are not there
+        b.scores[:] = -np.inf
+        b.scores[live] = scores[live]
+        b.check(n_out)
+    b.scores[:] = scores
+    b.scores[beams // 3] += 40                                                          # one row has all of it
+    b.check(n_out)
+
+
+@pytest.mark.parametrize("n_out", [8, 9, 40, 128])
+def test_masks_that_leave_stretches(n_out):
+    V = 50001
+    b = Beams(4, 3, V, "bf16", mask=[0.0], seed=n_out)
+    for row, parts in enumerate([[(0, 1100)], [(8192 - 600, 8192 + 600)], [(0, 700), (4096, 4796)], [(V - 849, V)], [(16384, 24576)], [(8, 16), (4104, 4112)],
+                                 [(100, 100 + n_out)], [(i, i + 3) for i in range(0, V, 61)], [(0, V)], [(20000, 22100)], [(0, 2048), (40000, 40001)], [(3, 4)]]):
+        for first, last in parts:
+            b.allowed[row, first:last] = True
+    b.check(n_out)
+    b.check(3, placed=True)
+
+
 def test_rows_that_masks_leave_nothing_and_beams_without_a_text():
     b = Beams(6, 4, 10000, "bf16", mask=[0.5], seed=2)
     b.scores[4:8] = [0.0, -np.inf, -np.inf, -np.inf]            # a first step
