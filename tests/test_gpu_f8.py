@@ -401,6 +401,28 @@ def test_rows_of_an_8_bit_matrix(n, V, K, out):
     _lookup_matches(buf[:n, :K], np.where(there[:, None], value, 0.0), factor, out)
 
 
+@pytest.mark.parametrize("out,low", [("bf16", False), ("f16", False), ("f16", True)])
+def test_products_next_to_the_middle_of_two_numbers(out, low):
+    """Products that 32 bits would put onto the middle, from either side; low: of numbers below the type's normal ones."""
+    V, K, factor = 512, 65536, np.float32(0.37)
+    rng = np.random.default_rng(5)
+    digits = 256 if out == "bf16" else 1024
+    shape = V // 128, K // 128
+    middle = (rng.integers(0, 200, shape) + 0.5) * 2.0 ** -24 if low else (digits // 2 + rng.integers(0, digits // 2, shape) + 0.5) * 2.0 ** rng.integers(-12, -6, shape)
+    scales = (middle / np.float64(factor)).astype(np.float32)
+    product = scales.astype(np.float64) * np.float64(factor)
+    assert ((product.astype(np.float32) == middle) & (product < middle)).sum() > 200 and ((product.astype(np.float32) == middle) & (product > middle)).sum() > 200
+    some = np.flatnonzero(np.isin(plain.e4m3(), [1, -1, 2, -2, 0.5, 4, 3, 0, -7]))
+    codes = torch.from_numpy(some[rng.integers(0, len(some), (V, K))]).to(torch.uint8).cuda()
+    ids = torch.arange(0, V, 64, dtype=torch.int32, device="cuda")
+    buf = torch.zeros((len(ids), K), dtype=TYPES[out][0], device="cuda")
+    on = torch.from_numpy(scales).cuda()
+    _xgm().f8_embed(ids.data_ptr(), len(ids), codes.data_ptr(), on.data_ptr(), V, K, float(factor), buf.data_ptr(), TYPES[out][1], K, _stream())
+    torch.cuda.synchronize()
+    at = ids.cpu().numpy()
+    _lookup_matches(buf, plain.e4m3()[codes.cpu().numpy()[at]] * np.repeat(scales.astype(np.float64)[at // 128], 128, 1), factor, out)
+
+
 @pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("scales_dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("n,V,K,group", [(1, 1, 32, 32), (3, 200, 160, 32), (64, 130, 1024, 128), (300, 5000, 2112, 64), (9, 40, 65536, 65536), (33, 77, 288, 96)])
