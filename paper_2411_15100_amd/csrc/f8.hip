@@ -157,7 +157,7 @@ struct List {
 __device__ __forceinline__ uint32_t allowed(const F8Head& h, int32_t b, int64_t token) {
   return h.mask[(size_t)b * h.W_mask + (min(token, (int64_t)h.V_mask - 1) >> 5)] >> (token & 31) & (uint32_t)(token < h.V_mask);
 }
-__device__ int32_t list_rows(const F8Head& h, Elem out_type, int32_t first_b, int32_t rows, int64_t base, int32_t here, List& list) {
+__device__ int32_t list_rows(const F8Head& h, Elem out_type, int32_t first_b, int32_t rows, int64_t base, int32_t here, bool wide, List& list) {
   int32_t tid = (int32_t)threadIdx.x;
   const int32_t threads = (int32_t)blockDim.x;
   asm volatile("" : "+v"(tid));  // (else places in the list are kept in registers while the matrix goes by)
@@ -184,10 +184,30 @@ __device__ int32_t list_rows(const F8Head& h, Elem out_type, int32_t first_b, in
       for (int32_t w = 0; w < r >> 5; ++w) place += __builtin_popcount(list.any[w]);
       list.row[place] = r;
       atomicAdd(&list.n, 1);
-    } else {
-      for (int32_t b = 0; b < rows; ++b) store_logit(h, out_type, (int64_t)(first_b + b) * h.logits_stride + base + r, -__builtin_inff());
     }
   }
+  // four rows at a time, of as many rows of the batch as there are threads
+  int32_t fours = (here + 3) / 4;
+  asm volatile("" : "+v"(fours));  // (as tid above)
+  const int32_t abreast = max(threads / fours, 1), b0 = tid / fours;
+  if (b0 < abreast)
+    for (int32_t i = tid - b0 * fours; i < fours; i += threads) {
+      const int32_t r = i * 4;
+      const uint32_t any = list.any[r >> 5] >> (r & 31) & 15u;
+      if (any == 15u) continue;
+      const float none[4] = {-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+#pragma unroll 1
+      for (int32_t b = b0; b < rows; b += abreast) {
+        const int64_t at = (int64_t)(first_b + b) * h.logits_stride + base + r;
+        if (wide && any == 0 && r + 4 <= here) {
+          store_logits(h, out_type, at, none);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (!(any >> k & 1u) && r + k < here) store_logit(h, out_type, at + k, none[k]);
+        }
+      }
+    }
   __syncthreads();
   return list.n;
 }
@@ -254,7 +274,7 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
   for (int64_t base = row0; base < row1; base += kListed) {
     const int32_t here = (int32_t)min((int64_t)kListed, row1 - base);
     int32_t count = here;
-    if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, list);
+    if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, wide, list);
     const int32_t tiles = (count + 15) / 16;
     int32_t sharing = 1;  // waves to a tile, no more than there are where masks leave no tile
     while (sharing * 2 <= n_steps && sharing * 2 * max(tiles, 1) <= waves) sharing *= 2;
@@ -358,20 +378,20 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
           codes = next_codes;
         }
       }
+      int32_t in = n, i0 = q * 4, me = tid;
+      asm volatile("" : "+v"(in), "+v"(i0), "+v"(me));  // (as in list_rows)
       if (sharing > 1) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          partial[tid] = acc[nb];
+          partial[me] = acc[nb];
           __syncthreads();
           if (sub == 0) {
 #pragma unroll 3
-            for (int32_t w = 1; w < sharing; ++w) acc[nb] += partial[tid + w * 64];
+            for (int32_t w = 1; w < sharing; ++w) acc[nb] += partial[me + w * 64];
           }
           __syncthreads();
         }
       }
-      int32_t in = n, i0 = q * 4;
-      asm volatile("" : "+v"(in), "+v"(i0));  // (as in list_rows)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         if (sub != 0 || t >= tiles || nb * 16 + in >= rows) continue;
@@ -496,7 +516,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
   for (int64_t base = row0; base < row1; base += kTogether) {
     const int32_t here = (int32_t)min(kTogether, row1 - base);
     int32_t count = here;
-    if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, list);
+    if constexpr (kMasked) count = list_rows(h, out_type, first_b, rows, base, here, wide, list);
     const int32_t tiles = (count + 15) / 16;
     auto row_of = [&](int32_t i) -> int32_t {
       const int32_t k = min(i, count - 1);
@@ -588,24 +608,28 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
         for (int m = 0; m < MW; ++m) acc[c][m] = float4v{0, 0, 0, 0};
       // Multiplies a block.  The loads of another one are seen to when the first reads of LDS are on their way: between the products, where they
       // keep nobody waiting, they come too late for the next barrier (1024 rows of 128256 x 4096: 642 us, and 676).
-      auto multiply = [&](const Buffer& s, auto&& load_other) {
+      auto multiply = [&](auto tiles_of_wave, const Buffer& s, auto&& load_other) {
+        constexpr int N = decltype(tiles_of_wave)::value;
+        // (registers: scales of rows are read where they are used, and a tile is scaled right behind the next: 85 rows of 50102 x 2048, most rows listed,
+        // 62 us and not 56, but 267 rows of 14681 x 2048 with few 29 and not 48, as waves without a tile have nothing to multiply)
+        constexpr bool kTight = kMasked && sizeof(Operand) > 32 && N * MW > 8;
         const int place = q ^ (n & 7);
         auto operand = [&](const uint4v* row) { return Operand(row[place], row[place ^ 4]); };
         const uint4v* const my_codes = &s.codes[(first * 16 + n) * 8];
         const uint4v* const my_states = &s.states[(wm * MW * 16 + n) * 8];
         uint4v lo = my_states[place], hi = my_states[place ^ 4];
         float state_scale = s.scales[wm * MW * 16 + n];
-        float4v scale[TW];
+        float4v scale[N];
 #pragma unroll
-        for (int c = 0; c < TW; ++c) {
-          if constexpr (kMasked) scale[c] = *reinterpret_cast<const float4v*>(&s.scales[Shape::kRows + (first + c) * 16 + q * 4]);
-          else scale[c][0] = s.scales[Shape::kRows + (first + c) * 16];
+        for (int c = 0; c < N; ++c) {
+          if constexpr (kMasked && !kTight) scale[c] = *reinterpret_cast<const float4v*>(&s.scales[Shape::kRows + (first + c) * 16 + q * 4]);
+          else if constexpr (!kMasked) scale[c][0] = s.scales[Shape::kRows + (first + c) * 16];
         }
-        const Operand a[4] = {operand(my_codes), operand(my_codes + (TW > 1) * 128), operand(my_codes + (TW > 2) * 256), operand(my_codes + (TW > 3) * 384)};
+        const Operand a[4] = {operand(my_codes), operand(my_codes + (N > 1) * 128), operand(my_codes + (N > 2) * 256), operand(my_codes + (N > 3) * 384)};
         // the sums of a tile are scaled while the next ones' products are made
         // (1024 rows of 128256 x 4096: one behind 643 us, two 639, four 617)
-        constexpr int kBehind = kMasked && sizeof(Operand) > 32 ? 2 : 4;  // (registers)
-        constexpr int kRoundsBehind = (kBehind + TW - 1) / TW;
+        constexpr int kBehind = kMasked && sizeof(Operand) > 32 ? N == 1 || kTight ? 1 : 2 : 4;  // (registers)
+        constexpr int kRoundsBehind = (kBehind + N - 1) / N;
         float4v sum[kBehind + 1];
         float scale_of[kRoundsBehind + 1];
         load_other();
@@ -619,14 +643,18 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
             state_scale = s.scales[(wm * MW + m + 1) * 16 + n];
           }
 #pragma unroll
-          for (int c = 0; c < TW; ++c) {
-            const int t = m * TW + c, was = t - kBehind;
+          for (int c = 0; c < N; ++c) {
+            const int t = m * N + c, was = t - kBehind;
             if (m < MW) sum[t % (kBehind + 1)] = products(a[c], x);
-            if (was >= 0 && was < MW * TW) {
-              float4v& to = acc[was % TW][was / TW];
-              const float state = scale_of[was / TW % (kRoundsBehind + 1)];
-              if constexpr (kMasked) to += sum[was % (kBehind + 1)] * (scale[was % TW] * state);
-              else to += sum[was % (kBehind + 1)] * (scale[was % TW][0] * state);
+            if (was >= 0 && was < MW * N) {
+              float4v& to = acc[was % N][was / N];
+              const float state = scale_of[was / N % (kRoundsBehind + 1)];
+              if constexpr (kTight) {
+                int at = q * 4;
+                asm volatile("" : "+v"(at));
+                to += sum[was % (kBehind + 1)] * (*reinterpret_cast<const float4v*>(&s.scales[Shape::kRows + (first + was % N) * 16 + at]) * state);
+              } else if constexpr (kMasked) to += sum[was % (kBehind + 1)] * (scale[was % N] * state);
+              else to += sum[was % (kBehind + 1)] * (scale[was % N][0] * state);
               asm volatile("" : "+v"(to));  // (here, and not when all products are made: they would not fit the registers)
             }
           }
@@ -641,15 +669,19 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
         if constexpr (Shape::kStages == 3) {
           if (block + 1 < blocks) barrier_behind_loads<kLoads>();
           else barrier_behind_loads<0>();
-          multiply(now, [&] {
+          auto load_next = [&] {
             if (block + 2 >= blocks) return;
             load_others(block + 2, other);
             load_codes(block + 2, other);
-          });
+          };
+          // Few tiles: waves without one have nothing to multiply (128 rows of 10000 x 4096 take 26.5 us, and 37 where all of them multiply TW).
+          if (mine > 1) multiply(std::integral_constant<int, TW>(), now, load_next);
+          else if (mine == 1) multiply(std::integral_constant<int, 1>(), now, load_next);
+          else load_next();
         } else {
           if (block + 1 < blocks) barrier_behind_loads<Shape::kCodeLoads>();
           else barrier_behind_loads<0>();
-          multiply(now, [&] {
+          multiply(std::integral_constant<int, TW>(), now, [&] {
             barrier_behind_loads<63>();  // (for reads of LDS alone)
             if (block + 1 < blocks) load_others(block + 1, other);
             if (block + 2 < blocks) load_codes(block + 2, now);
@@ -881,23 +913,26 @@ hipError_t launch_f8_quantize(const void* x, Elem type, int32_t B, int32_t K, in
 }
 
 namespace {
-// Which kernel takes a batch, by what a call takes them in us: a workgroup of few rows a start, its hidden states and its tiles; one of many rows (which
-// waits for a launch that brings hidden states to 8 bits) a time for each block of columns of each of its passes, which is that of a barrier and of
-// loads that come back, or where that is more the bytes of its tiles.  For bf16, few and many, us:
-//   4096 x 4096: 1 row 7 and 24, 16 rows 13 and 25, 32 rows 20 and 30, 40 rows 21 and 40
+// Which kernel takes a batch, by what a call takes them in us: a workgroup of few rows a start, its hidden states and its tiles (of one to four, loads come
+// back meanwhile); one of many rows (which waits for a launch that brings hidden states to 8 bits) a time for each block of columns of each of its passes,
+// which is that of a barrier and of loads that come back, less where no wave has more than a tile, or where that is more the bytes of its tiles.
+// For bf16, few and many, us:
+//   4096 x 4096: 1 row 7 and 19, 16 rows 13 and 19, 32 rows 20 and 20, 64 rows 20.5 and 24.5, 128 rows 24.4 and 21.7
+//   10000 x 4096: 16 rows 16.3 and 19.1, 32 rows 23.1 and 21.0, 64 rows 29.5 and 26.4
 //   50001 x 2080: 1 row 25.5 and 26.3, 16 rows 29.5 and 27.6, 32 rows 36.5 and 31.6
 //   128256 x 4096: 1 row 103 and 95, 16 rows 115 and 96, 32 rows 128 and 101; 151936 x 1024: 31 and 33, 36 and 37, 41 and 41
-// of many 500 rows of 2048 x 4096 37 in tiles of 128 rows and 64 in those of 256, 1024 of 128256 x 4096 700 and 628, 384 of them 270 and 349.
-// Logits in 32 bits, 128 rows of 4096 x 4096: few 25, many 63.
+// of many 500 rows of 2048 x 4096 24 in tiles of 128 rows and 64 in those of 256, 1024 of 128256 x 4096 700 and 628, 384 of them 270 and 349.
+// Logits in 32 bits, 128 rows of 4096 x 4096: few 24.3, many 25.7, of 10000 x 4096 40.8 and 36.9.
 enum class Many { kFew, k16, k32, k64, k128, k128Whole, k256 };
 int32_t few_rows(const F8Head& h) { return h.B <= 16 ? 16 : 32; }
 double few_time(const F8Head& h) {
   const int32_t each = few_tiles(h, few_rows(h)), rows = h.B < 32 ? h.B : 32;
-  return 5.0 + f8_blocks(h.K) * (0.09 * each + rows * (0.0115 + 0.0005 * each));
+  return 5.0 + f8_blocks(h.K) * ((each < 4 ? 0.05 * each : 0.1 * each - 0.15) + rows * (0.0125 + 0.0005 * each));
 }
-double many_time(const F8Head& h, int32_t rows, double start, double block, double tile) {
+// one, block: of a block of a pass in which no wave has more than a tile, and of others
+double many_time(const F8Head& h, int32_t rows, int32_t waves, double start, double one, double block, double tile) {
   const int32_t each = few_tiles(h, rows), passes = (each + 15) / 16;  // (a pass is 16 tiles in all of them)
-  const double latency = passes * block, bytes = each * tile;
+  const double latency = each <= waves ? one : passes * block, bytes = each * tile;
   return start + f8_blocks(h.K) * (latency > bytes ? latency : bytes);
 }
 Many kernel_of(const F8Head& h, Elem logits_type) {
@@ -908,12 +943,12 @@ Many kernel_of(const F8Head& h, Elem logits_type) {
     if (time == 0.0 || t < time) best = kernel, time = t;
   };
   const double start = h.hidden.scales ? 6.0 : 10.0;
-  if (h.B <= 16) offer(Many::k16, many_time(h, 16, start, 0.46, 0.083));
-  else if (h.B <= 32) offer(Many::k32, many_time(h, 32, start, 0.63, 0.09));
-  else if (h.B <= 64) offer(Many::k64, many_time(h, 64, start, 0.95, 0.09));
-  else if (whole) offer(Many::k128Whole, many_time(h, 128, 4.0, 1.8, 0.0));
-  else offer(Many::k128, many_time(h, 128, 4.0, 1.1, 0.0));
-  if (!whole && !h.mask && h.B > 128) offer(Many::k256, many_time(h, 256, 4.0, 1.95, 0.0));  // (with lists of rows its registers would not do)
+  if (h.B <= 16) offer(Many::k16, many_time(h, 16, 8, start, 0.28, 0.46, 0.083));
+  else if (h.B <= 32) offer(Many::k32, many_time(h, 32, 8, start, 0.32, 0.63, 0.09));
+  else if (h.B <= 64) offer(Many::k64, many_time(h, 64, 8, start, 0.43, 0.95, 0.09));
+  else if (whole) offer(Many::k128Whole, many_time(h, 128, 4, 10.0, 0.5, 1.85, 0.0));
+  else offer(Many::k128, many_time(h, 128, 4, 10.0, 0.48, 1.1, 0.0));
+  if (!whole && !h.mask && h.B > 128) offer(Many::k256, many_time(h, 256, 0, 10.0, 0.0, 1.95, 0.0));  // (with lists of rows its registers would not do)
   if (few_fits(h, h.B < 32 ? h.B : 32)) offer(Many::kFew, few_time(h));
   return best;
 }
