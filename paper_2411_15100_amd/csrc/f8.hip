@@ -447,7 +447,8 @@ struct StateScales {  // where the scale of a row and a block lies
 __device__ const uint4v kZeros = {0, 0, 0, 0};
 // 16 or 4 bytes a lane; `to` is the place of the wave's first lane.  (Written out because the compiler would let every read of LDS wait for all
 // of these; they have no result in a register, and who reads what they bring waits for them behind barrier_behind_loads.  Nor does it see to wait
-// states in such a text: a load to LDS comes one of them behind the instruction that sets its m0.)
+// states in such a text: a load to LDS comes one of them behind the instruction that sets its m0, and one with a scalar address five behind a vector
+// instruction that writes it, as those do that bring spilled ones back.)
 __device__ __forceinline__ uint32_t lds_place(const void* to) {
   return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)to);
 }
@@ -456,7 +457,7 @@ __device__ __forceinline__ void bring16(const void* from, const void* to) {
 }
 // the same from an address that all lanes share and an offset each
 __device__ __forceinline__ void bring16(const void* from, uint32_t offset, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_place(to)), "v"(offset), "s"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_place(to)), "v"(offset), "s"(from) : "memory");
 }
 __device__ __forceinline__ void bring4(const void* from, const void* to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_place(to)), "v"(from) : "memory");

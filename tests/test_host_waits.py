@@ -85,3 +85,11 @@ def test_loads_to_lds_come_a_wait_state_behind_their_m0(listing):
     assert loads > 100
     found = {kernel: len(m) for kernel, code in listing if (m := missing(code, into_lds, sets, 1))}
     assert not found, (sum(found.values()), loads, found)
+
+
+def test_loads_with_a_scalar_address_come_five_wait_states_behind_a_vector_instruction_that_writes_it(listing):
+    address = lambda name, operands: set().union(*map(scalars, operands)) if name.startswith(MEMORY) else set()     # noqa: E731
+    loads = sum(bool(address(*one)) for _, code in listing for one in code)
+    assert loads > 1000
+    found = {kernel: m[:2] for kernel, code in listing if (m := missing(code, address, written, 5))}
+    assert not found, (loads, found)
