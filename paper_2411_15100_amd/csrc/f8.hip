@@ -453,14 +453,14 @@ __device__ __forceinline__ uint32_t lds_place(const void* to) {
   return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)to);
 }
 __device__ __forceinline__ void bring16(const void* from, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_place(to)), "v"(from) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(lds_place(to)), "v"(from) : "memory");
 }
 // the same from an address that all lanes share and an offset each
 __device__ __forceinline__ void bring16(const void* from, uint32_t offset, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_place(to)), "v"(offset), "s"(from) : "memory");
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(lds_place(to)), "v"(offset), "s"(from) : "memory");
 }
 __device__ __forceinline__ void bring4(const void* from, const void* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_place(to)), "v"(from) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" : : "{m0}"(lds_place(to)), "v"(from) : "memory");
 }
 // A barrier for which a wave waits until no more than n of its loads are on their way, and none of its reads of LDS.
 template <int n> __device__ __forceinline__ void barrier_behind_loads() {

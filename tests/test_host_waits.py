@@ -88,8 +88,22 @@ def test_loads_to_lds_come_a_wait_state_behind_their_m0(listing):
 
 
 def test_loads_with_a_scalar_address_come_five_wait_states_behind_a_vector_instruction_that_writes_it(listing):
-    address = lambda name, operands: set().union(*map(scalars, operands)) if name.startswith(MEMORY) else set()     # noqa: E731
+    def address(name, operands):
+        return set().union(*map(scalars, operands), {"m0"} if "_load_lds" in name else ()) if name.startswith(MEMORY) else set()
+
     loads = sum(bool(address(*one)) for _, code in listing for one in code)
     assert loads > 1000
     found = {kernel: m[:2] for kernel, code in listing if (m := missing(code, address, written, 5))}
     assert not found, (loads, found)
+
+
+def test_texts_leave_m0_to_the_compiler():
+    """Loads to LDS take it as an operand; set in a text, it would change behind the compiler's back."""
+    found = 0
+    for name in os.listdir(lib_build.CSRC):
+        for text in re.findall(r"\basm\b[^;]*;", open(os.path.join(lib_build.CSRC, name)).read()):
+            assert not re.search(r"\bm0,", text), (name, text)
+            if "_load_lds" in text:
+                found += 1
+                assert '"{m0}"' in text, (name, text)
+    assert found
