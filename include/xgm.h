@@ -623,8 +623,9 @@ int xgm_sample(xgm_sampler* s, const void* d_logits, xgm_dtype dt, int32_t B, in
  * hidden_dt XGM_BF16 or XGM_F16: the call brings them to 8 bits itself, as xgm_f8_quantize does; d_hidden_scales is NULL,
  * and d_work is xgm_f8_work_bytes(B, K) bytes of device memory (a multiple of 16 bytes as an address) for the call to work in; calls with one d_work
  * must be ordered by the caller, as must replays of graphs that hold them.  With XGM_F8 d_work may be NULL; with it batches of more than 64 rows are faster.
- * Logits of 16 bits in batches of more than 64 rows may be made by the matrix instructions for 8 bits, which cut off a product below 2^-13 of
- * the largest of a group of neighbouring ones: beside the rounding at the end that is about 2^-15 of the largest product of a block of columns.
+ * Logits in bf16 of batches of more than 64 rows may be made by the matrix instructions for 8 bits, which cut off what products have below 2^-13 of
+ * the largest one's power of two among 8 neighbouring ones: beside the rounding at the end less than 7 * 2^-13 of the sum of these largest products.  With logits in f16 or
+ * 32 bits nothing is cut off.
  * d_codes: [V, K] bytes.  d_scales: [ceil(V / 128), ceil(K / 128)] floats.  K is a multiple of 16, at most XGM_MAX_HIDDEN;
  * B <= XGM_MAX_ROWS; d_hidden, its row pitch and d_codes must be multiples of 16 bytes.  d_logits: [B, V] of logits_dt (XGM_F32, XGM_BF16, XGM_F16),
  * row stride logits_stride_elems.  A matrix with the rows from 128 i on of a larger one takes d_bitmask + 4 i and the larger one's v_mask,

@@ -18,10 +18,12 @@ typedef int int8v __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// Codes go through the matrix instructions as f16, which holds every e4m3 number, or as they are: the instructions for 8 bits add up
-// neighbouring products with what lies from 2^-13 of the largest of them on (measured: 2^16 + 2^3 is exact, 2^16 + 2^2 is 2^16, unless they lie 8 columns
-// apart), and take half the time.  Sums of few rows and logits in 32 bits are made the first way, with the 24 bits of a float; where many rows are
-// rounded to 16 bits behind it, what the second way loses is less than the rounding: 2^-14.7 of the largest product of a block on average.
+// Codes go through the matrix instructions as f16, which holds every e4m3 number, or as they are: the instructions for 8 bits take half the time, but of
+// each 8 neighbouring products they cut off what lies below 2^-13 of the largest one's power of two (measured: 2^16 + 2^3 is exact, 2^16 + 2^2 is 2^16, unless
+// they lie in different eights; between eights nothing is lost down to 2^-23).  The largest loses nothing, the 7 others less than 2^-13 of it each: less
+// than 2^-10.2 of the sum of the eights' largest products, and so of the sum of all |products| (up to 2^-11.4 of that was seen in numbers at random, and 2^-10.4
+// in those made for it).  That is less than half a step of bf16, 2^-9, of a sum that does not cancel, and more than f16's, 2^-12 to 2^-11: the second way is
+// for logits in bf16 of more than 64 rows alone; all others have sums with the 24 bits of a float.
 __device__ __forceinline__ f16x8 halves(uint32_t lo, uint32_t hi) {
   const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.0f, true);
   const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.0f, true);
@@ -743,9 +745,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void f8_many_kernel(F8Head h, Stat
           }
         }
       };
-      if (out_type == Elem::kF32) store(std::integral_constant<Elem, Elem::kF32>());
-      else if (out_type == Elem::kBF16) store(std::integral_constant<Elem, Elem::kBF16>());
-      else store(std::integral_constant<Elem, Elem::kF16>());
+      if (std::is_same_v<Operand, Eights> || out_type == Elem::kBF16) store(std::integral_constant<Elem, Elem::kBF16>());
+      else if constexpr (!std::is_same_v<Operand, Eights>) {
+        if (out_type == Elem::kF32) store(std::integral_constant<Elem, Elem::kF32>());
+        else store(std::integral_constant<Elem, Elem::kF16>());
+      }
     }
   }
 }
@@ -924,7 +928,7 @@ namespace {
 //   50001 x 2080: 1 row 25.5 and 26.3, 16 rows 29.5 and 27.6, 32 rows 36.5 and 31.6
 //   128256 x 4096: 1 row 103 and 95, 16 rows 115 and 96, 32 rows 128 and 101; 151936 x 1024: 31 and 33, 36 and 37, 41 and 41
 // of many 500 rows of 2048 x 4096 24 in tiles of 128 rows and 64 in those of 256, 1024 of 128256 x 4096 700 and 628, 384 of them 270 and 349.
-// Logits in 32 bits, 128 rows of 4096 x 4096: few 24.3, many 25.7, of 10000 x 4096 40.8 and 36.9.
+// Logits in 32 bits or f16, 128 rows of 4096 x 4096: few 24.3, many 25.7, of 10000 x 4096 40.8 and 36.9.
 enum class Many { kFew, k16, k32, k64, k128, k128Whole, k256 };
 int32_t few_rows(const F8Head& h) { return h.B <= 16 ? 16 : 32; }
 double few_time(const F8Head& h) {
@@ -938,7 +942,7 @@ double many_time(const F8Head& h, int32_t rows, int32_t waves, double start, dou
   return start + f8_blocks(h.K) * (latency > bytes ? latency : bytes);
 }
 Many kernel_of(const F8Head& h, Elem logits_type) {
-  const bool whole = logits_type == Elem::kF32;
+  const bool whole = logits_type != Elem::kBF16;  // (sums of 24 bits)
   Many best = Many::k16;
   double time = 0.0;
   auto offer = [&](Many kernel, double t) {
