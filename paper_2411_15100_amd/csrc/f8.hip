@@ -769,10 +769,9 @@ int64_t padded(int32_t K) { return (int64_t)f8_blocks(K) * 128; }
 // as 64 bytes a thread; 16 bits are no faster so, 45 us and 44), 2^shift threads a row.  value * (scale * factor) in 64 bits, where both products are exact, rounded once.
 // 16384 rows of 4096 columns (8 bits to bf16) take 44 us, 4.4 TB/s: memory, as products in 32 bits would; 128 rows 3.4 us and a launch.
 constexpr int kEmbedThreads = 256;
-template <Elem S, Elem O, bool Q4> __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(Embed e, int shift, bool wide) {
+constexpr int32_t kMostEmbedGroups = 1 << 23;  // workgroups of a launch, which has to have less than 2^32 threads
+template <Elem S, Elem O, bool Q4> __device__ __forceinline__ void embed_row(const Embed& e, int32_t i, int32_t t, int shift, bool wide) {
   typedef typename Type<O>::bits bits;
-  const int32_t i = (int32_t)blockIdx.x * (kEmbedThreads >> shift) + ((int32_t)threadIdx.x >> shift), t = (int32_t)threadIdx.x & ((1 << shift) - 1);
-  if (i >= e.n) return;
   const int32_t id = e.ids[i];
   const bool there = id >= 0 && id < e.V;
   const int64_t v = there ? id : 0;
@@ -841,13 +840,20 @@ template <Elem S, Elem O, bool Q4> __global__ __launch_bounds__(kEmbedThreads) v
     }
   }
 }
+// A row's threads take another one where there are more rows than a launch has room for.
+template <Elem S, Elem O, bool Q4> __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(Embed e, int shift, bool wide) {
+  const int32_t t = (int32_t)threadIdx.x & ((1 << shift) - 1), rows = kEmbedThreads >> shift;
+  for (uint32_t i = blockIdx.x * (uint32_t)rows + (threadIdx.x >> shift); i < (uint32_t)e.n; i += (uint32_t)kMostEmbedGroups * (uint32_t)rows)
+    embed_row<S, O, Q4>(e, (int32_t)i, t, shift, wide);
+}
 template <Elem S, bool Q4> hipError_t launch_embed(const Embed& e, Elem out_type, hipStream_t stream) {
   int shift = 0;
   while (shift < 8 && (16 << shift) < e.K) ++shift;
   const int32_t rows = kEmbedThreads >> shift;
   const int size = out_type == Elem::kF32 ? 4 : 2;
   const bool wide = reinterpret_cast<uintptr_t>(e.out) % 16 == 0 && e.out_stride * size % 16 == 0;
-  const dim3 grid((uint32_t)((e.n + rows - 1) / rows));
+  const int32_t groups = (e.n + rows - 1) / rows;
+  const dim3 grid((uint32_t)(groups < kMostEmbedGroups ? groups : kMostEmbedGroups));
   if (out_type == Elem::kF32) hipLaunchKernelGGL((embed_kernel<S, Elem::kF32, Q4>), grid, dim3(kEmbedThreads), 0, stream, e, shift, wide);
   else if (out_type == Elem::kBF16) hipLaunchKernelGGL((embed_kernel<S, Elem::kBF16, Q4>), grid, dim3(kEmbedThreads), 0, stream, e, shift, wide);
   else hipLaunchKernelGGL((embed_kernel<S, Elem::kF16, Q4>), grid, dim3(kEmbedThreads), 0, stream, e, shift, wide);

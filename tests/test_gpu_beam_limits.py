@@ -30,3 +30,22 @@ def test_more_parts_than_a_launch_has_workgroups(source):
     xgm.reorder_rows(kept, on.data_ptr(), 3, _stream())
     torch.cuda.synchronize()
     assert torch.equal(x, want[0]) and torch.equal(y, want[1])
+
+
+def test_a_lookup_of_the_most_rows():
+    """2^24 rows of more columns than 256 threads take at once: a workgroup a row, and more of them than a launch may have.  69 GB."""
+    xgm = _xgm()
+    n, K, V = 1 << 24, 2064, 300
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        pytest.skip("not as much memory")
+    codes = torch.randint(0, 126, (V, K), dtype=torch.uint8, device="cuda")
+    scales = torch.full((-(-V // 128), -(-K // 128)), 0.25, device="cuda")
+    ids = torch.randint(-1, V, (n,), dtype=torch.int32, device="cuda")
+    out = torch.empty((n, K), dtype=torch.bfloat16, device="cuda")
+    xgm.f8_embed(ids.data_ptr(), n, codes.data_ptr(), scales.data_ptr(), V, K, 0.5, out.data_ptr(), xgm.DTYPE_BF16, K, _stream())
+    torch.cuda.synchronize()
+    table = torch.cat([codes.view(torch.float8_e4m3fn).float() / 8, torch.zeros((1, K), device="cuda")]).bfloat16()      # (exact; -1 is the last one)
+    for b in range(0, n, 1 << 19):
+        assert torch.equal(out[b:b + (1 << 19)], table[ids[b:b + (1 << 19)].long()]), b
+    del out
+    torch.cuda.empty_cache()

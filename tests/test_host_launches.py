@@ -20,7 +20,7 @@ def checks(tmp_path_factory):
     return out
 
 
-@pytest.mark.parametrize("what", ["rows", "projection", "beams"])
+@pytest.mark.parametrize("what", ["lookups", "rows", "projection", "beams"])
 def test_what_calls_accept_can_be_launched(checks, what):
     done = subprocess.run([checks, lib_build.LIB, what], capture_output=True, text=True, timeout=120)
     assert done.returncode == 0, done.stdout + done.stderr
