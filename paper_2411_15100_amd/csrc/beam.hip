@@ -569,6 +569,8 @@ __device__ __forceinline__ void copy_region(const Region& r, int32_t units, cons
   }
 }
 template <class T> __device__ __forceinline__ void move_any(const Region& r, int32_t units, const Moves& m) {
+  // (parts may be shorter than a region, those of some arrays many times)
+  while (units > kMoveThreads && (int64_t)(units / 2) * (int64_t)sizeof(T) >= r.end - r.begin) units /= 2;
   if (m.tangled) move_region<T, true>(r, units, m);
   else if (sizeof(T) == 16 && units % kMoveThreads == 0) copy_region(r, units, m);
   else move_region<T, false>(r, units, m);
@@ -681,7 +683,8 @@ hipError_t launch_reorder_rows(const RowData* data, int n, const int32_t* source
   }
   list.region = 1024;
   while (list.region > 64 && groups(list.region) < 1024) list.region /= 2;
-  while (list.region < (1 << 20) && groups(list.region) > (1 << 20)) list.region *= 2;
+  // (only while that makes fewer pieces of most: where parts are short, it would but leave the long ones of other arrays to few workgroups)
+  while (list.region < (1 << 20) && groups(list.region) > (1 << 20) && groups(list.region * 2) <= groups(list.region) / 4 * 3) list.region *= 2;
   list.pieces = groups(list.region);
   if (list.pieces <= kMostMoveGroups) hipLaunchKernelGGL(reorder_kernel<false>, dim3((uint32_t)list.pieces), dim3(kMoveThreads), 0, stream, list, n, source, B);
   else hipLaunchKernelGGL(reorder_kernel<true>, dim3(kMostMoveGroups), dim3(kMoveThreads), 0, stream, list, n, source, B);

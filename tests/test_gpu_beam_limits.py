@@ -1,5 +1,7 @@
 """Continuations of beams, and what rows keep, at the ends of what the calls accept."""
 
+import time
+
 import numpy as np
 import pytest
 
@@ -30,6 +32,25 @@ def test_more_parts_than_a_launch_has_workgroups(source):
     xgm.reorder_rows(kept, on.data_ptr(), 3, _stream())
     torch.cuda.synchronize()
     assert torch.equal(x, want[0]) and torch.equal(y, want[1])
+
+
+@pytest.mark.parametrize("parts", [1 << 21, 1 << 24])
+def test_short_parts_take_what_their_bytes_take(parts):
+    """Workgroups that each have a part of 4 bytes, or of 16, beside an array of long ones: not as long as if they had a long one."""
+    xgm = _xgm()
+    x = torch.randint(0, 99, (2, parts), dtype=torch.int32, device="cuda")
+    y = torch.randint(0, 99, (2, parts // 4, 4), dtype=torch.int32, device="cuda")
+    z = torch.randint(0, 99, (2, 1 << 26), dtype=torch.int32, device="cuda")
+    kept = xgm.RowSet(xgm.RowData(d_data=x.data_ptr(), row_stride=4 * parts, part_stride=4, part_bytes=4, n_outer=1, n_parts=parts),
+                      xgm.RowData(d_data=y.data_ptr(), row_stride=4 * parts, part_stride=16, part_bytes=16, n_outer=1, n_parts=parts // 4),
+                      xgm.RowData(d_data=z.data_ptr(), row_stride=4 << 26, part_bytes=4 << 26, n_outer=1, n_parts=1))
+    on = torch.tensor([-1, 0], dtype=torch.int32, device="cuda")
+    begin = time.perf_counter()
+    xgm.reorder_rows(kept, on.data_ptr(), 2, _stream())
+    torch.cuda.synchronize()
+    took = time.perf_counter() - begin
+    assert torch.equal(x[0], x[1]) and torch.equal(y[0], y[1]) and torch.equal(z[0], z[1])
+    assert took < 0.1 + parts * 30e-9          # (3 us a workgroup, of which a card has more than 100 at a time)
 
 
 def test_a_lookup_of_the_most_rows():
