@@ -672,7 +672,7 @@ void xgm_beams_destroy(xgm_beams* s);
  * placed (n_out must be n_beams): not 0: the first continuation of a row takes the row's own place, and the others, in their order, the
  * places that are left, lowest first: a text that goes on stays where it is, and whatever it keeps need not move.
  * d_out_scores may be d_scores where n_out is n_beams; the arrays must not overlap otherwise.  n_beams <= XGM_MAX_BEAMS.  The same inputs give the same results; a sum is exact to
- * (4 + |y| + |score|) 2^-50. */
+ * (18 + |y| + |score| + |largest y of the row|) 2^-50. */
 int xgm_beam_select(xgm_beams* s, const void* d_logits, xgm_dtype dt, int32_t requests, int32_t n_beams, int32_t V, int64_t row_stride_elems,
                     const xgm_logit_rules* rules, const float* d_scores, const int32_t* d_ended, int32_t n_out, int32_t placed, int32_t* d_rows,
                     int32_t* d_ids, float* d_out_scores, void* hip_stream);

@@ -1,11 +1,16 @@
-"""Continuations of beams, and what rows keep, at the ends of what the calls accept."""
+"""Continuations of beams, and what rows keep, at the ends of what the calls accept.
+
+Tolerances.  A sum y + (score - (top + log(weights / weight of top))), top the row's largest logit, is off by less than (18 + |y| + |score| + |top|) 2^-50 before it is
+rounded to 32 bits.  In steps of 2^-52: a weight is off by 2 + |y| of itself, the weights together by 2 + |top| + 14 (the mean of top - y under the weights is at most
+log 2^20 < 14) and by half a step for each of 39 additions at most, the largest one's own by 2 + |top|, the logarithm of at most 14 by 8: 46 + 2 |top|.  Three additions
+round by half a step of their results: (42 + |y| + 2 |score| + 3 |top|) / 2.  Together 67 + |y| / 2 + |score| + 3.5 |top|, a fourth of which in steps of 2^-50."""
 
 import time
 
 import numpy as np
 import pytest
 
-from test_gpu_beams import _stream, _xgm
+from test_gpu_beams import Beams, _stream, _xgm
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +75,51 @@ def test_a_lookup_of_the_most_rows():
         assert torch.equal(out[b:b + (1 << 19)], table[ids[b:b + (1 << 19)].long()]), b
     del out
     torch.cuda.empty_cache()
+
+
+def _bound(y, score, top):
+    return (18 + abs(y) + abs(score) + abs(top)) * 2.0 ** -50
+
+
+@pytest.mark.parametrize("score", [0.0, -3.0, 700.0])
+@pytest.mark.parametrize("top", [1.0, 40.0, 1000.0, 30000.0])
+def test_order_behind_a_token_that_has_all_the_weight(top, score):
+    """Two rows alike but for their second token, which is worth 0 and `more`, down to what 64 bits do not tell apart beside the largest logit."""
+    R, V = 60, 300
+    b = Beams(R, 2, V, "f32", seed=1)
+    x = b.logits
+    x[:] = -torch.rand(V, device="cuda") - 1.0
+    x[:, 7], x[:, 100] = top, 0.0
+    more = 2.0 ** -np.arange(R)
+    x[1::2, 100] = torch.from_numpy(more.astype(np.float32)).cuda() * min(0.5, top / 2)
+    b.scores[:] = score
+    rows, ids, sums = b.run(4)
+    y = x[1::2, 100].double().cpu().numpy()
+    told = 0
+    for r in range(R):
+        if y[r] / 2 > _bound(y[r], score, top) + _bound(0.0, score, top):      # (y itself raises the row's weight by less than half of it)
+            assert ids[r, 2] == 100 and ids[r, 3] == 100 and (rows[r, 2:] == [2 * r + 1, 2 * r]).all(), (r, y[r])
+            told += 1
+    assert told >= 30
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [0.0, 3.0, 300.0, 30000.0, -30000.0])
+def test_sums_next_to_zero(top, dtype):
+    """Scores as near to the logarithms of the rows' weights as 32 bits let them be: what is left of the second token's sum shows more of its bits."""
+    R, V = 64, 9000
+    b = Beams(R, 1, V, dtype, seed=3)
+    x = b.logits
+    x[:] = (x.float() * 0.5 + top).to(x.dtype)
+    y = x.double().cpu().numpy().astype(np.longdouble)
+    most = y.max(1, keepdims=True)
+    lse = (most + np.log(np.exp(y - most).sum(1, keepdims=True)))[:, 0]
+    order = np.argsort(-y.astype(np.float64), axis=1, kind="stable")[:, :3]
+    b.scores[:] = (lse - y[np.arange(R), order[:, 1]]).astype(np.float32)
+    rows, ids, sums = b.run(3)
+    assert np.array_equal(ids, order)
+    for k in range(3):
+        of = y[np.arange(R), order[:, k]]
+        want = of + (b.scores.astype(np.longdouble) - lse)
+        tol = 2.0 ** -24 * np.abs(want) + _bound(of, b.scores, most[:, 0])
+        assert (np.abs(sums[:, k] - want) <= tol).all(), (k, float((np.abs(sums[:, k] - want) / tol).max()))
