@@ -666,7 +666,7 @@ void xgm_beams_destroy(xgm_beams* s);
  * score is not finite has none (a beam without a text: -inf).
  * The first n_out <= XGM_MAX_CONTINUATIONS continuations of a request, in falling order of the sum (among equal ones the lower row first;
  * in a row the larger logit, then the lower id), become
- *   d_rows[r][j], the row continued (of all rows, as xgm_batch_fork and xgm_reorder_rows take it),
+ *   d_rows[r][j], the row continued (of all rows, as xgm_batch_fork and xgm_reorder_rows take it, where there are XGM_BATCH_MAX_ROWS of them at most),
  *   d_ids[r][j], the token (as xgm_batch_accept_tokens takes it), d_out_scores[r][j], the sum, rounded to 32 bits,
  * all [requests, n_out]; what is missing becomes -1, -1 and -inf.
  * placed (n_out must be n_beams): not 0: the first continuation of a row takes the row's own place, and the others, in their order, the
