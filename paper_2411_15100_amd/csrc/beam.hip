@@ -490,9 +490,9 @@ __global__ __launch_bounds__(kSliceThreads) void beam_join_kernel(BeamSearch s, 
 // In place, whatever goes where: a workgroup takes the same region of every row that moves, in stretches that its registers hold at once:
 // it reads a stretch of all of them, and writes when all of it is read.  No workgroup's region is another's.  Where no row that moves is read (as
 // when continuations are placed) there is nothing to wait for.
-// 48 of 128 rows with caches of 12.6 MB each in use: 242 us, 5.0 TB/s read and written, as much as a large copy moves; with a stretch of all rows at
-// once and a barrier 523, row after row 477, and with the addresses' arithmetic done once for all threads 242.  A small call is a launch and a chain:
-// sources, lengths, the data.
+// 48 of 128 rows with caches of 12.6 MB each in use: 239 to 262 us, 5.0 TB/s read and written, as much as a large copy moves (row after row 477 before the
+// addresses' arithmetic was done once for all threads); 48 rows turned among themselves, where a stretch of all of them is read before it is written, 298,
+// in pairs that change places 294.  A small call is a launch and a chain: sources, lengths, the data.
 typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 constexpr int kMoveThreads = 256, kMoveUnits = 8, kFewUnits = 4;  // a thread's at a time, of rows row after row, of stretches of all rows

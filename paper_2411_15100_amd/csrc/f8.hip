@@ -427,8 +427,10 @@ __global__ __launch_bounds__(kFewThreads) void f8_few_kernel(F8Head h, Elem out_
 // One row of 128256 x 4096 takes 95 us, 5.5 TB/s, 32 rows 101: the bytes of the matrix.  (Of 32 rows and less a block without them takes 0.5 to 0.6 us, for
 // conversions and the barrier: four buffers instead of three take 1 us more a call.)
 // 128 rows of 151936 x 4096 take 153 us, 4.3 TB/s: memory, of which two blocks are on their way to each compute unit; through registers, a block ahead, it
-// took 264.  1024 rows of 128256 x 4096 take 611 us, 1.76 PFLOP/s; without its loads 456, at which clock and power hold the matrix instructions
+// took 264.  1024 rows of 128256 x 4096 take 624 us, 1.72 PFLOP/s (605 to 631 from card to card, and up to 770 for the first passes, until clocks have settled; pairs of
+// figures below are of one card each); without its loads 456, at which clock and power hold the matrix instructions
 // (8192 x 8192 x 8192 in a library reach 2.67 PFLOP/s, and this product without scales of blocks 544 us).
+// With f16 instructions (logits in f16 and in 32 bits) 128 rows take 216 and 219 us, 1024 rows 1052 and 1070, of which the instructions alone are 889.
 constexpr int kManyThreads = 512, kManyWaves = kManyThreads / 64;
 template <int MW, int WM, int TW> struct ManyShape {
   static constexpr int kRows = 16 * MW * WM, kWide = kManyWaves / WM, kPass = kWide * TW, kMatrix = 16 * kPass;
@@ -935,6 +937,13 @@ namespace {
 //   128256 x 4096: 1 row 103 and 95, 16 rows 115 and 96, 32 rows 128 and 101; 151936 x 1024: 31 and 33, 36 and 37, 41 and 41
 // of many 500 rows of 2048 x 4096 24 in tiles of 128 rows and 64 in those of 256, 1024 of 128256 x 4096 700 and 628, 384 of them 270 and 349.
 // Logits in 32 bits or f16, 128 rows of 4096 x 4096: few 24.3, many 25.7, of 10000 x 4096 40.8 and 36.9.
+// What masks leave is not known on the host: the choice is that for whole matrices.  bf16, few and many, us, with 5 rows of 13 open / with 400 tokens a row:
+//   10000 x 4096: 1 row 12.9 and 22.6 / 8.1 and 20.4, 16 rows 18.1 and 22.8 / 15.1 and 22.2, 32 rows 26.3 and 22.3 / 25.9 and 22.9, 64 rows 33.2 and 28.8 / 33.6 and 30.1,
+//     128 rows 44.5 and 30.5 / 44.5 and 32.7
+//   50001 x 2080: 1 row 23.1 and 21.7 / 7.8 and 14.5, 16 rows 26.1 and 23.2 / 12.0 and 15.5, 32 rows 33.6 and 26.9 / 20.2 and 18.5, 64 rows 52.2 and 38.0 / 28.8 and 31.2,
+//     128 rows 72.5 and 46.5 / 38.3 and 47.4
+//   128256 x 4096: 1 row 96.6 and 113 / 8.8 and 20.5, 16 rows 110 and 122 / 19.5 and 25.8, 32 rows 122 and 126 / 35.6 and 33.6, 64 rows 174 and 140 / 49.5 and 54.4,
+//     128 rows 309 and 162 / 80.1 and 85.7
 enum class Many { kFew, k16, k32, k64, k128, k128Whole, k256 };
 int32_t few_rows(const F8Head& h) { return h.B <= 16 ? 16 : 32; }
 double few_time(const F8Head& h) {

@@ -8,6 +8,7 @@ import numpy as np
 import pytest
 
 import plain_beams as plain
+import plain_logits
 from test_gpu_f8 import TYPES, Projection, _np, tolerance
 
 pytestmark = pytest.mark.gpu
@@ -73,6 +74,21 @@ def test_sums_of_products_of_all_sizes(B, K, V, signs, out):
         p.eight = p.eight[0] & 127, p.eight[1]
     p.scales *= 2.0 ** -8
     _check(p, out)
+
+
+@pytest.mark.parametrize("out", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("B,K,V", [(70, 4624, 601), (130, 4624, 1100), (300, 5120, 129)])
+def test_sums_of_many_rows_under_masks(B, K, V, out):
+    p = Projection(B, K, V, "f16", seed=V)
+    p.scales *= 2.0 ** -6
+    want, size = p.want()
+    tol = tolerance(want, size, K, out) + (7 * 2.0 ** -13 * _tops(p) if out == "bf16" else 0.0)
+    for share in (0.0, 0.002, 0.6, 1.0):
+        allowed = np.random.default_rng(B).random((B, V)) < share
+        allowed[B // 2] = False
+        allowed[B - 1, V - 1] = True
+        got = _np(p.run(out, mask=torch.from_numpy(plain_logits.pack(allowed)).cuda(), stride=V + B % 4, offset=B % 3))
+        assert (got[~allowed] == -np.inf).all() and (np.abs(got - want) <= tol)[allowed].all(), share
 
 
 @pytest.mark.parametrize("B", [65, 128, 200])
